@@ -147,15 +147,16 @@ def _tiled(k, v):
     of 16), laid out as include/svl.h says: per 16 positions the K codes, the V
     codes, and the (scale, minimum) pairs of K and of V."""
     B, H, P, d = k.shape
-    n, G, e = P // TILE, d // GROUP, d // 16     # tiles, groups, dims of a V lane
+    n, G = P // TILE, d // GROUP                 # tiles, groups
     nibble = torch.arange(8, device=k.device)
     parts, pairs = [], []
     for x, is_v in ((k, False), (v, True)):
         c, s, lo = _quantised(x)
         c = c.to(torch.int32).flatten(-2)
         if is_v:
-            # [tile][quad][lane][dims / 2 words]: nibble i = dim i % 4 / 2 of the word's pair, position 2 (i % 2) + i / 4
-            c = c.view(B, H, n, 4, 4, 16, e // 2, 2).permute(0, 1, 2, 3, 5, 6, 4, 7)
+            # [quad][lane][group][2] words, the dims 4 lane .. 4 lane + 3 of each group in two pairs:
+            # nibble i = dim i % 4 / 2 of the word's pair, position 2 (i % 2) + i / 4 of the quad
+            c = c.view(B, H, n, 4, 4, G, 16, 2, 2).permute(0, 1, 2, 3, 6, 5, 7, 4, 8)
             w = c[..., 2 * (nibble % 2) + nibble // 4, nibble % 4 // 2]
         else:
             # word w (dims 8 w ..) of a row at place (w % 4) (words / 4) + w / 4
@@ -261,17 +262,17 @@ def _plain_cached(st):
     case = st["case"]
     rows, pos, ends = _lengths(case)
     A, H, d, dt = case["n_heads"], case["n_kv_heads"], case["head_dim"], _dtype(case)
-    B, n, G, e = len(rows), st["max_len"] // TILE, d // GROUP, d // 16
+    B, n, G = len(rows), st["max_len"] // TILE, d // GROUP
     w = st["cache"].view(torch.int32).view(B, H, n, -1)
     kw, vw, kp, vp = torch.split(w, [TILE * d // 8] * 2 + [TILE * G] * 2, -1)
     nibble = torch.arange(8, device=w.device, dtype=torch.int32)
     kc = (kw.reshape(B, H, n, TILE, 4, d // 32, 1) >> (4 * nibble)) & 15
     kc = kc.transpose(-3, -2).reshape(B, H, n * TILE, G, GROUP).float()
-    vc = (vw.reshape(B, H, n, 4, 16, e // 2, 1) >> (4 * nibble)) & 15
+    vc = (vw.reshape(B, H, n, 4, 16, G, 2, 1) >> (4 * nibble)) & 15
     # nibble of (dim of the pair, position of the quad)
     dim, at = torch.arange(2, device=w.device), torch.arange(4, device=w.device)
-    vc = vc[..., 2 * dim[:, None] + at // 2 + 4 * (at % 2)]          # [..][16][e/2][dim][position]
-    vc = vc.permute(0, 1, 2, 3, 7, 4, 5, 6).reshape(B, H, n * TILE, G, GROUP).float()
+    vc = vc[..., 2 * dim[:, None] + at // 2 + 4 * (at % 2)]          # [quad][lane][group][2][dim][position]
+    vc = vc.permute(0, 1, 2, 3, 8, 5, 4, 6, 7).reshape(B, H, n * TILE, G, GROUP).float()
 
     def pair(x):
         x = x.reshape(B, H, n, 4, G, 4).transpose(-2, -1).contiguous().view(dt).float()
@@ -417,15 +418,15 @@ def _exact_rows(x):
 def _exact_codes(case, st):
     """float64 K and V [B][KV][positions][d] that the cache bytes stand for, by bytes."""
     H, d = case["n_kv_heads"], case["head_dim"]
-    B, n, G, e = len(_ints(case["rows"])), st["max_len"] // TILE, d // GROUP, d // 16
+    B, n, G = len(_ints(case["rows"])), st["max_len"] // TILE, d // GROUP
     b = st["cache"].view(B, H, n, -1)
     code = torch.stack([b & 15, b >> 4], -1).flatten(-2)             # nibbles in address order
     size = TILE * d                                                  # nibbles of K codes
     i, c = torch.arange(TILE, device=b.device)[:, None], torch.arange(d, device=b.device)
     word = (c // 8 % 4) * (d // 32) + c // 32
     k = code[..., (i * d + word * 8 + c % 8).reshape(-1)].double().view(B, H, n, TILE, d)
-    lane, pair, odd = c // e, c % e // 2, c % 2
-    at = (i // 4 * 16 + lane) * (e // 2) + pair                      # word of V
+    lane, pair, odd = c % GROUP // 4, c // GROUP * 2 + c % 4 // 2, c % 2
+    at = (i // 4 * 16 + lane) * (2 * G) + pair                       # word of V
     v = code[..., (size + at * 8 + 2 * odd + i % 4 // 2 + 4 * (i % 2)).reshape(-1)].double().view(B, H, n, TILE, d)
     par = b[..., size:].contiguous().view(_dtype(case)).double()
     where = ((i // 4 * G + c // GROUP) * 4 + i % 4) * 2
