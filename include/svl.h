@@ -525,6 +525,120 @@ svl_status svl_decode_step_noalloc(const svl_config *cfg, const svl_layer_weight
                                    const uint8_t *ffn_mask, void *kv_cache, int32_t max_len,
                                    void *stream);
 
+/* ---- windowed attention and the 4-bit K / V cache ------------------------
+ * Attention whose key range is bounded, and a K / V cache of 4.5 bits a value:
+ * what a long generation reads at every step.  The operators below work on one
+ * layer's rows; svl_prefill_cache4 and svl_decode_step4 run the decoder on them.
+ *
+ * Visibility, the same in all of them: the query at position p sees key j iff
+ *   j <= p  and  (window == 0  or  j > p - window  or  j < sinks),
+ * so a window of w is the query's own position and the w - 1 before it, and the
+ * first `sinks` positions stay visible however far the sequence has grown.
+ * Keys are used as they are given (rotated at their absolute position).
+ *   out = sum_j softmax_j(scale q . k_j) v_j,
+ * query head h with K/V head h / (n_heads / n_kv_heads).  Scores, softmax and
+ * sums are float32; rows are fp16 or bf16 (`compute`), head_dim 64 or 128.
+ *
+ * Rows are [row][head][head_dim] with a row stride ld in elements, at least
+ * heads * head_dim and a multiple of 8, so Q, K and V may be slices of one packed
+ * projection.  cu_* are host arrays [batch + 1] of row offsets (from 0 or more,
+ * not decreasing; a sample may have no rows).  They are read before the call
+ * returns and travel with the launches: nothing is copied to the device, and a
+ * captured call keeps the lengths it was made with.  Rows outside the samples
+ * are neither read nor written.  No call needs another workspace state than its
+ * own: two captured graphs may share one as long as they do not run at once. */
+typedef struct {
+  int32_t n_heads, n_kv_heads, head_dim;
+  int32_t compute;   /* svl_compute: SVL_COMPUTE_F16 (fp16 rows) or SVL_COMPUTE_BF16 */
+  int32_t window;    /* 0: no window */
+  int32_t sinks;     /* without effect when window == 0 */
+  float scale;       /* finite and > 0; the decoder's is 1 / sqrt(head_dim) */
+} svl_attention;
+
+/* The 4-bit cache of one layer (dev): [batch][n_kv_heads][ceil(max_len / 16)]
+ * tiles of 16 positions.  Each group of 64 dims of a head's row stands for
+ *   lo + s c,  c in 0..15:  lo = min x,  s = (max x - min x) / 15 rounded towards
+ *   zero to the rows' type,  c = (x - lo) / s rounded to the nearest integer,
+ *   ties to even, at most 15 (0 where s = 0),
+ * so no value leaves its group's range and |x - value| <= s / 2, plus, at the top
+ * of the range, what rounding s took (15 units in its last place at most).  s and
+ * lo are kept in the rows' type.  A group that holds an inf or NaN gets
+ * s = lo = NaN: all of it reads as NaN.
+ * A tile, with G = head_dim / 64, in 32-bit little-endian words:
+ *   K codes  [16 positions][head_dim / 8]: the word of dims 8 w .. 8 w + 7 at place
+ *            (w % 4) (head_dim / 32) + w / 4 of its row, dim 8 w + i in bits 4 i ..
+ *   V codes  [4 quads][16 lanes][G][2]: word (quad, lane, g, t) holds dims
+ *            x = 64 g + 4 lane + 2 t and x + 1 at the quad's four positions: nibble i
+ *            is dim x + i % 4 / 2 at position 4 quad + 2 (i % 2) + i / 4
+ *   K pairs  [4 quads][G][4 positions]: s in the low half, lo in the high half
+ *   V pairs  the same
+ * (18 head_dim bytes: 2304 at 128).  Nothing in it has to be
+ * initialised: positions that were not appended are never used. */
+#define SVL_KV4_MAX_LEN (1 << 20)
+
+/* Bytes of one layer's cache (0 on bad arguments). */
+size_t svl_kv4_cache_bytes(const svl_attention *att, int32_t batch, int32_t max_len);
+
+/* Writes rows cu_rows[b] .. cu_rows[b+1]-1 of k and v (dev, [row][n_kv_heads][d])
+ * to positions pos[b] .. (host [batch]); pos[b] + rows <= max_len.  Other
+ * positions keep their values. */
+svl_status svl_kv4_append(const svl_attention *att, int32_t batch, const int32_t *cu_rows,
+                          const int32_t *pos, const void *k, int64_t ld_k, const void *v,
+                          int64_t ld_v, void *cache, int32_t max_len, void *stream);
+
+/* Reads the same positions back: lo + s c rounded once to the rows' type. */
+svl_status svl_kv4_read(const svl_attention *att, int32_t batch, const int32_t *cu_rows,
+                        const int32_t *pos, const void *cache, int32_t max_len, void *k,
+                        int64_t ld_k, void *v, int64_t ld_v, void *stream);
+
+/* Workspace bytes of svl_kv4_attention, for any batch and length (0 on a bad
+ * description). */
+size_t svl_kv4_workspace_bytes(const svl_attention *att);
+
+/* Attention of new rows over the cache: row cu_rows[b] + i of q is at position
+ * pos[b] + i, and positions 0 .. pos[b] + i (its own among them: append first)
+ * hold its keys.  One row per sample is a decode step; several are a prompt's
+ * next chunk or proposed tokens.  The products use the codes themselves: K and V
+ * are not rounded on the way; the softmax weights times s are rounded to 16 bits
+ * once. */
+svl_status svl_kv4_attention(const svl_attention *att, int32_t batch, const int32_t *cu_rows,
+                             const int32_t *pos, const void *q, int64_t ld_q, const void *cache,
+                             int32_t max_len, void *out, int64_t ld_out, void *ws, size_t ws_bytes,
+                             void *stream);
+
+/* Attention over packed rows: sample b's queries are rows cu_q[b] .. of q, its
+ * keys rows cu_k[b] .. of k and v (cu_k NULL: the same rows), and the queries are
+ * the last of the keys' positions (at most as many; else SVL_E_VALUE).
+ *   key_mask  dev uint8 [key row] or NULL: 0 hides a key from every query.  A
+ *             hidden row may hold anything.  A query that sees no key gets zeros
+ *             and a log-sum of -inf.
+ *   out       dev [query row][n_heads][d]
+ *   lse       dev float [query row][n_heads] or NULL: log sum_j exp(scale q . k_j),
+ *             which the backward needs.
+ * A row that sees an inf or NaN of V has non-finite outputs in that head; rows
+ * that do not see it are not touched by it. */
+svl_status svl_window_attention(const svl_attention *att, int32_t batch, const int32_t *cu_q,
+                                const int32_t *cu_k, const void *q, int64_t ld_q, const void *k,
+                                int64_t ld_k, const void *v, int64_t ld_v, const uint8_t *key_mask,
+                                void *out, int64_t ld_out, float *lse, void *stream);
+
+/* Workspace bytes of the backward for these lengths (0 on bad arguments). */
+size_t svl_window_workspace_bytes(const svl_attention *att, int32_t batch, const int32_t *cu_q,
+                                  const int32_t *cu_k);
+
+/* Gradients of svl_window_attention's out with respect to q, k and v, from its
+ * inputs, its out and lse and the gradient of out.  Every key row of the samples
+ * gets a gradient (zero where no query sees it), summed over its query heads and
+ * rows in a fixed order: the same bits on every call.  With fp16 rows dS is scaled
+ * by powers of two on the way, so small or loss-scaled gradients keep their
+ * digits. */
+svl_status svl_window_attention_backward(
+    const svl_attention *att, int32_t batch, const int32_t *cu_q, const int32_t *cu_k,
+    const void *q, int64_t ld_q, const void *k, int64_t ld_k, const void *v, int64_t ld_v,
+    const uint8_t *key_mask, const void *out, int64_t ld_out, const float *lse,
+    const void *grad_out, int64_t ld_grad_out, void *grad_q, int64_t ld_grad_q, void *grad_k,
+    int64_t ld_grad_k, void *grad_v, int64_t ld_grad_v, void *ws, size_t ws_bytes, void *stream);
+
 /* Message for the last non-OK status returned on this thread. */
 const char *svl_last_error(void);
 

@@ -14,4 +14,7 @@ from .binding import (  # noqa: F401
     svl_workspace_bytes, alloc_train_workspace, svl_train_params, svl_train_step,
     SVL_STATUS_NONFINITE, svl_workspace_status,
     svl_train_workspace_bytes, svl_train_workspace_bytes_full,
+    alloc_kv4_cache, alloc_kv4_workspace, alloc_window_workspace, make_attention, svl_attention,
+    svl_kv4_append, svl_kv4_attention, svl_kv4_cache_bytes, svl_kv4_read, svl_kv4_workspace_bytes,
+    svl_window_attention, svl_window_attention_backward, svl_window_workspace_bytes,
 )

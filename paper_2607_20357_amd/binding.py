@@ -75,6 +75,12 @@ class svl_train_params(ctypes.Structure):
                 ("prefix", ctypes.c_int32), ("units", ctypes.c_int32)]
 
 
+class svl_attention(ctypes.Structure):
+    _fields_ = [("n_heads", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("compute", ctypes.c_int32),
+                ("window", ctypes.c_int32), ("sinks", ctypes.c_int32), ("scale", ctypes.c_float)]
+
+
 class svl_flops(ctypes.Structure):
     _fields_ = [(n, ctypes.c_uint64) for n in ("q", "kv", "o", "attn", "ffn", "total")]
 
@@ -142,11 +148,26 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.svl_timing_enable.argtypes = [i32]
     lib.svl_timing_read.argtypes = [i32, ctypes.POINTER(ctypes.c_double),
                                     ctypes.POINTER(ctypes.c_int64)]
+    attp, i64 = ctypes.POINTER(svl_attention), ctypes.c_int64
+    lib.svl_kv4_cache_bytes.argtypes = [attp, i32, i32]
+    lib.svl_kv4_cache_bytes.restype = sz
+    lib.svl_kv4_workspace_bytes.argtypes = [attp]
+    lib.svl_kv4_workspace_bytes.restype = sz
+    lib.svl_window_workspace_bytes.argtypes = [attp, i32, P, P]
+    lib.svl_window_workspace_bytes.restype = sz
+    lib.svl_kv4_append.argtypes = [attp, i32, P, P, P, i64, P, i64, P, i32, P]
+    lib.svl_kv4_read.argtypes = [attp, i32, P, P, P, i32, P, i64, P, i64, P]
+    lib.svl_kv4_attention.argtypes = [attp, i32, P, P, P, i64, P, i32, P, i64, P, sz, P]
+    lib.svl_window_attention.argtypes = [attp, i32, P, P, P, i64, P, i64, P, i64, P, P, i64, P, P]
+    lib.svl_window_attention_backward.argtypes = [attp, i32, P, P, P, i64, P, i64, P, i64, P, P, i64,
+                                                  P, P, i64, P, i64, P, i64, P, i64, P, sz, P]
     for f in ("svl_select_tokens", "svl_layer_forward", "svl_prefill", "svl_count_flops",
               "svl_timing_enable", "svl_timing_read", "svl_count_positive", "svl_budget_project",
               "svl_prefill_cache", "svl_decode_step", "svl_decode_step_noalloc",
               "svl_prefill_controlled",
-              "svl_budget_loss", "svl_train_step", "svl_workspace_status"):
+              "svl_budget_loss", "svl_train_step", "svl_workspace_status", "svl_kv4_append",
+              "svl_kv4_read", "svl_kv4_attention", "svl_window_attention",
+              "svl_window_attention_backward"):
         getattr(lib, f).restype = i32
     _lib = lib
     return lib
@@ -788,3 +809,224 @@ def svl_train_step(cfg: svl_config, layers, params: svl_train_params, logits: to
         opt(out.get("grad_logits"), "grad_logits"), opt(out.get("grad_gate"), "grad_gate"),
         _dev(ws, "ws"), _nbytes(ws), _stream(stream)))
     return out
+
+
+# ------------------------------------------------------------------ windowed attention, 4-bit cache
+def make_attention(n_heads: int, n_kv_heads: int, head_dim: int, window: int = 0, sinks: int = 0,
+                   scale: Optional[float] = None, compute: str = "f16") -> svl_attention:
+    """svl_attention; scale defaults to 1 / sqrt(head_dim), compute is "f16" or "bf16"."""
+    if isinstance(compute, str):
+        if compute not in ("f16", "bf16"):
+            raise ValueError(f"compute must be 'f16' or 'bf16', not {compute!r}")
+        compute = SVL_COMPUTE_BF16 if compute == "bf16" else SVL_COMPUTE_F16
+    if scale is None:
+        scale = head_dim ** -0.5
+    return svl_attention(int(n_heads), int(n_kv_heads), int(head_dim), int(compute), int(window),
+                         int(sinks), float(scale))
+
+
+def _row_dtype(att: svl_attention) -> torch.dtype:
+    return torch.bfloat16 if att.compute == SVL_COMPUTE_BF16 else torch.float16
+
+
+def _cu(a, name: str):
+    """Host int32 [batch + 1] row offsets and their pointer."""
+    arr, ptr = _host_i32(a)
+    if arr.ndim != 1 or arr.shape[0] < 2:
+        raise ValueError(f"{name} must be a host array of batch + 1 entries")
+    return arr, ctypes.cast(ptr, ctypes.c_void_p)
+
+
+def _host_pos(a, batch: int):
+    arr, ptr = _host_i32(a)
+    if arr.shape != (batch,):
+        raise ValueError(f"pos has shape {arr.shape}, expected ({batch},)")
+    return arr, ctypes.cast(ptr, ctypes.c_void_p)
+
+
+def _row_stride(t: Optional[torch.Tensor], name: str, att: svl_attention, heads: int,
+                rows: int) -> int:
+    """Row stride of 16-bit rows [>= rows][heads][head_dim]: heads and dims contiguous, the
+    rows any multiple of 8 elements apart."""
+    if not isinstance(t, torch.Tensor):
+        raise ValueError(f"{name} must be a torch tensor")
+    if t.dtype != _row_dtype(att):
+        raise ValueError(f"{name} has dtype {t.dtype}, expected {_row_dtype(att)}")
+    d = att.head_dim
+    if t.dim() != 3 or tuple(t.shape[1:]) != (heads, d):
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected (rows, {heads}, {d})")
+    if t.shape[0] < rows:
+        raise ValueError(f"{name} holds {t.shape[0]} rows, needs at least {rows}")
+    if t.numel() == 0:
+        return heads * d
+    if t.stride(2) != 1 or (t.stride(1) != d and heads > 1):
+        raise ValueError(f"{name}: heads and dims must be contiguous, strides are {t.stride()}")
+    ld = t.stride(0) if t.shape[0] > 1 else heads * d
+    if ld < heads * d or ld % 8:
+        raise ValueError(f"{name}: row stride {ld} must be at least {heads * d} and a multiple of 8")
+    return ld
+
+
+def _rows(att: svl_attention, *arrays):
+    """(device pointer, row stride) of each (tensor, name, heads, rows), one after another;
+    all are checked before the first pointer is taken."""
+    strides = [_row_stride(t, name, att, heads, rows) for t, name, heads, rows in arrays]
+    return [x for (t, name, _, _), ld in zip(arrays, strides)
+            for x in (_on_device(t, name) if t.numel() else None, ld)]
+
+
+def _on_device(t: torch.Tensor, name: str) -> int:
+    """Device pointer of a GPU tensor of the current device, whatever its strides."""
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a GPU tensor (no CPU path exists)")
+    if t.device.index != torch.cuda.current_device():
+        raise ValueError(f"{name} is on {t.device}, the library launches on "
+                         f"cuda:{torch.cuda.current_device()}")
+    return t.data_ptr()
+
+
+def _log_sums(lse: Optional[torch.Tensor], att: svl_attention, rows: int) -> Optional[torch.Tensor]:
+    if lse is None:
+        return None
+    _expect(lse, "lse", torch.float32, rows * att.n_heads)
+    if lse.dim() != 2 or lse.shape[1] != att.n_heads:
+        raise ValueError(f"lse has shape {tuple(lse.shape)}, expected (rows, {att.n_heads})")
+    return lse
+
+
+def _mask(key_mask: Optional[torch.Tensor], keys: int) -> Optional[torch.Tensor]:
+    if key_mask is None:
+        return None
+    if isinstance(key_mask, torch.Tensor) and key_mask.dtype == torch.bool:
+        key_mask = key_mask.view(torch.uint8)
+    _expect(key_mask, "key_mask", torch.uint8, keys)
+    return key_mask
+
+
+def svl_kv4_cache_bytes(att: svl_attention, batch: int, max_len: int) -> int:
+    """Bytes of one layer's 4-bit cache."""
+    n = load_library().svl_kv4_cache_bytes(ctypes.byref(att), int(batch), int(max_len))
+    if n == 0:
+        raise SvlError(2, "svl_kv4_cache_bytes: " + load_library().svl_last_error().decode())
+    return int(n)
+
+
+def alloc_kv4_cache(att: svl_attention, batch: int, max_len: int, device="cuda") -> torch.Tensor:
+    """Caller-owned 4-bit cache of one layer (uninitialised: append fills it)."""
+    return torch.empty(svl_kv4_cache_bytes(att, batch, max_len), dtype=torch.uint8, device=device)
+
+
+def _cache_rows(att: svl_attention, cu_rows, pos, cache: torch.Tensor, max_len: int):
+    cu, cup = _cu(cu_rows, "cu_rows")
+    B = int(cu.shape[0]) - 1
+    ps, psp = _host_pos(pos, B)
+    _expect(cache, "cache", torch.uint8, svl_kv4_cache_bytes(att, B, max_len))
+    # the arrays stay referenced until the call is made
+    return B, max(int(cu[-1]), 0), cu, cup, ps, psp
+
+
+def svl_kv4_append(att: svl_attention, cu_rows, pos, k: torch.Tensor, v: torch.Tensor,
+                   cache: torch.Tensor, max_len: int, stream=None) -> None:
+    """Quantises rows cu_rows[b] .. of k and v [rows][KV][d] into positions pos[b] .. of the cache."""
+    B, n, cu, cup, ps, psp = _cache_rows(att, cu_rows, pos, cache, max_len)
+    H = att.n_kv_heads
+    kp, ldk, vp, ldv = _rows(att, (k, "k", H, n), (v, "v", H, n))
+    _check(load_library().svl_kv4_append(ctypes.byref(att), B, cup, psp, kp, ldk, vp, ldv,
+                                         _dev(cache, "cache"), int(max_len), _stream(stream)))
+
+
+def svl_kv4_read(att: svl_attention, cu_rows, pos, cache: torch.Tensor, max_len: int,
+                 k: torch.Tensor, v: torch.Tensor, stream=None) -> None:
+    """Reads positions pos[b] .. back into rows cu_rows[b] .. of k and v [rows][KV][d]."""
+    B, n, cu, cup, ps, psp = _cache_rows(att, cu_rows, pos, cache, max_len)
+    H = att.n_kv_heads
+    kp, ldk, vp, ldv = _rows(att, (k, "k", H, n), (v, "v", H, n))
+    _check(load_library().svl_kv4_read(ctypes.byref(att), B, cup, psp, _dev(cache, "cache"),
+                                       int(max_len), kp, ldk, vp, ldv, _stream(stream)))
+
+
+def svl_kv4_workspace_bytes(att: svl_attention) -> int:
+    n = load_library().svl_kv4_workspace_bytes(ctypes.byref(att))
+    if n == 0:
+        raise SvlError(2, "svl_kv4_workspace_bytes: " + load_library().svl_last_error().decode())
+    return int(n)
+
+
+def alloc_kv4_workspace(att: svl_attention, device="cuda") -> torch.Tensor:
+    """Workspace of svl_kv4_attention, for any batch and length."""
+    return torch.empty(svl_kv4_workspace_bytes(att), dtype=torch.uint8, device=device)
+
+
+def svl_kv4_attention(att: svl_attention, cu_rows, pos, q: torch.Tensor, cache: torch.Tensor,
+                      max_len: int, out: torch.Tensor, ws: torch.Tensor, stream=None) -> None:
+    """Attention of rows cu_rows[b] .. of q [rows][A][d], at positions pos[b] .., over the
+    4-bit cache, into the same rows of out."""
+    B, n, cu, cup, ps, psp = _cache_rows(att, cu_rows, pos, cache, max_len)
+    A = att.n_heads
+    _expect(ws, "ws", torch.uint8, 1)
+    qp, ldq, op, ldo = _rows(att, (q, "q", A, n), (out, "out", A, n))
+    _check(load_library().svl_kv4_attention(ctypes.byref(att), B, cup, psp, qp, ldq,
+                                            _dev(cache, "cache"), int(max_len), op, ldo,
+                                            _dev(ws, "ws"), _nbytes(ws), _stream(stream)))
+
+
+def _packed_rows(cu_q, cu_k):
+    cq, cqp = _cu(cu_q, "cu_q")
+    B = int(cq.shape[0]) - 1
+    if cu_k is None:
+        return B, cq, cqp, cq, None
+    ck, ckp = _cu(cu_k, "cu_k")
+    if ck.shape != cq.shape:
+        raise ValueError(f"cu_k has {ck.shape[0]} entries, cu_q has {cq.shape[0]}")
+    return B, cq, cqp, ck, ckp
+
+
+def svl_window_attention(att: svl_attention, cu_q, cu_k, q: torch.Tensor, k: torch.Tensor,
+                         v: torch.Tensor, out: torch.Tensor, lse: Optional[torch.Tensor] = None,
+                         key_mask: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Causal attention with att's window and sinks over packed rows, q and out [rows][A][d],
+    k and v [keys][KV][d]; cu_k None: the keys are the queries' rows.  lse, if given, gets
+    the log-sums [rows][A] (float32) that the backward reads."""
+    B, cq, cqp, ck, ckp = _packed_rows(cu_q, cu_k)
+    n, m = max(int(cq[-1]), 0), max(int(ck[-1]), 0)
+    A, H = att.n_heads, att.n_kv_heads
+    mask, lse = _mask(key_mask, m), _log_sums(lse, att, n)
+    *ins, op, ldo = _rows(att, (q, "q", A, n), (k, "k", H, m), (v, "v", H, m), (out, "out", A, n))
+    _check(load_library().svl_window_attention(
+        ctypes.byref(att), B, cqp, ckp, *ins, None if mask is None else _dev(mask, "key_mask"), op, ldo,
+        None if lse is None else _dev(lse, "lse"), _stream(stream)))
+
+
+def svl_window_workspace_bytes(att: svl_attention, cu_q, cu_k=None) -> int:
+    """Workspace bytes of svl_window_attention_backward for these lengths."""
+    B, cq, cqp, ck, ckp = _packed_rows(cu_q, cu_k)
+    n = load_library().svl_window_workspace_bytes(ctypes.byref(att), B, cqp, ckp)
+    if n == 0:
+        raise SvlError(2, "svl_window_workspace_bytes: " + load_library().svl_last_error().decode())
+    return int(n)
+
+
+def alloc_window_workspace(att: svl_attention, cu_q, cu_k=None, device="cuda") -> torch.Tensor:
+    return torch.empty(svl_window_workspace_bytes(att, cu_q, cu_k), dtype=torch.uint8, device=device)
+
+
+def svl_window_attention_backward(att: svl_attention, cu_q, cu_k, q: torch.Tensor, k: torch.Tensor,
+                                  v: torch.Tensor, out: torch.Tensor, lse: torch.Tensor,
+                                  grad_out: torch.Tensor, grad_q: torch.Tensor, grad_k: torch.Tensor,
+                                  grad_v: torch.Tensor, ws: torch.Tensor,
+                                  key_mask: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Gradients of svl_window_attention with respect to q, k and v into grad_q, grad_k and
+    grad_v (shapes of q, k and v), from its inputs, out, lse and the gradient of out."""
+    B, cq, cqp, ck, ckp = _packed_rows(cu_q, cu_k)
+    n, m = max(int(cq[-1]), 0), max(int(ck[-1]), 0)
+    A, H = att.n_heads, att.n_kv_heads
+    if lse is None:
+        raise ValueError("lse is required")
+    mask, lse = _mask(key_mask, m), _log_sums(lse, att, n)
+    _expect(ws, "ws", torch.uint8, 1)
+    arrays = _rows(att, (q, "q", A, n), (k, "k", H, m), (v, "v", H, m), (out, "out", A, n),
+                   (grad_out, "grad_out", A, n), (grad_q, "grad_q", A, n), (grad_k, "grad_k", H, m),
+                   (grad_v, "grad_v", H, m))
+    _check(load_library().svl_window_attention_backward(
+        ctypes.byref(att), B, cqp, ckp, *arrays[:6], None if mask is None else _dev(mask, "key_mask"),
+        *arrays[6:8], _dev(lse, "lse"), *arrays[8:], _dev(ws, "ws"), _nbytes(ws), _stream(stream)))

@@ -564,6 +564,10 @@ svl_status set_error(svl_status st, const char* msg) {
 }
 svl_status validate_config(const svl_config* c) { return check_config(c); }
 
+hipError_t timed_call(int kernel_class, hipStream_t st, hipError_t (*f)(const void*), const void* arg) {
+  return timed(kernel_class, st, [&] { return f(arg); });
+}
+
 }  // namespace svl
 
 using namespace svl;

@@ -1,0 +1,315 @@
+"""The 4-bit K / V cache and the attention over it, against the float64 oracle:
+the cache's bytes exactly, what it reads back as to the last rounding, the
+attention within the bounds of its roundings (attention_helpers)."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2607_20357_amd as svl
+from attention_helpers import (cached_rows, check_cached, draw, dtype_of, f64, fill_cache, half_step,
+                               offsets)
+from oracle import attention as oa
+
+pytestmark = pytest.mark.gpu
+COMPUTES = ["f16", "bf16"]
+
+
+def _gen(seed):
+    return torch.Generator(device="cuda").manual_seed(seed)
+
+
+def _heads(d):
+    return (4, 2, d) if d == 128 else (6, 3, d)
+
+
+# ------------------------------------------------------------------ append and read
+@pytest.mark.parametrize("compute", COMPUTES)
+@pytest.mark.parametrize("d", [64, 128])
+def test_cache_bytes_are_the_definition(compute, d):
+    """Appended in pieces that end inside tiles; bytes of positions outside stay."""
+    A, H, _ = _heads(d)
+    att = svl.make_attention(A, H, d, compute=compute)
+    B, max_len = 2, 70                                  # tiles of 16: the last one is cut
+    k, v = draw(_gen(1), (B, max_len, H, d), compute), draw(_gen(2), (B, max_len, H, d), compute, 0.03)
+    cache = svl.alloc_kv4_cache(att, B, max_len)
+    cache.fill_(0xa5)
+    for lo, hi in ((0, 1), (1, 3), (3, 21), (21, 22), (22, 63)):       # positions 63.. not appended
+        rows = [hi - lo] * B
+        svl.svl_kv4_append(att, offsets(rows), [lo] * B, k[:, lo:hi].reshape(-1, H, d),
+                           v[:, lo:hi].reshape(-1, H, d), cache, max_len)
+    torch.cuda.synchronize()
+    n, G = -(-max_len // 16), d // 64
+    words = cache.cpu().numpy().view(np.uint32).reshape(B, H, n, -1)
+    (kc, ks, kl), (vc, vs, vl), _, _ = cached_rows(k, v, compute)
+    dt = dtype_of(compute)
+    bits = lambda x: torch.from_numpy(np.ascontiguousarray(x)).to(dt).view(torch.int16).numpy().astype(np.uint16)
+    for b in range(B):
+        for h in range(H):
+            for t in range(n):
+                kt, vt = np.zeros((16, d), int), np.zeros((16, d), int)
+                there = [p for p in range(16) if 16 * t + p < 63]
+                for p in range(16):
+                    # positions that were not appended keep the fill's nibbles (5 and 10)
+                    if p in there:
+                        kt[p], vt[p] = kc[b, 16 * t + p, h], vc[b, 16 * t + p, h]
+                want = oa.tile_words(kt, vt, d)
+                mine = oa.tile_words(np.isin(np.arange(16), there)[:, None] * np.full((16, d), 15),
+                                     np.isin(np.arange(16), there)[:, None] * np.full((16, d), 15), d)
+                got = words[b, h, t]
+                nk = len(want)
+                assert np.array_equal(got[:nk] & mine, want), (b, h, t)
+                assert np.array_equal(got[:nk] & ~mine, np.full(nk, 0xa5a5a5a5, np.uint32) & ~mine)
+                for which, (s, lo) in enumerate(((ks, kl), (vs, vl))):
+                    par = got[nk + which * 16 * G:nk + (which + 1) * 16 * G].reshape(4, G, 4)
+                    for p in range(16):
+                        w = par[p // 4, :, p % 4]
+                        if p in there:
+                            assert np.array_equal(w & 0xffff, bits(s[b, 16 * t + p, h]))
+                            assert np.array_equal(w >> 16, bits(lo[b, 16 * t + p, h]))
+                        else:
+                            assert (w == 0xa5a5a5a5).all()
+
+
+def _hard_rows(compute, d, H):
+    """Values where codes and scales are decided: ties, flat groups, subnormals, the type's
+    extremes, tiny and wide ranges, an inf and a NaN."""
+    dt = dtype_of(compute)
+    rng = np.random.default_rng(5)
+    rows = [rng.integers(-30, 31, (H, d)) * 0.5, rng.integers(0, 16, (H, d)) * 1.0 + 0.5,
+            np.full((H, d), -3.25), np.zeros((H, d)), rng.standard_normal((H, d)) * 2.0 ** -22,
+            rng.standard_normal((H, d)) * 1e-6, rng.integers(0, 4, (H, d)) * 2.0 ** -24,
+            rng.choice([-1.0, 1.0], (H, d)) * (65504.0 if compute == "f16" else 3.0e38),
+            np.exp(rng.uniform(-9, 9, (H, d))), 1000.0 + rng.standard_normal((H, d))]
+    x = torch.from_numpy(np.stack(rows)).to(dt)
+    bad = torch.from_numpy(rng.standard_normal((3, H, d))).to(dt)
+    bad[0, 0, 3], bad[1, H - 1, d - 1], bad[2, 0, 0] = float("inf"), float("nan"), -float("inf")
+    return torch.cat([x, bad])
+
+
+@pytest.mark.parametrize("compute", COMPUTES)
+@pytest.mark.parametrize("d", [64, 128])
+def test_hard_values_read_back(compute, d):
+    A, H, _ = _heads(d)
+    att = svl.make_attention(A, H, d, compute=compute)
+    x = _hard_rows(compute, d, H)
+    n, max_len = x.shape[0], 40
+    k, v = x.cuda(), x.flip(0).contiguous().cuda()
+    cache = svl.alloc_kv4_cache(att, 1, max_len)
+    cache.fill_(0xff)
+    svl.svl_kv4_append(att, [0, n], [7], k, v, cache, max_len)
+    ko, vo = torch.zeros_like(k), torch.zeros_like(v)
+    svl.svl_kv4_read(att, [0, n], [7], cache, max_len, ko, vo)
+    torch.cuda.synchronize()
+    _, _, kk, vv = cached_rows(k, v, compute)
+    u = half_step(compute)
+    low = 2.0 ** -25 if compute == "f16" else 2.0 ** -134
+    for got, want, src in ((f64(ko), kk, f64(k)), (f64(vo), vv, f64(v))):
+        assert np.array_equal(np.isnan(got), np.isnan(want))
+        fine = ~np.isnan(want)
+        # rounded to float32 and then to the type
+        assert (np.abs(got - want)[fine] <= (np.abs(want) * (u + 2.0 ** -23) + low)[fine]).all()
+        assert np.isfinite(got[fine]).all()
+        # a group never leaves its range
+        g = src.reshape(n, H, -1, 64)
+        with np.errstate(invalid="ignore"):
+            inside = (got.reshape(g.shape) <= g.max(-1, keepdims=True)) & (got.reshape(g.shape) >= g.min(-1, keepdims=True))
+        assert inside[~np.isnan(got.reshape(g.shape))].all()
+
+
+@pytest.mark.parametrize("compute", COMPUTES)
+def test_read_takes_ragged_rows_strides_and_leaves_the_rest(compute):
+    A, H, d, max_len = 4, 2, 128, 400
+    att = svl.make_attention(A, H, d, compute=compute)
+    rows, pos = [1, 0, 17, 100, 33], [399, 5, 15, 31, 0]
+    cu = offsets(rows) + 2                                 # rows 0, 1 belong to nobody
+    total = int(cu[-1]) + 3
+    qkv = draw(_gen(7), (total, A + 2 * H, d), compute)    # slices of packed projections
+    k, v = qkv[:, A:A + H], qkv[:, A + H:]
+    cache = svl.alloc_kv4_cache(att, len(rows), max_len)
+    cache.fill_(0xff)
+    svl.svl_kv4_append(att, cu, pos, k, v, cache, max_len)
+    back = torch.full((total, 3 * H, d), 77.0, dtype=dtype_of(compute), device="cuda")
+    svl.svl_kv4_read(att, cu, pos, cache, max_len, back[:, :H], back[:, 2 * H:])
+    torch.cuda.synchronize()
+    _, _, kk, vv = cached_rows(k, v, compute)
+    got = f64(back)
+    u = half_step(compute) + 2.0 ** -23
+    at = slice(int(cu[0]), int(cu[-1]))
+    assert (np.abs(got[at, :H] - kk[at]) <= u * np.abs(kk[at]) + 2.0 ** -25).all()
+    assert (np.abs(got[at, 2 * H:] - vv[at]) <= u * np.abs(vv[at]) + 2.0 ** -25).all()
+    assert (got[:, H:2 * H] == 77).all() and (got[:2] == 77).all() and (got[int(cu[-1]):] == 77).all()
+
+
+def test_cache_past_four_gigabytes():
+    """A head whose bytes lie past 2^32 in the cache."""
+    A, H, d, max_len, B = 32, 32, 128, 1 << 19, 2        # 2.4 GB a sample
+    att = svl.make_attention(A, H, d, window=100, sinks=2)
+    cache = svl.alloc_kv4_cache(att, B, max_len)
+    assert cache.numel() > 1 << 32
+    n = 40
+    k, v = draw(_gen(3), (B * n, H, d), "f16"), draw(_gen(4), (B * n, H, d), "f16")
+    cu, pos = offsets([n] * B), [max_len - n] * B
+    svl.svl_kv4_append(att, cu, pos, k, v, cache, max_len)
+    svl.svl_kv4_append(att, offsets([2] * B), [0] * B, k[:2 * B], v[:2 * B], cache, max_len)
+    ko, vo = torch.zeros_like(k), torch.zeros_like(v)
+    svl.svl_kv4_read(att, cu, pos, cache, max_len, ko, vo)
+    _, _, kk, vv = cached_rows(k, v, "f16")
+    u = half_step("f16") + 2.0 ** -23
+    assert (np.abs(f64(ko) - kk) <= u * np.abs(kk) + 2.0 ** -25).all()
+    assert (np.abs(f64(vo) - vv) <= u * np.abs(vv) + 2.0 ** -25).all()
+    # the last row of the second sample sees its 40 rows and, through the sinks, two more
+    att.window = n
+    q, out, ws = draw(_gen(5), (B, A, d), "f16"), torch.empty((B, A, d), dtype=torch.float16, device="cuda"), \
+        svl.alloc_kv4_workspace(att)
+    svl.svl_kv4_attention(att, offsets([1] * B), [max_len - 1] * B, q, cache, max_len, out, ws)
+    torch.cuda.synchronize()
+    for b in range(B):
+        sink = slice(2 * b, 2 * b + 2)
+        ks, vs = (np.concatenate([x[sink], x[b * n:(b + 1) * n]]) for x in (kk, vv))
+        ref = oa.attention(f64(q)[b:b + 1], ks, vs, np.ones((1, n + 2), bool), att.scale)["out"]
+        # softmax weights to 2^-11, values below 4, and the output's rounding
+        assert np.abs(f64(out)[b:b + 1] - ref).max() <= 2.0 ** -11 * 4 * 2
+
+
+# ------------------------------------------------------------------ attention
+def _case(heads, compute, rows, pos, window=0, sinks=0, max_len=None, seed=0, scale=None):
+    A, H, d = heads
+    att = svl.make_attention(A, H, d, window=window, sinks=sinks, compute=compute, scale=scale)
+    B, ends = len(rows), [a + b for a, b in zip(rows, pos)]
+    max_len = max_len or max(ends)
+    gen = _gen(seed)
+    k, v = draw(gen, (B, max(ends), H, d), compute), draw(gen, (B, max(ends), H, d), compute)
+    k[..., 5::32] *= 4
+    cache = svl.alloc_kv4_cache(att, B, max_len)
+    cache.fill_(0xff)                                     # NaN where nothing was appended
+    for b in range(B):                                    # each sample its own length
+        cu = np.zeros(B + 1, np.int32)
+        cu[b + 1:] = ends[b]
+        svl.svl_kv4_append(att, cu, [0] * B, k[b], v[b], cache, max_len)
+    cu = offsets(rows)
+    q = draw(gen, (int(cu[-1]), A, d), compute)
+    out = torch.full_like(q, float("nan"))
+    ws = svl.alloc_kv4_workspace(att)
+    ws.fill_(0xff)
+    svl.svl_kv4_attention(att, cu, pos, q, cache, max_len, out, ws)
+    torch.cuda.synchronize()
+    return att, cu, q, k, v, cache, out, ws, max_len
+
+
+@pytest.mark.parametrize("compute", COMPUTES)
+@pytest.mark.parametrize("heads", [(4, 4, 128), (4, 4, 64), (7, 1, 128), (28, 4, 128), (8, 2, 64), (20, 1, 64), (40, 1, 128)])
+def test_single_tokens(heads, compute):
+    """One token per sample from the first position on, odd lengths, around the tiles' ends."""
+    pos = [0, 1, 15, 16, 31, 32, 33, 100, 257, 700]
+    att, cu, q, k, v, _, out, _, _ = _case(heads, compute, [1] * len(pos), pos, seed=heads[0])
+    check_cached(att, compute, cu, pos, q, k, v, out)
+
+
+@pytest.mark.parametrize("compute", COMPUTES)
+@pytest.mark.parametrize("window,sinks", [(1, 0), (1, 1), (16, 4), (33, 0), (64, 40), (100, 500), (5000, 3)])
+def test_windows_and_sinks(window, sinks, compute):
+    pos = [0, 3, 40, 129, 600, 601]
+    att, cu, q, k, v, _, out, _, _ = _case((4, 2, 128), compute, [1] * len(pos), pos, window, sinks, seed=window)
+    check_cached(att, compute, cu, pos, q, k, v, out)
+
+
+@pytest.mark.parametrize("compute", COMPUTES)
+@pytest.mark.parametrize("heads", [(4, 4, 128), (8, 1, 64), (14, 2, 128)])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (20, 3)])
+def test_several_rows(heads, window, sinks, compute):
+    rows, pos = [5, 0, 1, 70, 33], [0, 9, 300, 130, 31]
+    att, cu, q, k, v, _, out, _, _ = _case(heads, compute, rows, pos, window, sinks, seed=11)
+    check_cached(att, compute, cu, pos, q, k, v, out)
+
+
+@pytest.mark.parametrize("compute", COMPUTES)
+def test_long_context_in_many_pieces(compute):
+    """A cache long enough that one row's positions are cut into pieces and joined."""
+    pos = [9000, 4097]
+    att, cu, q, k, v, _, out, _, _ = _case((2, 1, 128), compute, [1, 3], pos, seed=2)
+    check_cached(att, compute, cu, pos, q, k, v, out)
+
+
+def test_a_batch_of_more_than_one_launch():
+    B = 150
+    pos = [(37 * b) % 90 for b in range(B)]
+    att, cu, q, k, v, _, out, _, _ = _case((2, 2, 64), "f16", [1] * B, pos, seed=4)
+    check_cached(att, "f16", cu, pos, q, k, v, out)
+
+
+@pytest.mark.parametrize("compute,spread", [("f16", 1e-4), ("f16", 60.0), ("bf16", 1e-20), ("bf16", 1e12)])
+def test_values_of_other_sizes(compute, spread):
+    """V far from 1, and queries far from 1 with the scale that makes up for it."""
+    A, H, d, n = 4, 2, 128, 300
+    att = svl.make_attention(A, H, d, compute=compute, scale=float(d ** -0.5 / (spread if spread < 1e3 else 1e3)))
+    gen = _gen(9)
+    k, v = draw(gen, (1, n, H, d), compute), draw(gen, (1, n, H, d), compute, spread)
+    v[:, :7] *= 0.01                                       # scales of other exponents first
+    q = draw(gen, (1, A, d), compute, spread if spread < 1e3 else 1e3)
+    cache = fill_cache(att, k, v, n)
+    out, ws = torch.full_like(q, float("nan")), svl.alloc_kv4_workspace(att)
+    svl.svl_kv4_attention(att, [0, 1], [n - 1], q, cache, n, out, ws)
+    torch.cuda.synchronize()
+    check_cached(att, compute, offsets([1]), [n - 1], q, k, v, out)
+
+
+def test_an_inf_stays_with_those_that_see_it():
+    """Rows with an inf or NaN that a query does not see leave it alone; one that does is NaN."""
+    A, H, d, n = 4, 2, 64, 200
+    att = svl.make_attention(A, H, d, window=20, sinks=2)
+    gen = _gen(6)
+    k, v = draw(gen, (1, n, H, d), "f16"), draw(gen, (1, n, H, d), "f16")
+    clean_k, clean_v = k.clone(), v.clone()
+    v[0, 50, 0, 3], k[0, 60, 1, 9] = float("inf"), float("nan")
+    cu, rows, pos = offsets([n]), [n], [0]
+    q = draw(gen, (n, A, d), "f16")
+    outs = []
+    for kk, vv in ((k, v), (clean_k, clean_v)):
+        cache = fill_cache(att, kk, vv, n)
+        out = torch.empty_like(q)
+        svl.svl_kv4_attention(att, cu, pos, q, cache, n, out, svl.alloc_kv4_workspace(att))
+        outs.append(f64(out))
+    for h in range(A):
+        hit = 50 if h < 2 else 60
+        sees = np.array([hit <= p < hit + 20 for p in range(n)])
+        assert np.array_equal(outs[0][~sees, h], outs[1][~sees, h])
+        assert np.isnan(outs[0][sees, h]).any(1).all()
+
+
+def test_same_bits_on_every_call_and_in_graphs():
+    """Eager calls repeat to the bit; two captured calls of different lengths share a
+    workspace and replay with eager work between them."""
+    att, cu, q, k, v, cache, out, ws, max_len = _case((28, 4, 128), "bf16", [1, 1, 1], [5000, 77, 900], seed=1)
+    again = torch.empty_like(out)
+    ws.fill_(0x7f)
+    svl.svl_kv4_attention(att, cu, [5000, 77, 900], q, cache, max_len, again, ws)
+    assert torch.equal(out, again)
+    pos2 = [3000, 70, 12]
+    want2 = torch.empty_like(out)
+    svl.svl_kv4_attention(att, cu, pos2, q, cache, max_len, want2, ws)
+    a, b = torch.empty_like(out), torch.empty_like(out)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graphs = []
+    for o, p in ((a, [5000, 77, 900]), (b, pos2)):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=side):
+            svl.svl_kv4_attention(att, cu, p, q, cache, max_len, o, ws)
+        graphs.append(g)
+    for _ in range(3):
+        a.fill_(3)
+        b.fill_(3)
+        graphs[0].replay()
+        graphs[1].replay()
+        svl.svl_kv4_attention(att, cu, pos2, q, cache, max_len, again, ws)
+        torch.cuda.synchronize()
+        assert torch.equal(a, out) and torch.equal(b, want2) and torch.equal(again, want2)
+
+
+def test_on_another_stream():
+    att, cu, q, k, v, cache, out, ws, max_len = _case((4, 4, 128), "f16", [1, 2], [700, 12], seed=8)
+    side, again = torch.cuda.Stream(), torch.empty_like(out)
+    side.wait_stream(torch.cuda.current_stream())
+    svl.svl_kv4_attention(att, cu, [700, 12], q, cache, max_len, again, ws, stream=side)
+    side.synchronize()
+    assert torch.equal(out, again)
