@@ -363,7 +363,7 @@ svl_status svl_budget_loss(const svl_config *cfg, const svl_budget_loss_params *
  * With fp16 activations (SVL_COMPUTE_F16) a value outside fp16's range
  * becomes inf when it is converted, and the inf (or the NaN it produces)
  * reaches the output rows; the call itself still returns SVL_OK.  At its
- * end every svl_prefill, svl_prefill_cache and svl_prefill_controlled clears
+ * end every svl_prefill, svl_prefill_cache(4) and svl_prefill_controlled clears
  * a status word in the last four bytes of its workspace buffer
  * (ws + (ws_bytes & ~3) - 4) and sets it to SVL_STATUS_NONFINITE if any of
  * its output values (resid rows 0 .. sum S_b - 1, S_b the final lengths) is
@@ -638,6 +638,34 @@ svl_status svl_window_attention_backward(
     const uint8_t *key_mask, const void *out, int64_t ld_out, const float *lse,
     const void *grad_out, int64_t ld_grad_out, void *grad_q, int64_t ld_grad_q, void *grad_k,
     int64_t ld_grad_k, void *grad_v, int64_t ld_grad_v, void *ws, size_t ws_bytes, void *stream);
+
+/* The prefill and the decode step on a 4-bit cache, with a window and sinks
+ * (0, 0: the whole causal range), on the 16-bit path (SVL_BF16 storage).
+ * svl_prefill_cache4 is svl_prefill_cache with two differences: its attention is
+ * svl_window_attention's, and the K / V rows it computed go into the 4-bit cache
+ * (its own rows see each other as they were computed).  svl_decode_step4 is
+ * svl_decode_step over that cache: the new row's K / V are appended, and its
+ * attention is svl_kv4_attention's, its own position included as the cache
+ * stands for it.  Arguments, masks and lengths as there (max_len <= 32768).
+ *   cache   dev, svl_cache4_bytes: [n_layers] caches of svl_kv4_cache_bytes, for
+ *           the decoder's heads; entries of skipped layers and inactive heads are
+ *           neither written nor read
+ *   ws      of svl_workspace_bytes for the prefill, svl_decode4_workspace_bytes
+ *           for the step */
+size_t svl_cache4_bytes(const svl_config *cfg, int32_t batch, int32_t max_len);
+size_t svl_decode4_workspace_bytes(const svl_config *cfg, int32_t batch, int32_t max_len);
+svl_status svl_prefill_cache4(const svl_config *cfg, const svl_layer_weights *layers,
+                              const svl_batch *batch, const float *scores, const void *vision,
+                              const void *text, const uint8_t *layer_mask,
+                              const uint8_t *head_mask, const uint8_t *ffn_mask, int32_t window,
+                              int32_t sinks, int32_t *kept_idx, float *resid, int32_t *cu_seqlens,
+                              void *cache, int32_t max_len, void *ws, size_t ws_bytes,
+                              void *stream);
+svl_status svl_decode_step4(const svl_config *cfg, const svl_layer_weights *layers, int32_t batch,
+                            float *x, const int32_t *cache_len, const uint8_t *layer_mask,
+                            const uint8_t *head_mask, const uint8_t *ffn_mask, int32_t window,
+                            int32_t sinks, void *cache, int32_t max_len, void *ws,
+                            size_t ws_bytes, void *stream);
 
 /* Message for the last non-OK status returned on this thread. */
 const char *svl_last_error(void);

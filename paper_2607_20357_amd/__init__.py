@@ -17,4 +17,5 @@ from .binding import (  # noqa: F401
     alloc_kv4_cache, alloc_kv4_workspace, alloc_window_workspace, make_attention, svl_attention,
     svl_kv4_append, svl_kv4_attention, svl_kv4_cache_bytes, svl_kv4_read, svl_kv4_workspace_bytes,
     svl_window_attention, svl_window_attention_backward, svl_window_workspace_bytes,
+    alloc_cache4, alloc_decode4_workspace, svl_cache4_bytes, svl_decode_step4, svl_prefill_cache4,
 )

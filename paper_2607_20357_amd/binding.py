@@ -148,6 +148,14 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.svl_timing_enable.argtypes = [i32]
     lib.svl_timing_read.argtypes = [i32, ctypes.POINTER(ctypes.c_double),
                                     ctypes.POINTER(ctypes.c_int64)]
+    lib.svl_cache4_bytes.argtypes = [cfgp, i32, i32]
+    lib.svl_cache4_bytes.restype = sz
+    lib.svl_decode4_workspace_bytes.argtypes = [cfgp, i32, i32]
+    lib.svl_decode4_workspace_bytes.restype = sz
+    lib.svl_prefill_cache4.argtypes = [cfgp, ctypes.POINTER(svl_layer_weights), ctypes.POINTER(svl_batch),
+                                       P, P, P, P, P, P, i32, i32, P, P, ctypes.POINTER(i32), P, i32, P, sz, P]
+    lib.svl_decode_step4.argtypes = [cfgp, ctypes.POINTER(svl_layer_weights), i32, P, P, P, P, P, i32, i32,
+                                     P, i32, P, sz, P]
     attp, i64 = ctypes.POINTER(svl_attention), ctypes.c_int64
     lib.svl_kv4_cache_bytes.argtypes = [attp, i32, i32]
     lib.svl_kv4_cache_bytes.restype = sz
@@ -167,7 +175,7 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
               "svl_prefill_controlled",
               "svl_budget_loss", "svl_train_step", "svl_workspace_status", "svl_kv4_append",
               "svl_kv4_read", "svl_kv4_attention", "svl_window_attention",
-              "svl_window_attention_backward"):
+              "svl_window_attention_backward", "svl_prefill_cache4", "svl_decode_step4"):
         getattr(lib, f).restype = i32
     _lib = lib
     return lib
@@ -1030,3 +1038,74 @@ def svl_window_attention_backward(att: svl_attention, cu_q, cu_k, q: torch.Tenso
     _check(load_library().svl_window_attention_backward(
         ctypes.byref(att), B, cqp, ckp, *arrays[:6], None if mask is None else _dev(mask, "key_mask"),
         *arrays[6:8], _dev(lse, "lse"), *arrays[8:], _dev(ws, "ws"), _nbytes(ws), _stream(stream)))
+
+
+def svl_cache4_bytes(cfg: svl_config, batch: int, max_len: int) -> int:
+    n = int(load_library().svl_cache4_bytes(ctypes.byref(cfg), int(batch), int(max_len)))
+    if n == 0:
+        raise SvlError(2, "bad 4-bit cache shape")
+    return n
+
+
+def alloc_cache4(cfg: svl_config, batch: int, max_len: int, device="cuda") -> torch.Tensor:
+    """Caller-owned 4-bit cache of every layer, as [layer][bytes]: row l is the cache of
+    svl_kv4_read and svl_kv4_attention for layer l."""
+    return torch.empty((cfg.n_layers, svl_cache4_bytes(cfg, batch, max_len) // cfg.n_layers),
+                       dtype=torch.uint8, device=device)
+
+
+def alloc_decode4_workspace(cfg: svl_config, batch: int, max_len: int, device="cuda") -> torch.Tensor:
+    n = int(load_library().svl_decode4_workspace_bytes(ctypes.byref(cfg), int(batch), int(max_len)))
+    if n == 0:
+        raise SvlError(2, "bad decode workspace shape")
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+def svl_prefill_cache4(cfg: svl_config, layers, keep, scores: torch.Tensor, vision: torch.Tensor,
+                       text: torch.Tensor, layer_mask, head_mask, ffn_mask, window: int, sinks: int,
+                       kept_idx: torch.Tensor, resid: torch.Tensor, cache: torch.Tensor, max_len: int,
+                       ws: torch.Tensor, stream=None) -> np.ndarray:
+    """svl_prefill_cache with a window and sinks, into a 4-bit cache; returns cu_seqlens."""
+    kp, kpp = _host_i32(keep)
+    B, N, T = _batch_dims(scores, text)
+    R = _check_keep(kp, B, N) + B * T
+    L, A, G = cfg.n_layers, cfg.n_heads, cfg.n_groups
+    _check_hidden(cfg, B, N, T, scores, vision, text, kept_idx)
+    _expect(resid, "resid", torch.float32, R * cfg.d_model)
+    _expect(cache, "cache", torch.uint8, svl_cache4_bytes(cfg, B, max_len))
+    batch = svl_batch(int(B), int(N), int(T), kpp)
+    lm, lmp = _host_mask(layer_mask, "layer_mask", (B, L))
+    hm, hmp = _host_mask(head_mask, "head_mask", (B, L, A))
+    fm, fmp = (None, None) if ffn_mask is None else _host_mask(ffn_mask, "ffn_mask", (B, L, G))
+    cu = np.zeros(B + 1, dtype=np.int32)
+    table = _table(cfg, layers)
+    _check(load_library().svl_prefill_cache4(
+        ctypes.byref(cfg), table.array, ctypes.byref(batch), _dev(scores, "scores"),
+        _dev(vision, "vision"), _dev(text, "text"), lmp, hmp, fmp, int(window), int(sinks),
+        _dev(kept_idx, "kept_idx"), _dev(resid, "resid"),
+        cu.ctypes.data_as(ctypes.POINTER(ctypes.c_int32)), _dev(cache, "cache"), int(max_len),
+        _dev(ws, "ws"), _nbytes(ws), _stream(stream)))
+    return cu
+
+
+def svl_decode_step4(cfg: svl_config, layers, x: torch.Tensor, cache_len, layer_mask, head_mask,
+                     ffn_mask, window: int, sinks: int, cache: torch.Tensor, max_len: int,
+                     ws: torch.Tensor, stream=None) -> None:
+    """One decode step on the 4-bit cache, x [B][D] float32 updated in place; the caller
+    advances cache_len."""
+    if not isinstance(x, torch.Tensor) or x.dim() != 2:
+        raise ValueError("x must be a [B][D] tensor")
+    B = int(x.shape[0])
+    L, A, G = cfg.n_layers, cfg.n_heads, cfg.n_groups
+    _expect(x, "x", torch.float32, B * cfg.d_model, (B, cfg.d_model))
+    _expect(cache, "cache", torch.uint8, svl_cache4_bytes(cfg, B, max_len))
+    cl, clp = _host_i32(cache_len)
+    if cl.shape != (B,):
+        raise ValueError(f"cache_len has shape {cl.shape}, expected ({B},)")
+    lm, lmp = _host_mask(layer_mask, "layer_mask", (B, L))
+    hm, hmp = _host_mask(head_mask, "head_mask", (B, L, A))
+    fm, fmp = (None, None) if ffn_mask is None else _host_mask(ffn_mask, "ffn_mask", (B, L, G))
+    table = _table(cfg, layers)
+    _check(load_library().svl_decode_step4(
+        ctypes.byref(cfg), table.array, B, _dev(x, "x"), clp, lmp, hmp, fmp, int(window), int(sinks),
+        _dev(cache, "cache"), int(max_len), _dev(ws, "ws"), _nbytes(ws), _stream(stream)))

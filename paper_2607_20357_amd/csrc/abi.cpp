@@ -13,6 +13,7 @@
 #include <vector>
 
 #include "../../include/svl.h"
+#include "attn_ops.h"
 #include "budget.h"
 #include "plan.h"
 #include "svl_internal.h"
@@ -192,6 +193,11 @@ struct Exec {
   int32_t max_len = 0;
   int32_t batch = 0;
   bool decode = false;   // one new row per sample: attention over the cache
+  // 4-bit cache in place of the 16-bit one, and the attention's key range
+  // (svl_prefill_cache4, svl_decode_step4)
+  uint8_t* cache4 = nullptr;
+  int32_t window = 0, sinks = 0;
+  float* partial4 = nullptr;   // decode: pieces of long key ranges
 
   template <class T>
   const T* at(int64_t off) const { return reinterpret_cast<const T*>(ws + L.plan + off); }
@@ -312,6 +318,76 @@ struct Exec {
     return timed(K_NORM, st, [&] { return launch_resid_norm(a, out_kind, st); });
   }
 
+  // The layer's attention with a window and a 4-bit cache: this call's K / V rows
+  // into the cache, then a prefill's rows among themselves (as they are), or a
+  // decode step's over the cache (its own row among it).
+  hipError_t attention4(const LayerPlan& P, int32_t l) const {
+    const int A = c.n_heads, KV = c.n_kv_heads, d = c.head_dim, qkv_w = (A + 2 * KV) * d;
+    const bool f16 = c.compute == SVL_COMPUTE_F16;
+    const uint16_t* qkv = reinterpret_cast<const uint16_t*>(ws + L.qkv);
+    // the launches take their segments from the host's copy of the plan
+    const AttnGroup* groups = reinterpret_cast<const AttnGroup*>(plan.image.data() + P.attn.groups_off);
+    const int64_t tiles = (max_len + KV4_TILE - 1) / KV4_TILE;
+    Kv4Args a{};
+    a.kv_table = at<int32_t>(P.attn.kvheads_off);
+    a.n_kv_heads = KV;
+    a.rep = A / KV;
+    a.k = qkv + A * d;
+    a.v = qkv + (A + KV) * d;
+    a.ldk = a.ldv = a.ldq = qkv_w;
+    a.cache = cache4 + (int64_t)l * batch * KV * tiles * kv4_tile_bytes(d);
+    a.tiles = tiles;
+    a.scale = 1.0f / std::sqrt((float)d);
+    a.window = window;
+    a.sinks = sinks;
+    const auto seg = [](const void* ctx, int32_t i) {
+      const AttnGroup& g = static_cast<const AttnGroup*>(ctx)[i];
+      CacheSeg s{};
+      s.row0 = g.row0;
+      s.rows = g.S;
+      s.pos0 = g.pos_base;
+      s.sample = g.sample;
+      s.kv_off = g.kv_off;
+      s.kv_cnt = g.kv_cnt;
+      return s;
+    };
+    hipError_t e = kv4_append_segments(a, seg, groups, P.attn.ngroups, d, f16, st);
+    if (e != hipSuccess) return e;
+    if (decode) {
+      a.q = qkv;
+      a.out = ws + L.attn_out;
+      a.ldo = A * d;
+      a.partial = partial4;
+      return kv4_attention_segments(a, seg, groups, P.attn.ngroups, d, f16, st);
+    }
+    WinArgs w{};
+    w.head_table = at<int32_t>(P.attn.heads_off);
+    w.n_heads = A;
+    w.n_kv_heads = KV;
+    w.q = qkv;
+    w.k = a.k;
+    w.v = a.v;
+    w.ldq = w.ldk = w.ldv = qkv_w;
+    w.out = ws + L.attn_out;
+    w.ldo = A * d;
+    w.packed = 1;
+    w.scale = a.scale;
+    w.window = window;
+    w.sinks = sinks;
+    return window_segments(
+        w,
+        [](const void* ctx, int32_t i) {
+          const AttnGroup& g = static_cast<const AttnGroup*>(ctx)[i];
+          WinSeg s{};
+          s.q0 = s.k0 = g.row0;
+          s.nq = s.nk = g.S;
+          s.h_off = g.h_off;
+          s.h_cnt = g.h_cnt;
+          return s;
+        },
+        groups, P.attn.ngroups, d, f16, st);
+  }
+
   // Output / down projection: straight into the residual, or split-K
   // pieces into the partial slices the next residual-finish launch adds.
   static int resid_epi(const GemmLaunch& g) { return g.nsplit > 1 ? EPI_PARTIAL : EPI_RESID; }
@@ -347,6 +423,9 @@ struct Exec {
       a.ldo = A * d;
       a.rope = reinterpret_cast<const float2*>(ws + L.rope);
       a.scale = 1.0f / std::sqrt((float)d);
+      if (cache4) {
+        if ((e = attention4(P, l)) != hipSuccess) return e;
+      }
       // active K/V heads per group: the cache append and the grouped-K/V
       // prefill attention read them
       a.kvhead_table = at<int32_t>(P.attn.kvheads_off);
@@ -361,7 +440,7 @@ struct Exec {
           if (e != hipSuccess) return e;
         }
       }
-      e = timed(K_ATTN, st, [&] {
+      if (!cache4) e = timed(K_ATTN, st, [&] {
         if (decode) return launch_attn_decode(a, d, c.compute == SVL_COMPUTE_F16, st);
         return mfma ? launch_attn_mfma(a, d, c.compute == SVL_COMPUTE_F16, st)
                     : launch_attn_f32(a, d, st);
@@ -700,6 +779,22 @@ static svl_status check_layers(const svl_config& c, const svl_layer_weights* lay
   return SVL_OK;
 }
 
+// A 4-bit cache and the key range of the attention that goes with it.
+struct Cache4 {
+  void* cache;
+  int32_t window, sinks;
+};
+
+static svl_status check_cache4(const svl_config& c, const Cache4& k, int32_t max_len) {
+  if (c.dtype != SVL_BF16) return fail(SVL_E_DTYPE, "the KV cache is on the 16-bit path only");
+  if (!k.cache) return fail(SVL_E_NULL, "cache is NULL");
+  if (!aligned16(k.cache)) return fail(SVL_E_ALIGN, "cache not 16-byte aligned");
+  if (k.window < 0 || k.sinks < 0)
+    return fail(SVL_E_VALUE, "window = %d and sinks = %d must not be negative", k.window, k.sinks);
+  if (max_len <= 0 || max_len > 32768) return fail(SVL_E_SHAPE, "max_len outside [1, 32768]");
+  return SVL_OK;
+}
+
 // The prefill, optionally writing every layer's K / V rows into a cache.
 static svl_status prefill_impl(const svl_config* cfg, const svl_layer_weights* layers,
                                const svl_batch* batch, const float* scores, const void* vision,
@@ -707,9 +802,10 @@ static svl_status prefill_impl(const svl_config* cfg, const svl_layer_weights* l
                                const uint8_t* head_mask, const uint8_t* ffn_mask,
                                int32_t* kept_idx, float* resid, int32_t* cu_seqlens,
                                svl_flops* flops, void* ws, size_t ws_bytes, void* stream,
-                               void* cache, int32_t max_len) {
+                               void* cache, int32_t max_len, const Cache4* cache4 = nullptr) {
   svl_status s = check_config(cfg);
   if (s != SVL_OK) return s;
+  if (cache4 && (s = check_cache4(*cfg, *cache4, max_len)) != SVL_OK) return s;
   if ((s = check_batch(*cfg, batch)) != SVL_OK) return s;
   if (!layer_mask || !head_mask || !cu_seqlens) return fail(SVL_E_NULL, "NULL argument");
   const int32_t B = batch->batch, L = cfg->n_layers, A = cfg->n_heads, G = cfg->n_groups;
@@ -725,6 +821,8 @@ static svl_status prefill_impl(const svl_config* cfg, const svl_layer_weights* l
     if (cfg->dtype != SVL_BF16) return fail(SVL_E_DTYPE, "the KV cache is on the 16-bit path only");
     if (!aligned16(cache)) return fail(SVL_E_ALIGN, "kv_cache not 16-byte aligned");
     if (max_len <= 0 || max_len > 32768) return fail(SVL_E_SHAPE, "max_len outside [1, 32768]");
+  }
+  if (cache || cache4) {
     for (int32_t b = 0; b < B; ++b)
       if (seq[b] > max_len) return fail(SVL_E_SHAPE, "sample %d has %d rows > max_len %d", b, seq[b], max_len);
   }
@@ -745,6 +843,11 @@ static svl_status prefill_impl(const svl_config* cfg, const svl_layer_weights* l
   ex.cache = static_cast<uint8_t*>(cache);
   ex.max_len = max_len;
   ex.batch = B;
+  if (cache4) {
+    ex.cache4 = static_cast<uint8_t*>(cache4->cache);
+    ex.window = cache4->window;
+    ex.sinks = cache4->sinks;
+  }
   if ((s = stage(ex, true)) != SVL_OK) return s;
   if ((s = select_and_gather(ex, *batch, scores, vision, text, kept_idx, R)) != SVL_OK) return s;
   for (int32_t l = 0; l < L; ++l) {
@@ -783,6 +886,17 @@ svl_status svl_prefill_cache(const svl_config* cfg, const svl_layer_weights* lay
                       kept_idx, resid, cu_seqlens, nullptr, ws, ws_bytes, stream, kv_cache, max_len);
 }
 
+svl_status svl_prefill_cache4(const svl_config* cfg, const svl_layer_weights* layers,
+                              const svl_batch* batch, const float* scores, const void* vision,
+                              const void* text, const uint8_t* layer_mask, const uint8_t* head_mask,
+                              const uint8_t* ffn_mask, int32_t window, int32_t sinks,
+                              int32_t* kept_idx, float* resid, int32_t* cu_seqlens, void* cache,
+                              int32_t max_len, void* ws, size_t ws_bytes, void* stream) {
+  const Cache4 c4{cache, window, sinks};
+  return prefill_impl(cfg, layers, batch, scores, vision, text, layer_mask, head_mask, ffn_mask,
+                      kept_idx, resid, cu_seqlens, nullptr, ws, ws_bytes, stream, nullptr, max_len, &c4);
+}
+
 svl_status svl_workspace_status(const void* ws, size_t ws_bytes, uint32_t* status, void* stream) {
   if (!ws || !status) return fail(SVL_E_NULL, "ws and status are required");
   if (!aligned16(ws)) return fail(SVL_E_ALIGN, "workspace not 16-byte aligned");
@@ -805,6 +919,19 @@ size_t svl_kv_cache_bytes(const svl_config* cfg, int32_t batch, int32_t max_len)
 size_t svl_decode_workspace_bytes(const svl_config* cfg, int32_t batch, int32_t max_len) {
   if (check_config(cfg) != SVL_OK || batch <= 0 || max_len <= 0 || max_len > 32768) return 0;
   return (size_t)ws_layout(*cfg, batch, batch, max_len).total;
+}
+
+size_t svl_cache4_bytes(const svl_config* cfg, int32_t batch, int32_t max_len) {
+  if (check_config(cfg) != SVL_OK || cfg->dtype != SVL_BF16 || batch <= 0 || max_len <= 0 ||
+      max_len > 32768)
+    return 0;
+  return (size_t)cfg->n_layers * batch * cfg->n_kv_heads * ((max_len + KV4_TILE - 1) / KV4_TILE) *
+         kv4_tile_bytes(cfg->head_dim);
+}
+
+size_t svl_decode4_workspace_bytes(const svl_config* cfg, int32_t batch, int32_t max_len) {
+  const size_t n = svl_decode_workspace_bytes(cfg, batch, max_len);
+  return n == 0 || cfg->dtype != SVL_BF16 ? 0 : n + kv4_partial_bytes(cfg->head_dim);
 }
 
 // Device scratch of svl_decode_step_noalloc: one copy per GPU, held until
@@ -846,10 +973,14 @@ static svl_status decode_impl(const svl_config* cfg, const svl_layer_weights* la
                               float* x, const int32_t* cache_len, const uint8_t* layer_mask,
                               const uint8_t* head_mask, const uint8_t* ffn_mask, void* kv_cache,
                               int32_t max_len, void* ws, size_t ws_bytes, void* stream,
-                              bool noalloc) {
+                              bool noalloc, const Cache4* cache4 = nullptr) {
   svl_status s = check_config(cfg);
   if (s != SVL_OK) return s;
   if (cfg->dtype != SVL_BF16) return fail(SVL_E_DTYPE, "decode runs on the 16-bit path only");
+  if (cache4) {
+    if ((s = check_cache4(*cfg, *cache4, max_len)) != SVL_OK) return s;
+    kv_cache = cache4->cache;
+  }
   if (batch <= 0) return fail(SVL_E_SHAPE, "batch must be positive");
   if (!x || !cache_len || !layer_mask || !head_mask || !kv_cache || (!noalloc && !ws))
     return fail(SVL_E_NULL, "NULL argument");
@@ -874,8 +1005,9 @@ static svl_status decode_impl(const svl_config* cfg, const svl_layer_weights* la
     if ((s = scratch_address(&ws)) != SVL_OK) return s;
     ws_bytes = SVL_NOALLOC_SCRATCH_BYTES;
   }
-  if ((int64_t)ws_bytes < WL.total)
-    return fail(SVL_E_WORKSPACE, "workspace %zu bytes < %lld needed", ws_bytes, (long long)WL.total);
+  const int64_t need = WL.total + (cache4 ? (int64_t)kv4_partial_bytes(cfg->head_dim) : 0);
+  if ((int64_t)ws_bytes < need)
+    return fail(SVL_E_WORKSPACE, "workspace %zu bytes < %lld needed", ws_bytes, (long long)need);
   std::vector<int32_t> seq(batch, 1);
   std::vector<LayerMasks> masks;
   std::vector<uint8_t> lon;
@@ -884,10 +1016,16 @@ static svl_status decode_impl(const svl_config* cfg, const svl_layer_weights* la
   if (!build_plan(*cfg, batch, nullptr, seq.data(), L, masks.data(), &t_plan, &err, cache_len))
     return fail(SVL_E_VALUE, "%s", err.c_str());
   Exec ex{*cfg, (hipStream_t)stream, static_cast<uint8_t*>(ws), WL, t_plan, x};
-  ex.cache = static_cast<uint8_t*>(kv_cache);
+  ex.cache = cache4 ? nullptr : static_cast<uint8_t*>(kv_cache);
   ex.max_len = max_len;
   ex.batch = batch;
   ex.decode = true;
+  if (cache4) {
+    ex.cache4 = static_cast<uint8_t*>(cache4->cache);
+    ex.window = cache4->window;
+    ex.sinks = cache4->sinks;
+    ex.partial4 = reinterpret_cast<float*>(ex.ws + WL.total);
+  }
   if ((s = stage(ex, true, noalloc)) != SVL_OK) return s;
   for (int32_t l = 0; l < L; ++l) {
     hipError_t e = ex.layer(t_plan.layers[l], layers[l], l);
@@ -913,6 +1051,16 @@ svl_status svl_decode_step_noalloc(const svl_config* cfg, const svl_layer_weight
                                    void* stream) {
   return decode_impl(cfg, layers, batch, x, cache_len, layer_mask, head_mask, ffn_mask, kv_cache,
                      max_len, nullptr, 0, stream, true);
+}
+
+svl_status svl_decode_step4(const svl_config* cfg, const svl_layer_weights* layers, int32_t batch,
+                            float* x, const int32_t* cache_len, const uint8_t* layer_mask,
+                            const uint8_t* head_mask, const uint8_t* ffn_mask, int32_t window,
+                            int32_t sinks, void* cache, int32_t max_len, void* ws, size_t ws_bytes,
+                            void* stream) {
+  const Cache4 c4{cache, window, sinks};
+  return decode_impl(cfg, layers, batch, x, cache_len, layer_mask, head_mask, ffn_mask, nullptr, max_len,
+                     ws, ws_bytes, stream, false, &c4);
 }
 
 svl_status svl_count_positive(int32_t batch, int32_t n_vision, const float* logits,

@@ -23,8 +23,9 @@ def test_exports():
     assert names == {"svl_kv4_cache_bytes", "svl_kv4_append", "svl_kv4_read", "svl_kv4_workspace_bytes",
                      "svl_kv4_attention", "svl_window_attention", "svl_window_workspace_bytes",
                      "svl_window_attention_backward"}
-    for n in names:
+    for n in names | {"svl_cache4_bytes", "svl_prefill_cache4", "svl_decode_step4"}:
         assert hasattr(svl.load_library(), n) and hasattr(svl, n)
+    assert hasattr(svl.load_library(), "svl_decode4_workspace_bytes")
 
 
 def test_cache_bytes():
