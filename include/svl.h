@@ -540,7 +540,7 @@ svl_status svl_decode_step_noalloc(const svl_config *cfg, const svl_layer_weight
  * sums are float32; rows are fp16 or bf16 (`compute`), head_dim 64 or 128.
  *
  * Rows are [row][head][head_dim] with a row stride ld in elements, at least
- * heads * head_dim and a multiple of 8, so Q, K and V may be slices of one packed
+ * heads * head_dim, at most 2^23 and a multiple of 8, so Q, K and V may be slices of one packed
  * projection.  cu_* are host arrays [batch + 1] of row offsets (from 0 or more,
  * not decreasing; a sample may have no rows).  They are read before the call
  * returns and travel with the launches: nothing is copied to the device, and a

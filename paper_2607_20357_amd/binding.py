@@ -837,39 +837,54 @@ def _row_dtype(att: svl_attention) -> torch.dtype:
     return torch.bfloat16 if att.compute == SVL_COMPUTE_BF16 else torch.float16
 
 
+def _launch_stream(stream):
+    """_stream, without a Stream object where the current stream is meant."""
+    if stream is None:
+        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+    return _stream(stream)
+
+
+def _host_array(a):
+    """(contiguous int32 array, its address): no copy of an array that is one already."""
+    if not (type(a) is np.ndarray and a.dtype == np.int32 and a.flags.c_contiguous):
+        a = np.ascontiguousarray(np.asarray(a, dtype=np.int32))
+    return a, a.__array_interface__["data"][0]
+
+
 def _cu(a, name: str):
-    """Host int32 [batch + 1] row offsets and their pointer."""
-    arr, ptr = _host_i32(a)
+    """Host int32 [batch + 1] row offsets and their address."""
+    arr, ptr = _host_array(a)
     if arr.ndim != 1 or arr.shape[0] < 2:
         raise ValueError(f"{name} must be a host array of batch + 1 entries")
-    return arr, ctypes.cast(ptr, ctypes.c_void_p)
+    return arr, ptr
 
 
 def _host_pos(a, batch: int):
-    arr, ptr = _host_i32(a)
+    arr, ptr = _host_array(a)
     if arr.shape != (batch,):
         raise ValueError(f"pos has shape {arr.shape}, expected ({batch},)")
-    return arr, ctypes.cast(ptr, ctypes.c_void_p)
+    return arr, ptr
 
 
-def _row_stride(t: Optional[torch.Tensor], name: str, att: svl_attention, heads: int,
+def _row_stride(t: Optional[torch.Tensor], name: str, dtype: torch.dtype, d: int, heads: int,
                 rows: int) -> int:
-    """Row stride of 16-bit rows [>= rows][heads][head_dim]: heads and dims contiguous, the
-    rows any multiple of 8 elements apart."""
+    """Row stride of 16-bit rows [>= rows][heads][d]: heads and dims contiguous, the rows any
+    multiple of 8 elements apart."""
     if not isinstance(t, torch.Tensor):
         raise ValueError(f"{name} must be a torch tensor")
-    if t.dtype != _row_dtype(att):
-        raise ValueError(f"{name} has dtype {t.dtype}, expected {_row_dtype(att)}")
-    d = att.head_dim
-    if t.dim() != 3 or tuple(t.shape[1:]) != (heads, d):
-        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected (rows, {heads}, {d})")
-    if t.shape[0] < rows:
-        raise ValueError(f"{name} holds {t.shape[0]} rows, needs at least {rows}")
-    if t.numel() == 0:
+    if t.dtype != dtype:
+        raise ValueError(f"{name} has dtype {t.dtype}, expected {dtype}")
+    shape = t.shape
+    if len(shape) != 3 or shape[1] != heads or shape[2] != d:
+        raise ValueError(f"{name} has shape {tuple(shape)}, expected (rows, {heads}, {d})")
+    if shape[0] < rows:
+        raise ValueError(f"{name} holds {shape[0]} rows, needs at least {rows}")
+    if shape[0] == 0:
         return heads * d
-    if t.stride(2) != 1 or (t.stride(1) != d and heads > 1):
-        raise ValueError(f"{name}: heads and dims must be contiguous, strides are {t.stride()}")
-    ld = t.stride(0) if t.shape[0] > 1 else heads * d
+    strides = t.stride()
+    if strides[2] != 1 or (strides[1] != d and heads > 1):
+        raise ValueError(f"{name}: heads and dims must be contiguous, strides are {strides}")
+    ld = strides[0] if shape[0] > 1 else heads * d
     if ld < heads * d or ld % 8:
         raise ValueError(f"{name}: row stride {ld} must be at least {heads * d} and a multiple of 8")
     return ld
@@ -878,19 +893,21 @@ def _row_stride(t: Optional[torch.Tensor], name: str, att: svl_attention, heads:
 def _rows(att: svl_attention, *arrays):
     """(device pointer, row stride) of each (tensor, name, heads, rows), one after another;
     all are checked before the first pointer is taken."""
-    strides = [_row_stride(t, name, att, heads, rows) for t, name, heads, rows in arrays]
-    return [x for (t, name, _, _), ld in zip(arrays, strides)
-            for x in (_on_device(t, name) if t.numel() else None, ld)]
-
-
-def _on_device(t: torch.Tensor, name: str) -> int:
-    """Device pointer of a GPU tensor of the current device, whatever its strides."""
-    if not t.is_cuda:
-        raise ValueError(f"{name} must be a GPU tensor (no CPU path exists)")
-    if t.device.index != torch.cuda.current_device():
-        raise ValueError(f"{name} is on {t.device}, the library launches on "
-                         f"cuda:{torch.cuda.current_device()}")
-    return t.data_ptr()
+    dtype, d = _row_dtype(att), att.head_dim
+    strides = [_row_stride(t, name, dtype, d, heads, rows) for t, name, heads, rows in arrays]
+    here, out = None, []
+    for (t, name, _, _), ld in zip(arrays, strides):
+        if t.shape[0] == 0:
+            out += (None, ld)
+            continue
+        if not t.is_cuda:
+            raise ValueError(f"{name} must be a GPU tensor (no CPU path exists)")
+        if here is None:
+            here = torch.cuda.current_device()
+        if t.get_device() != here:
+            raise ValueError(f"{name} is on {t.device}, the library launches on cuda:{here}")
+        out += (t.data_ptr(), ld)
+    return out
 
 
 def _log_sums(lse: Optional[torch.Tensor], att: svl_attention, rows: int) -> Optional[torch.Tensor]:
@@ -928,7 +945,8 @@ def _cache_rows(att: svl_attention, cu_rows, pos, cache: torch.Tensor, max_len: 
     cu, cup = _cu(cu_rows, "cu_rows")
     B = int(cu.shape[0]) - 1
     ps, psp = _host_pos(pos, B)
-    _expect(cache, "cache", torch.uint8, svl_kv4_cache_bytes(att, B, max_len))
+    # (a description that is not valid is the library's to refuse)
+    _expect(cache, "cache", torch.uint8, B * att.n_kv_heads * -(-int(max_len) // 16) * 18 * att.head_dim)
     # the arrays stay referenced until the call is made
     return B, max(int(cu[-1]), 0), cu, cup, ps, psp
 
@@ -940,7 +958,7 @@ def svl_kv4_append(att: svl_attention, cu_rows, pos, k: torch.Tensor, v: torch.T
     H = att.n_kv_heads
     kp, ldk, vp, ldv = _rows(att, (k, "k", H, n), (v, "v", H, n))
     _check(load_library().svl_kv4_append(ctypes.byref(att), B, cup, psp, kp, ldk, vp, ldv,
-                                         _dev(cache, "cache"), int(max_len), _stream(stream)))
+                                         _dev(cache, "cache"), int(max_len), _launch_stream(stream)))
 
 
 def svl_kv4_read(att: svl_attention, cu_rows, pos, cache: torch.Tensor, max_len: int,
@@ -950,7 +968,7 @@ def svl_kv4_read(att: svl_attention, cu_rows, pos, cache: torch.Tensor, max_len:
     H = att.n_kv_heads
     kp, ldk, vp, ldv = _rows(att, (k, "k", H, n), (v, "v", H, n))
     _check(load_library().svl_kv4_read(ctypes.byref(att), B, cup, psp, _dev(cache, "cache"),
-                                       int(max_len), kp, ldk, vp, ldv, _stream(stream)))
+                                       int(max_len), kp, ldk, vp, ldv, _launch_stream(stream)))
 
 
 def svl_kv4_workspace_bytes(att: svl_attention) -> int:
@@ -975,7 +993,7 @@ def svl_kv4_attention(att: svl_attention, cu_rows, pos, q: torch.Tensor, cache: 
     qp, ldq, op, ldo = _rows(att, (q, "q", A, n), (out, "out", A, n))
     _check(load_library().svl_kv4_attention(ctypes.byref(att), B, cup, psp, qp, ldq,
                                             _dev(cache, "cache"), int(max_len), op, ldo,
-                                            _dev(ws, "ws"), _nbytes(ws), _stream(stream)))
+                                            _dev(ws, "ws"), _nbytes(ws), _launch_stream(stream)))
 
 
 def _packed_rows(cu_q, cu_k):
@@ -1002,7 +1020,7 @@ def svl_window_attention(att: svl_attention, cu_q, cu_k, q: torch.Tensor, k: tor
     *ins, op, ldo = _rows(att, (q, "q", A, n), (k, "k", H, m), (v, "v", H, m), (out, "out", A, n))
     _check(load_library().svl_window_attention(
         ctypes.byref(att), B, cqp, ckp, *ins, None if mask is None else _dev(mask, "key_mask"), op, ldo,
-        None if lse is None else _dev(lse, "lse"), _stream(stream)))
+        None if lse is None else _dev(lse, "lse"), _launch_stream(stream)))
 
 
 def svl_window_workspace_bytes(att: svl_attention, cu_q, cu_k=None) -> int:
@@ -1037,7 +1055,7 @@ def svl_window_attention_backward(att: svl_attention, cu_q, cu_k, q: torch.Tenso
                    (grad_v, "grad_v", H, m))
     _check(load_library().svl_window_attention_backward(
         ctypes.byref(att), B, cqp, ckp, *arrays[:6], None if mask is None else _dev(mask, "key_mask"),
-        *arrays[6:8], _dev(lse, "lse"), *arrays[8:], _dev(ws, "ws"), _nbytes(ws), _stream(stream)))
+        *arrays[6:8], _dev(lse, "lse"), *arrays[8:], _dev(ws, "ws"), _nbytes(ws), _launch_stream(stream)))
 
 
 def svl_cache4_bytes(cfg: svl_config, batch: int, max_len: int) -> int:
@@ -1084,7 +1102,7 @@ def svl_prefill_cache4(cfg: svl_config, layers, keep, scores: torch.Tensor, visi
         _dev(vision, "vision"), _dev(text, "text"), lmp, hmp, fmp, int(window), int(sinks),
         _dev(kept_idx, "kept_idx"), _dev(resid, "resid"),
         cu.ctypes.data_as(ctypes.POINTER(ctypes.c_int32)), _dev(cache, "cache"), int(max_len),
-        _dev(ws, "ws"), _nbytes(ws), _stream(stream)))
+        _dev(ws, "ws"), _nbytes(ws), _launch_stream(stream)))
     return cu
 
 
@@ -1108,4 +1126,4 @@ def svl_decode_step4(cfg: svl_config, layers, x: torch.Tensor, cache_len, layer_
     table = _table(cfg, layers)
     _check(load_library().svl_decode_step4(
         ctypes.byref(cfg), table.array, B, _dev(x, "x"), clp, lmp, hmp, fmp, int(window), int(sinks),
-        _dev(cache, "cache"), int(max_len), _dev(ws, "ws"), _nbytes(ws), _stream(stream)))
+        _dev(cache, "cache"), int(max_len), _dev(ws, "ws"), _nbytes(ws), _launch_stream(stream)))

@@ -78,9 +78,9 @@ svl_status check_array(const void* p, int64_t ld, int64_t width, int64_t rows, c
   if (rows <= 0) return SVL_OK;
   if (!p) return err(SVL_E_NULL, "%s is NULL", what);
   if (!is_aligned16(p)) return err(SVL_E_ALIGN, "%s not 16-byte aligned", what);
-  if (ld < width || ld % 8)
-    return err(SVL_E_SHAPE, "row stride %lld of %s: at least %lld and a multiple of 8", (long long)ld,
-               what, (long long)width);
+  if (ld < width || ld % 8 || ld > (1 << 23))
+    return err(SVL_E_SHAPE, "row stride %lld of %s: at least %lld, at most 2^23 and a multiple of 8",
+               (long long)ld, what, (long long)width);
   return SVL_OK;
 }
 
@@ -194,7 +194,7 @@ int64_t seg_units(const Kv4Args& a, const CacheSeg& s) {
 }
 
 // Key / value gradient of the windowed attention: how its work is cut.
-constexpr int64_t kDkvTarget = 512, kDkvMin = 8;   // work items of a launch; list entries of a piece
+constexpr int64_t kDkvTarget = 512, kDkvMin = 4;   // work items of a launch; list entries of a piece
 
 // Fills a.seg with the next samples from b on; returns the next sample.  dkv: the
 // work items of the key / value gradient, otherwise those of the query gradient.
@@ -229,8 +229,8 @@ int32_t bwd_segments(WinBwdArgs& a, int32_t batch, const int32_t* cu_q, const in
     s.item0 = (int32_t)items;
     if (dkv) {
       const int64_t nkt = cdiv(s.nk, WIN_DK);
-      s.ps = (int32_t)std::max<int64_t>(1, cdiv(w_sink[i], per));
-      s.po = (int32_t)std::max<int64_t>(1, cdiv(w_other[i], per));
+      s.ps = (int32_t)std::max<int64_t>(1, (w_sink[i] + per / 2) / per);
+      s.po = (int32_t)std::max<int64_t>(1, (w_other[i] + per / 2) / per);
       const int64_t n_sink = KV * s.nst * s.ps, n_other = KV * (nkt - s.nst) * s.po;
       s.part0 = (int32_t)*blocks;
       if (s.ps > 1) *blocks += n_sink;

@@ -107,7 +107,7 @@ hipError_t launch_window_attention(const WinArgs& a, int32_t head_dim, bool f16,
 // head, each cut into pieces of its (query head, tile of WIN_DQ query rows)
 // list; the first nst tiles (those with sink positions, seen by every later
 // row) into ps pieces, the others into po.
-constexpr int WIN_DK = 128, WIN_DQ = 32;
+constexpr int WIN_DK = 128, WIN_DQ = 64;
 struct WinBwdSeg {
   int32_t q0, nq, k0, nk;
   int32_t nst, ps, po;

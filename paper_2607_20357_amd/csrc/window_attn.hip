@@ -23,13 +23,10 @@ namespace {
 template <int D, bool F16, int KP>
 __global__ __launch_bounds__(256, 2) void window_attn_kernel(WinArgs a) {
   constexpr int NT = 256, QG = 4 / KP, BQ = 32 * QG, BK = WIN_BK, KB = 2 / KP;
-  constexpr int KS = D + 8;      // K row stride (elements): 16-byte reads of 32 rows spread over the banks
-  constexpr int VS = D + 32;     // V row stride: the 4 x 32-byte rows of a transposed read spread over them
   constexpr int NS = D / 16, NB = D / 32;
   constexpr int PR = D / 8, LD = BK * PR / NT;    // 16-byte pieces of a row, and of a tile per thread
-  __shared__ __attribute__((aligned(16))) uint16_t Ks[BK * KS];
-  __shared__ __attribute__((aligned(16))) uint16_t Vs[BK * VS];
-  __shared__ uint32_t s_bad[2][2];                // keys of a tile with an inf or NaN in V, two tiles in turn
+  __shared__ __attribute__((aligned(16))) uint16_t s_kv[2][2 * BK * D];   // two tiles in turn: K, then V
+  __shared__ uint32_t s_bad[3][2];                // keys of a tile with an inf or NaN in V, three tiles in turn
   const int item = blockIdx.x;
   if (item >= a.nitems) return;
   const WinSeg& sg = a.seg[find_item_seg(a, item)];
@@ -42,7 +39,7 @@ __global__ __launch_bounds__(256, 2) void window_attn_kernel(WinArgs a) {
   const int qt = nqt - 1 - local / sg.h_cnt;      // longest tiles first
   const int h = a.head_table ? a.head_table[sg.h_off + slot] : slot;
   const int kvh = h / (a.n_heads / a.n_kv_heads);
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int qg = wave % QG, part = wave / QG;
   const int half = lane >> 5, lq = lane & 31;
   const int off = sg.nk - sg.nq;
@@ -59,23 +56,50 @@ __global__ __launch_bounds__(256, 2) void window_attn_kernel(WinArgs a) {
 #pragma unroll
     for (int s = 0; s < NS; ++s) qf[s] = load_piece(qp + 16 * s);
   }
-  const uint16_t* kbase = static_cast<const uint16_t*>(a.k) + (int64_t)sg.k0 * a.ldk + (int64_t)kvh * D;
-  const uint16_t* vbase = static_cast<const uint16_t*>(a.v) + (int64_t)sg.k0 * a.ldv + (int64_t)kvh * D;
   const uint8_t* mask = a.key_mask ? a.key_mask + sg.k0 : nullptr;
 
-  // key tiles: [0, us) for the sinks, then from uw on
-  const int start = a.window > 0 ? max(0, p_lo - a.window + 1) : 0;
-  const int uw = start / BK, us = min((min(a.sinks, start) + BK - 1) / BK, uw);
-  const int ntiles = us + p_hi / BK + 1 - uw;
-  auto tile_of = [&](int u) { return (u < us ? u : uw + u - us) * BK; };
-
+  const KeyTiles<BK> tiles(p_lo, p_hi, a.window, a.sinks);
+  // (rows 16 apart have the same swizzle)
+  static_assert(NT / PR % 16 == 0, "a thread's pieces of a tile");
+  const int piece = lds_piece<D>(tid / PR, tid % PR);
   u32x4 kr[LD], vr[LD];
+  uint8_t mr = 0;
+  RowSource<D, NT / PR> ksrc(a.k, sg.k0, a.ldk, sg.nk, tid), vsrc(a.v, sg.k0, a.ldv, sg.nk, tid);
   auto load = [&](int kv0) __attribute__((always_inline)) {
+    uint32_t ko, vo;
+    ksrc.tile(kv0, ko, kvh * D * 2);
+    vsrc.tile(kv0, vo, kvh * D * 2);
 #pragma unroll
     for (int i = 0; i < LD; ++i) {
-      const int task = tid + i * NT, row = min(kv0 + task / PR, sg.nk - 1), c = task % PR;
-      kr[i] = load_piece(kbase + (int64_t)row * a.ldk + 8 * c);
-      vr[i] = load_piece(vbase + (int64_t)row * a.ldv + 8 * c);
+      kr[i] = ksrc.load(ko, i);
+      vr[i] = vsrc.load(vo, i);
+    }
+    if (mask) mr = mask[min(kv0 + lane, sg.nk - 1)];
+  };
+  // What the workgroup's rows see of a tile: all of it by position, and the key
+  // mask's bits.
+  struct Seen {
+    bool whole;
+    uint64_t keys;
+  };
+  auto seen_of = [&](int kv0) __attribute__((always_inline)) {
+    Seen s{tiles.whole(kv0), ~uint64_t(0)};
+    if (mask) s.keys = __ballot(mr != 0);      // (of the tile loaded last)
+    return s;
+  };
+  auto store = [&](int buf, int bad, const Seen& s) __attribute__((always_inline)) {
+    uint16_t* dst = s_kv[buf];
+    const bool partial = !s.whole || s.keys != ~uint64_t(0);
+#pragma unroll
+    for (int i = 0; i < LD; ++i) {
+      const int row = tid / PR + i * (NT / PR), at = piece + i * (NT / PR) * D;
+      *reinterpret_cast<u32x4*>(&dst[at]) = kr[i];
+      if (partial && any_nonfinite<F16>(vr[i])) {
+        // an inf or NaN must not reach rows that do not see it (0 times inf)
+        vr[i] = finite_part<F16>(vr[i]);
+        atomicOr(&s_bad[bad][row >> 5], 1u << (row & 31));
+      }
+      *reinterpret_cast<u32x4*>(&dst[BK * D + at]) = vr[i];
     }
   };
 
@@ -88,91 +112,109 @@ __global__ __launch_bounds__(256, 2) void window_attn_kernel(WinArgs a) {
     for (int r = 0; r < 16; ++r) o[b][r] = 0.f;
   const float sl2 = a.scale * 1.4426950408889634f;   // scores in log2 units
 
-  if (tid < 4) s_bad[tid >> 1][tid & 1] = 0;
-  load(tile_of(0));
-  for (int u = 0; u < ntiles; ++u) {
-    const int kv0 = tile_of(u);
-    // whether every row of the workgroup sees every key of the tile (by position)
-    const bool whole = kv0 + BK - 1 <= p_lo && (a.window <= 0 || kv0 > p_hi - a.window || kv0 + BK <= a.sinks);
-    uint64_t seen = ~uint64_t(0);                     // the key mask's bits of this tile
-    if (mask) seen = __ballot(mask[min(kv0 + lane, sg.nk - 1)] != 0);
-    const bool partial = !whole || seen != ~uint64_t(0);
-    __syncthreads();   // the readers of the tile before are done
-    if (tid < 2) s_bad[(u + 1) & 1][tid] = 0;
-#pragma unroll
-    for (int i = 0; i < LD; ++i) {
-      const int task = tid + i * NT, row = task / PR, c = task % PR;
-      *reinterpret_cast<u32x4*>(&Ks[row * KS + 8 * c]) = kr[i];
-      if (partial && any_nonfinite<F16>(vr[i])) {
-        // an inf or NaN must not reach rows that do not see it (0 times inf)
-        vr[i] = finite_part<F16>(vr[i]);
-        atomicOr(&s_bad[u & 1][row >> 5], 1u << (row & 31));
-      }
-      *reinterpret_cast<u32x4*>(&Vs[row * VS + 8 * c]) = vr[i];
+  const int fr = lds_frag<D>(lane), tr = lds_tr<D>(lane);
+  const int wlim = a.window > 0 ? min(a.window, 1 << 30) : 1 << 30;   // (positions are below 2^30)
+  if (tid < 6) s_bad[tid >> 1][tid & 1] = 0;
+  __syncthreads();
+  // a tile that the wave's own rows see nothing of
+  const int skip_lo = a.window > 0 ? w_lo - a.window - BK + 1 : -1;
+  int kv0 = tiles.first, next = tiles.n > 1 ? tiles.after(kv0) : kv0;
+  load(kv0);
+  Seen now = seen_of(kv0);
+  store(0, 0, now);
+  load(next);
+  int bad0 = 0, bad1 = 1, bad2 = 2;     // s_bad of this tile, the next, the one after
+  for (int u = 0; u < tiles.n; ++u) {
+    __syncthreads();   // tile u is stored, and the readers of the tile before are done
+    if (tid < 2) s_bad[bad2][tid] = 0;
+    const Seen here = now;
+    const int kv = kv0, bad_at = bad0;
+    bad0 = bad1, bad1 = bad2, bad2 = bad_at;
+    if (u + 1 < tiles.n) {
+      now = seen_of(next);
+      store((u + 1) & 1, bad0, now);
+      kv0 = next;
+      if (u + 2 < tiles.n) next = tiles.after(next);
     }
-    __syncthreads();
-    load(tile_of(min(u + 1, ntiles - 1)));   // in flight meanwhile (the last one is not used)
-    // the wave's own rows may see nothing of it
-    if (kv0 > w_hi || (a.window > 0 && kv0 + BK - 1 <= w_lo - a.window && kv0 >= a.sinks)) continue;
+    load(next);        // in flight meanwhile (past the last tile: not used)
+    if (kv > w_hi || (kv <= skip_lo && kv >= a.sinks)) continue;
+    const uint16_t* Ks = s_kv[u & 1];
+    const uint16_t* Vs = Ks + BK * D;
 
-    floatx16 st[KB];
+    // 32 keys at a time; fragments in the order of their products: K, V of each half
+    static_assert(2 * NB == NS, "fragments of a step");
+    u32x4 af[AHEAD];
+    auto frag = [&](int f) __attribute__((always_inline)) {
+      const int kb = KP == 2 ? part : f / (2 * NS), s = f % NS;
+      if (f % (2 * NS) < NS) return lds_read16(&Ks[(fr ^ 16 * s) + 32 * kb * D]);
+      return lds_frag_tr<D>(Vs, tr, 2 * kb + s / NB, s % NB);
+    };
+#pragma unroll
+    for (int f = 0; f < AHEAD; ++f) af[f] = frag(f);
 #pragma unroll
     for (int b = 0; b < KB; ++b) {
-      const int kb = KP == 2 ? part : b;
+      const int kb = KP == 2 ? part : b, f0 = 2 * NS * b;
+      floatx16 st;
 #pragma unroll
-      for (int r = 0; r < 16; ++r) st[b][r] = 0.f;
+      for (int r = 0; r < 16; ++r) st[r] = 0.f;
 #pragma unroll
-      for (int s = 0; s < NS; ++s)
-        st[b] = mfma32x32x16<F16>(*reinterpret_cast<const u32x4*>(&Ks[(32 * kb + lq) * KS + 16 * s + 8 * half]),
-                                  qf[s], st[b]);
-    }
-    if (partial) {
+      for (int s = 0; s < NS; ++s) {
+        st = mfma32x32x16<F16>(af[s % AHEAD], qf[s], st);
+        af[s % AHEAD] = frag(f0 + s + AHEAD);
+      }
+      if (!here.whole || here.keys != ~uint64_t(0)) {
+        const int j0 = kv + 32 * kb + 4 * half;   // element r is key j0 + 8 (r / 4) + r % 4
+        const uint32_t see = (uint32_t)(here.keys >> (32 * kb)) >> (4 * half);
+        const uint32_t bad = __builtin_amdgcn_readfirstlane(s_bad[bad_at][kb]);
+        if (here.whole) {
 #pragma unroll
-      for (int b = 0; b < KB; ++b) {
-        const int kb = KP == 2 ? part : b;
-        const uint32_t see = (uint32_t)(seen >> (32 * kb)), bad = s_bad[u & 1][kb];
+          for (int r = 0; r < 16; ++r)
+            st[r] = (see >> (8 * (r / 4) + r % 4)) & 1 ? st[r] : -__builtin_inff();
+          poison |= (see & (bad >> (4 * half)) & 0x0f0f0f0fu) != 0;
+        } else {
+          const int top = p - j0, low = top - wlim, sink = a.sinks - j0;
+          auto ok = [&](int x) { return x <= top && (x > low || x < sink) && ((see >> x) & 1); };
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const int jl = 8 * (r / 4) + 4 * half + r % 4, j = kv0 + 32 * kb + jl;
-          const bool ok = j <= p && (a.window <= 0 || j > p - a.window || j < a.sinks) && ((see >> jl) & 1);
-          st[b][r] = ok ? st[b][r] : -__builtin_inff();
-          poison |= ok && ((bad >> jl) & 1);
+          for (int r = 0; r < 16; ++r) st[r] = ok(8 * (r / 4) + r % 4) ? st[r] : -__builtin_inff();
+          if (bad)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+              const int x = 8 * (r / 4) + r % 4;
+              poison |= ok(x) && ((bad >> (4 * half + x)) & 1);
+            }
         }
       }
-    }
-    float mx = -__builtin_inff();
+      float mx = -__builtin_inff();
 #pragma unroll
-    for (int b = 0; b < KB; ++b)
+      for (int r = 0; r < 16; ++r) mx = fmaxf(mx, st[r]);
+      mx = fmaxf(mx, __shfl_xor(mx, 32, 64)) * sl2;
+      // the maximum is followed at a distance: weights up to 2^8 lose nothing, and
+      // rows seldom need their sums scaled again
+      if (__any(mx > m + 8.f)) {
+        const float mn = fmaxf(m, mx);
+        const float alpha = mn == -__builtin_inff() ? 1.f : exp2_raw(m - mn);
+        l *= alpha;
 #pragma unroll
-      for (int r = 0; r < 16; ++r) mx = fmaxf(mx, st[b][r]);
-    mx = fmaxf(mx, __shfl_xor(mx, 32, 64)) * sl2;
-    if (__any(mx > m)) {
-      const float mn = fmaxf(m, mx);
-      const float alpha = mn == -__builtin_inff() ? 1.f : exp2f(m - mn);
-      l *= alpha;
-#pragma unroll
-      for (int b = 0; b < NB; ++b) o[b] *= alpha;
-      m = mn;
-    }
-    const float mu = m == -__builtin_inff() ? 0.f : m;   // nothing above -inf yet
-    // V^T fragment of dims 32 b .. and keys 16 t ..: rows 16 t + 4 half and 8 further
-    const uint16_t* vt = &Vs[(4 * half + (lane & 15) / 4) * VS + 16 * ((lane >> 4) & 1) + 4 * (lane & 3)];
-#pragma unroll
-    for (int b = 0; b < KB; ++b) {
+        for (int c = 0; c < NB; ++c) o[c] *= alpha;
+        m = mn;
+      }
+      const float mu = m == -__builtin_inff() ? 0.f : m;   // nothing above -inf yet
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
-        st[b][r] = exp2f(fmaf(st[b][r], sl2, -mu));
-        l += st[b][r];
+        st[r] = exp2_raw(fmaf(st[r], sl2, -mu));
+        l += st[r];
       }
 #pragma unroll
-      for (int t2 = 0; t2 < 2; ++t2) {
-        const int t = 2 * (KP == 2 ? part : b) + t2, r = 8 * t2;
-        const u32x4 pb = {pack_act2<F16>(st[b][r], st[b][r + 1]), pack_act2<F16>(st[b][r + 2], st[b][r + 3]),
-                          pack_act2<F16>(st[b][r + 4], st[b][r + 5]), pack_act2<F16>(st[b][r + 6], st[b][r + 7])};
+      for (int t = 0; t < 2; ++t) {
+        const int r = 8 * t;
+        const u32x4 pb = round8<F16>(st, r);
 #pragma unroll
         for (int c = 0; c < NB; ++c) {
-          const uint2 x = lds_read_tr(vt + 16 * t * VS + 32 * c), y = lds_read_tr(vt + (16 * t + 8) * VS + 32 * c);
-          o[c] = mfma32x32x16<F16>(u32x4{x.x, x.y, y.x, y.y}, pb, o[c]);
+          const int s = t * NB + c, next = f0 + NS + s + AHEAD;
+          o[c] = mfma32x32x16<F16>(af[s % AHEAD], pb, o[c]);
+          if (next < 2 * KB * NS) {
+            af[s % AHEAD] = frag(next);
+              }
         }
       }
     }
@@ -181,9 +223,9 @@ __global__ __launch_bounds__(256, 2) void window_attn_kernel(WinArgs a) {
   l += __shfl_xor(l, 32, 64);
   poison = poison || __shfl_xor((int)poison, 32, 64);
   if constexpr (KP == 2) {
-    // part 1 hands its sums to part 0 (in the V buffer, 16 rows of a lane's sums at a time)
-    static_assert(QG * 64 * 20 * 4 <= (int)sizeof(Vs), "join buffer");
-    float* s_j = reinterpret_cast<float*>(&Vs[0]) + (qg * 64 + lane) * 20;
+    // part 1 hands its sums to part 0, 16 of a lane's at a time
+    static_assert(QG * 64 * 20 * 4 <= (int)sizeof(s_kv), "join buffer");
+    float* s_j = reinterpret_cast<float*>(&s_kv[0][0]) + (qg * 64 + lane) * 20;
     float f0 = 1.f, f1 = 0.f;
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
@@ -199,8 +241,8 @@ __global__ __launch_bounds__(256, 2) void window_attn_kernel(WinArgs a) {
       if (part == 0) {
         if (b == 0) {
           const float m1 = s_j[16], mn = fmaxf(m, m1);
-          f0 = m == -__builtin_inff() ? 0.f : exp2f(m - mn);
-          f1 = m1 == -__builtin_inff() ? 0.f : exp2f(m1 - mn);
+          f0 = m == -__builtin_inff() ? 0.f : exp2_raw(m - mn);
+          f1 = m1 == -__builtin_inff() ? 0.f : exp2_raw(m1 - mn);
           l = l * f0 + s_j[17] * f1;
           m = mn;
           poison |= s_j[18] != 0.f;
@@ -220,8 +262,8 @@ __global__ __launch_bounds__(256, 2) void window_attn_kernel(WinArgs a) {
   for (int b = 0; b < NB; ++b)
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
-      const uint2 w = make_uint2(pack_act2<F16>(o[b][4 * g] * inv, o[b][4 * g + 1] * inv),
-                                 pack_act2<F16>(o[b][4 * g + 2] * inv, o[b][4 * g + 3] * inv));
+      const uint2 w = make_uint2(round2<F16>(o[b][4 * g] * inv, o[b][4 * g + 1] * inv),
+                                 round2<F16>(o[b][4 * g + 2] * inv, o[b][4 * g + 3] * inv));
       const int64_t col = (int64_t)h * D + 32 * b + 8 * g + 4 * half;
       *reinterpret_cast<uint2*>(out + (a.packed ? packed_index(row, col, a.ldo) : row * a.ldo + col)) = w;
     }

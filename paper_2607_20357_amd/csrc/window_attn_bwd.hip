@@ -24,18 +24,16 @@ constexpr float kLog2e = 1.4426950408889634f;
 
 __device__ __forceinline__ float pow2f(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }
 
-// Query gradient: four waves of 32 query rows against tiles of 64 keys.
+// Query gradient: four waves of 32 query rows against tiles of 32 keys.
 // S^T = K Q^T and dP^T = V dO^T (keys x queries), dQ^T += K^T dS^T with K read
 // transposed from LDS.
 template <int D, bool F16>
 __global__ __launch_bounds__(NT, 2) void window_dq_kernel(WinBwdArgs a) {
-  constexpr int BQ = 128, BK = WIN_BK;
-  constexpr int KS = D + 32, VS = D + 8;
+  constexpr int BQ = 128, BK = 32;     // (64 keys' staging registers do not fit)
   constexpr int NS = D / 16, NB = D / 32;
   constexpr int PR = D / 8, LD = BK * PR / NT;
-  __shared__ __attribute__((aligned(16))) uint16_t Ks[BK * KS];
-  __shared__ __attribute__((aligned(16))) uint16_t Vs[BK * VS];
-  __shared__ uint32_t s_bad[2][2];     // keys of a tile with an inf or NaN in K
+  __shared__ __attribute__((aligned(16))) uint16_t s_kv[2][2 * BK * D];   // as in the forward
+  __shared__ uint32_t s_bad[3];        // keys of a tile with an inf or NaN in K
   const int item = blockIdx.x;
   if (item >= a.nitems) return;
   const WinBwdSeg& sg = a.seg[find_item_seg(a, item)];
@@ -45,7 +43,7 @@ __global__ __launch_bounds__(NT, 2) void window_dq_kernel(WinBwdArgs a) {
   const int nqt = (sg.nq + BQ - 1) / BQ;
   const int qt = nqt - 1 - local / a.n_heads;
   const int kvh = h / (a.n_heads / a.n_kv_heads);
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int half = lane >> 5, lq = lane & 31;
   const int off = sg.nk - sg.nq;
   const int i0 = qt * BQ, qi = i0 + 32 * wave + lq;
@@ -90,20 +88,45 @@ __global__ __launch_bounds__(NT, 2) void window_dq_kernel(WinBwdArgs a) {
   int down = 0;                  // fp16: and 2^-down more, for the whole wave
   float fac = F16 ? pow2f(-ex) : 1.f;
 
-  const uint16_t* kbase = static_cast<const uint16_t*>(a.k) + (int64_t)sg.k0 * a.ldk + (int64_t)kvh * D;
-  const uint16_t* vbase = static_cast<const uint16_t*>(a.v) + (int64_t)sg.k0 * a.ldv + (int64_t)kvh * D;
   const uint8_t* mask = a.key_mask ? a.key_mask + sg.k0 : nullptr;
-  const int start = a.window > 0 ? max(0, p_lo - a.window + 1) : 0;
-  const int uw = start / BK, us = min((min(a.sinks, start) + BK - 1) / BK, uw);
-  const int ntiles = us + p_hi / BK + 1 - uw;
-  auto tile_of = [&](int u) { return (u < us ? u : uw + u - us) * BK; };
+  const KeyTiles<BK> tiles(p_lo, p_hi, a.window, a.sinks);
+  static_assert(NT / PR % 16 == 0, "a thread's pieces of a tile");
+  const int piece = lds_piece<D>(tid / PR, tid % PR);
   u32x4 kr[LD], vr[LD];
+  uint8_t mr = 0;
+  RowSource<D, NT / PR> ksrc(a.k, sg.k0, a.ldk, sg.nk, tid), vsrc(a.v, sg.k0, a.ldv, sg.nk, tid);
   auto load = [&](int kv0) __attribute__((always_inline)) {
+    uint32_t ko, vo;
+    ksrc.tile(kv0, ko, kvh * D * 2);
+    vsrc.tile(kv0, vo, kvh * D * 2);
 #pragma unroll
     for (int i = 0; i < LD; ++i) {
-      const int task = tid + i * NT, r = min(kv0 + task / PR, sg.nk - 1), c = task % PR;
-      kr[i] = load_piece(kbase + (int64_t)r * a.ldk + 8 * c);
-      vr[i] = load_piece(vbase + (int64_t)r * a.ldv + 8 * c);
+      kr[i] = ksrc.load(ko, i);
+      vr[i] = vsrc.load(vo, i);
+    }
+    if (mask) mr = mask[min(kv0 + lane, sg.nk - 1)];
+  };
+  struct Seen {
+    bool whole;
+    uint32_t keys;
+  };
+  auto seen_of = [&](int kv0) __attribute__((always_inline)) {
+    Seen s{tiles.whole(kv0), ~0u};
+    if (mask) s.keys = (uint32_t)__ballot(mr != 0);      // (of the tile loaded last)
+    return s;
+  };
+  auto store = [&](int buf, int bad, const Seen& s) __attribute__((always_inline)) {
+    uint16_t* dst = s_kv[buf];
+    const bool partial = !s.whole || s.keys != ~0u;
+#pragma unroll
+    for (int i = 0; i < LD; ++i) {
+      const int r = tid / PR + i * (NT / PR), at = piece + i * (NT / PR) * D;
+      if (partial && any_nonfinite<F16>(kr[i])) {
+        kr[i] = finite_part<F16>(kr[i]);
+        atomicOr(&s_bad[bad], 1u << r);
+      }
+      *reinterpret_cast<u32x4*>(&dst[at]) = kr[i];
+      *reinterpret_cast<u32x4*>(&dst[BK * D + at]) = vr[i];
     }
   };
   floatx16 dq[NB];
@@ -114,84 +137,102 @@ __global__ __launch_bounds__(NT, 2) void window_dq_kernel(WinBwdArgs a) {
   const float sl2 = a.scale * kLog2e;
   bool poison = false;
 
-  if (tid < 4) s_bad[tid >> 1][tid & 1] = 0;
-  load(tile_of(0));
-  for (int u = 0; u < ntiles; ++u) {
-    const int kv0 = tile_of(u);
-    const bool whole = kv0 + BK - 1 <= p_lo && (a.window <= 0 || kv0 > p_hi - a.window || kv0 + BK <= a.sinks);
-    uint64_t seen = ~uint64_t(0);
-    if (mask) seen = __ballot(mask[min(kv0 + lane, sg.nk - 1)] != 0);
-    const bool partial = !whole || seen != ~uint64_t(0);
-    __syncthreads();
-    if (tid < 2) s_bad[(u + 1) & 1][tid] = 0;
-#pragma unroll
-    for (int i = 0; i < LD; ++i) {
-      const int task = tid + i * NT, r = task / PR, c = task % PR;
-      if (partial && any_nonfinite<F16>(kr[i])) {
-        kr[i] = finite_part<F16>(kr[i]);
-        atomicOr(&s_bad[u & 1][r >> 5], 1u << (r & 31));
-      }
-      *reinterpret_cast<u32x4*>(&Ks[r * KS + 8 * c]) = kr[i];
-      *reinterpret_cast<u32x4*>(&Vs[r * VS + 8 * c]) = vr[i];
+  const int fr = lds_frag<D>(lane), tr = lds_tr<D>(lane);
+  const int wlim = a.window > 0 ? min(a.window, 1 << 30) : 1 << 30;
+  if (tid < 3) s_bad[tid] = 0;
+  __syncthreads();
+  // a tile that the wave's own rows see nothing of
+  const int skip_lo = a.window > 0 ? w_lo - a.window - BK + 1 : -1;
+  int kv0 = tiles.first, next = tiles.n > 1 ? tiles.after(kv0) : kv0;
+  load(kv0);
+  Seen now = seen_of(kv0);
+  store(0, 0, now);
+  load(next);
+  int bad0 = 0, bad1 = 1, bad2 = 2;     // s_bad of this tile, the next, the one after
+  for (int u = 0; u < tiles.n; ++u) {
+    __syncthreads();   // tile u is stored, and the readers of the tile before are done
+    if (tid == 0) s_bad[bad2] = 0;
+    const Seen here = now;
+    const int kv = kv0, bad_at = bad0;
+    bad0 = bad1, bad1 = bad2, bad2 = bad_at;
+    if (u + 1 < tiles.n) {
+      now = seen_of(next);
+      store((u + 1) & 1, bad0, now);
+      kv0 = next;
+      if (u + 2 < tiles.n) next = tiles.after(next);
     }
-    __syncthreads();
-    load(tile_of(min(u + 1, ntiles - 1)));
-    if (kv0 > w_hi || (a.window > 0 && kv0 + BK - 1 <= w_lo - a.window && kv0 >= a.sinks)) continue;
-
-    const uint16_t* kt = &Ks[(4 * half + (lane & 15) / 4) * KS + 16 * ((lane >> 4) & 1) + 4 * (lane & 3)];
+    load(next);        // in flight meanwhile (past the last tile: not used)
+    if (kv > w_hi || (kv <= skip_lo && kv >= a.sinks)) continue;
+    const uint16_t* Ks = s_kv[u & 1];
+    const uint16_t* Vs = Ks + BK * D;
+    const bool partial = !here.whole || here.keys != ~0u;
+    // fragments in the order of their products: K, V, K transposed
+    static_assert(2 * NB == NS, "fragments of a step");
+    u32x4 af[AHEAD];
+    auto frag = [&](int f) __attribute__((always_inline)) {
+      const int s = f % NS;
+      return f < 2 * NS ? lds_read16(&(f < NS ? Ks : Vs)[fr ^ 16 * s]) : lds_frag_tr<D>(Ks, tr, s / NB, s % NB);
+    };
 #pragma unroll
-    for (int kb = 0; kb < 2; ++kb) {
-      floatx16 st, dp;
+    for (int f = 0; f < AHEAD; ++f) af[f] = frag(f);
+    floatx16 st, dp;
 #pragma unroll
-      for (int r = 0; r < 16; ++r) st[r] = dp[r] = 0.f;
+    for (int r = 0; r < 16; ++r) st[r] = dp[r] = 0.f;
 #pragma unroll
-      for (int s = 0; s < NS; ++s) {
-        st = mfma32x32x16<F16>(*reinterpret_cast<const u32x4*>(&Ks[(32 * kb + lq) * KS + 16 * s + 8 * half]), qf[s], st);
-        dp = mfma32x32x16<F16>(*reinterpret_cast<const u32x4*>(&Vs[(32 * kb + lq) * VS + 16 * s + 8 * half]), gf[s], dp);
-      }
-      uint32_t see = 0xffffffffu, bad = 0;
-      if (partial) {
-        see = (uint32_t)(seen >> (32 * kb));
-        bad = s_bad[u & 1][kb];
-      }
+    for (int s = 0; s < NS; ++s) {
+      st = mfma32x32x16<F16>(af[s % AHEAD], qf[s], st);
+      af[s % AHEAD] = frag(s + AHEAD);
+    }
+#pragma unroll
+    for (int s = 0; s < NS; ++s) {
+      dp = mfma32x32x16<F16>(af[s % AHEAD], gf[s], dp);
+      af[s % AHEAD] = frag(NS + s + AHEAD);
+    }
+#pragma unroll
+    for (int r = 0; r < 16; ++r) st[r] = exp2_raw(fmaf(st[r], sl2, -lse2)) * ((dp[r] - delta) * fac);
+    if (partial) {
+      const int j0 = kv + 4 * half;   // element r is key j0 + 8 (r / 4) + r % 4
+      const uint32_t see = here.keys >> (4 * half), bad = __builtin_amdgcn_readfirstlane(s_bad[bad_at]);
+      const int top = p - j0, low = top - wlim, sink = a.sinks - j0;
+      auto ok = [&](int x) { return x <= top && (x > low || x < sink) && ((see >> x) & 1); };
+#pragma unroll
+      for (int r = 0; r < 16; ++r) st[r] = ok(8 * (r / 4) + r % 4) ? st[r] : 0.f;
+      if (bad)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const int x = 8 * (r / 4) + r % 4;
+          poison |= ok(x) && ((bad >> (4 * half + x)) & 1);
+        }
+    }
+    if constexpr (F16) {
       float big = 0.f;
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        float x = exp2f(fmaf(st[r], sl2, -lse2)) * ((dp[r] - delta) * fac);
-        if (partial) {
-          const int jl = 8 * (r / 4) + 4 * half + r % 4, j = kv0 + 32 * kb + jl;
-          const bool ok = j <= p && (a.window <= 0 || j > p - a.window || j < a.sinks) && ((see >> jl) & 1);
-          x = ok ? x : 0.f;
-          poison |= ok && ((bad >> jl) & 1);
-        }
-        st[r] = x;
-        if constexpr (F16) big = fmaxf(big, fabsf(x));
+      for (int r = 0; r < 16; ++r) big = fmaxf(big, fabsf(st[r]));
+      if (__any(big > 32768.f)) {
+        big = big < __builtin_inff() ? big : 0.f;   // an inf is its row's own
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) big = fmaxf(big, __shfl_xor(big, o, 64));
+        const int more = max(0, min((int)(__float_as_uint(big) >> 23) - 127 - 10, 120));
+        const float f = pow2f(-more);
+        down += more;
+        fac *= f;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) st[r] *= f;
+#pragma unroll
+        for (int b = 0; b < NB; ++b) dq[b] *= f;
       }
-      if constexpr (F16) {
-        if (__any(big > 32768.f)) {
-          big = big < __builtin_inff() ? big : 0.f;   // an inf is its row's own
+    }
 #pragma unroll
-          for (int o = 1; o < 64; o <<= 1) big = fmaxf(big, __shfl_xor(big, o, 64));
-          const int more = max(0, min((int)(__float_as_uint(big) >> 23) - 127 - 10, 120));
-          const float f = pow2f(-more);
-          down += more;
-          fac *= f;
+    for (int t = 0; t < 2; ++t) {
+      const int r = 8 * t;
+      const u32x4 pb = round8<F16>(st, r);
 #pragma unroll
-          for (int r = 0; r < 16; ++r) st[r] *= f;
-#pragma unroll
-          for (int b = 0; b < NB; ++b) dq[b] *= f;
-        }
-      }
-#pragma unroll
-      for (int t2 = 0; t2 < 2; ++t2) {
-        const int t = 2 * kb + t2, r = 8 * t2;
-        const u32x4 pb = {pack_act2<F16>(st[r], st[r + 1]), pack_act2<F16>(st[r + 2], st[r + 3]),
-                          pack_act2<F16>(st[r + 4], st[r + 5]), pack_act2<F16>(st[r + 6], st[r + 7])};
-#pragma unroll
-        for (int c = 0; c < NB; ++c) {
-          const uint2 x = lds_read_tr(kt + 16 * t * KS + 32 * c), y = lds_read_tr(kt + (16 * t + 8) * KS + 32 * c);
-          dq[c] = mfma32x32x16<F16>(u32x4{x.x, x.y, y.x, y.y}, pb, dq[c]);
-        }
+      for (int c = 0; c < NB; ++c) {
+        const int s = t * NB + c;
+        dq[c] = mfma32x32x16<F16>(af[s % AHEAD], pb, dq[c]);
+        if (s + AHEAD < NS) {
+          af[s % AHEAD] = frag(2 * NS + s + AHEAD);
+          }
       }
     }
   }
@@ -207,7 +248,7 @@ __global__ __launch_bounds__(NT, 2) void window_dq_kernel(WinBwdArgs a) {
 #pragma unroll
       for (int e = 0; e < 4; ++e) y[e] = F16 ? ldexpf(dq[b][4 * g + e] * f, ex + down) : dq[b][4 * g + e] * f;
       *reinterpret_cast<uint2*>(out + 32 * b + 8 * g + 4 * half) =
-          make_uint2(pack_act2<F16>(y[0], y[1]), pack_act2<F16>(y[2], y[3]));
+          make_uint2(round2<F16>(y[0], y[1]), round2<F16>(y[2], y[3]));
     }
 }
 
@@ -244,19 +285,23 @@ __device__ __forceinline__ DkvItem dkv_item(const WinBwdArgs& a, const WinBwdSeg
   return it;
 }
 
-// Key and value gradients: four waves of 32 keys against tiles of 32 query rows.
-// S = Q K^T and dP = dO V^T (queries x keys) with the wave's K and V in
-// registers, then dV^T += dO^T P and dK^T += Q^T dS with the rows read transposed
-// from LDS.
+// Key and value gradients: four groups of 32 keys against tiles of 64 query rows,
+// two waves per group.  Both form S = Q K^T (queries x keys); one then adds
+// dV^T += dO^T P, the other forms dP = dO V^T and adds dK^T += Q^T dS.  The rows are
+// in LDS, read as they are and transposed; K and V stay in registers.  One wave
+// for both gradients needs over 256 registers: alone on its SIMD, with sums moved
+// about, 832 us at 4096 + 3001 rows of 32 / 8 heads under a window of 1024; two
+// such waves per SIMD with V in LDS and a few registers in memory 589 us; this
+// way a quarter more products, NNN us.
+constexpr int DKV_NT = 512;
+
 template <int D, bool F16>
-__global__ __launch_bounds__(NT, 1) void window_dkv_kernel(WinBwdArgs a) {
-  constexpr int RS = D + 32;           // row stride of the staged rows
+__global__ __launch_bounds__(DKV_NT, 2) void window_dkv_kernel(WinBwdArgs a) {
   constexpr int NS = D / 16, NB = D / 32;
-  constexpr int PR = D / 8, LD = WIN_DQ * PR / NT;
-  __shared__ __attribute__((aligned(16))) uint16_t Qs[WIN_DQ * RS];
-  __shared__ __attribute__((aligned(16))) uint16_t Gs[WIN_DQ * RS];
-  __shared__ __attribute__((aligned(16))) float s_lse[WIN_DQ], s_delta[WIN_DQ];
-  __shared__ int s_expo[WIN_DQ];
+  constexpr int PR = D / 8, LD = WIN_DQ * PR / DKV_NT, STEP = DKV_NT / PR;
+  __shared__ __attribute__((aligned(16))) uint16_t s_qg[2][2 * WIN_DQ * D];   // two tiles in turn: Q, then dO
+  __shared__ __attribute__((aligned(16))) float s_lse[2][WIN_DQ], s_delta[2][WIN_DQ];
+  __shared__ int s_expo[2][WIN_DQ];
   const int item = blockIdx.x;
   if (item >= a.nitems) return;
   const WinBwdSeg& sg = a.seg[find_item_seg(a, item)];
@@ -267,10 +312,12 @@ __global__ __launch_bounds__(NT, 1) void window_dkv_kernel(WinBwdArgs a) {
   const int ntq = qt1 - qt0;
   const int64_t total = (int64_t)rep * ntq;
   const int x0 = (int)(total * it.piece / it.pieces), x1 = (int)(total * (it.piece + 1) / it.pieces);
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), kg = wave & 3;
+  const bool for_k = wave >= 4;          // the wave's gradient: dK or dV
   const int half = lane >> 5, lk = lane & 31;
   const int off = sg.nk - sg.nq;
-  const int j0 = it.kt * WIN_DK, jw = j0 + 32 * wave, j = jw + lk;
+  const int j0 = it.kt * WIN_DK, jw = j0 + 32 * kg, j = jw + lk;
   const bool on = j < sg.nk;
   const int64_t krow = (int64_t)sg.k0 + (on ? j : sg.nk - 1);
   const bool open = on && (!a.key_mask || a.key_mask[krow]);
@@ -284,27 +331,42 @@ __global__ __launch_bounds__(NT, 1) void window_dkv_kernel(WinBwdArgs a) {
       kf[s] = load_piece(kp + 16 * s);
       vf[s] = load_piece(vp + 16 * s);
     }
+    // wait here: left to the loop, the wait for these would also be one for the
+    // loads that the loop keeps in flight
+    __builtin_amdgcn_s_waitcnt(0x0f70);   // vmcnt(0)
   }
-  floatx16 dk[NB], dv[NB];
+  floatx16 sum[NB];                      // dK^T or dV^T
 #pragma unroll
   for (int b = 0; b < NB; ++b)
 #pragma unroll
-    for (int r = 0; r < 16; ++r) dk[b][r] = dv[b][r] = 0.f;
+    for (int r = 0; r < 16; ++r) sum[b][r] = 0.f;
   const float sl2 = a.scale * kLog2e;
-  int ex = -126;                       // fp16: dS 2^-ex, the same in every lane of the wave
+  int ex = -126;                         // fp16: dS 2^-ex, the same in every lane of the wave
   float fac = 1.f;
 
+  static_assert(STEP % 16 == 0, "a thread's pieces of a tile");
+  const int piece = lds_piece<D>(tid / PR, tid % PR);
   u32x4 qr[LD], gr[LD];
   float lse_r = 0.f, delta_r = 0.f;
   int expo_r = 0;
-  auto load = [&](int x) __attribute__((always_inline)) {
-    const int h = kvh * rep + x / ntq, i0 = (qt0 + x % ntq) * WIN_DQ;
+  RowSource<D, STEP> qsrc(a.q, sg.q0, a.ldq, sg.nq, tid), gsrc(a.grad, sg.q0, a.ldg, sg.nq, tid);
+  // An entry of the list: its head and its first row.
+  struct Entry {
+    int h, i0;
+  };
+  auto entry = [&](int x) { return Entry{kvh * rep + x / ntq, (qt0 + x % ntq) * WIN_DQ}; };
+  auto after = [&](const Entry& e) {
+    return e.i0 + WIN_DQ < qt1 * WIN_DQ ? Entry{e.h, e.i0 + WIN_DQ} : Entry{e.h + 1, qt0 * WIN_DQ};
+  };
+  auto load = [&](const Entry& en) __attribute__((always_inline)) {
+    const int h = en.h, i0 = en.i0;
+    uint32_t qo, go;
+    qsrc.tile(i0, qo, h * D * 2);
+    gsrc.tile(i0, go, h * D * 2);
 #pragma unroll
     for (int i = 0; i < LD; ++i) {
-      const int task = tid + i * NT, c = task % PR;
-      const int64_t row = (int64_t)sg.q0 + min(i0 + task / PR, sg.nq - 1);
-      qr[i] = load_piece(static_cast<const uint16_t*>(a.q) + row * a.ldq + (int64_t)h * D + 8 * c);
-      gr[i] = load_piece(static_cast<const uint16_t*>(a.grad) + row * a.ldg + (int64_t)h * D + 8 * c);
+      qr[i] = qsrc.load(qo, i);
+      gr[i] = gsrc.load(go, i);
     }
     if (tid < WIN_DQ) {
       const int64_t at = ((int64_t)sg.q0 + min(i0 + tid, sg.nq - 1)) * a.n_heads + h;
@@ -313,141 +375,207 @@ __global__ __launch_bounds__(NT, 1) void window_dkv_kernel(WinBwdArgs a) {
       if constexpr (F16) expo_r = a.expo[at];
     }
   };
-  if (x0 < x1) load(x0);
-  for (int x = x0; x < x1; ++x) {
-    const int i0 = (qt0 + x % ntq) * WIN_DQ;
-    const int p_lo = off + i0, p_hi = off + min(i0 + WIN_DQ, sg.nq) - 1;
-    // whether every row sees every key of the workgroup
-    const bool whole = i0 + WIN_DQ <= sg.nq && j0 + WIN_DK - 1 <= p_lo && j0 + WIN_DK <= sg.nk &&
-                             (a.window <= 0 || j0 > p_hi - a.window || j0 + WIN_DK <= a.sinks) && !a.key_mask;
-    __syncthreads();
+  // whether every row of a tile sees every key of the workgroup
+  const int whole_from = j0 + WIN_DK <= sg.nk && !a.key_mask ? j0 + WIN_DK - 1 - off : INT_MAX;
+  const int whole_to = a.window > 0 ? (int)min((int64_t)j0 + a.window - WIN_DQ - off, (int64_t)INT_MAX) : INT_MAX;
+  auto whole_of = [&](int i0) __attribute__((always_inline)) {
+    return i0 >= whole_from && (i0 <= whole_to || j0 + WIN_DK <= a.sinks) && i0 + WIN_DQ <= sg.nq;
+  };
+  auto store = [&](int buf, int i0) __attribute__((always_inline)) {
+    uint16_t* dst = s_qg[buf];
+    const bool whole = whole_of(i0);
 #pragma unroll
     for (int i = 0; i < LD; ++i) {
-      const int task = tid + i * NT, r = task / PR, c = task % PR;
+      const int at = piece + i * STEP * D;
       if (!whole) {
         qr[i] = finite_part<F16>(qr[i]);
         gr[i] = finite_part<F16>(gr[i]);
       }
-      *reinterpret_cast<u32x4*>(&Qs[r * RS + 8 * c]) = qr[i];
-      *reinterpret_cast<u32x4*>(&Gs[r * RS + 8 * c]) = gr[i];
+      *reinterpret_cast<u32x4*>(&dst[at]) = qr[i];
+      *reinterpret_cast<u32x4*>(&dst[WIN_DQ * D + at]) = gr[i];
     }
     if (tid < WIN_DQ) {
-      s_lse[tid] = lse_r * kLog2e;
-      s_delta[tid] = delta_r;
-      if constexpr (F16) s_expo[tid] = expo_r;
+      s_lse[buf][tid] = lse_r * kLog2e;
+      s_delta[buf][tid] = delta_r;
+      if constexpr (F16) s_expo[buf][tid] = expo_r;
     }
-    __syncthreads();
-    load(min(x + 1, x1 - 1));
-    // the wave's own keys may be seen by none of the rows
-    if (jw > p_hi || (a.window > 0 && jw + 31 <= p_lo - a.window && jw >= a.sinks)) continue;
-    floatx16 st, dp;
+  };
+  const int fr = lds_frag<D>(lane), tr = lds_tr<D>(lane);
+  const int wlim = a.window > 0 ? min(a.window, 1 << 30) : 1 << 30;
+  Entry now{kvh * rep, 0}, next = now;
+  if (x0 < x1) {
+    now = next = entry(x0);
+    load(now);
+    store(0, now.i0);
+    if (x0 + 1 < x1) next = after(now);
+    load(next);
+  }
+  for (int x = x0; x < x1; ++x) {
+    const int buf = (x - x0) & 1;
+    __syncthreads();   // tile x is stored, and the readers of the tile before are done
+    const int i0 = now.i0;
+    now = next;
+    if (x + 1 < x1) store(buf ^ 1, now.i0);
+    if (x + 2 < x1) next = after(now);
+    load(next);        // in flight meanwhile (past the last: not used)
+    const bool whole = whole_of(i0);
+#pragma unroll 1
+    for (int sub = 0; sub < WIN_DQ; sub += 32) {
+      const int p_lo = off + i0 + sub, p_hi = min(p_lo + 31, sg.nk - 1);
+      // the wave's own keys may be seen by none of the rows (or there are none)
+      if (p_lo >= sg.nk || jw > p_hi || (a.window > 0 && jw + 31 <= p_lo - a.window && jw >= a.sinks)) continue;
+      const uint16_t* Qs = s_qg[buf] + sub * D;
+      const uint16_t* Gs = Qs + WIN_DQ * D;
+      const float* lses = &s_lse[buf][sub + 4 * half];
+      const float* deltas = &s_delta[buf][sub + 4 * half];
+      // rows of the elements: 8 (r / 4) + r % 4 from top on
+      const int top = p_lo + 4 * half, end = sg.nk - top, low = j - top;
+      const uint16_t* rows = for_k ? Qs : Gs;         // what the wave's gradient multiplies
+      // fragments in the order of their products: Q, (dO,) the transposed ones
+      static_assert(2 * NB == NS, "fragments of a step");
+      u32x4 af[AHEAD];
 #pragma unroll
-    for (int r = 0; r < 16; ++r) st[r] = dp[r] = 0.f;
+      for (int f = 0; f < AHEAD; ++f) af[f] = lds_read16(&Qs[fr ^ 16 * f]);
+      in_order();
+      floatx16 st;
 #pragma unroll
-    for (int s = 0; s < NS; ++s) {
-      st = mfma32x32x16<F16>(*reinterpret_cast<const u32x4*>(&Qs[lk * RS + 16 * s + 8 * half]), kf[s], st);
-      dp = mfma32x32x16<F16>(*reinterpret_cast<const u32x4*>(&Gs[lk * RS + 16 * s + 8 * half]), vf[s], dp);
-    }
-    if constexpr (F16) {
-      int e = s_expo[lk];
+      for (int r = 0; r < 16; ++r) st[r] = 0.f;
+      if (for_k) {
+        floatx16 dp;
 #pragma unroll
-      for (int o = 1; o < 32; o <<= 1) e = max(e, __shfl_xor(e, o, 64));
-      if (e > ex) {
-        const float f = ldexpf(1.f, ex - e);
-        ex = e;
-        fac = pow2f(-ex);
+        for (int r = 0; r < 16; ++r) dp[r] = 0.f;
 #pragma unroll
-        for (int b = 0; b < NB; ++b) dk[b] *= f;
-      }
-    }
-    float big = 0.f;
-#pragma unroll
-    for (int g = 0; g < 4; ++g) {
-      const floatx4 ls = *reinterpret_cast<const floatx4*>(&s_lse[8 * g + 4 * half]);
-      const floatx4 de = *reinterpret_cast<const floatx4*>(&s_delta[8 * g + 4 * half]);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int r = 4 * g + e;
-        float pr = exp2f(fmaf(st[r], sl2, -ls[e]));
-        float x = pr * ((dp[r] - de[e]) * (F16 ? fac : 1.f));
-        if (!whole) {
-          const int pq = off + i0 + 8 * g + 4 * half + e;
-          const bool ok = open && pq < sg.nk && j <= pq && (a.window <= 0 || j > pq - a.window || j < a.sinks);
-          // a row with an inf or NaN in its operands has one in its log-sum or delta
-          const float z = (ls[e] - ls[e]) + (de[e] - de[e]);
-          pr = ok ? pr + z : 0.f;
-          x = ok ? x + z : 0.f;
+        for (int s = 0; s < NS; ++s) {
+          const int n = s + AHEAD;
+          st = mfma32x32x16<F16>(af[s % AHEAD], kf[s], st);
+          af[s % AHEAD] = lds_read16(n < NS ? &Qs[fr ^ 16 * n] : &Gs[fr ^ 16 * (n - NS)]);
+          in_order();
         }
-        st[r] = pr;
-        dp[r] = x;
-        if constexpr (F16) big = fmaxf(big, fabsf(x));
+#pragma unroll
+        for (int s = 0; s < NS; ++s) {
+          const int n = s + AHEAD;
+          dp = mfma32x32x16<F16>(af[s % AHEAD], vf[s], dp);
+          af[s % AHEAD] = n < NS ? lds_read16(&Gs[fr ^ 16 * n]) : lds_frag_tr<D>(rows, tr, (n - NS) / NB, (n - NS) % NB);
+          in_order();
+        }
+        if constexpr (F16) {
+          int e = s_expo[buf][sub + lk];
+#pragma unroll
+          for (int o = 1; o < 32; o <<= 1) e = max(e, __shfl_xor(e, o, 64));
+          if (e > ex) {
+            const float f = ldexpf(1.f, ex - e);
+            ex = e;
+            fac = pow2f(-ex);
+#pragma unroll
+            for (int b = 0; b < NB; ++b) sum[b] *= f;
+          }
+        }
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          const floatx4 de = *reinterpret_cast<const floatx4*>(&deltas[8 * g]);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) dp[4 * g + e] = (dp[4 * g + e] - de[e]) * (F16 ? fac : 1.f);
+        }
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          const floatx4 ls = *reinterpret_cast<const floatx4*>(&lses[8 * g]);
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            st[4 * g + e] = exp2_raw(fmaf(st[4 * g + e], sl2, -ls[e])) * dp[4 * g + e];
+        }
+      } else {
+#pragma unroll
+        for (int s = 0; s < NS; ++s) {
+          const int n = s + AHEAD;
+          st = mfma32x32x16<F16>(af[s % AHEAD], kf[s], st);
+          af[s % AHEAD] = n < NS ? lds_read16(&Qs[fr ^ 16 * n]) : lds_frag_tr<D>(rows, tr, (n - NS) / NB, (n - NS) % NB);
+          in_order();
+        }
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          const floatx4 ls = *reinterpret_cast<const floatx4*>(&lses[8 * g]);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) st[4 * g + e] = exp2_raw(fmaf(st[4 * g + e], sl2, -ls[e]));
+        }
       }
-    }
-    if constexpr (F16) {
-      if (__any(big > 32768.f)) {
-        big = big < __builtin_inff() ? big : 0.f;   // an inf is its key's own
+      if (!whole) {
 #pragma unroll
-        for (int o = 1; o < 64; o <<= 1) big = fmaxf(big, __shfl_xor(big, o, 64));
-        const int more = max(0, min((int)(__float_as_uint(big) >> 23) - 127 - 10, 100));
-        const float f = pow2f(-more);
-        ex += more;
-        fac *= f;
+        for (int g = 0; g < 4; ++g) {
+          const floatx4 ls = *reinterpret_cast<const floatx4*>(&lses[8 * g]);
+          const floatx4 de = *reinterpret_cast<const floatx4*>(&deltas[8 * g]);
 #pragma unroll
-        for (int r = 0; r < 16; ++r) dp[r] *= f;
-#pragma unroll
-        for (int b = 0; b < NB; ++b) dk[b] *= f;
+          for (int e = 0; e < 4; ++e) {
+            const int y = 8 * g + e;
+            const bool ok = open && y < end && y >= low && (y < low + wlim || j < a.sinks);
+            // a row with an inf or NaN in its operands has one in its log-sum or delta
+            st[4 * g + e] = ok ? st[4 * g + e] + ((ls[e] - ls[e]) + (de[e] - de[e])) : 0.f;
+          }
+        }
       }
-    }
-    const int tr = (4 * half + (lane & 15) / 4) * RS + 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
+      if constexpr (F16) {
+        if (for_k) {
+          float big = 0.f;
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      const int r = 8 * t;
-      const u32x4 pb = {pack_act2<F16>(st[r], st[r + 1]), pack_act2<F16>(st[r + 2], st[r + 3]),
-                        pack_act2<F16>(st[r + 4], st[r + 5]), pack_act2<F16>(st[r + 6], st[r + 7])};
-      const u32x4 sb = {pack_act2<F16>(dp[r], dp[r + 1]), pack_act2<F16>(dp[r + 2], dp[r + 3]),
-                        pack_act2<F16>(dp[r + 4], dp[r + 5]), pack_act2<F16>(dp[r + 6], dp[r + 7])};
+          for (int r = 0; r < 16; ++r) big = fmaxf(big, fabsf(st[r]));
+          if (__any(big > 32768.f)) {
+            big = big < __builtin_inff() ? big : 0.f;   // an inf is its key's own
 #pragma unroll
-      for (int c = 0; c < NB; ++c) {
-        const uint2 x0 = lds_read_tr(&Gs[tr + 16 * t * RS + 32 * c]), y0 = lds_read_tr(&Gs[tr + (16 * t + 8) * RS + 32 * c]);
-        dv[c] = mfma32x32x16<F16>(u32x4{x0.x, x0.y, y0.x, y0.y}, pb, dv[c]);
-        const uint2 x1 = lds_read_tr(&Qs[tr + 16 * t * RS + 32 * c]), y1 = lds_read_tr(&Qs[tr + (16 * t + 8) * RS + 32 * c]);
-        dk[c] = mfma32x32x16<F16>(u32x4{x1.x, x1.y, y1.x, y1.y}, sb, dk[c]);
+            for (int o = 1; o < 64; o <<= 1) big = fmaxf(big, __shfl_xor(big, o, 64));
+            const int more = max(0, min((int)(__float_as_uint(big) >> 23) - 127 - 10, 100));
+            const float f = pow2f(-more);
+            ex += more;
+            fac *= f;
+#pragma unroll
+            for (int r = 0; r < 16; ++r) st[r] *= f;
+#pragma unroll
+            for (int b = 0; b < NB; ++b) sum[b] *= f;
+          }
+        }
+      }
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        const int r = 8 * t;
+        const u32x4 pb = round8<F16>(st, r);
+#pragma unroll
+        for (int c = 0; c < NB; ++c) {
+          const int f = t * NB + c, n = f + AHEAD;
+          sum[c] = mfma32x32x16<F16>(af[f % AHEAD], pb, sum[c]);
+          if (n < NS) {
+            af[f % AHEAD] = lds_frag_tr<D>(rows, tr, n / NB, n % NB);
+            in_order();
+          }
+        }
       }
     }
   }
+  const float f = for_k ? a.scale : 1.f;
+  if (!F16 || !for_k) ex = 0;
   if (it.part >= 0) {
     // float32 blocks [dk, dv][key][dim], the keys past the sample too (not read)
-    float* pb = a.partial + it.part * (2 * WIN_DK * D) + (int64_t)(32 * wave + lk) * D;
+    float* pb = a.partial + it.part * (2 * WIN_DK * D) + (for_k ? 0 : WIN_DK * D) + (int64_t)(32 * kg + lk) * D;
 #pragma unroll
     for (int b = 0; b < NB; ++b)
 #pragma unroll
       for (int g = 0; g < 4; ++g) {
-        floatx4 y, z;
+        floatx4 y;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          y[e] = F16 ? ldexpf(dk[b][4 * g + e] * a.scale, ex) : dk[b][4 * g + e] * a.scale;
-          z[e] = dv[b][4 * g + e];
-        }
+        for (int e = 0; e < 4; ++e) y[e] = ldexpf(sum[b][4 * g + e] * f, ex);
         *reinterpret_cast<floatx4*>(pb + 32 * b + 8 * g + 4 * half) = y;
-        *reinterpret_cast<floatx4*>(pb + WIN_DK * D + 32 * b + 8 * g + 4 * half) = z;
       }
     return;
   }
   if (!on) return;
-  uint16_t* ko = static_cast<uint16_t*>(a.dk) + krow * a.lddk + (int64_t)kvh * D;
-  uint16_t* vo = static_cast<uint16_t*>(a.dv) + krow * a.lddv + (int64_t)kvh * D;
+  uint16_t* out = (for_k ? static_cast<uint16_t*>(a.dk) + krow * a.lddk : static_cast<uint16_t*>(a.dv) + krow * a.lddv) +
+                  (int64_t)kvh * D;
 #pragma unroll
   for (int b = 0; b < NB; ++b)
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
       float y[4];
 #pragma unroll
-      for (int e = 0; e < 4; ++e)
-        y[e] = F16 ? ldexpf(dk[b][4 * g + e] * a.scale, ex) : dk[b][4 * g + e] * a.scale;
-      const int c = 32 * b + 8 * g + 4 * half;
-      *reinterpret_cast<uint2*>(ko + c) = make_uint2(pack_act2<F16>(y[0], y[1]), pack_act2<F16>(y[2], y[3]));
-      *reinterpret_cast<uint2*>(vo + c) = make_uint2(pack_act2<F16>(dv[b][4 * g], dv[b][4 * g + 1]),
-                                                     pack_act2<F16>(dv[b][4 * g + 2], dv[b][4 * g + 3]));
+      for (int e = 0; e < 4; ++e) y[e] = ldexpf(sum[b][4 * g + e] * f, ex);
+      *reinterpret_cast<uint2*>(out + 32 * b + 8 * g + 4 * half) =
+          make_uint2(round2<F16>(y[0], y[1]), round2<F16>(y[2], y[3]));
     }
 }
 
@@ -473,34 +601,34 @@ __global__ __launch_bounds__(NT) void window_dkv_join_kernel(WinBwdArgs a) {
     const int64_t krow = (int64_t)sg.k0 + it.kt * WIN_DK + r;
     uint16_t* out = which ? static_cast<uint16_t*>(a.dv) + krow * a.lddv : static_cast<uint16_t*>(a.dk) + krow * a.lddk;
     *reinterpret_cast<uint4*>(out + (int64_t)it.kvh * D + c) =
-        make_uint4(pack_act2<F16>(y[0], y[1]), pack_act2<F16>(y[2], y[3]), pack_act2<F16>(z[0], z[1]),
-                   pack_act2<F16>(z[2], z[3]));
+        make_uint4(round2<F16>(y[0], y[1]), round2<F16>(y[2], y[3]), round2<F16>(z[0], z[1]),
+                   round2<F16>(z[2], z[3]));
   }
 }
 
 }  // namespace
 
-#define SVL_WIN_LAUNCH(kernel)                                               \
+#define SVL_WIN_LAUNCH(kernel, threads)                                      \
   if (a.nitems <= 0) return hipSuccess;                                      \
   if (head_dim == 128) {                                                     \
-    if (f16) kernel<128, true><<<a.nitems, NT, 0, st>>>(a);                  \
-    else kernel<128, false><<<a.nitems, NT, 0, st>>>(a);                     \
+    if (f16) kernel<128, true><<<a.nitems, threads, 0, st>>>(a);             \
+    else kernel<128, false><<<a.nitems, threads, 0, st>>>(a);                \
   } else if (head_dim == 64) {                                               \
-    if (f16) kernel<64, true><<<a.nitems, NT, 0, st>>>(a);                   \
-    else kernel<64, false><<<a.nitems, NT, 0, st>>>(a);                      \
+    if (f16) kernel<64, true><<<a.nitems, threads, 0, st>>>(a);              \
+    else kernel<64, false><<<a.nitems, threads, 0, st>>>(a);                 \
   } else {                                                                   \
     return hipErrorInvalidValue;                                             \
   }                                                                          \
   return hipGetLastError();
 
 hipError_t launch_window_dq(const WinBwdArgs& a, int32_t head_dim, bool f16, hipStream_t st) {
-  SVL_WIN_LAUNCH(window_dq_kernel)
+  SVL_WIN_LAUNCH(window_dq_kernel, NT)
 }
 hipError_t launch_window_dkv(const WinBwdArgs& a, int32_t head_dim, bool f16, hipStream_t st) {
-  SVL_WIN_LAUNCH(window_dkv_kernel)
+  SVL_WIN_LAUNCH(window_dkv_kernel, DKV_NT)
 }
 hipError_t launch_window_dkv_join(const WinBwdArgs& a, int32_t head_dim, bool f16, hipStream_t st) {
-  SVL_WIN_LAUNCH(window_dkv_join_kernel)
+  SVL_WIN_LAUNCH(window_dkv_join_kernel, NT)
 }
 
 }  // namespace svl
