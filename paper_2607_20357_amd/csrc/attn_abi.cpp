@@ -287,22 +287,29 @@ hipError_t kv4_attention_segments(Kv4Args& a, CacheSegOf get, const void* ctx, i
     for (int32_t k = 0; k < a.nsegs; ++k)
       units += cdiv((int64_t)a.seg[k].rows * a.rep, 16 * ncb) * a.seg[k].kv_cnt * seg_units(a, a.seg[k]);
     const int64_t per = std::max<int64_t>(KV4_MIN_UNITS, cdiv(units, KV4_TARGET_ITEMS));
-    int64_t items = 0, parts = 0;
+    int64_t items = 0, parts = 0, cut = 0;
     for (int32_t k = 0; k < a.nsegs; ++k) {
       CacheSeg& s = a.seg[k];
       const int64_t blocks = cdiv((int64_t)s.rows * a.rep, 16 * ncb) * s.kv_cnt;
-      s.nsplit = (int32_t)cdiv(seg_units(a, s), per);
+      // (a cut pays for its join from two pieces' worth of work on)
+      const int64_t u = seg_units(a, s);
+      s.nsplit = u < 2 * per ? 1 : (int32_t)cdiv(u, per);
       s.item0 = (int32_t)items;
       s.part0 = (int32_t)parts;
+      s.join0 = (int32_t)cut;
       items += blocks * s.nsplit;
-      if (s.nsplit > 1) parts += blocks * s.nsplit;
+      if (s.nsplit > 1) {
+        parts += blocks * s.nsplit;
+        cut += blocks;
+      }
       if (items > INT32_MAX / 64) return hipErrorInvalidValue;
     }
     a.nitems = (int32_t)items;
     hipError_t e = timed_launch(K_ATTN, st, [&] { return launch_kv4_attention(a, head_dim, f16, ncb, st); });
     if (e != hipSuccess) return e;
-    if (parts > 0) {
-      e = timed_launch(K_ATTN, st, [&] { return launch_kv4_join(a, head_dim, f16, ncb, st); });
+    if (cut > 0) {
+      const int32_t most = (int32_t)std::min<int64_t>(columns, 16 * ncb);
+      e = timed_launch(K_ATTN, st, [&] { return launch_kv4_join(a, head_dim, f16, ncb, (int32_t)cut, most, st); });
       if (e != hipSuccess) return e;
     }
   }

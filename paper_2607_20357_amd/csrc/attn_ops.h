@@ -28,7 +28,7 @@ struct CacheSeg {
   int32_t item0;            // first work item of the segment
   int32_t nsplit;           // attention: pieces of its key range
   int32_t part0;            // attention: first partial block (nsplit > 1)
-  int32_t pad;
+  int32_t join0;            // attention: blocks of earlier cut segments (the join's grid)
 };
 
 struct Kv4Args {
@@ -56,9 +56,10 @@ struct Kv4Args {
 constexpr int kv4_ncb(int64_t columns) { return columns <= 16 ? 1 : 2; }
 constexpr int KV4_MAX_NCB = 2;
 constexpr int KV4_UNIT = 2 * KV4_TILE;     // positions that a wave takes at a time
-// A launch is cut into about this many work items (256 CUs, three workgroups
+// A launch is cut into about this many work items (256 CUs, two workgroups
 // each), and a piece has this many units at least (two per wave).
-constexpr int KV4_TARGET_ITEMS = 768, KV4_MIN_UNITS = 8;
+constexpr int KV4_TARGET_ITEMS = 512, KV4_MIN_UNITS = 8;
+constexpr int KV4_MAX_PIECES = KV4_TARGET_ITEMS + 1;   // of one block
 // Floats of a partial block: per column the maximum, the sum and d outputs.
 constexpr int64_t kv4_partial_floats(int ncb, int d) { return (int64_t)16 * ncb * (d + 2); }
 
@@ -66,9 +67,10 @@ hipError_t launch_kv4_append(const Kv4Args& a, int32_t head_dim, bool f16, hipSt
 hipError_t launch_kv4_read(const Kv4Args& a, int32_t head_dim, bool f16, hipStream_t st);
 hipError_t launch_kv4_attention(const Kv4Args& a, int32_t head_dim, bool f16, int32_t ncb,
                                 hipStream_t st);
-// Joins the pieces of the segments with nsplit > 1.
+// Joins the pieces of the segments with nsplit > 1: `blocks` of them, of up to
+// `columns` columns each.
 hipError_t launch_kv4_join(const Kv4Args& a, int32_t head_dim, bool f16, int32_t ncb,
-                           hipStream_t st);
+                           int32_t blocks, int32_t columns, hipStream_t st);
 
 // ---------------------------------------------------------------- packed rows
 // One sample: queries at rows q0 .. q0 + nq - 1, keys at rows k0 .. k0 + nk - 1;

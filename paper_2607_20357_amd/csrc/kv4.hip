@@ -46,16 +46,21 @@ __device__ __forceinline__ uint32_t round_down_bits(double q) {
 
 constexpr int NT = 256;   // append and read: four waves, each the K or the V half of a tile
 
-// One wave quantises the K or V half of a tile: lane = (row, quarter of its
-// dims).  Bound by memory: 2 d bytes in and d / 2 + d / 16 out per row.  The
-// codes are decided in float32 except within 2e-5 of a border between two
-// codes (float32's own error is below 5e-6 there), where float64 decides.
+// One wave quantises the K or V half of a tile: lane = (row, quarter), the quarter
+// holding the 16-byte pieces 4 i + quarter of its row, so a load takes 64 bytes a
+// row and a lane's K words are neighbours in the cache.  Bound by memory: 2 d bytes
+// in and d / 2 + d / 16 out per row.  A code is exact: k, the
+// floor of the rounded quotient, is it or one below, and x - lo (with the error of
+// its subtraction) is compared with the border (k + 1/2) s, which float32 holds
+// exactly.  (Float64 where float32 is near a border: ties are common among values
+// of 8 bits, 163 us for 15211 rows of 32 heads of 128 against 100.)
 template <int D, bool F16>
 __global__ __launch_bounds__(NT) void kv4_append_kernel(Kv4Args a) {
   typedef Tile<D> T;
-  constexpr int EL = D / 4, LG = KV4_GROUP / EL;   // dims of a lane, lanes of a group
-  __shared__ __attribute__((aligned(16))) uint8_t s_code[NT / 64][KV4_TILE][D];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  constexpr int NP = D / 32, G = T::G, PG = NP / G;   // pieces of a lane, of them in a group
+  constexpr int CS = D + 8;                           // row stride of the codes in LDS
+  __shared__ __attribute__((aligned(16))) uint8_t s_code[NT / 64][KV4_TILE][CS];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int item = blockIdx.x * (NT / 128) + (wave >> 1);
   const bool is_v = wave & 1;
   if (item >= a.nitems) return;
@@ -68,78 +73,91 @@ __global__ __launch_bounds__(NT) void kv4_append_kernel(Kv4Args a) {
   const int last = min(sg.pos0 + sg.rows - tile * KV4_TILE, KV4_TILE);       // [first, last)
   const int r = lane >> 2, qd = lane & 3;
   const bool on = r >= first && r < last;
-  uint32_t w[EL / 2];
+  uint4 w[NP];
+#pragma unroll
+  for (int i = 0; i < NP; ++i) w[i] = make_uint4(0, 0, 0, 0);
   if (on) {
     const int64_t row = (int64_t)sg.row0 + (tile * KV4_TILE + r - sg.pos0);
-    const uint16_t* src = static_cast<const uint16_t*>(is_v ? a.v : a.k) +
-                          row * (is_v ? a.ldv : a.ldk) + kvh * D + qd * EL;
+    const uint16_t* src = static_cast<const uint16_t*>(is_v ? a.v : a.k) + row * (is_v ? a.ldv : a.ldk) + kvh * D + 8 * qd;
 #pragma unroll
-    for (int i = 0; i < EL / 8; ++i) {
-      const uint4 x = reinterpret_cast<const uint4*>(src)[i];
-      w[4 * i] = x.x; w[4 * i + 1] = x.y; w[4 * i + 2] = x.z; w[4 * i + 3] = x.w;
-    }
-  } else {
-#pragma unroll
-    for (int i = 0; i < EL / 2; ++i) w[i] = 0;
+    for (int i = 0; i < NP; ++i) w[i] = *reinterpret_cast<const uint4*>(src + 32 * i);
   }
-  float lo = __builtin_inff(), hi = -__builtin_inff();
-  uint32_t top = 0;   // largest magnitude, as bits: tells inf and NaN
-#pragma unroll
-  for (int i = 0; i < EL / 2; ++i) {
-    const float x0 = act_bits_to_f32<F16>(w[i] & 0xffffu), x1 = act_bits_to_f32<F16>(w[i] >> 16);
-    lo = fminf(lo, fminf(x0, x1));
-    hi = fmaxf(hi, fmaxf(x0, x1));
-    top = max(top, max(w[i] & 0x7fffu, (w[i] >> 16) & 0x7fffu));
-  }
-#pragma unroll
-  for (int o = 1; o < LG; o <<= 1) {
-    lo = fminf(lo, __shfl_xor(lo, o, 64));
-    hi = fmaxf(hi, __shfl_xor(hi, o, 64));
-    top = max(top, (uint32_t)__shfl_xor((int)top, o, 64));
-  }
-  const bool bad = top >= (F16 ? 0x7c00u : 0x7f80u);
-  const uint32_t sb = bad ? (F16 ? 0x7e00u : 0x7fc0u) : round_down_bits<F16>(((double)hi - lo) / 15.0);
-  const uint32_t lb = bad ? (F16 ? 0x7e00u : 0x7fc0u) : f32_to_act_bits<F16>(lo);
-  const float s = act_bits_to_f32<F16>(sb);
-  const bool flat = bad || sb == 0;
-  const float inv = 1.0f / s;
-  auto code = [&](float x) -> uint32_t {
-    const float t = (x - lo) * inv;
-    float c = rintf(t);
-    if (!(fabsf(t - c) < 0.49998f)) c = (float)rint(((double)x - lo) / s);
-    return flat ? 0u : (uint32_t)fminf(fmaxf(c, 0.f), 15.f);
-  };
   uint8_t* tp = tile_ptr<D>(a, sg.sample, kvh, tile);
-  if (on && qd % LG == 0) {
-    uint32_t* par = reinterpret_cast<uint32_t*>(tp + 2 * T::CODES + (is_v ? T::PARAMS : 0));
-    par[((r >> 2) * T::G + qd / LG) * 4 + (r & 3)] = sb | (lb << 16);
+  uint32_t words[NP];       // eight codes of each piece
+#pragma unroll
+  for (int g = 0; g < G; ++g) {
+    float lo = __builtin_inff(), hi = -__builtin_inff();
+    uint32_t top = 0;       // largest magnitude, as bits: tells inf and NaN
+#pragma unroll
+    for (int i = g * PG; i < (g + 1) * PG; ++i) {
+      const uint32_t v[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float x0 = act_bits_to_f32<F16>(v[e] & 0xffffu), x1 = act_bits_to_f32<F16>(v[e] >> 16);
+        lo = fminf(lo, fminf(x0, x1));
+        hi = fmaxf(hi, fmaxf(x0, x1));
+        top = max(top, max(v[e] & 0x7fffu, (v[e] >> 16) & 0x7fffu));
+      }
+    }
+#pragma unroll
+    for (int o = 1; o < 4; o <<= 1) {
+      lo = fminf(lo, __shfl_xor(lo, o, 64));
+      hi = fmaxf(hi, __shfl_xor(hi, o, 64));
+      top = max(top, (uint32_t)__shfl_xor((int)top, o, 64));
+    }
+    const bool bad = top >= (F16 ? 0x7c00u : 0x7f80u);
+    const uint32_t sb = bad ? (F16 ? 0x7e00u : 0x7fc0u) : round_down_bits<F16>(((double)hi - lo) / 15.0);
+    const uint32_t lb = bad ? (F16 ? 0x7e00u : 0x7fc0u) : f32_to_act_bits<F16>(lo);
+    const float s = act_bits_to_f32<F16>(sb);
+    const bool flat = bad || sb == 0;
+    if (on && qd == g) {
+      uint32_t* par = reinterpret_cast<uint32_t*>(tp + 2 * T::CODES + (is_v ? T::PARAMS : 0));
+      par[((r >> 2) * G + g) * 4 + (r & 3)] = sb | (lb << 16);
+    }
+    // RARE: a step below the type's normal range may leave codes above 15; bf16's
+    // reciprocal or the range itself may overflow (then all is scaled by 2^100).
+    auto codes = [&]<bool RARE>() __attribute__((always_inline)) {
+      const float big = !RARE || F16 ? 1.f : s < 0x1p-100f ? 0x1p100f : s > 0x1p100f ? 0x1p-100f : 1.f;
+      const float sx = s * big, lx = lo * big, inv = 1.0f / sx, half = 0.5f * sx;
+#pragma unroll
+      for (int i = g * PG; i < (g + 1) * PG; ++i) {
+        const uint32_t v[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
+        uint32_t word = 0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          float x = act_bits_to_f32<F16>(e & 1 ? v[e / 2] >> 16 : v[e / 2] & 0xffffu);
+          if constexpr (RARE) x *= big;
+          const float d = x - lx, back = d - x;
+          const float err = (x - (d - back)) - (lx + back);     // x - lo = d + err
+          uint32_t c = (uint32_t)(d * inv);
+          const float over = (d - fmaf((float)c, sx, half)) + err;
+          // one more above the border, and on it if that makes c even (a sum that is 0 is +0)
+          c += (int)(__float_as_uint(over) + (c & 1)) > 0 ? 1u : 0u;
+          if constexpr (RARE) c = min(c, 15u);
+          word |= c << (4 * e);
+        }
+        words[i] = flat ? 0u : word;
+      }
+    };
+    if (__any(!flat && (s < (F16 ? 0x1p-14f : 0x1p-100f) || s > 0x1p100f))) codes.template operator()<true>();
+    else codes.template operator()<false>();
   }
   if (!is_v) {
-    // word j of the lane holds the dims of row word (qd EL / 8 + j)
+    // place of row word 4 i + qd: the lane's words are neighbours
     if (!on) return;
-#pragma unroll
-    for (int j = 0; j < EL / 8; ++j) {
-      uint32_t word = 0;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        word |= code(act_bits_to_f32<F16>(w[4 * j + i] & 0xffffu)) << (8 * i);
-        word |= code(act_bits_to_f32<F16>(w[4 * j + i] >> 16)) << (8 * i + 4);
-      }
-      const int row_word = qd * (EL / 8) + j;
-      const int place = (row_word & 3) * T::KW + (row_word >> 2);
-      reinterpret_cast<uint32_t*>(tp)[r * (D / 8) + place] = word;
-    }
+    uint32_t* dst = reinterpret_cast<uint32_t*>(tp) + r * (D / 8) + qd * T::KW;
+    if constexpr (NP == 4) *reinterpret_cast<uint4*>(dst) = make_uint4(words[0], words[1], words[2], words[3]);
+    else *reinterpret_cast<uint2*>(dst) = make_uint2(words[0], words[1]);
     return;
   }
   // V words hold two dims of four positions: exchange through LDS, and keep the
   // nibbles of positions outside this call
 #pragma unroll
-  for (int i = 0; i < EL / 4; ++i) {
-    const uint32_t c4 = code(act_bits_to_f32<F16>(w[2 * i] & 0xffffu)) |
-                        code(act_bits_to_f32<F16>(w[2 * i] >> 16)) << 8 |
-                        code(act_bits_to_f32<F16>(w[2 * i + 1] & 0xffffu)) << 16 |
-                        code(act_bits_to_f32<F16>(w[2 * i + 1] >> 16)) << 24;
-    *reinterpret_cast<uint32_t*>(&s_code[wave][r][qd * EL + 4 * i]) = c4;
+  for (int i = 0; i < NP; ++i) {
+    // a nibble to a byte
+    const uint32_t even = words[i] & 0x0f0f0f0fu, odd = (words[i] >> 4) & 0x0f0f0f0fu;
+    *reinterpret_cast<uint2*>(&s_code[wave][r][8 * (4 * i + qd)]) =
+        make_uint2(__builtin_amdgcn_perm(odd, even, 0x05010400u), __builtin_amdgcn_perm(odd, even, 0x07030602u));
   }
   wave_lds_handoff();
   uint32_t* vw = reinterpret_cast<uint32_t*>(tp + T::CODES);
@@ -152,7 +170,7 @@ __global__ __launch_bounds__(NT) void kv4_append_kernel(Kv4Args a) {
     for (int p = 0; p < 4; ++p) {
       const uint32_t two = *reinterpret_cast<const uint16_t*>(&s_code[wave][4 * quad + p][dim]);
       const int sh = 4 * (p >> 1) + 16 * (p & 1);    // dim 0; dim 1 eight bits above
-      word |= ((two & 15u) | (two >> 8) << 8) << sh;
+      word |= two << sh;
       const int pos = 4 * quad + p;
       if (pos >= first && pos < last) mine |= 0x0f0fu << sh;
     }
@@ -162,56 +180,70 @@ __global__ __launch_bounds__(NT) void kv4_append_kernel(Kv4Args a) {
   }
 }
 
-// One wave reads back the K or V half of a tile: lane = (row, quarter).  Bound
-// by memory, as the append.
+// One wave reads back the K or V half of a tile.  K: lane = (row, quarter) as in
+// the append.  V: lane = (quad of positions, 4 dims of each group), whose words are
+// neighbours.  Bound by memory, as the append.
 template <int D, bool F16>
 __global__ __launch_bounds__(NT) void kv4_read_kernel(Kv4Args a) {
   typedef Tile<D> T;
-  constexpr int EL = D / 4, LG = KV4_GROUP / EL;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  constexpr int NP = D / 32, G = T::G, PG = NP / G;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int item = blockIdx.x * (NT / 128) + (wave >> 1);
-  const bool is_v = wave & 1;
   if (item >= a.nitems) return;
   const CacheSeg& sg = a.seg[find_seg(a, item)];
   const int local = item - sg.item0;
   const int slot = local % sg.kv_cnt;
   const int tile = sg.pos0 / KV4_TILE + local / sg.kv_cnt;
   const int kvh = a.kv_table ? a.kv_table[sg.kv_off + slot] : slot;
+  const uint8_t* tp = tile_ptr<D>(a, sg.sample, kvh, tile);
+  auto value = [](uint32_t pair, uint32_t c) {
+    return fmaf(act_bits_to_f32<F16>(pair & 0xffffu), (float)c, act_bits_to_f32<F16>(pair >> 16));
+  };
+  if (wave & 1) {
+    const int quad = lane >> 4, L = lane & 15;
+    const uint32_t* vw = reinterpret_cast<const uint32_t*>(tp + T::CODES) + lane * T::VW;
+    const uint4* par = reinterpret_cast<const uint4*>(tp + 2 * T::CODES + T::PARAMS) + quad * G;
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+      const uint2 x = reinterpret_cast<const uint2*>(vw)[g];
+      const uint4 pr = par[g];
+      const uint32_t pairs[4] = {pr.x, pr.y, pr.z, pr.w};
+#pragma unroll
+      for (int p = 0; p < 4; ++p) {
+        const int pos = tile * KV4_TILE + 4 * quad + p, sh = 4 * (p >> 1) + 16 * (p & 1);
+        if (pos < sg.pos0 || pos >= sg.pos0 + sg.rows) continue;
+        uint16_t* dst = static_cast<uint16_t*>(a.v_out) + ((int64_t)sg.row0 + pos - sg.pos0) * a.ldv + kvh * D +
+                        KV4_GROUP * g + 4 * L;
+        *reinterpret_cast<uint2*>(dst) =
+            make_uint2(pack_act2<F16>(value(pairs[p], (x.x >> sh) & 15u), value(pairs[p], (x.x >> (sh + 8)) & 15u)),
+                       pack_act2<F16>(value(pairs[p], (x.y >> sh) & 15u), value(pairs[p], (x.y >> (sh + 8)) & 15u)));
+      }
+    }
+    return;
+  }
   const int r = lane >> 2, qd = lane & 3;
   const int pos = tile * KV4_TILE + r;
   if (pos < sg.pos0 || pos >= sg.pos0 + sg.rows) return;
-  const uint8_t* tp = tile_ptr<D>(a, sg.sample, kvh, tile);
-  const uint32_t pr = reinterpret_cast<const uint32_t*>(
-      tp + 2 * T::CODES + (is_v ? T::PARAMS : 0))[((r >> 2) * T::G + qd / LG) * 4 + (r & 3)];
-  const float s = act_bits_to_f32<F16>(pr & 0xffffu), lo = act_bits_to_f32<F16>(pr >> 16);
-  auto value = [&](uint32_t c) { return fmaf(s, (float)c, lo); };
-  uint32_t w[EL / 2];
-  if (!is_v) {
-    const uint32_t* kw = reinterpret_cast<const uint32_t*>(tp) + r * (D / 8);
-#pragma unroll
-    for (int j = 0; j < EL / 8; ++j) {
-      const int row_word = qd * (EL / 8) + j;
-      const uint32_t x = kw[(row_word & 3) * T::KW + (row_word >> 2)];
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        w[4 * j + i] = pack_act2<F16>(value((x >> (8 * i)) & 15u), value((x >> (8 * i + 4)) & 15u));
-    }
+  const uint32_t* par = reinterpret_cast<const uint32_t*>(tp + 2 * T::CODES) + (r >> 2) * G * 4 + (r & 3);
+  uint32_t words[NP];
+  const uint32_t* kw = reinterpret_cast<const uint32_t*>(tp) + r * (D / 8) + qd * T::KW;
+  if constexpr (NP == 4) {
+    const uint4 x = *reinterpret_cast<const uint4*>(kw);
+    words[0] = x.x, words[1] = x.y, words[2] = x.z, words[3] = x.w;
   } else {
-    const uint32_t* vw = reinterpret_cast<const uint32_t*>(tp + T::CODES);
-    const int sh = 4 * ((r >> 1) & 1) + 16 * (r & 1);
-#pragma unroll
-    for (int i = 0; i < EL / 4; ++i) {
-      const int dim = qd * EL + 4 * i, g = dim / KV4_GROUP, L = dim % KV4_GROUP / 4;
-      const uint2 x = *reinterpret_cast<const uint2*>(vw + ((r >> 2) * 16 + L) * T::VW + 2 * g);
-      w[2 * i] = pack_act2<F16>(value((x.x >> sh) & 15u), value((x.x >> (sh + 8)) & 15u));
-      w[2 * i + 1] = pack_act2<F16>(value((x.y >> sh) & 15u), value((x.y >> (sh + 8)) & 15u));
-    }
+    const uint2 x = *reinterpret_cast<const uint2*>(kw);
+    words[0] = x.x, words[1] = x.y;
   }
-  uint16_t* dst = static_cast<uint16_t*>(is_v ? a.v_out : a.k_out) +
-                  ((int64_t)sg.row0 + pos - sg.pos0) * (is_v ? a.ldv : a.ldk) + kvh * D + qd * EL;
+  uint16_t* dst = static_cast<uint16_t*>(a.k_out) + ((int64_t)sg.row0 + pos - sg.pos0) * a.ldk + kvh * D + 8 * qd;
 #pragma unroll
-  for (int i = 0; i < EL / 8; ++i)
-    reinterpret_cast<uint4*>(dst)[i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+  for (int i = 0; i < NP; ++i) {
+    const uint32_t pair = par[i / PG * 4], x = words[i];
+    uint32_t y[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      y[e] = pack_act2<F16>(value(pair, (x >> (8 * e)) & 15u), value(pair, (x >> (8 * e + 4)) & 15u));
+    *reinterpret_cast<uint4*>(dst + 32 * i) = make_uint4(y[0], y[1], y[2], y[3]);
+  }
 }
 
 // ---------------------------------------------------------------- attention
@@ -248,16 +280,43 @@ __device__ __forceinline__ Units units_of(int p_lo, int p_hi, int window, int si
 
 __device__ __forceinline__ float pow2f(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }
 
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 template <int N> struct Words;
-template <> struct Words<4> { typedef uint4 type; };
-template <> struct Words<2> { typedef uint2 type; };
+template <> struct Words<4> { typedef u32x4 type; };
+template <> struct Words<2> { typedef u32x2 type; };
+
+template <int N>
+__device__ __forceinline__ typename Words<N>::type load_words(__amdgpu_buffer_rsrc_t r, uint32_t voff, uint32_t soff) {
+  if constexpr (N == 4) return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, voff, soff, 0));
+  else return __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(r, voff, soff, 0));
+}
+
+// Maximum over the four lanes of a column (lane, lane ^ 16, lane ^ 32, lane ^ 48).
+__device__ __forceinline__ float column_max(float x) {
+  const u32x2 a = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false));
+  x = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+  const u32x2 b = __builtin_bit_cast(u32x2, __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false));
+  return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+
+// Two codes of a word as fp16 subnormals: nibbles 0 and 4 (c 2^-24), 1 and 5 (c 2^-20).
+__device__ __forceinline__ u32x4 four_pairs(uint32_t w) {
+  return u32x4{w & 0x000f000fu, w & 0x00f000f0u, (w >> 8) & 0x000f000fu, (w >> 8) & 0x00f000f0u};
+}
+
+__device__ __forceinline__ floatx4 mfma_codes(const u32x4& a, const u32x4& b, const floatx4& c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8_t, a), __builtin_bit_cast(f16x8_t, b), c, 0, 0, 0);
+}
+
+__device__ __forceinline__ uint32_t round_pair(float lo, float hi) { return pack_act2<true>(lo, hi); }
 
 template <int D, bool F16, int NCB>
-__global__ __launch_bounds__(AT) void kv4_attn_kernel(Kv4Args a) {
+__global__ __launch_bounds__(AT, NCB == 1 ? 2 : 1) void kv4_attn_kernel(Kv4Args a) {
   typedef Tile<D> T;
   constexpr int G = T::G, NS = D / 32;
-  typedef typename Words<T::KW>::type KWords;
-  typedef typename Words<T::VW>::type VWords;
+  typedef typename Words<T::KW>::type CodeWords;   // (K and V: as many words a lane)
+  static_assert(T::KW == T::VW, "code words of a lane");
   __shared__ float s_o[AW][16][D + 4];
   __shared__ float s_m[AW][16], s_l[AW][16];
   const int item = blockIdx.x;
@@ -267,7 +326,7 @@ __global__ __launch_bounds__(AT) void kv4_attn_kernel(Kv4Args a) {
   const int local = item - sg.item0, split = local % sg.nsplit, block = local / sg.nsplit;
   const int cb = block % ncb, slot = block / ncb;
   const int kvh = a.kv_table ? a.kv_table[sg.kv_off + slot] : slot;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int gq = lane >> 4, lq = lane & 15;
   const int c0 = cb * 16 * NCB;
   const int p_lo = sg.pos0 + c0 / rep, p_hi = sg.pos0 + (min(c0 + 16 * NCB, cols) - 1) / rep;
@@ -278,7 +337,7 @@ __global__ __launch_bounds__(AT) void kv4_attn_kernel(Kv4Args a) {
   // query fragments; a pair of codes is (dim i, dim i + 4) of a word, the pairs
   // 1 and 3 carry a factor 16
   const float sl2 = a.scale * 1.4426950408889634f;   // scores in log2 units
-  uint4 qf[NCB][NS];
+  u32x4 qf[NCB][NS];
   float qs[NCB][G], fl[NCB];
   int pq[NCB];                                       // the column's position
 #pragma unroll
@@ -324,8 +383,8 @@ __global__ __launch_bounds__(AT) void kv4_attn_kernel(Kv4Args a) {
     for (int s = 0; s < NS; ++s) {
       const float* y = x[s];
       const float up4 = up * 0.0625f;
-      qf[n][s] = make_uint4(pack_act2<true>(y[0] * up, y[4] * up), pack_act2<true>(y[1] * up4, y[5] * up4),
-                            pack_act2<true>(y[2] * up, y[6] * up), pack_act2<true>(y[3] * up4, y[7] * up4));
+      qf[n][s] = u32x4{round_pair(y[0] * up, y[4] * up), round_pair(y[1] * up4, y[5] * up4),
+                       round_pair(y[2] * up, y[6] * up), round_pair(y[3] * up4, y[7] * up4)};
     }
   }
 
@@ -346,96 +405,112 @@ __global__ __launch_bounds__(AT) void kv4_attn_kernel(Kv4Args a) {
   // largest scale seen
   int ve = F16 ? 2 : 126;
 
-  const uint8_t* head = tile_ptr<D>(a, sg.sample, kvh, 0);
-  const int64_t last_tile = a.tiles - 1;
-  for (int u = u0 + wave; u < u1; u += AW) {
-    const int unit = u < un.us ? u : un.uw + (u - un.us);
-    const int kv0 = unit * UNIT;
-    KWords kw[2];
-    VWords vw[2];
-    uint4 kp[2][G], vp[2][G];
+  // a head's cache is below 2^28 bytes; tiles past its end (the second of the last
+  // unit) read as zeros
+  const __amdgpu_buffer_rsrc_t head = make_rsrc(tile_ptr<D>(a, sg.sample, kvh, 0), (uint32_t)(a.tiles * T::BYTES));
+  const uint32_t at_k = (lq * 4 + gq) * T::KW * 4, at_v = T::CODES + lane * T::VW * 4;
+  const uint32_t at_p = 2 * T::CODES + gq * G * 16;
+  const int wlim = a.window > 0 ? a.window : 1 << 30;   // (positions are below 2^20)
+
+  struct Loaded {
+    CodeWords kw[2], vw[2];
+    u32x4 kp[2][G], vp[2][G];
+  };
+  auto load = [&](int unit) __attribute__((always_inline)) {
+    Loaded x;
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
-      // the second tile of the last unit may lie past the cache: any tile will do
-      const uint8_t* tp = head + min((int64_t)2 * unit + t, last_tile) * T::BYTES;
-      kw[t] = reinterpret_cast<const KWords*>(tp)[lq * 4 + gq];
-      vw[t] = reinterpret_cast<const VWords*>(tp + T::CODES)[lane];
+      const uint32_t tile = (uint32_t)(2 * unit + t) * T::BYTES;
+      x.kw[t] = load_words<T::KW>(head, at_k, tile);
 #pragma unroll
-      for (int g = 0; g < G; ++g) {
-        kp[t][g] = reinterpret_cast<const uint4*>(tp + 2 * T::CODES)[gq * G + g];
-        vp[t][g] = reinterpret_cast<const uint4*>(tp + 2 * T::CODES + T::PARAMS)[gq * G + g];
-      }
+      for (int g = 0; g < G; ++g) x.kp[t][g] = load_words<4>(head, at_p + 16 * g, tile);
+      x.vw[t] = load_words<T::VW>(head, at_v, tile);
+#pragma unroll
+      for (int g = 0; g < G; ++g) x.vp[t][g] = load_words<4>(head, at_p + T::PARAMS + 16 * g, tile);
     }
-    // whether every column sees every position of the unit
-    const bool whole = kv0 + UNIT - 1 <= p_lo &&
-                       (a.window <= 0 || kv0 > p_hi - a.window || kv0 + UNIT <= a.sinks);
-    uint4 kf[2][NS];
-#pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      const uint32_t* w = reinterpret_cast<const uint32_t*>(&kw[t]);
-#pragma unroll
-      for (int s = 0; s < NS; ++s)
-        kf[t][s] = make_uint4(w[s] & 0x000f000fu, w[s] & 0x00f000f0u, (w[s] >> 8) & 0x000f000fu,
-                              (w[s] >> 8) & 0x00f000f0u);
-    }
-    float vmax = 0.f;
-    if constexpr (!F16) {
+    return x;
+  };
+  // One unit; PART: some column does not see some position of it.
+  auto unit_of = [&](int u) { return u < un.us ? u : un.uw + (u - un.us); };
+  auto add_unit = [&]<bool PART>(Loaded x, int kv0) __attribute__((always_inline)) {
+    if constexpr (PART) {
+      // a position that no column sees may hold anything
 #pragma unroll
       for (int t = 0; t < 2; ++t)
 #pragma unroll
-        for (int g = 0; g < G; ++g) {
-          const uint32_t* pw = reinterpret_cast<const uint32_t*>(&vp[t][g]);
+        for (int r = 0; r < 4; ++r) {
+          const int j = kv0 + 16 * t + 4 * gq + r;
 #pragma unroll
-          for (int r = 0; r < 4; ++r)
-            if (kv0 + 16 * t + 4 * gq + r <= p_hi) vmax = fmaxf(vmax, bf16_bits_to_f32(pw[r] & 0xffffu));
+          for (int g = 0; g < G; ++g) x.vp[t][g][r] = j <= p_hi ? x.vp[t][g][r] : 0u;
         }
-      vmax = fmaxf(vmax, __shfl_xor(vmax, 16, 64));
-      vmax = fmaxf(vmax, __shfl_xor(vmax, 32, 64));
+    }
+    u32x4 kf[2][NS];
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int s = 0; s < NS; ++s) kf[t][s] = four_pairs(x.kw[t][s]);
+    if constexpr (!F16) {
+      float vmax = 0.f;
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int g = 0; g < G; ++g)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) vmax = fmaxf(vmax, bf16_bits_to_f32(x.vp[t][g][r] & 0xffffu));
+      vmax = column_max(vmax);
       // scales below 2^(e + 1) with e the largest one's exponent: P' < 2^15
       const int want = max(-126, min(126, 14 - ((int)(__float_as_uint(vmax) >> 23) - 127)));
-      if (want < ve) {   // the same in every lane
-        const float f = ldexpf(1.0f, want - ve);
+      if (__any(want < ve)) {   // (the same in every lane)
+        const float f = ldexpf(1.0f, min(want - ve, 0));
 #pragma unroll
         for (int n = 0; n < NCB; ++n)
 #pragma unroll
           for (int g = 0; g < G; ++g)
 #pragma unroll
             for (int j = 0; j < 4; ++j) o[n][g][j] *= f;
-        ve = want;
+        ve = min(ve, want);
       }
     }
-    const float pf0 = pow2f(ve), pf1 = pf0 * 0.0625f;
+    const float pf0 = F16 ? 4.f : pow2f(ve), pf1 = pf0 * 0.0625f;
 #pragma unroll
     for (int n = 0; n < NCB; ++n) {
       float sc[2][4];
-      bool vis[2][4];
-      float mx = -__builtin_inff();
+      uint32_t vis = 0xffu;
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
         floatx4 acc[G];
 #pragma unroll
         for (int g = 0; g < G; ++g) {
-          acc[g] = floatx4{0.f, 0.f, 0.f, 0.f};
-          acc[g] = mfma16x16x32<true>(kf[t][2 * g], qf[n][2 * g], acc[g]);
-          acc[g] = mfma16x16x32<true>(kf[t][2 * g + 1], qf[n][2 * g + 1], acc[g]);
+          acc[g] = mfma_codes(kf[t][2 * g], qf[n][2 * g], floatx4{0.f, 0.f, 0.f, 0.f});
+          acc[g] = mfma_codes(kf[t][2 * g + 1], qf[n][2 * g + 1], acc[g]);
         }
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           float v = 0.f;
 #pragma unroll
           for (int g = 0; g < G; ++g) {
-            const uint32_t pw = reinterpret_cast<const uint32_t*>(&kp[t][g])[r];
+            const uint32_t pw = x.kp[t][g][r];
             v = fmaf(act_bits_to_f32<F16>(pw & 0xffffu), acc[g][r], v);
             v = fmaf(act_bits_to_f32<F16>(pw >> 16), qs[n][g], v);
           }
-          const int j = kv0 + 16 * t + 4 * gq + r;
-          vis[t][r] = whole || (j <= pq[n] && (a.window <= 0 || j > pq[n] - a.window || j < a.sinks));
-          sc[t][r] = vis[t][r] ? v : -__builtin_inff();
-          mx = fmaxf(mx, sc[t][r]);
+          sc[t][r] = v;
         }
       }
-      mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
-      mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+      if constexpr (PART) {
+        vis = 0;
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const int j = kv0 + 16 * t + 4 * gq + r;
+            const bool ok = (j <= pq[n]) & ((j > pq[n] - wlim) | (j < a.sinks));   // (no short cuts: branches)
+            sc[t][r] = ok ? sc[t][r] : -__builtin_inff();
+            vis |= (uint32_t)ok << (4 * t + r);
+          }
+      }
+      float mx = fmaxf(fmaxf(fmaxf(sc[0][0], sc[0][1]), fmaxf(sc[0][2], sc[0][3])),
+                       fmaxf(fmaxf(sc[1][0], sc[1][1]), fmaxf(sc[1][2], sc[1][3])));
+      mx = column_max(mx);
       if (__any(mx > m[n])) {
         const float mn = fmaxf(m[n], mx);
         const float alpha = mn == -__builtin_inff() ? 1.f : __builtin_amdgcn_exp2f((m[n] - mn) * fl[n]);
@@ -448,13 +523,13 @@ __global__ __launch_bounds__(AT) void kv4_attn_kernel(Kv4Args a) {
         }
         m[n] = mn;
       }
-      const float mu = m[n] == -__builtin_inff() ? 0.f : m[n];   // nothing above -inf yet
+      const float mf = m[n] == -__builtin_inff() ? 0.f : -m[n] * fl[n];   // nothing above -inf yet: 0
       float p[2][4];
 #pragma unroll
       for (int t = 0; t < 2; ++t)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          p[t][r] = vis[t][r] ? __builtin_amdgcn_exp2f((sc[t][r] - mu) * fl[n]) : 0.f;
+          p[t][r] = __builtin_amdgcn_exp2f(fmaf(sc[t][r], fl[n], mf));
           l[n] += p[t][r];
         }
 #pragma unroll
@@ -464,22 +539,35 @@ __global__ __launch_bounds__(AT) void kv4_attn_kernel(Kv4Args a) {
         for (int t = 0; t < 2; ++t)
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
-            const uint32_t pw = reinterpret_cast<const uint32_t*>(&vp[t][g])[r];
-            const float vs = act_bits_to_f32<F16>(pw & 0xffffu), vl = act_bits_to_f32<F16>(pw >> 16);
-            // a position that is not seen may hold anything
-            ol[n][g] = vis[t][r] ? fmaf(p[t][r], vl, ol[n][g]) : ol[n][g];
-            ps[t][r] = vis[t][r] ? p[t][r] * vs * (r < 2 ? pf0 : pf1) : 0.f;
+            uint32_t pw = x.vp[t][g][r];
+            if constexpr (PART) pw = (vis >> (4 * t + r)) & 1 ? pw : 0u;
+            ol[n][g] = fmaf(p[t][r], act_bits_to_f32<F16>(pw >> 16), ol[n][g]);
+            ps[t][r] = p[t][r] * (r < 2 ? pf0 : pf1) * act_bits_to_f32<F16>(pw & 0xffffu);
           }
-        const uint4 pb = make_uint4(pack_act2<true>(ps[0][0], ps[0][1]), pack_act2<true>(ps[0][2], ps[0][3]),
-                                    pack_act2<true>(ps[1][0], ps[1][1]), pack_act2<true>(ps[1][2], ps[1][3]));
+        const u32x4 pb = {round_pair(ps[0][0], ps[0][1]), round_pair(ps[0][2], ps[0][3]),
+                          round_pair(ps[1][0], ps[1][1]), round_pair(ps[1][2], ps[1][3])};
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          const uint32_t x = reinterpret_cast<const uint32_t*>(&vw[0])[2 * g + j / 2] >> (8 * (j & 1));
-          const uint32_t y = reinterpret_cast<const uint32_t*>(&vw[1])[2 * g + j / 2] >> (8 * (j & 1));
-          const uint4 vf = make_uint4(x & 0x000f000fu, x & 0x00f000f0u, y & 0x000f000fu, y & 0x00f000f0u);
-          o[n][g][j] = mfma16x16x32<true>(vf, pb, o[n][g][j]);
+          const uint32_t y = x.vw[0][2 * g + j / 2] >> (8 * (j & 1)), z = x.vw[1][2 * g + j / 2] >> (8 * (j & 1));
+          o[n][g][j] = mfma_codes(u32x4{y & 0x000f000fu, y & 0x00f000f0u, z & 0x000f000fu, z & 0x00f000f0u}, pb, o[n][g][j]);
         }
       }
+    }
+  };
+  // whether every column sees every position of a unit
+  const int whole_hi = p_lo - UNIT + 1, whole_lo = a.window > 0 ? p_hi - a.window : -1, whole_sink = a.sinks - UNIT;
+  int u = u0 + wave;
+  if (u < u1) {
+    Loaded next = load(unit_of(u));
+    for (; u < u1; u += AW) {
+      const Loaded x = next;
+      const int kv0 = unit_of(u) * UNIT;
+      // the next unit in flight meanwhile (8 x 8192 positions of 32 heads: 86 -> 71 us);
+      // with 32 columns there are more products to hide it behind, and no registers
+      if constexpr (NCB == 1) next = load(unit_of(min(u + AW, u1 - 1)));
+      if (kv0 <= whole_hi && (kv0 > whole_lo || kv0 <= whole_sink)) add_unit.template operator()<false>(x, kv0);
+      else add_unit.template operator()<true>(x, kv0);
+      if constexpr (NCB > 1) next = load(unit_of(min(u + AW, u1 - 1)));
     }
   }
 
@@ -549,57 +637,75 @@ __global__ __launch_bounds__(AT) void kv4_attn_kernel(Kv4Args a) {
   }
 }
 
-// Joins a column's pieces in piece order: one wave per column, D / 64 dims a lane.
+// Joins the pieces of one column of a cut block, in piece order within each of four
+// waves.  Bound by latency: the pieces' maxima are weighed at once, their outputs
+// read eight at a time per wave (78 pieces by one wave, a load after the other: 26 us).
 template <int D, bool F16>
 __global__ __launch_bounds__(AT) void kv4_join_kernel(Kv4Args a, int ncb16) {
-  const int lane = threadIdx.x & 63;
-  const int64_t id = (int64_t)blockIdx.x * AW + (threadIdx.x >> 6);   // column among the items'
-  const int item = (int)(id / ncb16), col = (int)(id % ncb16);
-  if (item >= a.nitems) return;
-  const CacheSeg& sg = a.seg[find_seg(a, item)];
-  const int local = item - sg.item0;
-  if (sg.nsplit == 1 || local % sg.nsplit) return;
-  const int block = local / sg.nsplit;
+  constexpr int DL = D / 64;
+  __shared__ float s_f[KV4_MAX_PIECES];
+  __shared__ float s_red[2][AW], s_y[AW][D];
+  int k = 0;
+  for (int lo = 0, hi = a.nsegs - 1; lo <= hi;) {   // the last segment that begins at or before the block
+    const int mid = (lo + hi) >> 1;
+    if (a.seg[mid].join0 <= (int)blockIdx.x) k = mid, lo = mid + 1; else hi = mid - 1;
+  }
+  const CacheSeg& sg = a.seg[k];
+  const int block = (int)blockIdx.x - sg.join0, n = sg.nsplit;
   const int rep = a.rep, cols = sg.rows * rep, ncb = (cols + ncb16 - 1) / ncb16;
-  const int c = block % ncb * ncb16 + col, slot = block / ncb;
+  const int col = blockIdx.y, c = block % ncb * ncb16 + col, slot = block / ncb;
   if (c >= cols) return;
   const int kvh = a.kv_table ? a.kv_table[sg.kv_off + slot] : slot;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int64_t stride = (int64_t)ncb16 * (D + 2);
-  const float* pb = a.partial + ((int64_t)sg.part0 + (int64_t)block * sg.nsplit) * stride + (int64_t)col * (D + 2);
-  constexpr int DL = D / 64;
-  float M = -__builtin_inff(), L = 0.f, y[DL];
+  const float* pb = a.partial + ((int64_t)sg.part0 + (int64_t)block * n) * stride + (int64_t)col * (D + 2);
+  float M = -__builtin_inff();
+  for (int s = tid; s < n; s += AT) {
+    s_f[s] = pb[s * stride];
+    M = fmaxf(M, s_f[s]);
+  }
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor(M, o, 64));
+  if (lane == 0) s_red[0][wave] = M;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < AW; ++w) M = fmaxf(M, s_red[0][w]);
+  float L = 0.f;
+  for (int s = tid; s < n; s += AT) {
+    const float f = s_f[s] == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f(s_f[s] - M);
+    s_f[s] = f;
+    L = fmaf(f, pb[s * stride + 1], L);
+  }
+  L = warp_sum(L);
+  if (lane == 0) s_red[1][wave] = L;
+  __syncthreads();
+  float y[DL];
 #pragma unroll
   for (int e = 0; e < DL; ++e) y[e] = 0.f;
-  // 64 pieces at a time: a lane weighs one, then the outputs are added with the
-  // weights passed around, eight loads in flight (a load that waits for the one
-  // before: 26 us for 78 pieces)
-  for (int s0 = 0; s0 < sg.nsplit; s0 += 64) {
-    const bool there = s0 + lane < sg.nsplit;
-    const float m = there ? pb[(s0 + lane) * stride] : -__builtin_inff();
-    const float l = there ? pb[(s0 + lane) * stride + 1] : 0.f;
-    float mn = fmaxf(M, m);
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) mn = fmaxf(mn, __shfl_xor(mn, o, 64));
-    const float f = m == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f(m - mn);
-    const float back = M == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f(M - mn);
-    L = fmaf(L, back, warp_sum(f * l));
-#pragma unroll
-    for (int e = 0; e < DL; ++e) y[e] *= back;
-    M = mn;
-    const int n = min(64, sg.nsplit - s0);
 #pragma unroll 8
-    for (int s = 0; s < n; ++s) {
-      const float* p = pb + (s0 + s) * stride + 2 + DL * lane;
-      const float fs = __shfl(f, s, 64);
+  for (int s = wave; s < n; s += AW) {
+    const float* p = pb + s * stride + 2 + DL * lane;
+    const float f = s_f[s];
 #pragma unroll
-      for (int e = 0; e < DL; ++e) y[e] = fmaf(fs, p[e], y[e]);
-    }
+    for (int e = 0; e < DL; ++e) y[e] = fmaf(f, p[e], y[e]);
   }
+#pragma unroll
+  for (int e = 0; e < DL; ++e) s_y[wave][DL * lane + e] = y[e];
+  __syncthreads();
+  if (wave) return;
+  L = s_red[1][0] + s_red[1][1] + s_red[1][2] + s_red[1][3];
   const float inv = 1.0f / L;
+#pragma unroll
+  for (int e = 0; e < DL; ++e) {
+    y[e] = 0.f;
+#pragma unroll
+    for (int w = 0; w < AW; ++w) y[e] += s_y[w][DL * lane + e];
+    y[e] *= inv;
+  }
   uint16_t* out = static_cast<uint16_t*>(a.out) + ((int64_t)sg.row0 + c / rep) * a.ldo +
                   ((int64_t)kvh * rep + c % rep) * D + DL * lane;
-  if constexpr (DL == 2) *reinterpret_cast<uint32_t*>(out) = pack_act2<F16>(y[0] * inv, y[1] * inv);
-  else *out = f32_to_act_bits<F16>(y[0] * inv);
+  if constexpr (DL == 2) *reinterpret_cast<uint32_t*>(out) = pack_act2<F16>(y[0], y[1]);
+  else *out = f32_to_act_bits<F16>(y[0]);
 }
 
 template <int D, bool F16>
@@ -653,9 +759,9 @@ hipError_t launch_kv4_attention(const Kv4Args& a, int32_t head_dim, bool f16, in
 }
 
 hipError_t launch_kv4_join(const Kv4Args& a, int32_t head_dim, bool f16, int32_t ncb,
-                           hipStream_t st) {
-  if (a.nitems <= 0) return hipSuccess;
-  const int grid = (int)(((int64_t)a.nitems * 16 * ncb + AW - 1) / AW);
+                           int32_t blocks, int32_t columns, hipStream_t st) {
+  if (blocks <= 0) return hipSuccess;
+  const dim3 grid((unsigned)blocks, (unsigned)columns);
   if (head_dim == 128) {
     if (f16) kv4_join_kernel<128, true><<<grid, AT, 0, st>>>(a, 16 * ncb);
     else kv4_join_kernel<128, false><<<grid, AT, 0, st>>>(a, 16 * ncb);

@@ -164,13 +164,6 @@ __device__ __forceinline__ u32x4 lds_frag_tr(const uint16_t* rows, int tr, int t
   return u32x4{lo.x, lo.y, hi.x, hi.y};
 }
 
-// Keeps the order of what stands before and after it.  Each product is followed
-// by the read of the fragment AHEAD products later, into the registers that it
-// frees.  Left to itself the compiler reads one or two ahead, and an LDS read
-// takes longer than a product; with eight ahead the registers do not suffice.
-constexpr int AHEAD = 4;
-__device__ __forceinline__ void in_order() { __builtin_amdgcn_sched_barrier(0); }
-
 // Two values rounded to 16 bits, in one instruction for either type.
 template <bool F16>
 __device__ __forceinline__ uint32_t round2(float lo, float hi) {

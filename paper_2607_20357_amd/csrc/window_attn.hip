@@ -141,27 +141,16 @@ __global__ __launch_bounds__(256, 2) void window_attn_kernel(WinArgs a) {
     const uint16_t* Ks = s_kv[u & 1];
     const uint16_t* Vs = Ks + BK * D;
 
-    // 32 keys at a time; fragments in the order of their products: K, V of each half
-    static_assert(2 * NB == NS, "fragments of a step");
-    u32x4 af[AHEAD];
-    auto frag = [&](int f) __attribute__((always_inline)) {
-      const int kb = KP == 2 ? part : f / (2 * NS), s = f % NS;
-      if (f % (2 * NS) < NS) return lds_read16(&Ks[(fr ^ 16 * s) + 32 * kb * D]);
-      return lds_frag_tr<D>(Vs, tr, 2 * kb + s / NB, s % NB);
-    };
-#pragma unroll
-    for (int f = 0; f < AHEAD; ++f) af[f] = frag(f);
+    // 32 keys at a time
 #pragma unroll
     for (int b = 0; b < KB; ++b) {
-      const int kb = KP == 2 ? part : b, f0 = 2 * NS * b;
+      const int kb = KP == 2 ? part : b;
       floatx16 st;
 #pragma unroll
       for (int r = 0; r < 16; ++r) st[r] = 0.f;
 #pragma unroll
-      for (int s = 0; s < NS; ++s) {
-        st = mfma32x32x16<F16>(af[s % AHEAD], qf[s], st);
-        af[s % AHEAD] = frag(f0 + s + AHEAD);
-      }
+      for (int s = 0; s < NS; ++s)
+        st = mfma32x32x16<F16>(lds_read16(&Ks[(fr ^ 16 * s) + 32 * kb * D]), qf[s], st);
       if (!here.whole || here.keys != ~uint64_t(0)) {
         const int j0 = kv + 32 * kb + 4 * half;   // element r is key j0 + 8 (r / 4) + r % 4
         const uint32_t see = (uint32_t)(here.keys >> (32 * kb)) >> (4 * half);
@@ -173,14 +162,15 @@ __global__ __launch_bounds__(256, 2) void window_attn_kernel(WinArgs a) {
           poison |= (see & (bad >> (4 * half)) & 0x0f0f0f0fu) != 0;
         } else {
           const int top = p - j0, low = top - wlim, sink = a.sinks - j0;
-          auto ok = [&](int x) { return x <= top && (x > low || x < sink) && ((see >> x) & 1); };
+          // (no short cuts: they would be branches)
+          auto ok = [&](int x) { return bool((x <= top) & ((x > low) | (x < sink)) & ((see >> x) & 1)); };
 #pragma unroll
           for (int r = 0; r < 16; ++r) st[r] = ok(8 * (r / 4) + r % 4) ? st[r] : -__builtin_inff();
           if (bad)
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
               const int x = 8 * (r / 4) + r % 4;
-              poison |= ok(x) && ((bad >> (4 * half + x)) & 1);
+              poison |= ok(x) & ((bad >> (4 * half + x)) & 1);
             }
         }
       }
@@ -209,13 +199,8 @@ __global__ __launch_bounds__(256, 2) void window_attn_kernel(WinArgs a) {
         const int r = 8 * t;
         const u32x4 pb = round8<F16>(st, r);
 #pragma unroll
-        for (int c = 0; c < NB; ++c) {
-          const int s = t * NB + c, next = f0 + NS + s + AHEAD;
-          o[c] = mfma32x32x16<F16>(af[s % AHEAD], pb, o[c]);
-          if (next < 2 * KB * NS) {
-            af[s % AHEAD] = frag(next);
-              }
-        }
+        for (int c = 0; c < NB; ++c)
+          o[c] = mfma32x32x16<F16>(lds_frag_tr<D>(Vs, tr, 2 * kb + t, c), pb, o[c]);
       }
     }
   }

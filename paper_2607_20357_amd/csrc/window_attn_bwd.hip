@@ -166,27 +166,13 @@ __global__ __launch_bounds__(NT, 2) void window_dq_kernel(WinBwdArgs a) {
     const uint16_t* Ks = s_kv[u & 1];
     const uint16_t* Vs = Ks + BK * D;
     const bool partial = !here.whole || here.keys != ~0u;
-    // fragments in the order of their products: K, V, K transposed
-    static_assert(2 * NB == NS, "fragments of a step");
-    u32x4 af[AHEAD];
-    auto frag = [&](int f) __attribute__((always_inline)) {
-      const int s = f % NS;
-      return f < 2 * NS ? lds_read16(&(f < NS ? Ks : Vs)[fr ^ 16 * s]) : lds_frag_tr<D>(Ks, tr, s / NB, s % NB);
-    };
-#pragma unroll
-    for (int f = 0; f < AHEAD; ++f) af[f] = frag(f);
     floatx16 st, dp;
 #pragma unroll
     for (int r = 0; r < 16; ++r) st[r] = dp[r] = 0.f;
 #pragma unroll
     for (int s = 0; s < NS; ++s) {
-      st = mfma32x32x16<F16>(af[s % AHEAD], qf[s], st);
-      af[s % AHEAD] = frag(s + AHEAD);
-    }
-#pragma unroll
-    for (int s = 0; s < NS; ++s) {
-      dp = mfma32x32x16<F16>(af[s % AHEAD], gf[s], dp);
-      af[s % AHEAD] = frag(NS + s + AHEAD);
+      st = mfma32x32x16<F16>(lds_read16(&Ks[fr ^ 16 * s]), qf[s], st);
+      dp = mfma32x32x16<F16>(lds_read16(&Vs[fr ^ 16 * s]), gf[s], dp);
     }
 #pragma unroll
     for (int r = 0; r < 16; ++r) st[r] = exp2_raw(fmaf(st[r], sl2, -lse2)) * ((dp[r] - delta) * fac);
@@ -194,14 +180,15 @@ __global__ __launch_bounds__(NT, 2) void window_dq_kernel(WinBwdArgs a) {
       const int j0 = kv + 4 * half;   // element r is key j0 + 8 (r / 4) + r % 4
       const uint32_t see = here.keys >> (4 * half), bad = __builtin_amdgcn_readfirstlane(s_bad[bad_at]);
       const int top = p - j0, low = top - wlim, sink = a.sinks - j0;
-      auto ok = [&](int x) { return x <= top && (x > low || x < sink) && ((see >> x) & 1); };
+      // (no short cuts: they would be branches)
+      auto ok = [&](int x) { return bool((x <= top) & ((x > low) | (x < sink)) & ((see >> x) & 1)); };
 #pragma unroll
       for (int r = 0; r < 16; ++r) st[r] = ok(8 * (r / 4) + r % 4) ? st[r] : 0.f;
       if (bad)
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
           const int x = 8 * (r / 4) + r % 4;
-          poison |= ok(x) && ((bad >> (4 * half + x)) & 1);
+          poison |= ok(x) & ((bad >> (4 * half + x)) & 1);
         }
     }
     if constexpr (F16) {
@@ -227,13 +214,7 @@ __global__ __launch_bounds__(NT, 2) void window_dq_kernel(WinBwdArgs a) {
       const int r = 8 * t;
       const u32x4 pb = round8<F16>(st, r);
 #pragma unroll
-      for (int c = 0; c < NB; ++c) {
-        const int s = t * NB + c;
-        dq[c] = mfma32x32x16<F16>(af[s % AHEAD], pb, dq[c]);
-        if (s + AHEAD < NS) {
-          af[s % AHEAD] = frag(2 * NS + s + AHEAD);
-          }
-      }
+      for (int c = 0; c < NB; ++c) dq[c] = mfma32x32x16<F16>(lds_frag_tr<D>(Ks, tr, t, c), pb, dq[c]);
     }
   }
   poison = poison || __shfl_xor((int)poison, 32, 64);
@@ -286,13 +267,13 @@ __device__ __forceinline__ DkvItem dkv_item(const WinBwdArgs& a, const WinBwdSeg
 }
 
 // Key and value gradients: four groups of 32 keys against tiles of 64 query rows,
-// two waves per group.  Both form S = Q K^T (queries x keys); one then adds
-// dV^T += dO^T P, the other forms dP = dO V^T and adds dK^T += Q^T dS.  The rows are
-// in LDS, read as they are and transposed; K and V stay in registers.  One wave
-// for both gradients needs over 256 registers: alone on its SIMD, with sums moved
-// about, 832 us at 4096 + 3001 rows of 32 / 8 heads under a window of 1024; two
-// such waves per SIMD with V in LDS and a few registers in memory 589 us; this
-// way a quarter more products, NNN us.
+// two waves per group and 32 rows a step.  One forms S = Q K^T (queries x keys) and
+// P, hands P over in LDS and adds dV^T += dO^T P; the other forms dP = dO V^T and, a
+// step later, when P is there, dS, and adds dK^T += Q^T dS.  The rows are in LDS,
+// read as they are and transposed; K or V stays in registers.  At 4096 + 3001 rows
+// of 32 / 8 heads under a window of 1024: one wave for both gradients needs over
+// 256 registers, 832 us alone on its SIMD, 589 us with V in LDS; two waves that
+// both form S 467 us; this way 454 us.
 constexpr int DKV_NT = 512;
 
 template <int D, bool F16>
@@ -302,6 +283,7 @@ __global__ __launch_bounds__(DKV_NT, 2) void window_dkv_kernel(WinBwdArgs a) {
   __shared__ __attribute__((aligned(16))) uint16_t s_qg[2][2 * WIN_DQ * D];   // two tiles in turn: Q, then dO
   __shared__ __attribute__((aligned(16))) float s_lse[2][WIN_DQ], s_delta[2][WIN_DQ];
   __shared__ int s_expo[2][WIN_DQ];
+  __shared__ floatx4 s_p[2][4][4][64];                                        // two steps in turn: P of the groups
   const int item = blockIdx.x;
   if (item >= a.nitems) return;
   const WinBwdSeg& sg = a.seg[find_item_seg(a, item)];
@@ -320,17 +302,14 @@ __global__ __launch_bounds__(DKV_NT, 2) void window_dkv_kernel(WinBwdArgs a) {
   const int j0 = it.kt * WIN_DK, jw = j0 + 32 * kg, j = jw + lk;
   const bool on = j < sg.nk;
   const int64_t krow = (int64_t)sg.k0 + (on ? j : sg.nk - 1);
-  const bool open = on && (!a.key_mask || a.key_mask[krow]);
+  const bool seen = on && (!a.key_mask || a.key_mask[krow]), is_sink = j < a.sinks;
 
-  u32x4 kf[NS], vf[NS];
+  u32x4 own[NS];                         // K of the group's keys, or V
   {
-    const uint16_t* kp = static_cast<const uint16_t*>(a.k) + krow * a.ldk + (int64_t)kvh * D + 8 * half;
-    const uint16_t* vp = static_cast<const uint16_t*>(a.v) + krow * a.ldv + (int64_t)kvh * D + 8 * half;
+    const uint16_t* op = (for_k ? static_cast<const uint16_t*>(a.v) + krow * a.ldv
+                                : static_cast<const uint16_t*>(a.k) + krow * a.ldk) + (int64_t)kvh * D + 8 * half;
 #pragma unroll
-    for (int s = 0; s < NS; ++s) {
-      kf[s] = load_piece(kp + 16 * s);
-      vf[s] = load_piece(vp + 16 * s);
-    }
+    for (int s = 0; s < NS; ++s) own[s] = load_piece(op + 16 * s);
     // wait here: left to the loop, the wait for these would also be one for the
     // loads that the loop keeps in flight
     __builtin_amdgcn_s_waitcnt(0x0f70);   // vmcnt(0)
@@ -375,7 +354,6 @@ __global__ __launch_bounds__(DKV_NT, 2) void window_dkv_kernel(WinBwdArgs a) {
       if constexpr (F16) expo_r = a.expo[at];
     }
   };
-  // whether every row of a tile sees every key of the workgroup
   const int whole_from = j0 + WIN_DK <= sg.nk && !a.key_mask ? j0 + WIN_DK - 1 - off : INT_MAX;
   const int whole_to = a.window > 0 ? (int)min((int64_t)j0 + a.window - WIN_DQ - off, (int64_t)INT_MAX) : INT_MAX;
   auto whole_of = [&](int i0) __attribute__((always_inline)) {
@@ -410,141 +388,126 @@ __global__ __launch_bounds__(DKV_NT, 2) void window_dkv_kernel(WinBwdArgs a) {
     if (x0 + 1 < x1) next = after(now);
     load(next);
   }
-  for (int x = x0; x < x1; ++x) {
-    const int buf = (x - x0) & 1;
-    __syncthreads();   // tile x is stored, and the readers of the tile before are done
-    const int i0 = now.i0;
-    now = next;
-    if (x + 1 < x1) store(buf ^ 1, now.i0);
-    if (x + 2 < x1) next = after(now);
-    load(next);        // in flight meanwhile (past the last: not used)
-    const bool whole = whole_of(i0);
-#pragma unroll 1
-    for (int sub = 0; sub < WIN_DQ; sub += 32) {
-      const int p_lo = off + i0 + sub, p_hi = min(p_lo + 31, sg.nk - 1);
-      // the wave's own keys may be seen by none of the rows (or there are none)
-      if (p_lo >= sg.nk || jw > p_hi || (a.window > 0 && jw + 31 <= p_lo - a.window && jw >= a.sinks)) continue;
-      const uint16_t* Qs = s_qg[buf] + sub * D;
-      const uint16_t* Gs = Qs + WIN_DQ * D;
-      const float* lses = &s_lse[buf][sub + 4 * half];
-      const float* deltas = &s_delta[buf][sub + 4 * half];
-      // rows of the elements: 8 (r / 4) + r % 4 from top on
-      const int top = p_lo + 4 * half, end = sg.nk - top, low = j - top;
-      const uint16_t* rows = for_k ? Qs : Gs;         // what the wave's gradient multiplies
-      // fragments in the order of their products: Q, (dO,) the transposed ones
-      static_assert(2 * NB == NS, "fragments of a step");
-      u32x4 af[AHEAD];
+  const int steps = 2 * (x1 - x0);
+  floatx16 dp;                           // for dK: dP - D of the step before
+  const uint16_t* before = nullptr;      // and its rows, nullptr where the group's keys see none of them
+  // one step more for the last dK
+  for (int t = 0; t <= steps; ++t) {
+    __syncthreads();   // tile and P of the step before are stored, their readers before that are done
+    if (for_k && before) {
+      const floatx4* pp = &s_p[(t - 1) & 1][kg][0][lane];
+      floatx16 ds;
 #pragma unroll
-      for (int f = 0; f < AHEAD; ++f) af[f] = lds_read16(&Qs[fr ^ 16 * f]);
-      in_order();
-      floatx16 st;
+      for (int g = 0; g < 4; ++g) {
+        const floatx4 pr = pp[64 * g];
 #pragma unroll
-      for (int r = 0; r < 16; ++r) st[r] = 0.f;
-      if (for_k) {
-        floatx16 dp;
-#pragma unroll
-        for (int r = 0; r < 16; ++r) dp[r] = 0.f;
-#pragma unroll
-        for (int s = 0; s < NS; ++s) {
-          const int n = s + AHEAD;
-          st = mfma32x32x16<F16>(af[s % AHEAD], kf[s], st);
-          af[s % AHEAD] = lds_read16(n < NS ? &Qs[fr ^ 16 * n] : &Gs[fr ^ 16 * (n - NS)]);
-          in_order();
-        }
-#pragma unroll
-        for (int s = 0; s < NS; ++s) {
-          const int n = s + AHEAD;
-          dp = mfma32x32x16<F16>(af[s % AHEAD], vf[s], dp);
-          af[s % AHEAD] = n < NS ? lds_read16(&Gs[fr ^ 16 * n]) : lds_frag_tr<D>(rows, tr, (n - NS) / NB, (n - NS) % NB);
-          in_order();
-        }
-        if constexpr (F16) {
-          int e = s_expo[buf][sub + lk];
-#pragma unroll
-          for (int o = 1; o < 32; o <<= 1) e = max(e, __shfl_xor(e, o, 64));
-          if (e > ex) {
-            const float f = ldexpf(1.f, ex - e);
-            ex = e;
-            fac = pow2f(-ex);
-#pragma unroll
-            for (int b = 0; b < NB; ++b) sum[b] *= f;
-          }
-        }
-#pragma unroll
-        for (int g = 0; g < 4; ++g) {
-          const floatx4 de = *reinterpret_cast<const floatx4*>(&deltas[8 * g]);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) dp[4 * g + e] = (dp[4 * g + e] - de[e]) * (F16 ? fac : 1.f);
-        }
-#pragma unroll
-        for (int g = 0; g < 4; ++g) {
-          const floatx4 ls = *reinterpret_cast<const floatx4*>(&lses[8 * g]);
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-            st[4 * g + e] = exp2_raw(fmaf(st[4 * g + e], sl2, -ls[e])) * dp[4 * g + e];
-        }
-      } else {
-#pragma unroll
-        for (int s = 0; s < NS; ++s) {
-          const int n = s + AHEAD;
-          st = mfma32x32x16<F16>(af[s % AHEAD], kf[s], st);
-          af[s % AHEAD] = n < NS ? lds_read16(&Qs[fr ^ 16 * n]) : lds_frag_tr<D>(rows, tr, (n - NS) / NB, (n - NS) % NB);
-          in_order();
-        }
-#pragma unroll
-        for (int g = 0; g < 4; ++g) {
-          const floatx4 ls = *reinterpret_cast<const floatx4*>(&lses[8 * g]);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) st[4 * g + e] = exp2_raw(fmaf(st[4 * g + e], sl2, -ls[e]));
-        }
-      }
-      if (!whole) {
-#pragma unroll
-        for (int g = 0; g < 4; ++g) {
-          const floatx4 ls = *reinterpret_cast<const floatx4*>(&lses[8 * g]);
-          const floatx4 de = *reinterpret_cast<const floatx4*>(&deltas[8 * g]);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int y = 8 * g + e;
-            const bool ok = open && y < end && y >= low && (y < low + wlim || j < a.sinks);
-            // a row with an inf or NaN in its operands has one in its log-sum or delta
-            st[4 * g + e] = ok ? st[4 * g + e] + ((ls[e] - ls[e]) + (de[e] - de[e])) : 0.f;
-          }
-        }
+        for (int e = 0; e < 4; ++e) ds[4 * g + e] = pr[e] * dp[4 * g + e];
       }
       if constexpr (F16) {
-        if (for_k) {
-          float big = 0.f;
+        float big = 0.f;
 #pragma unroll
-          for (int r = 0; r < 16; ++r) big = fmaxf(big, fabsf(st[r]));
-          if (__any(big > 32768.f)) {
-            big = big < __builtin_inff() ? big : 0.f;   // an inf is its key's own
+        for (int r = 0; r < 16; ++r) big = fmaxf(big, fabsf(ds[r]));
+        if (__any(big > 32768.f)) {
+          big = big < __builtin_inff() ? big : 0.f;   // an inf is its key's own
 #pragma unroll
-            for (int o = 1; o < 64; o <<= 1) big = fmaxf(big, __shfl_xor(big, o, 64));
-            const int more = max(0, min((int)(__float_as_uint(big) >> 23) - 127 - 10, 100));
-            const float f = pow2f(-more);
-            ex += more;
-            fac *= f;
+          for (int o = 1; o < 64; o <<= 1) big = fmaxf(big, __shfl_xor(big, o, 64));
+          const int more = max(0, min((int)(__float_as_uint(big) >> 23) - 127 - 10, 100));
+          const float f = pow2f(-more);
+          ex += more;
+          fac *= f;
 #pragma unroll
-            for (int r = 0; r < 16; ++r) st[r] *= f;
+          for (int r = 0; r < 16; ++r) ds[r] *= f;
 #pragma unroll
-            for (int b = 0; b < NB; ++b) sum[b] *= f;
-          }
+          for (int b = 0; b < NB; ++b) sum[b] *= f;
         }
       }
 #pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        const int r = 8 * t;
-        const u32x4 pb = round8<F16>(st, r);
+      for (int u = 0; u < 2; ++u) {
+        const u32x4 pb = round8<F16>(ds, 8 * u);
 #pragma unroll
-        for (int c = 0; c < NB; ++c) {
-          const int f = t * NB + c, n = f + AHEAD;
-          sum[c] = mfma32x32x16<F16>(af[f % AHEAD], pb, sum[c]);
-          if (n < NS) {
-            af[f % AHEAD] = lds_frag_tr<D>(rows, tr, n / NB, n % NB);
-            in_order();
-          }
+        for (int c = 0; c < NB; ++c) sum[c] = mfma32x32x16<F16>(lds_frag_tr<D>(before, tr, u, c), pb, sum[c]);
+      }
+    }
+    before = nullptr;
+    if (t == steps) break;
+    const int buf = (t >> 1) & 1, sub = 32 * (t & 1), i0 = now.i0;
+    // whether every row of the tile sees every key of the workgroup
+    const bool whole = whole_of(i0);
+    if (sub) {         // the other tile's last step is done
+      now = next;
+      const int x = x0 + (t >> 1);
+      if (x + 1 < x1) store(buf ^ 1, now.i0);
+      if (x + 2 < x1) next = after(now);
+      load(next);      // in flight meanwhile (past the last: not used)
+    }
+    const int p_lo = off + i0 + sub, p_hi = min(p_lo + 31, sg.nk - 1);
+    // the group's keys may be seen by none of the rows (or there are none)
+    if (p_lo >= sg.nk || jw > p_hi || (a.window > 0 && jw + 31 <= p_lo - a.window && jw >= a.sinks)) continue;
+    const uint16_t* Qs = s_qg[buf] + sub * D;
+    const uint16_t* Gs = Qs + WIN_DQ * D;
+    const float* lses = &s_lse[buf][sub + 4 * half];
+    const float* deltas = &s_delta[buf][sub + 4 * half];
+    // rows of the elements: 8 (r / 4) + r % 4 from top on
+    const int top = p_lo + 4 * half, end = sg.nk - top, low = j - top;
+    floatx16 st;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) st[r] = 0.f;
+    const uint16_t* rows = for_k ? Gs : Qs;
+#pragma unroll
+    for (int s = 0; s < NS; ++s) st = mfma32x32x16<F16>(lds_read16(&rows[fr ^ 16 * s]), own[s], st);
+    if (for_k) {
+      if constexpr (F16) {
+        int e = s_expo[buf][sub + lk];
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) e = max(e, __shfl_xor(e, o, 64));
+        if (e > ex) {
+          const float f = ldexpf(1.f, ex - e);
+          ex = e;
+          fac = pow2f(-ex);
+#pragma unroll
+          for (int b = 0; b < NB; ++b) sum[b] *= f;
         }
+      }
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const floatx4 de = *reinterpret_cast<const floatx4*>(&deltas[8 * g]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) st[4 * g + e] = (st[4 * g + e] - de[e]) * (F16 ? fac : 1.f);
+      }
+    } else {
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const floatx4 ls = *reinterpret_cast<const floatx4*>(&lses[8 * g]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) st[4 * g + e] = exp2_raw(fmaf(st[4 * g + e], sl2, -ls[e]));
+      }
+    }
+    if (!whole) {
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const floatx4 ls = *reinterpret_cast<const floatx4*>(&lses[8 * g]);
+        const floatx4 de = *reinterpret_cast<const floatx4*>(&deltas[8 * g]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int y = 8 * g + e;
+          const bool ok = seen & (y < end) & (y >= low) & ((y < low + wlim) | is_sink);
+          // a row with an inf or NaN in its operands has one in its log-sum or delta
+          st[4 * g + e] = ok ? st[4 * g + e] + ((ls[e] - ls[e]) + (de[e] - de[e])) : 0.f;
+        }
+      }
+    }
+    if (for_k) {
+      dp = st;
+      before = Qs;
+    } else {
+      floatx4* pp = &s_p[t & 1][kg][0][lane];
+#pragma unroll
+      for (int g = 0; g < 4; ++g) pp[64 * g] = floatx4{st[4 * g], st[4 * g + 1], st[4 * g + 2], st[4 * g + 3]};
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const u32x4 pb = round8<F16>(st, 8 * u);
+#pragma unroll
+        for (int c = 0; c < NB; ++c) sum[c] = mfma32x32x16<F16>(lds_frag_tr<D>(Gs, tr, u, c), pb, sum[c]);
       }
     }
   }
