@@ -193,8 +193,12 @@ int64_t seg_units(const Kv4Args& a, const CacheSeg& s) {
   return us + p1 / KV4_UNIT + 1 - uw;
 }
 
-// Key / value gradient of the windowed attention: how its work is cut.
-constexpr int64_t kDkvTarget = 512, kDkvMin = 4;   // work items of a launch; list entries of a piece
+// Key / value gradient of the windowed attention: how its work is cut.  Two items a
+// compute unit (rows of 4096 and 3001 in a window of 1024, 32 on 8 heads, with the
+// join: 256 items 734 us, 512 475, 640 464, 768 503), and no piece of fewer than 8
+// list entries (rows of 640 and 577, 32 heads: from 4 on cut, with the join 83 us,
+// from 8 on not, 42).
+constexpr int64_t kDkvTarget = 512, kDkvMin = 8;   // work items of a launch; list entries of a piece
 
 // Fills a.seg with the next samples from b on; returns the next sample.  dkv: the
 // work items of the key / value gradient, otherwise those of the query gradient.

@@ -472,6 +472,7 @@ __global__ __launch_bounds__(AT, NCB == 1 ? 2 : 1) void kv4_attn_kernel(Kv4Args 
       }
     }
     const float pf0 = F16 ? 4.f : pow2f(ve), pf1 = pf0 * 0.0625f;
+    const float back0 = -7.5f / pf0, back1 = -7.5f / pf1;
 #pragma unroll
     for (int n = 0; n < NCB; ++n) {
       float sc[2][4];
@@ -541,11 +542,18 @@ __global__ __launch_bounds__(AT, NCB == 1 ? 2 : 1) void kv4_attn_kernel(Kv4Args 
           for (int r = 0; r < 4; ++r) {
             uint32_t pw = x.vp[t][g][r];
             if constexpr (PART) pw = (vis >> (4 * t + r)) & 1 ? pw : 0u;
-            ol[n][g] = fmaf(p[t][r], act_bits_to_f32<F16>(pw >> 16), ol[n][g]);
-            ps[t][r] = p[t][r] * (r < 2 ? pf0 : pf1) * act_bits_to_f32<F16>(pw & 0xffffu);
+            const float vs = act_bits_to_f32<F16>(pw & 0xffffu);
+            ol[n][g] = fmaf(p[t][r], fmaf(vs, 7.5f, act_bits_to_f32<F16>(pw >> 16)), ol[n][g]);
+            ps[t][r] = p[t][r] * (r < 2 ? pf0 : pf1) * vs;
           }
         const u32x4 pb = {round_pair(ps[0][0], ps[0][1]), round_pair(ps[0][2], ps[0][3]),
                           round_pair(ps[1][0], ps[1][1]), round_pair(ps[1][2], ps[1][3])};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float back = i & 1 ? back1 : back0;
+          ol[n][g] = fmaf(act_bits_to_f32<true>(pb[i] & 0xffffu), back, ol[n][g]);
+          ol[n][g] = fmaf(act_bits_to_f32<true>(pb[i] >> 16), back, ol[n][g]);
+        }
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           const uint32_t y = x.vw[0][2 * g + j / 2] >> (8 * (j & 1)), z = x.vw[1][2 * g + j / 2] >> (8 * (j & 1));

@@ -183,4 +183,15 @@ __device__ __forceinline__ u32x4 round8(const floatx16& x, int r) {
                round2<F16>(x[r + 6], x[r + 7])};
 }
 
+// What rounding elements r .. r + 7 to `hi` took, as a second fragment.
+template <bool F16>
+__device__ __forceinline__ u32x4 rest8(const floatx16& x, int r, const u32x4& hi) {
+  u32x4 lo;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    lo[i] = round2<F16>(x[r + 2 * i] - act_bits_to_f32<F16>(hi[i] & 0xffffu),
+                        x[r + 2 * i + 1] - act_bits_to_f32<F16>(hi[i] >> 16));
+  return lo;
+}
+
 }  // namespace svl

@@ -1,7 +1,11 @@
 // Gradients of the windowed attention (window_attn.hip) on 16-bit MFMA, from the
 // rows' log-sums: P = exp(scale q.k - lse), D = rowsum(dO * O), dP = dO V^T,
 // dS = P (dP - D), then dQ = scale dS K, dK = scale dS^T Q, dV = P^T dO.  Sums,
-// P, dP and dS are float32; P and dS are rounded to 16 bits once, as operands.
+// P, dP and dS are float32 and rounded to 16 bits once, as operands.  D comes from
+// an output that is rounded too; as sum(P) is 1, a row's sum(dS) is what that took
+// off D, so the query gradient's kernel puts it right for the key gradient, and for
+// itself, where its sums are begun by then, takes dS as two 16-bit terms instead.
+// (Either error by itself is as large as the rounding of the result.)
 //
 // Two launches, so that every sum has one owner and a fixed order (no atomics):
 // the query gradient by tiles of query rows, the key and value gradients by
@@ -81,10 +85,9 @@ __global__ __launch_bounds__(NT, 2) void window_dq_kernel(WinBwdArgs a) {
   int ex = 0;
   if constexpr (F16)
     ex = top > 0 && top < kNonfinite<true> ? (int)(__float_as_uint(act_bits_to_f32<true>(top)) >> 23) - 127 : -24;
-  if (on && half == 0) {
-    a.delta[row * a.n_heads + h] = delta;
-    if constexpr (F16) a.expo[row * a.n_heads + h] = ex;
-  }
+  if constexpr (F16)
+    if (on && half == 0) a.expo[row * a.n_heads + h] = ex;
+  float off_d = 0.f;             // sum(dS), times fac
   int down = 0;                  // fp16: and 2^-down more, for the whole wave
   float fac = F16 ? pow2f(-ex) : 1.f;
 
@@ -203,6 +206,7 @@ __global__ __launch_bounds__(NT, 2) void window_dq_kernel(WinBwdArgs a) {
         const float f = pow2f(-more);
         down += more;
         fac *= f;
+        off_d *= f;
 #pragma unroll
         for (int r = 0; r < 16; ++r) st[r] *= f;
 #pragma unroll
@@ -210,15 +214,23 @@ __global__ __launch_bounds__(NT, 2) void window_dq_kernel(WinBwdArgs a) {
       }
     }
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      const int r = 8 * t;
-      const u32x4 pb = round8<F16>(st, r);
+    for (int r = 0; r < 16; ++r) off_d += st[r];
 #pragma unroll
-      for (int c = 0; c < NB; ++c) dq[c] = mfma32x32x16<F16>(lds_frag_tr<D>(Ks, tr, t, c), pb, dq[c]);
+    for (int t = 0; t < 2; ++t) {
+      const u32x4 hi = round8<F16>(st, 8 * t), lo = rest8<F16>(st, 8 * t, hi);
+#pragma unroll
+      for (int c = 0; c < NB; ++c) {
+        const u32x4 kt = lds_frag_tr<D>(Ks, tr, t, c);
+        dq[c] = mfma32x32x16<F16>(kt, hi, dq[c]);
+        dq[c] = mfma32x32x16<F16>(kt, lo, dq[c]);
+      }
     }
   }
   poison = poison || __shfl_xor((int)poison, 32, 64);
+  off_d += __shfl_xor(off_d, 32, 64);
   if (!on) return;
+  // (a poisoned row's dS has 0 in place of an inf of K)
+  if (half == 0) a.delta[row * a.n_heads + h] = poison ? delta : delta + ldexpf(off_d, ex + down);
   const float f = poison ? __builtin_nanf("") : a.scale;
   uint16_t* out = static_cast<uint16_t*>(a.dq) + row * a.lddq + (int64_t)h * D;
 #pragma unroll

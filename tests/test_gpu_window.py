@@ -5,7 +5,7 @@ import pytest
 import torch
 
 import paper_2607_20357_amd as svl
-from attention_helpers import check_window, draw, f64, offsets, run_window
+from attention_helpers import check_window, draw, dtype_of, f64, half_step, offsets, run_window
 from oracle import attention as oa
 
 pytestmark = pytest.mark.gpu
@@ -201,3 +201,25 @@ def test_gradient_against_differences():
         size = float((grad.double() ** 2).sum() ** 0.5)
         tol = size * (2.0 ** -11 / e + 4 * e * e * (0 if i == 2 else 1)) + 2.0 ** -10 * abs(want)
         assert abs(got - want) <= tol, (i, got, want, tol)
+
+
+@pytest.mark.parametrize("compute", COMPUTES)
+def test_key_gradient_under_large_outputs(compute):
+    """Values near 100, so that the output's rounding is large beside the differences that
+    the gradient is made of: it must not reach the key gradient."""
+    heads, n, d = (2, 1, 64), 150, 64
+    att = svl.make_attention(*heads, window=60, sinks=2, compute=compute)
+    gen = torch.Generator(device="cuda").manual_seed(11)
+    q, k, grad = (draw(gen, (n, h, d), compute) for h in (2, 1, 2))
+    v = (100 + torch.randn((n, 1, d), generator=gen, device="cuda")).to(dtype_of(compute))
+    cu = np.array([0, n], np.int32)
+    dk = run_window(att, cu, None, q, k, v, None, grad)[3]
+    w = oa.attention(f64(q), f64(k), f64(v), oa.visible(np.arange(n), n, 60, 2), d ** -0.5, f64(grad))
+    # dS is rounded once as an operand and dK once as the result.  What float32 leaves of D
+    # is some 2^-18 of the terms of the products grad . v, in every dS by its P
+    h, aq = half_step(compute), np.abs(f64(q)).transpose(1, 0, 2)                  # [A][n][d]
+    terms = (np.abs(f64(grad)) * np.abs(f64(v))).sum(-1).max(0)                    # [A]
+    each = h * np.abs(w["ds"]) + 2.0 ** -18 * terms[:, None, None] * w["p"]        # [A][n][m]
+    bound = 1.01 * ((each.transpose(0, 2, 1) @ aq).sum(0)[:, None] * d ** -0.5 + h * np.abs(w["dk"]))
+    err = np.abs(f64(dk) - w["dk"])
+    assert (err <= bound).all(), float((err / bound).max())
