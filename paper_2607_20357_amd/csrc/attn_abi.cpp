@@ -271,7 +271,7 @@ hipError_t kv4_read_segments(Kv4Args& a, CacheSegOf get, const void* ctx, int32_
 // A piece has at least 1 / KV4_TARGET_ITEMS of the launch's units, so the pieces
 // of segments that are cut are at most twice KV4_TARGET_ITEMS.
 size_t kv4_partial_bytes(int32_t head_dim) {
-  return (size_t)(2 * KV4_TARGET_ITEMS * kv4_partial_floats(KV4_MAX_NCB, head_dim) * 4);
+  return (size_t)(2 * KV4_TARGET_ITEMS * kv4_partial_floats(head_dim) * 4);
 }
 
 hipError_t kv4_attention_segments(Kv4Args& a, CacheSegOf get, const void* ctx, int32_t n,
@@ -286,15 +286,14 @@ hipError_t kv4_attention_segments(Kv4Args& a, CacheSegOf get, const void* ctx, i
       a.seg[a.nsegs++] = s;
     }
     if (a.nsegs == 0) continue;
-    const int32_t ncb = kv4_ncb(columns);
     int64_t units = 0;
     for (int32_t k = 0; k < a.nsegs; ++k)
-      units += cdiv((int64_t)a.seg[k].rows * a.rep, 16 * ncb) * a.seg[k].kv_cnt * seg_units(a, a.seg[k]);
+      units += cdiv((int64_t)a.seg[k].rows * a.rep, KV4_COLS) * a.seg[k].kv_cnt * seg_units(a, a.seg[k]);
     const int64_t per = std::max<int64_t>(KV4_MIN_UNITS, cdiv(units, KV4_TARGET_ITEMS));
     int64_t items = 0, parts = 0, cut = 0;
     for (int32_t k = 0; k < a.nsegs; ++k) {
       CacheSeg& s = a.seg[k];
-      const int64_t blocks = cdiv((int64_t)s.rows * a.rep, 16 * ncb) * s.kv_cnt;
+      const int64_t blocks = cdiv((int64_t)s.rows * a.rep, KV4_COLS) * s.kv_cnt;
       // (a cut pays for its join from two pieces' worth of work on)
       const int64_t u = seg_units(a, s);
       s.nsplit = u < 2 * per ? 1 : (int32_t)cdiv(u, per);
@@ -309,11 +308,11 @@ hipError_t kv4_attention_segments(Kv4Args& a, CacheSegOf get, const void* ctx, i
       if (items > INT32_MAX / 64) return hipErrorInvalidValue;
     }
     a.nitems = (int32_t)items;
-    hipError_t e = timed_launch(K_ATTN, st, [&] { return launch_kv4_attention(a, head_dim, f16, ncb, st); });
+    hipError_t e = timed_launch(K_ATTN, st, [&] { return launch_kv4_attention(a, head_dim, f16, st); });
     if (e != hipSuccess) return e;
     if (cut > 0) {
-      const int32_t most = (int32_t)std::min<int64_t>(columns, 16 * ncb);
-      e = timed_launch(K_ATTN, st, [&] { return launch_kv4_join(a, head_dim, f16, ncb, (int32_t)cut, most, st); });
+      const int32_t most = (int32_t)std::min<int64_t>(columns, KV4_COLS);
+      e = timed_launch(K_ATTN, st, [&] { return launch_kv4_join(a, head_dim, f16, (int32_t)cut, most, st); });
       if (e != hipSuccess) return e;
     }
   }

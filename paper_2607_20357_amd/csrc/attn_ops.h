@@ -51,26 +51,26 @@ struct Kv4Args {
   float* partial;           // partial blocks (nsplit > 1)
 };
 
-// Columns (query row, head of the group) of an attention work item: 16 ncb, the
-// same for every segment of a launch.
-constexpr int kv4_ncb(int64_t columns) { return columns <= 16 ? 1 : 2; }
-constexpr int KV4_MAX_NCB = 2;
+// Columns (query row, head of the group) of an attention work item.
+constexpr int KV4_COLS = 16;
 constexpr int KV4_UNIT = 2 * KV4_TILE;     // positions that a wave takes at a time
 // A launch is cut into about this many work items (256 CUs, two workgroups
-// each), and a piece has this many units at least (two per wave).
+// each), and a piece has this many units at least (two per wave).  With 1024 items
+// sixteen samples in a window of 2048, 32 heads on 8, take 21 us in place of 17 and
+// eight of 8192 positions 63 in place of 59; eight ragged ones up to 20001, 28 heads
+// on 4, 15 in place of 17.  Pieces of 4 units are no faster.
 constexpr int KV4_TARGET_ITEMS = 512, KV4_MIN_UNITS = 8;
 constexpr int KV4_MAX_PIECES = KV4_TARGET_ITEMS + 1;   // of one block
 // Floats of a partial block: per column the maximum, the sum and d outputs.
-constexpr int64_t kv4_partial_floats(int ncb, int d) { return (int64_t)16 * ncb * (d + 2); }
+constexpr int64_t kv4_partial_floats(int d) { return (int64_t)KV4_COLS * (d + 2); }
 
 hipError_t launch_kv4_append(const Kv4Args& a, int32_t head_dim, bool f16, hipStream_t st);
 hipError_t launch_kv4_read(const Kv4Args& a, int32_t head_dim, bool f16, hipStream_t st);
-hipError_t launch_kv4_attention(const Kv4Args& a, int32_t head_dim, bool f16, int32_t ncb,
-                                hipStream_t st);
+hipError_t launch_kv4_attention(const Kv4Args& a, int32_t head_dim, bool f16, hipStream_t st);
 // Joins the pieces of the segments with nsplit > 1: `blocks` of them, of up to
 // `columns` columns each.
-hipError_t launch_kv4_join(const Kv4Args& a, int32_t head_dim, bool f16, int32_t ncb,
-                           int32_t blocks, int32_t columns, hipStream_t st);
+hipError_t launch_kv4_join(const Kv4Args& a, int32_t head_dim, bool f16, int32_t blocks,
+                           int32_t columns, hipStream_t st);
 
 // ---------------------------------------------------------------- packed rows
 // One sample: queries at rows q0 .. q0 + nq - 1, keys at rows k0 .. k0 + nk - 1;

@@ -247,10 +247,12 @@ __global__ __launch_bounds__(NT) void kv4_read_kernel(Kv4Args a) {
 }
 
 // ---------------------------------------------------------------- attention
-// One workgroup: up to 16 NCB columns (query row, head of the K/V head's
-// group) of one K/V head, over one piece of the visible positions; four waves
-// take 32 positions (a unit) in turn, each with a running maximum and sum, and
-// are joined at the end.
+// One workgroup: up to 16 columns (query row, head of the K/V head's group) of
+// one K/V head, over one piece of the visible positions; four waves take 32
+// positions (a unit) in turn, each with a running maximum and sum, and are joined
+// at the end.  (32 columns share what is made of the codes but hold twice the sums,
+// with half the waves: two chunks of 512 rows at 4096 and 3000 positions, 32 heads
+// on 8, take 307 us in place of 232, and four of 64 at 900 53 in place of 20.)
 //
 // The products run on the codes themselves.  A nibble in the low ten bits of a
 // half word is an fp16 subnormal, c 2^-24 (or c 2^-20 four bits higher), and the
@@ -260,6 +262,9 @@ __global__ __launch_bounds__(NT) void kv4_read_kernel(Kv4Args a) {
 // value), then s S + lo sum(q) per position and group, in float32.
 // Values: O^T = V^T P'^T per group with P' = p s, rounded to fp16 once, plus
 // sum(p lo) in float32.  So neither K nor V is rounded to 16 bits on the way.
+// What the rounding takes from P' is put back for the mean code, 7.5, in float32:
+// what is left meets codes of mean 0 (error against float64 2.0 -> 1.35 times that
+// of one rounding of the output, at no cost in time).
 // The lanes' positions and dims are laid out so that an accumulator of the
 // first product is an operand of the second.
 constexpr int AT = 256, AW = AT / 64;
@@ -311,8 +316,8 @@ __device__ __forceinline__ floatx4 mfma_codes(const u32x4& a, const u32x4& b, co
 
 __device__ __forceinline__ uint32_t round_pair(float lo, float hi) { return pack_act2<true>(lo, hi); }
 
-template <int D, bool F16, int NCB>
-__global__ __launch_bounds__(AT, NCB == 1 ? 2 : 1) void kv4_attn_kernel(Kv4Args a) {
+template <int D, bool F16>
+__global__ __launch_bounds__(AT, 2) void kv4_attn_kernel(Kv4Args a) {
   typedef Tile<D> T;
   constexpr int G = T::G, NS = D / 32;
   typedef typename Words<T::KW>::type CodeWords;   // (K and V: as many words a lane)
@@ -322,14 +327,14 @@ __global__ __launch_bounds__(AT, NCB == 1 ? 2 : 1) void kv4_attn_kernel(Kv4Args 
   const int item = blockIdx.x;
   if (item >= a.nitems) return;
   const CacheSeg& sg = a.seg[find_seg(a, item)];
-  const int rep = a.rep, cols = sg.rows * rep, ncb = (cols + 16 * NCB - 1) / (16 * NCB);
+  const int rep = a.rep, cols = sg.rows * rep, ncb = (cols + KV4_COLS - 1) / KV4_COLS;
   const int local = item - sg.item0, split = local % sg.nsplit, block = local / sg.nsplit;
   const int cb = block % ncb, slot = block / ncb;
   const int kvh = a.kv_table ? a.kv_table[sg.kv_off + slot] : slot;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int gq = lane >> 4, lq = lane & 15;
-  const int c0 = cb * 16 * NCB;
-  const int p_lo = sg.pos0 + c0 / rep, p_hi = sg.pos0 + (min(c0 + 16 * NCB, cols) - 1) / rep;
+  const int c0 = cb * KV4_COLS;
+  const int p_lo = sg.pos0 + c0 / rep, p_hi = sg.pos0 + (min(c0 + KV4_COLS, cols) - 1) / rep;
   const Units un = units_of(p_lo, p_hi, a.window, a.sinks);
   const int u0 = (int)((int64_t)un.n * split / sg.nsplit);
   const int u1 = (int)((int64_t)un.n * (split + 1) / sg.nsplit);
@@ -337,21 +342,20 @@ __global__ __launch_bounds__(AT, NCB == 1 ? 2 : 1) void kv4_attn_kernel(Kv4Args 
   // query fragments; a pair of codes is (dim i, dim i + 4) of a word, the pairs
   // 1 and 3 carry a factor 16
   const float sl2 = a.scale * 1.4426950408889634f;   // scores in log2 units
-  u32x4 qf[NCB][NS];
-  float qs[NCB][G], fl[NCB];
-  int pq[NCB];                                       // the column's position
-#pragma unroll
-  for (int n = 0; n < NCB; ++n) {
-    const int c = c0 + 16 * n + lq;
+  u32x4 qf[NS];
+  float qs[G], fl;
+  int pq;                              // the column's position
+  {
+    const int c = c0 + lq;
     const bool on = c < cols;
     const int i = on ? c / rep : 0, h = kvh * rep + (on ? c % rep : 0);
-    pq[n] = on ? sg.pos0 + i : -1;
+    pq = on ? sg.pos0 + i : -1;
     const uint16_t* qp = static_cast<const uint16_t*>(a.q) + ((int64_t)sg.row0 + i) * a.ldq +
                          (int64_t)h * D + 8 * gq;
     float x[NS][8];
     float top = 0.f;
 #pragma unroll
-    for (int g = 0; g < G; ++g) qs[n][g] = 0.f;
+    for (int g = 0; g < G; ++g) qs[g] = 0.f;
 #pragma unroll
     for (int s = 0; s < NS; ++s) {
       const uint4 v = on ? *reinterpret_cast<const uint4*>(qp + 32 * s) : make_uint4(0, 0, 0, 0);
@@ -363,7 +367,7 @@ __global__ __launch_bounds__(AT, NCB == 1 ? 2 : 1) void kv4_attn_kernel(Kv4Args 
       }
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        qs[n][s / 2] += x[s][e];
+        qs[s / 2] += x[s][e];
         top = fmaxf(top, fabsf(x[s][e]));
       }
     }
@@ -371,35 +375,30 @@ __global__ __launch_bounds__(AT, NCB == 1 ? 2 : 1) void kv4_attn_kernel(Kv4Args 
     for (int o = 16; o < 64; o <<= 1) {
       top = fmaxf(top, __shfl_xor(top, o, 64));
 #pragma unroll
-      for (int g = 0; g < G; ++g) qs[n][g] += __shfl_xor(qs[n][g], o, 64);
+      for (int g = 0; g < G; ++g) qs[g] += __shfl_xor(qs[g], o, 64);
     }
     // 2^k brings the largest magnitude into [2^14, 2^15)
     const int k = top > 0.f ? max(-100, min(100, 141 - (int)(__float_as_uint(top) >> 23))) : 0;
     const float up = pow2f(k);
-    fl[n] = ldexpf(sl2, 24 - k);
+    fl = ldexpf(sl2, 24 - k);
 #pragma unroll
-    for (int g = 0; g < G; ++g) qs[n][g] *= pow2f(k - 24);
+    for (int g = 0; g < G; ++g) qs[g] *= pow2f(k - 24);
 #pragma unroll
     for (int s = 0; s < NS; ++s) {
       const float* y = x[s];
       const float up4 = up * 0.0625f;
-      qf[n][s] = u32x4{round_pair(y[0] * up, y[4] * up), round_pair(y[1] * up4, y[5] * up4),
-                       round_pair(y[2] * up, y[6] * up), round_pair(y[3] * up4, y[7] * up4)};
+      qf[s] = u32x4{round_pair(y[0] * up, y[4] * up), round_pair(y[1] * up4, y[5] * up4),
+                    round_pair(y[2] * up, y[6] * up), round_pair(y[3] * up4, y[7] * up4)};
     }
   }
 
-  float m[NCB], l[NCB], ol[NCB][G];
-  floatx4 o[NCB][G][4];
+  float m = -__builtin_inff(), l = 0.f, ol[G];
+  floatx4 o[G][4];
 #pragma unroll
-  for (int n = 0; n < NCB; ++n) {
-    m[n] = -__builtin_inff();
-    l[n] = 0.f;
+  for (int g = 0; g < G; ++g) {
+    ol[g] = 0.f;
 #pragma unroll
-    for (int g = 0; g < G; ++g) {
-      ol[n][g] = 0.f;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) o[n][g][j] = floatx4{0.f, 0.f, 0.f, 0.f};
-    }
+    for (int j = 0; j < 4; ++j) o[g][j] = floatx4{0.f, 0.f, 0.f, 0.f};
   }
   // P' = p s 2^ve: fp16 scales fit with a fixed factor; bf16 ones follow the
   // largest scale seen
@@ -463,102 +462,97 @@ __global__ __launch_bounds__(AT, NCB == 1 ? 2 : 1) void kv4_attn_kernel(Kv4Args 
       if (__any(want < ve)) {   // (the same in every lane)
         const float f = ldexpf(1.0f, min(want - ve, 0));
 #pragma unroll
-        for (int n = 0; n < NCB; ++n)
+        for (int g = 0; g < G; ++g)
 #pragma unroll
-          for (int g = 0; g < G; ++g)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) o[n][g][j] *= f;
+          for (int j = 0; j < 4; ++j) o[g][j] *= f;
         ve = min(ve, want);
       }
     }
     const float pf0 = F16 ? 4.f : pow2f(ve), pf1 = pf0 * 0.0625f;
     const float back0 = -7.5f / pf0, back1 = -7.5f / pf1;
+    float sc[2][4];
+    uint32_t vis = 0xffu;
 #pragma unroll
-    for (int n = 0; n < NCB; ++n) {
-      float sc[2][4];
-      uint32_t vis = 0xffu;
+    for (int t = 0; t < 2; ++t) {
+      floatx4 acc[G];
 #pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        floatx4 acc[G];
+      for (int g = 0; g < G; ++g) {
+        acc[g] = mfma_codes(kf[t][2 * g], qf[2 * g], floatx4{0.f, 0.f, 0.f, 0.f});
+        acc[g] = mfma_codes(kf[t][2 * g + 1], qf[2 * g + 1], acc[g]);
+      }
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        float v = 0.f;
 #pragma unroll
         for (int g = 0; g < G; ++g) {
-          acc[g] = mfma_codes(kf[t][2 * g], qf[n][2 * g], floatx4{0.f, 0.f, 0.f, 0.f});
-          acc[g] = mfma_codes(kf[t][2 * g + 1], qf[n][2 * g + 1], acc[g]);
+          const uint32_t pw = x.kp[t][g][r];
+          v = fmaf(act_bits_to_f32<F16>(pw & 0xffffu), acc[g][r], v);
+          v = fmaf(act_bits_to_f32<F16>(pw >> 16), qs[g], v);
         }
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          float v = 0.f;
-#pragma unroll
-          for (int g = 0; g < G; ++g) {
-            const uint32_t pw = x.kp[t][g][r];
-            v = fmaf(act_bits_to_f32<F16>(pw & 0xffffu), acc[g][r], v);
-            v = fmaf(act_bits_to_f32<F16>(pw >> 16), qs[n][g], v);
-          }
-          sc[t][r] = v;
-        }
+        sc[t][r] = v;
       }
-      if constexpr (PART) {
-        vis = 0;
-#pragma unroll
-        for (int t = 0; t < 2; ++t)
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            const int j = kv0 + 16 * t + 4 * gq + r;
-            const bool ok = (j <= pq[n]) & ((j > pq[n] - wlim) | (j < a.sinks));   // (no short cuts: branches)
-            sc[t][r] = ok ? sc[t][r] : -__builtin_inff();
-            vis |= (uint32_t)ok << (4 * t + r);
-          }
-      }
-      float mx = fmaxf(fmaxf(fmaxf(sc[0][0], sc[0][1]), fmaxf(sc[0][2], sc[0][3])),
-                       fmaxf(fmaxf(sc[1][0], sc[1][1]), fmaxf(sc[1][2], sc[1][3])));
-      mx = column_max(mx);
-      if (__any(mx > m[n])) {
-        const float mn = fmaxf(m[n], mx);
-        const float alpha = mn == -__builtin_inff() ? 1.f : __builtin_amdgcn_exp2f((m[n] - mn) * fl[n]);
-        l[n] *= alpha;
-#pragma unroll
-        for (int g = 0; g < G; ++g) {
-          ol[n][g] *= alpha;
-#pragma unroll
-          for (int j = 0; j < 4; ++j) o[n][g][j] *= alpha;
-        }
-        m[n] = mn;
-      }
-      const float mf = m[n] == -__builtin_inff() ? 0.f : -m[n] * fl[n];   // nothing above -inf yet: 0
-      float p[2][4];
+    }
+    if constexpr (PART) {
+      vis = 0;
 #pragma unroll
       for (int t = 0; t < 2; ++t)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          p[t][r] = __builtin_amdgcn_exp2f(fmaf(sc[t][r], fl[n], mf));
-          l[n] += p[t][r];
+          const int j = kv0 + 16 * t + 4 * gq + r;
+          const bool ok = (j <= pq) & ((j > pq - wlim) | (j < a.sinks));   // (no short cuts: branches)
+          sc[t][r] = ok ? sc[t][r] : -__builtin_inff();
+          vis |= (uint32_t)ok << (4 * t + r);
         }
+    }
+    float mx = fmaxf(fmaxf(fmaxf(sc[0][0], sc[0][1]), fmaxf(sc[0][2], sc[0][3])),
+                     fmaxf(fmaxf(sc[1][0], sc[1][1]), fmaxf(sc[1][2], sc[1][3])));
+    mx = column_max(mx);
+    if (__any(mx > m)) {
+      const float mn = fmaxf(m, mx);
+      const float alpha = mn == -__builtin_inff() ? 1.f : __builtin_amdgcn_exp2f((m - mn) * fl);
+      l *= alpha;
 #pragma unroll
       for (int g = 0; g < G; ++g) {
-        float ps[2][4];
+        ol[g] *= alpha;
 #pragma unroll
-        for (int t = 0; t < 2; ++t)
+        for (int j = 0; j < 4; ++j) o[g][j] *= alpha;
+      }
+      m = mn;
+    }
+    const float mf = m == -__builtin_inff() ? 0.f : -m * fl;   // nothing above -inf yet: 0
+    float p[2][4];
 #pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            uint32_t pw = x.vp[t][g][r];
-            if constexpr (PART) pw = (vis >> (4 * t + r)) & 1 ? pw : 0u;
-            const float vs = act_bits_to_f32<F16>(pw & 0xffffu);
-            ol[n][g] = fmaf(p[t][r], fmaf(vs, 7.5f, act_bits_to_f32<F16>(pw >> 16)), ol[n][g]);
-            ps[t][r] = p[t][r] * (r < 2 ? pf0 : pf1) * vs;
-          }
-        const u32x4 pb = {round_pair(ps[0][0], ps[0][1]), round_pair(ps[0][2], ps[0][3]),
-                          round_pair(ps[1][0], ps[1][1]), round_pair(ps[1][2], ps[1][3])};
+    for (int t = 0; t < 2; ++t)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float back = i & 1 ? back1 : back0;
-          ol[n][g] = fmaf(act_bits_to_f32<true>(pb[i] & 0xffffu), back, ol[n][g]);
-          ol[n][g] = fmaf(act_bits_to_f32<true>(pb[i] >> 16), back, ol[n][g]);
+      for (int r = 0; r < 4; ++r) {
+        p[t][r] = __builtin_amdgcn_exp2f(fmaf(sc[t][r], fl, mf));
+        l += p[t][r];
+      }
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+      float ps[2][4];
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          uint32_t pw = x.vp[t][g][r];
+          if constexpr (PART) pw = (vis >> (4 * t + r)) & 1 ? pw : 0u;
+          const float vs = act_bits_to_f32<F16>(pw & 0xffffu);
+          ol[g] = fmaf(p[t][r], fmaf(vs, 7.5f, act_bits_to_f32<F16>(pw >> 16)), ol[g]);
+          ps[t][r] = p[t][r] * (r < 2 ? pf0 : pf1) * vs;
         }
+      const u32x4 pb = {round_pair(ps[0][0], ps[0][1]), round_pair(ps[0][2], ps[0][3]),
+                        round_pair(ps[1][0], ps[1][1]), round_pair(ps[1][2], ps[1][3])};
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const uint32_t y = x.vw[0][2 * g + j / 2] >> (8 * (j & 1)), z = x.vw[1][2 * g + j / 2] >> (8 * (j & 1));
-          o[n][g][j] = mfma_codes(u32x4{y & 0x000f000fu, y & 0x00f000f0u, z & 0x000f000fu, z & 0x00f000f0u}, pb, o[n][g][j]);
-        }
+      for (int i = 0; i < 4; ++i) {
+        const float back = i & 1 ? back1 : back0;
+        ol[g] = fmaf(act_bits_to_f32<true>(pb[i] & 0xffffu), back, ol[g]);
+        ol[g] = fmaf(act_bits_to_f32<true>(pb[i] >> 16), back, ol[g]);
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const uint32_t y = x.vw[0][2 * g + j / 2] >> (8 * (j & 1)), z = x.vw[1][2 * g + j / 2] >> (8 * (j & 1));
+        o[g][j] = mfma_codes(u32x4{y & 0x000f000fu, y & 0x00f000f0u, z & 0x000f000fu, z & 0x00f000f0u}, pb, o[g][j]);
       }
     }
   };
@@ -570,77 +564,71 @@ __global__ __launch_bounds__(AT, NCB == 1 ? 2 : 1) void kv4_attn_kernel(Kv4Args 
     for (; u < u1; u += AW) {
       const Loaded x = next;
       const int kv0 = unit_of(u) * UNIT;
-      // the next unit in flight meanwhile (8 x 8192 positions of 32 heads: 86 -> 71 us);
-      // with 32 columns there are more products to hide it behind, and no registers
-      if constexpr (NCB == 1) next = load(unit_of(min(u + AW, u1 - 1)));
+      // the next unit in flight meanwhile (8 x 8192 positions of 32 heads: 86 -> 71 us)
+      next = load(unit_of(min(u + AW, u1 - 1)));
       if (kv0 <= whole_hi && (kv0 > whole_lo || kv0 <= whole_sink)) add_unit.template operator()<false>(x, kv0);
       else add_unit.template operator()<true>(x, kv0);
-      if constexpr (NCB > 1) next = load(unit_of(min(u + AW, u1 - 1)));
     }
   }
 
-  // join: each wave's outputs (times its own scale) in LDS, 16 columns at a time
+  // join: each wave's outputs (times its own scale) in LDS
+  float ls = l, os[G];
 #pragma unroll
-  for (int n = 0; n < NCB; ++n) {
-    float ls = l[n], os[G];
+  for (int g = 0; g < G; ++g) os[g] = ol[g];
 #pragma unroll
-    for (int g = 0; g < G; ++g) os[g] = ol[n][g];
+  for (int sft = 16; sft < 64; sft <<= 1) {
+    ls += __shfl_xor(ls, sft, 64);
 #pragma unroll
-    for (int sft = 16; sft < 64; sft <<= 1) {
-      ls += __shfl_xor(ls, sft, 64);
+    for (int g = 0; g < G; ++g) os[g] += __shfl_xor(os[g], sft, 64);
+  }
 #pragma unroll
-      for (int g = 0; g < G; ++g) os[g] += __shfl_xor(os[g], sft, 64);
+  for (int g = 0; g < G; ++g)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      float* dst = &s_o[wave][lq][KV4_GROUP * g + 16 * gq + 4 * r];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) dst[j] = ldexpf(o[g][j][r], 24 - ve) + os[g];
     }
-    if (n > 0) __syncthreads();
+  if (gq == 0) {
+    s_m[wave][lq] = m == -__builtin_inff() ? m : m * fl;
+    s_l[wave][lq] = ls;
+  }
+  __syncthreads();
+  // 16 threads per column, D / 16 dims each
+  constexpr int DT = D / 16;
+  const int col = tid >> 4, part = tid & 15, c = c0 + col;
+  if (c < cols) {
+    float M = s_m[0][col];
 #pragma unroll
-    for (int g = 0; g < G; ++g)
+    for (int w = 1; w < AW; ++w) M = fmaxf(M, s_m[w][col]);
+    float L = 0.f, y[DT];
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        float* dst = &s_o[wave][lq][KV4_GROUP * g + 16 * gq + 4 * r];
+    for (int e = 0; e < DT; ++e) y[e] = 0.f;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) dst[j] = ldexpf(o[n][g][j][r], 24 - ve) + os[g];
-      }
-    if (gq == 0) {
-      s_m[wave][lq] = m[n] == -__builtin_inff() ? m[n] : m[n] * fl[n];
-      s_l[wave][lq] = ls;
+    for (int w = 0; w < AW; ++w) {
+      // a wave that saw nothing has weight 0 (its sums are 0 too)
+      const float f = s_m[w][col] == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f(s_m[w][col] - M);
+      L = fmaf(f, s_l[w][col], L);
+#pragma unroll
+      for (int e = 0; e < DT; ++e) y[e] = fmaf(f, s_o[w][col][DT * part + e], y[e]);
     }
-    __syncthreads();
-    // 16 threads per column, D / 16 dims each
-    constexpr int DT = D / 16;
-    const int col = tid >> 4, part = tid & 15, c = c0 + 16 * n + col;
-    if (c < cols) {
-      float M = s_m[0][col];
+    if (sg.nsplit == 1) {
+      const float inv = 1.0f / L;
+      uint16_t* out = static_cast<uint16_t*>(a.out) + ((int64_t)sg.row0 + c / rep) * a.ldo +
+                      ((int64_t)kvh * rep + c % rep) * D + DT * part;
 #pragma unroll
-      for (int w = 1; w < AW; ++w) M = fmaxf(M, s_m[w][col]);
-      float L = 0.f, y[DT];
-#pragma unroll
-      for (int e = 0; e < DT; ++e) y[e] = 0.f;
-#pragma unroll
-      for (int w = 0; w < AW; ++w) {
-        // a wave that saw nothing has weight 0 (its sums are 0 too)
-        const float f = s_m[w][col] == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f(s_m[w][col] - M);
-        L = fmaf(f, s_l[w][col], L);
-#pragma unroll
-        for (int e = 0; e < DT; ++e) y[e] = fmaf(f, s_o[w][col][DT * part + e], y[e]);
+      for (int e = 0; e < DT; e += 4)
+        *reinterpret_cast<uint2*>(out + e) = make_uint2(pack_act2<F16>(y[e] * inv, y[e + 1] * inv),
+                                                        pack_act2<F16>(y[e + 2] * inv, y[e + 3] * inv));
+    } else {
+      float* pb = a.partial + ((int64_t)sg.part0 + (int64_t)block * sg.nsplit + split) * kv4_partial_floats(D) +
+                  (int64_t)col * (D + 2);
+      if (part == 0) {
+        pb[0] = M;
+        pb[1] = L;
       }
-      if (sg.nsplit == 1) {
-        const float inv = 1.0f / L;
-        uint16_t* out = static_cast<uint16_t*>(a.out) + ((int64_t)sg.row0 + c / rep) * a.ldo +
-                        ((int64_t)kvh * rep + c % rep) * D + DT * part;
 #pragma unroll
-        for (int e = 0; e < DT; e += 4)
-          *reinterpret_cast<uint2*>(out + e) = make_uint2(pack_act2<F16>(y[e] * inv, y[e + 1] * inv),
-                                                          pack_act2<F16>(y[e + 2] * inv, y[e + 3] * inv));
-      } else {
-        float* pb = a.partial + ((int64_t)sg.part0 + (int64_t)block * sg.nsplit + split) * kv4_partial_floats(NCB, D) +
-                    (int64_t)(16 * n + col) * (D + 2);
-        if (part == 0) {
-          pb[0] = M;
-          pb[1] = L;
-        }
-#pragma unroll
-        for (int e = 0; e < DT; ++e) pb[2 + DT * part + e] = y[e];
-      }
+      for (int e = 0; e < DT; ++e) pb[2 + DT * part + e] = y[e];
     }
   }
 }
@@ -649,7 +637,7 @@ __global__ __launch_bounds__(AT, NCB == 1 ? 2 : 1) void kv4_attn_kernel(Kv4Args 
 // waves.  Bound by latency: the pieces' maxima are weighed at once, their outputs
 // read eight at a time per wave (78 pieces by one wave, a load after the other: 26 us).
 template <int D, bool F16>
-__global__ __launch_bounds__(AT) void kv4_join_kernel(Kv4Args a, int ncb16) {
+__global__ __launch_bounds__(AT) void kv4_join_kernel(Kv4Args a) {
   constexpr int DL = D / 64;
   __shared__ float s_f[KV4_MAX_PIECES];
   __shared__ float s_red[2][AW], s_y[AW][D];
@@ -660,12 +648,12 @@ __global__ __launch_bounds__(AT) void kv4_join_kernel(Kv4Args a, int ncb16) {
   }
   const CacheSeg& sg = a.seg[k];
   const int block = (int)blockIdx.x - sg.join0, n = sg.nsplit;
-  const int rep = a.rep, cols = sg.rows * rep, ncb = (cols + ncb16 - 1) / ncb16;
-  const int col = blockIdx.y, c = block % ncb * ncb16 + col, slot = block / ncb;
+  const int rep = a.rep, cols = sg.rows * rep, ncb = (cols + KV4_COLS - 1) / KV4_COLS;
+  const int col = blockIdx.y, c = block % ncb * KV4_COLS + col, slot = block / ncb;
   if (c >= cols) return;
   const int kvh = a.kv_table ? a.kv_table[sg.kv_off + slot] : slot;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int64_t stride = (int64_t)ncb16 * (D + 2);
+  const int64_t stride = (int64_t)KV4_COLS * (D + 2);
   const float* pb = a.partial + ((int64_t)sg.part0 + (int64_t)block * n) * stride + (int64_t)col * (D + 2);
   float M = -__builtin_inff();
   for (int s = tid; s < n; s += AT) {
@@ -716,16 +704,6 @@ __global__ __launch_bounds__(AT) void kv4_join_kernel(Kv4Args a, int ncb16) {
   else *out = f32_to_act_bits<F16>(y[0]);
 }
 
-template <int D, bool F16>
-hipError_t launch_attn_ncb(const Kv4Args& a, int ncb, hipStream_t st) {
-  switch (ncb) {
-    case 1: kv4_attn_kernel<D, F16, 1><<<a.nitems, AT, 0, st>>>(a); break;
-    case 2: kv4_attn_kernel<D, F16, 2><<<a.nitems, AT, 0, st>>>(a); break;
-    default: return hipErrorInvalidValue;
-  }
-  return hipGetLastError();
-}
-
 }  // namespace
 
 hipError_t launch_kv4_append(const Kv4Args& a, int32_t head_dim, bool f16, hipStream_t st) {
@@ -758,24 +736,30 @@ hipError_t launch_kv4_read(const Kv4Args& a, int32_t head_dim, bool f16, hipStre
   return hipGetLastError();
 }
 
-hipError_t launch_kv4_attention(const Kv4Args& a, int32_t head_dim, bool f16, int32_t ncb,
-                                hipStream_t st) {
+hipError_t launch_kv4_attention(const Kv4Args& a, int32_t head_dim, bool f16, hipStream_t st) {
   if (a.nitems <= 0) return hipSuccess;
-  if (head_dim == 128) return f16 ? launch_attn_ncb<128, true>(a, ncb, st) : launch_attn_ncb<128, false>(a, ncb, st);
-  if (head_dim == 64) return f16 ? launch_attn_ncb<64, true>(a, ncb, st) : launch_attn_ncb<64, false>(a, ncb, st);
-  return hipErrorInvalidValue;
+  if (head_dim == 128) {
+    if (f16) kv4_attn_kernel<128, true><<<a.nitems, AT, 0, st>>>(a);
+    else kv4_attn_kernel<128, false><<<a.nitems, AT, 0, st>>>(a);
+  } else if (head_dim == 64) {
+    if (f16) kv4_attn_kernel<64, true><<<a.nitems, AT, 0, st>>>(a);
+    else kv4_attn_kernel<64, false><<<a.nitems, AT, 0, st>>>(a);
+  } else {
+    return hipErrorInvalidValue;
+  }
+  return hipGetLastError();
 }
 
-hipError_t launch_kv4_join(const Kv4Args& a, int32_t head_dim, bool f16, int32_t ncb,
-                           int32_t blocks, int32_t columns, hipStream_t st) {
+hipError_t launch_kv4_join(const Kv4Args& a, int32_t head_dim, bool f16, int32_t blocks,
+                           int32_t columns, hipStream_t st) {
   if (blocks <= 0) return hipSuccess;
   const dim3 grid((unsigned)blocks, (unsigned)columns);
   if (head_dim == 128) {
-    if (f16) kv4_join_kernel<128, true><<<grid, AT, 0, st>>>(a, 16 * ncb);
-    else kv4_join_kernel<128, false><<<grid, AT, 0, st>>>(a, 16 * ncb);
+    if (f16) kv4_join_kernel<128, true><<<grid, AT, 0, st>>>(a);
+    else kv4_join_kernel<128, false><<<grid, AT, 0, st>>>(a);
   } else if (head_dim == 64) {
-    if (f16) kv4_join_kernel<64, true><<<grid, AT, 0, st>>>(a, 16 * ncb);
-    else kv4_join_kernel<64, false><<<grid, AT, 0, st>>>(a, 16 * ncb);
+    if (f16) kv4_join_kernel<64, true><<<grid, AT, 0, st>>>(a);
+    else kv4_join_kernel<64, false><<<grid, AT, 0, st>>>(a);
   } else {
     return hipErrorInvalidValue;
   }
