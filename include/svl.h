@@ -540,13 +540,15 @@ svl_status svl_decode_step_noalloc(const svl_config *cfg, const svl_layer_weight
  * sums are float32; rows are fp16 or bf16 (`compute`), head_dim 64 or 128.
  *
  * Rows are [row][head][head_dim] with a row stride ld in elements, at least
- * heads * head_dim, at most 2^23 and a multiple of 8, so Q, K and V may be slices of one packed
- * projection.  cu_* are host arrays [batch + 1] of row offsets (from 0 or more,
- * not decreasing; a sample may have no rows).  They are read before the call
- * returns and travel with the launches: nothing is copied to the device, and a
- * captured call keeps the lengths it was made with.  Rows outside the samples
- * are neither read nor written.  No call needs another workspace state than its
- * own: two captured graphs may share one as long as they do not run at once. */
+ * heads * head_dim, at most 2^23 and a multiple of 8, so Q, K and V may be
+ * slices of one packed projection.  cu_* are host arrays [batch + 1] of row
+ * offsets (from 0 or more, not decreasing; a sample may have no rows).  They are
+ * read before the call returns and travel with the launches: nothing is copied to
+ * the device, and a captured call keeps the lengths it was made with.  Rows
+ * outside the samples are neither read nor written.  Samples of one call do not
+ * share rows, and nothing that a call writes may be part of another of its arrays.
+ * No call needs another workspace state than its own: two captured graphs may
+ * share one as long as they do not run at once. */
 typedef struct {
   int32_t n_heads, n_kv_heads, head_dim;
   int32_t compute;   /* svl_compute: SVL_COMPUTE_F16 (fp16 rows) or SVL_COMPUTE_BF16 */

@@ -338,7 +338,7 @@ struct Exec {
     a.cache = cache4 + (int64_t)l * batch * KV * tiles * kv4_tile_bytes(d);
     a.tiles = tiles;
     a.scale = 1.0f / std::sqrt((float)d);
-    a.window = window;
+    a.window = window_of(window);
     a.sinks = sinks;
     const auto seg = [](const void* ctx, int32_t i) {
       const AttnGroup& g = static_cast<const AttnGroup*>(ctx)[i];
@@ -372,7 +372,7 @@ struct Exec {
     w.ldo = A * d;
     w.packed = 1;
     w.scale = a.scale;
-    w.window = window;
+    w.window = a.window;
     w.sinks = sinks;
     return window_segments(
         w,

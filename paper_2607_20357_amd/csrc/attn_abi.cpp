@@ -155,7 +155,7 @@ Kv4Args kv4_args(const svl_attention& t, void* cache, int32_t max_len) {
   a.cache = static_cast<uint8_t*>(cache);
   a.tiles = cdiv(max_len, KV4_TILE);
   a.scale = t.scale;
-  a.window = t.window;
+  a.window = window_of(t.window);
   a.sinks = t.sinks;
   return a;
 }
@@ -450,7 +450,7 @@ svl_status svl_window_attention(const svl_attention* att, int32_t batch, const i
   a.lse = lse;
   a.key_mask = key_mask;
   a.scale = att->scale;
-  a.window = att->window;
+  a.window = window_of(att->window);
   a.sinks = att->sinks;
   const PackedRows r{cu_q, cu_k, att->n_heads};
   return hip_status(window_segments(a, win_seg, &r, batch, att->head_dim,
@@ -465,7 +465,7 @@ size_t svl_window_workspace_bytes(const svl_attention* att, int32_t batch, const
   WinBwdArgs a{};
   a.n_heads = att->n_heads;
   a.n_kv_heads = att->n_kv_heads;
-  a.window = att->window;
+  a.window = window_of(att->window);
   a.sinks = att->sinks;
   int64_t most = 0;
   for (int32_t b = 0; b < batch;) {
@@ -522,7 +522,7 @@ svl_status svl_window_attention_backward(const svl_attention* att, int32_t batch
   a.expo = reinterpret_cast<int32_t*>(w + rb);
   a.partial = reinterpret_cast<float*>(w + 2 * rb);
   a.scale = att->scale;
-  a.window = att->window;
+  a.window = window_of(att->window);
   a.sinks = att->sinks;
   const bool f16 = att->compute == SVL_COMPUTE_F16;
   const hipStream_t st = (hipStream_t)stream;

@@ -72,6 +72,10 @@ hipError_t launch_kv4_attention(const Kv4Args& a, int32_t head_dim, bool f16, hi
 hipError_t launch_kv4_join(const Kv4Args& a, int32_t head_dim, bool f16, int32_t blocks,
                            int32_t columns, hipStream_t st);
 
+// Positions are below 2^30: a wider window hides nothing, and the kernels' sums of a
+// position and the window stay in 32 bits.
+constexpr int32_t window_of(int32_t window) { return window < 1 << 30 ? window : 1 << 30; }
+
 // ---------------------------------------------------------------- packed rows
 // One sample: queries at rows q0 .. q0 + nq - 1, keys at rows k0 .. k0 + nk - 1;
 // query i is at position nk - nq + i.

@@ -113,7 +113,7 @@ __global__ __launch_bounds__(256, 2) void window_attn_kernel(WinArgs a) {
   const float sl2 = a.scale * 1.4426950408889634f;   // scores in log2 units
 
   const int fr = lds_frag<D>(lane), tr = lds_tr<D>(lane);
-  const int wlim = a.window > 0 ? min(a.window, 1 << 30) : 1 << 30;   // (positions are below 2^30)
+  const int wlim = a.window > 0 ? a.window : 1 << 30;   // (positions are below 2^30)
   if (tid < 6) s_bad[tid >> 1][tid & 1] = 0;
   __syncthreads();
   // a tile that the wave's own rows see nothing of

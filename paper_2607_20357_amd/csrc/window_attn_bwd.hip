@@ -141,7 +141,7 @@ __global__ __launch_bounds__(NT, 2) void window_dq_kernel(WinBwdArgs a) {
   bool poison = false;
 
   const int fr = lds_frag<D>(lane), tr = lds_tr<D>(lane);
-  const int wlim = a.window > 0 ? min(a.window, 1 << 30) : 1 << 30;
+  const int wlim = a.window > 0 ? a.window : 1 << 30;
   if (tid < 3) s_bad[tid] = 0;
   __syncthreads();
   // a tile that the wave's own rows see nothing of
@@ -391,7 +391,7 @@ __global__ __launch_bounds__(DKV_NT, 2) void window_dkv_kernel(WinBwdArgs a) {
     }
   };
   const int fr = lds_frag<D>(lane), tr = lds_tr<D>(lane);
-  const int wlim = a.window > 0 ? min(a.window, 1 << 30) : 1 << 30;
+  const int wlim = a.window > 0 ? a.window : 1 << 30;
   Entry now{kvh * rep, 0}, next = now;
   if (x0 < x1) {
     now = next = entry(x0);

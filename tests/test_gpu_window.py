@@ -223,3 +223,16 @@ def test_key_gradient_under_large_outputs(compute):
     bound = 1.01 * ((each.transpose(0, 2, 1) @ aq).sum(0)[:, None] * d ** -0.5 + h * np.abs(w["dk"]))
     err = np.abs(f64(dk) - w["dk"])
     assert (err <= bound).all(), float((err / bound).max())
+
+
+@pytest.mark.parametrize("compute", COMPUTES)
+def test_the_largest_window_is_no_window(compute):
+    """window and sinks at the largest integer: the causal range, bit for bit."""
+    heads, n = (2, 1, 64), [150, 70]
+    cu, _, q, k, v, grad, _ = _inputs(heads, compute, n, n, 12)
+    most = 2 ** 31 - 1
+    base = run_window(svl.make_attention(*heads, compute=compute), cu, None, q, k, v, None, grad)
+    for window, sinks in ((most, 0), (most, most), (2 ** 30, 1), (5, most)):
+        att = svl.make_attention(*heads, window=window, sinks=sinks, compute=compute)
+        for x, y in zip(base, run_window(att, cu, None, q, k, v, None, grad)):
+            assert torch.equal(x, y), (window, sinks)
