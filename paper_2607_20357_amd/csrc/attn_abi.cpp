@@ -195,8 +195,8 @@ int64_t seg_units(const Kv4Args& a, const CacheSeg& s) {
 
 // Key / value gradient of the windowed attention: how its work is cut.  Two items a
 // compute unit (rows of 4096 and 3001 in a window of 1024, 32 on 8 heads, with the
-// join: 256 items 734 us, 512 475, 640 464, 768 503), and no piece of fewer than 8
-// list entries (rows of 640 and 577, 32 heads: from 4 on cut, with the join 83 us,
+// join: 256 items 727 us, 512 460, 640 444, 768 475), and no piece of fewer than 8
+// list entries (rows of 640 and 577, 32 heads: from 4 on cut, with the join 76 us,
 // from 8 on not, 42).
 constexpr int64_t kDkvTarget = 512, kDkvMin = 8;   // work items of a launch; list entries of a piece
 

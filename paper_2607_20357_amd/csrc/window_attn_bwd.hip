@@ -554,21 +554,24 @@ __global__ __launch_bounds__(DKV_NT, 2) void window_dkv_kernel(WinBwdArgs a) {
     }
 }
 
-// Adds the pieces of the cut key tiles, in piece order: one workgroup per work
-// item that is a first piece, 32 bytes of a row per thread and pass.
+// Adds the pieces of the cut key tiles, in piece order.  Bound by latency: the
+// workgroups of a tile's pieces share its rows, 32 bytes of a row per thread and
+// pass, four pieces in flight (16 sink tiles of some 15 pieces: 11 us, with one
+// workgroup a tile 25).
 template <int D, bool F16>
 __global__ __launch_bounds__(NT) void window_dkv_join_kernel(WinBwdArgs a) {
   const int item = blockIdx.x;
   if (item >= a.nitems) return;
   const WinBwdSeg& sg = a.seg[find_item_seg(a, item)];
   const DkvItem it = dkv_item(a, sg, item - sg.item0);
-  if (it.part < 0 || it.piece != 0) return;
+  if (it.part < 0) return;
   const int rows = min(WIN_DK, sg.nk - it.kt * WIN_DK);
-  const float* base = a.partial + it.part * (2 * WIN_DK * D);
-  for (int t = threadIdx.x; t < 2 * rows * (D / 8); t += NT) {
+  const float* base = a.partial + (it.part - it.piece) * (2 * WIN_DK * D);
+  for (int t = it.piece * NT + threadIdx.x; t < 2 * rows * (D / 8); t += it.pieces * NT) {
     const int c = t % (D / 8) * 8, r = t / (D / 8) % rows, which = t / (D / 8) / rows;
     const float* src = base + ((int64_t)which * WIN_DK + r) * D + c;
     floatx4 y = {0.f, 0.f, 0.f, 0.f}, z = y;
+#pragma unroll 4
     for (int s = 0; s < it.pieces; ++s) {
       y += *reinterpret_cast<const floatx4*>(src + (int64_t)s * 2 * WIN_DK * D);
       z += *reinterpret_cast<const floatx4*>(src + (int64_t)s * 2 * WIN_DK * D + 4);
