@@ -331,7 +331,9 @@ hipError_t window_segments(WinArgs& a, WinSegOf get, const void* ctx, int32_t n,
       a.seg[a.nsegs++] = s;
     }
     if (a.nsegs == 0) continue;
-    // two workgroups fit a CU: with fewer of 128 rows, 64 rows each
+    // two workgroups fit a CU: with fewer of 128 rows, 64 rows each (640 rows of 32
+    // heads in a window of 256: 19 us against 25, causal rows of 640 and 577 25.5
+    // against 28; up to 3008 rows of 28 heads on 4 264 against 219)
     const int32_t bq = items < 512 ? 64 : 128;
     items = 0;
     for (int32_t k = 0; k < a.nsegs; ++k) {
