@@ -633,7 +633,8 @@ size_t svl_window_workspace_bytes(const svl_attention *att, int32_t batch, const
  * gets a gradient (zero where no query sees it), summed over its query heads and
  * rows in a fixed order: the same bits on every call.  With fp16 rows dS is scaled
  * by powers of two on the way, so small or loss-scaled gradients keep their
- * digits. */
+ * digits.  What the rounding of out changes in rowsum(grad_out * out) is put back
+ * for grad_k; in grad_q it stays. */
 svl_status svl_window_attention_backward(
     const svl_attention *att, int32_t batch, const int32_t *cu_q, const int32_t *cu_k,
     const void *q, int64_t ld_q, const void *k, int64_t ld_k, const void *v, int64_t ld_v,
