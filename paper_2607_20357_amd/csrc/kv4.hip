@@ -11,6 +11,8 @@
 namespace svl {
 namespace {
 
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+
 __device__ __forceinline__ int find_seg(const Kv4Args& a, int item) {
   int lo = 0, hi = a.nsegs - 1;
   while (lo < hi) {
@@ -35,25 +37,36 @@ __device__ __forceinline__ uint8_t* tile_ptr(const Kv4Args& a, int sample, int k
   return a.cache + (((int64_t)sample * a.n_kv_heads + kvh) * a.tiles + tile) * Tile<D>::BYTES;
 }
 
-// The largest 16-bit value that is not above q >= 0.
+// The largest 16-bit value that is not above (hi - lo) / 15, as bits: the float32
+// quotient is next to it, and 15 times a candidate is exact, so it is compared with
+// the difference and its error.  Only bf16's range can overflow the difference.
 template <bool F16>
-__device__ __forceinline__ uint32_t round_down_bits(double q) {
-  uint32_t b = f32_to_act_bits<F16>((float)q);
-  if ((double)act_bits_to_f32<F16>(b) > q) return b - 1;
-  if ((double)act_bits_to_f32<F16>(b + 1) <= q) return b + 1;
-  return b;
+__device__ __forceinline__ uint32_t step_bits(float lo, float hi) {
+  const float d = hi - lo, back = d - hi;
+  if (!F16 && __any(d == __builtin_inff())) {
+    const double q = ((double)hi - lo) / 15.0;
+    const uint32_t b = f32_to_act_bits<F16>((float)q);
+    if ((double)act_bits_to_f32<F16>(b) > q) return b - 1;
+    return (double)act_bits_to_f32<F16>(b + 1) <= q ? b + 1 : b;
+  }
+  const float err = (hi - (d - back)) - (lo + back);     // hi - lo = d + err
+  const uint32_t b = f32_to_act_bits<F16>(d * (1.0f / 15.0f));
+  auto above = [&](uint32_t x) { return (15.0f * act_bits_to_f32<F16>(x) - d) - err > 0.f; };
+  return above(b) ? b - 1 : above(b + 1) ? b : b + 1;
 }
 
 constexpr int NT = 256;   // append and read: four waves, each the K or the V half of a tile
 
 // One wave quantises the K or V half of a tile: lane = (row, quarter), the quarter
 // holding the 16-byte pieces 4 i + quarter of its row, so a load takes 64 bytes a
-// row and a lane's K words are neighbours in the cache.  Bound by memory: 2 d bytes
-// in and d / 2 + d / 16 out per row.  A code is exact: k, the
-// floor of the rounded quotient, is it or one below, and x - lo (with the error of
-// its subtraction) is compared with the border (k + 1/2) s, which float32 holds
-// exactly.  (Float64 where float32 is near a border: ties are common among values
-// of 8 bits, 163 us for 15211 rows of 32 heads of 128 against 100.)
+// row and a lane's K words are neighbours in the cache.  2 d bytes in and d / 2 + d / 16 out
+// per row; bound by the issue of some 24 instructions a value (82% of the cycles):
+// 15211 rows of 32 heads of 128 in bf16 95 us, 3.4 TB/s, where a copy would take 63.
+// A code is exact: k, the floor of the rounded quotient, is it or one below, and
+// x - lo (with the error of its subtraction, where it has one) is compared with the
+// border (k + 1/2) s, which float32 holds exactly.  (Float64 where float32 is near a
+// border: ties are common among values of 8 bits, 163 us; the step in float64 and the
+// subtraction's error always: 101.)
 template <int D, bool F16>
 __global__ __launch_bounds__(NT) void kv4_append_kernel(Kv4Args a) {
   typedef Tile<D> T;
@@ -87,7 +100,7 @@ __global__ __launch_bounds__(NT) void kv4_append_kernel(Kv4Args a) {
 #pragma unroll
   for (int g = 0; g < G; ++g) {
     float lo = __builtin_inff(), hi = -__builtin_inff();
-    uint32_t top = 0;       // largest magnitude, as bits: tells inf and NaN
+    u16x2 tops = {0, 0}, lows = {0xffff, 0xffff};   // magnitudes as bits: the largest, the least but 0 less 1
 #pragma unroll
     for (int i = g * PG; i < (g + 1) * PG; ++i) {
       const uint32_t v[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
@@ -96,17 +109,21 @@ __global__ __launch_bounds__(NT) void kv4_append_kernel(Kv4Args a) {
         const float x0 = act_bits_to_f32<F16>(v[e] & 0xffffu), x1 = act_bits_to_f32<F16>(v[e] >> 16);
         lo = fminf(lo, fminf(x0, x1));
         hi = fmaxf(hi, fmaxf(x0, x1));
-        top = max(top, max(v[e] & 0x7fffu, (v[e] >> 16) & 0x7fffu));
+        const u16x2 m = __builtin_bit_cast(u16x2, v[e] & 0x7fff7fffu);
+        tops = __builtin_elementwise_max(tops, m);
+        lows = __builtin_elementwise_min(lows, u16x2(m - u16x2{1, 1}));
       }
     }
+    uint32_t top = max(tops[0], tops[1]), low = min(lows[0], lows[1]);
 #pragma unroll
     for (int o = 1; o < 4; o <<= 1) {
       lo = fminf(lo, __shfl_xor(lo, o, 64));
       hi = fmaxf(hi, __shfl_xor(hi, o, 64));
       top = max(top, (uint32_t)__shfl_xor((int)top, o, 64));
+      low = min(low, (uint32_t)__shfl_xor((int)low, o, 64));
     }
     const bool bad = top >= (F16 ? 0x7c00u : 0x7f80u);
-    const uint32_t sb = bad ? (F16 ? 0x7e00u : 0x7fc0u) : round_down_bits<F16>(((double)hi - lo) / 15.0);
+    const uint32_t sb = bad ? (F16 ? 0x7e00u : 0x7fc0u) : step_bits<F16>(lo, hi);
     const uint32_t lb = bad ? (F16 ? 0x7e00u : 0x7fc0u) : f32_to_act_bits<F16>(lo);
     const float s = act_bits_to_f32<F16>(sb);
     const bool flat = bad || sb == 0;
@@ -114,8 +131,15 @@ __global__ __launch_bounds__(NT) void kv4_append_kernel(Kv4Args a) {
       uint32_t* par = reinterpret_cast<uint32_t*>(tp + 2 * T::CODES + (is_v ? T::PARAMS : 0));
       par[((r >> 2) * G + g) * 4 + (r & 3)] = sb | (lb << 16);
     }
-    // RARE: a step below the type's normal range may leave codes above 15; bf16's
-    // reciprocal or the range itself may overflow (then all is scaled by 2^100).
+    // x and lo are multiples of the least magnitude's last place and their difference is
+    // below four times the largest's power of two: within these many powers of two it
+    // is exact in float32 (of 1024 normal values, 93% of the cases in bf16, two thirds
+    // in fp16)
+    constexpr uint32_t P = F16 ? 10 : 7;
+    const bool wide = (top >> P) > max((low + 1) >> P, 1u) + 22 - P;
+    // RARE: otherwise its error is taken along; a step below the type's normal range
+    // may leave codes above 15; bf16's reciprocal or the range itself may overflow
+    // (then all is scaled by 2^100).
     auto codes = [&]<bool RARE>() __attribute__((always_inline)) {
       const float big = !RARE || F16 ? 1.f : s < 0x1p-100f ? 0x1p100f : s > 0x1p100f ? 0x1p-100f : 1.f;
       const float sx = s * big, lx = lo * big, inv = 1.0f / sx, half = 0.5f * sx;
@@ -127,10 +151,13 @@ __global__ __launch_bounds__(NT) void kv4_append_kernel(Kv4Args a) {
         for (int e = 0; e < 8; ++e) {
           float x = act_bits_to_f32<F16>(e & 1 ? v[e / 2] >> 16 : v[e / 2] & 0xffffu);
           if constexpr (RARE) x *= big;
-          const float d = x - lx, back = d - x;
-          const float err = (x - (d - back)) - (lx + back);     // x - lo = d + err
+          const float d = x - lx;
           uint32_t c = (uint32_t)(d * inv);
-          const float over = (d - fmaf((float)c, sx, half)) + err;
+          float over = d - fmaf((float)c, sx, half);
+          if constexpr (RARE) {
+            const float back = d - x;
+            over += (x - (d - back)) - (lx + back);             // x - lo = d + that
+          }
           // one more above the border, and on it if that makes c even (a sum that is 0 is +0)
           c += (int)(__float_as_uint(over) + (c & 1)) > 0 ? 1u : 0u;
           if constexpr (RARE) c = min(c, 15u);
@@ -139,7 +166,7 @@ __global__ __launch_bounds__(NT) void kv4_append_kernel(Kv4Args a) {
         words[i] = flat ? 0u : word;
       }
     };
-    if (__any(!flat && (s < (F16 ? 0x1p-14f : 0x1p-100f) || s > 0x1p100f))) codes.template operator()<true>();
+    if (__any(!flat & (wide | (s < (F16 ? 0x1p-14f : 0x1p-100f)) | (s > 0x1p100f)))) codes.template operator()<true>();
     else codes.template operator()<false>();
   }
   if (!is_v) {
