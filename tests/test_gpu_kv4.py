@@ -117,6 +117,30 @@ def test_hard_values_read_back(compute, d):
 
 
 @pytest.mark.parametrize("compute", COMPUTES)
+def test_a_tie_that_a_tiny_value_decides(compute):
+    """Steps of 16 from -136 (the largest value 104): 0 is on a border, and values of either
+    sign beside it are not, however small; their difference from -136 does not fit float32."""
+    d, n, dt = 64, 24, dtype_of(compute)
+    att = svl.make_attention(1, 1, d, compute=compute)
+    x = np.zeros((n, d))
+    x[:, 0], x[:, 1], x[:, 2:20] = -136.0, 104.0, np.arange(18) * 12.0 - 110.0
+    for r in range(n):
+        tiny = 2.0 ** -(r + 1)                                  # fp16's smallest subnormal at last
+        x[r, 20:40:2], x[r, 21:40:2] = tiny, -tiny
+    rows = torch.from_numpy(x).to(dt).reshape(n, 1, d)
+    assert np.array_equal(f64(rows)[:, 0, 20:40], x[:, 20:40])
+    k = rows.cuda()
+    cache = svl.alloc_kv4_cache(att, 1, n)
+    svl.svl_kv4_append(att, [0, n], [0], k, k.flip(0).contiguous(), cache, n)
+    ko, vo = torch.zeros_like(k), torch.zeros_like(k)
+    svl.svl_kv4_read(att, [0, n], [0], cache, n, ko, vo)
+    # multiples of 8 below 256: exact in both types
+    want = cached_rows(k, k, compute)[2]
+    assert np.array_equal(np.unique(want[:, 0, 20:40:2]), [8.0]) and np.array_equal(np.unique(want[:, 0, 21:40:2]), [-8.0])
+    assert np.array_equal(f64(ko), want) and np.array_equal(f64(vo)[::-1], want)
+
+
+@pytest.mark.parametrize("compute", COMPUTES)
 def test_read_takes_ragged_rows_strides_and_leaves_the_rest(compute):
     A, H, d, max_len = 4, 2, 128, 400
     att = svl.make_attention(A, H, d, compute=compute)
