@@ -79,7 +79,9 @@ __global__ __launch_bounds__(NT, 2) void window_dq_kernel(WinBwdArgs a) {
   }
   delta += __shfl_xor(delta, 32, 64);
   top = max(top, (uint32_t)__shfl_xor((int)top, 32, 64));
-  const float lse2 = a.lse[row * a.n_heads + h] * kLog2e;
+  // (a lane past the sample has the operands of row 0: no weights, or those of keys that
+  // row 0 does not see would set the wave's scale)
+  const float lse2 = on ? a.lse[row * a.n_heads + h] * kLog2e : __builtin_inff();
   // fp16: dS 2^-ex, which brings the row's largest gradient into [1, 2) (a row of
   // zeros, or with an inf or NaN, asks for nothing: fp16's smallest exponent)
   int ex = 0;
