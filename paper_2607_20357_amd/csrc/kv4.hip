@@ -459,15 +459,20 @@ __global__ __launch_bounds__(AT, 2) void kv4_attn_kernel(Kv4Args a) {
   // One unit; PART: some column does not see some position of it.
   auto unit_of = [&](int u) { return u < un.us ? u : un.uw + (u - un.us); };
   auto add_unit = [&]<bool PART>(Loaded x, int kv0) __attribute__((always_inline)) {
+    uint32_t vis = 0xffu;
     if constexpr (PART) {
-      // a position that no column sees may hold anything
+      // a position that the column does not see may hold anything: neither its values
+      // nor its scale may count
+      vis = 0;
 #pragma unroll
       for (int t = 0; t < 2; ++t)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           const int j = kv0 + 16 * t + 4 * gq + r;
+          const bool ok = (j <= pq) & ((j > pq - wlim) | (j < a.sinks));   // (no short cuts: branches)
+          vis |= (uint32_t)ok << (4 * t + r);
 #pragma unroll
-          for (int g = 0; g < G; ++g) x.vp[t][g][r] = j <= p_hi ? x.vp[t][g][r] : 0u;
+          for (int g = 0; g < G; ++g) x.vp[t][g][r] = ok ? x.vp[t][g][r] : 0u;
         }
     }
     u32x4 kf[2][NS];
@@ -486,7 +491,7 @@ __global__ __launch_bounds__(AT, 2) void kv4_attn_kernel(Kv4Args a) {
       vmax = column_max(vmax);
       // scales below 2^(e + 1) with e the largest one's exponent: P' < 2^15
       const int want = max(-126, min(126, 14 - ((int)(__float_as_uint(vmax) >> 23) - 127)));
-      if (__any(want < ve)) {   // (the same in every lane)
+      if (__any(want < ve)) {   // (a column's own)
         const float f = ldexpf(1.0f, min(want - ve, 0));
 #pragma unroll
         for (int g = 0; g < G; ++g)
@@ -498,7 +503,6 @@ __global__ __launch_bounds__(AT, 2) void kv4_attn_kernel(Kv4Args a) {
     const float pf0 = F16 ? 4.f : pow2f(ve), pf1 = pf0 * 0.0625f;
     const float back0 = -7.5f / pf0, back1 = -7.5f / pf1;
     float sc[2][4];
-    uint32_t vis = 0xffu;
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
       floatx4 acc[G];
@@ -520,16 +524,10 @@ __global__ __launch_bounds__(AT, 2) void kv4_attn_kernel(Kv4Args a) {
       }
     }
     if constexpr (PART) {
-      vis = 0;
 #pragma unroll
       for (int t = 0; t < 2; ++t)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const int j = kv0 + 16 * t + 4 * gq + r;
-          const bool ok = (j <= pq) & ((j > pq - wlim) | (j < a.sinks));   // (no short cuts: branches)
-          sc[t][r] = ok ? sc[t][r] : -__builtin_inff();
-          vis |= (uint32_t)ok << (4 * t + r);
-        }
+        for (int r = 0; r < 4; ++r) sc[t][r] = (vis >> (4 * t + r)) & 1 ? sc[t][r] : -__builtin_inff();
     }
     float mx = fmaxf(fmaxf(fmaxf(sc[0][0], sc[0][1]), fmaxf(sc[0][2], sc[0][3])),
                      fmaxf(fmaxf(sc[1][0], sc[1][1]), fmaxf(sc[1][2], sc[1][3])));
@@ -562,8 +560,7 @@ __global__ __launch_bounds__(AT, 2) void kv4_attn_kernel(Kv4Args a) {
       for (int t = 0; t < 2; ++t)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          uint32_t pw = x.vp[t][g][r];
-          if constexpr (PART) pw = (vis >> (4 * t + r)) & 1 ? pw : 0u;
+          const uint32_t pw = x.vp[t][g][r];
           const float vs = act_bits_to_f32<F16>(pw & 0xffffu);
           ol[g] = fmaf(p[t][r], fmaf(vs, 7.5f, act_bits_to_f32<F16>(pw >> 16)), ol[g]);
           ps[t][r] = p[t][r] * (r < 2 ? pf0 : pf1) * vs;

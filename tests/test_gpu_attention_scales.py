@@ -1,5 +1,5 @@
-"""Windowed attention and its gradient where scores span many powers of two, against
-the float64 oracle."""
+"""Windowed attention, its gradient and the cached attention where scores or the cache's
+scales span many powers of two."""
 import pytest
 import torch
 
@@ -29,3 +29,29 @@ def test_gradients_under_large_scores(heads, n, window, sinks, compute):
         v, grad = (draw(gen, (int(cu[-1]), h, d), compute) for h in (H, A))
         got = run_window(att, cu, cu, q, k, v, None, grad)
         check_window(att, compute, cu, cu, q, k, v, got, None, grad)
+
+
+# ------------------------------------------------------------------ cached attention
+@pytest.mark.parametrize("compute", COMPUTES)
+def test_what_the_window_hides_may_hold_anything(compute):
+    """Positions before the window that were never appended: the bytes under them, read as
+    scales, are zeros or near the type's largest value."""
+    A, H, d, max_len = 4, 2, 128, 700
+    for window, sinks, rows, pos in ((20, 0, 1, 600), (20, 3, 1, 661), (50, 0, 5, 450), (9, 2, 30, 641)):
+        att = svl.make_attention(A, H, d, window=window, sinks=sinks, compute=compute)
+        gen, first = _gen(window), pos - window + 1
+        m = pos + rows - first
+        k, v = (draw(gen, (m, H, d), compute, 0.01) for _ in range(2))
+        q = draw(gen, (rows, A, d), compute, 100.0)
+        outs = []
+        for byte in (0x00, 0x7b):
+            cache = svl.alloc_kv4_cache(att, 1, max_len)
+            cache.fill_(byte)
+            svl.svl_kv4_append(att, [0, m], [first], k, v, cache, max_len)
+            if sinks:
+                svl.svl_kv4_append(att, [0, sinks], [0], k[:sinks], v[:sinks], cache, max_len)
+            out = torch.full_like(q, float("nan"))
+            svl.svl_kv4_attention(att, [0, rows], [pos], q, cache, max_len, out, svl.alloc_kv4_workspace(att))
+            outs.append(out)
+        assert torch.isfinite(outs[0]).all()
+        assert torch.equal(outs[0], outs[1]), (window, sinks, rows)
