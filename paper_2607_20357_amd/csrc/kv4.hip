@@ -427,9 +427,10 @@ __global__ __launch_bounds__(AT, 2) void kv4_attn_kernel(Kv4Args a) {
 #pragma unroll
     for (int j = 0; j < 4; ++j) o[g][j] = floatx4{0.f, 0.f, 0.f, 0.f};
   }
-  // P' = p s 2^ve: fp16 scales fit with a fixed factor; bf16 ones follow the
-  // largest scale seen
-  int ve = F16 ? 2 : 126;
+  // P' = p s 2^ve follows the largest scale seen, so that it is in fp16's normal range for
+  // weights down to 2^-24 whatever the size of V (a fixed factor of 4, which fits any
+  // fp16 scale, loses the digits of small values and of long tails behind a first key)
+  int ve = 126;
 
   // a head's cache is below 2^28 bytes; tiles past its end (the second of the last
   // unit) read as zeros
@@ -480,14 +481,14 @@ __global__ __launch_bounds__(AT, 2) void kv4_attn_kernel(Kv4Args a) {
     for (int t = 0; t < 2; ++t)
 #pragma unroll
       for (int s = 0; s < NS; ++s) kf[t][s] = four_pairs(x.kw[t][s]);
-    if constexpr (!F16) {
+    {
       float vmax = 0.f;
 #pragma unroll
       for (int t = 0; t < 2; ++t)
 #pragma unroll
         for (int g = 0; g < G; ++g)
 #pragma unroll
-          for (int r = 0; r < 4; ++r) vmax = fmaxf(vmax, bf16_bits_to_f32(x.vp[t][g][r] & 0xffffu));
+          for (int r = 0; r < 4; ++r) vmax = fmaxf(vmax, act_bits_to_f32<F16>(x.vp[t][g][r] & 0xffffu));
       vmax = column_max(vmax);
       // scales below 2^(e + 1) with e the largest one's exponent: P' < 2^15
       const int want = max(-126, min(126, 14 - ((int)(__float_as_uint(vmax) >> 23) - 127)));
@@ -500,8 +501,8 @@ __global__ __launch_bounds__(AT, 2) void kv4_attn_kernel(Kv4Args a) {
         ve = min(ve, want);
       }
     }
-    const float pf0 = F16 ? 4.f : pow2f(ve), pf1 = pf0 * 0.0625f;
-    const float back0 = -7.5f / pf0, back1 = -7.5f / pf1;
+    const float pf0 = pow2f(ve), pf1 = pf0 * 0.0625f;
+    const float back0 = -7.5f * pow2f(-ve), back1 = 16.f * back0;
     float sc[2][4];
 #pragma unroll
     for (int t = 0; t < 2; ++t) {

@@ -1,10 +1,12 @@
-"""Windowed attention, its gradient and the cached attention where scores or the cache's
-scales span many powers of two."""
+"""Windowed attention, its gradient and the cached attention where scores, softmax
+weights or the cache's scales span many powers of two."""
+import numpy as np
 import pytest
 import torch
 
 import paper_2607_20357_amd as svl
-from attention_helpers import check_window, draw, offsets, run_window
+from attention_helpers import U32, cached_rows, check_window, draw, f64, half_step, offsets, run_window, worst
+from oracle import attention as oa
 
 pytestmark = pytest.mark.gpu
 COMPUTES = ["f16", "bf16"]
@@ -55,3 +57,87 @@ def test_what_the_window_hides_may_hold_anything(compute):
             outs.append(out)
         assert torch.isfinite(outs[0]).all()
         assert torch.equal(outs[0], outs[1]), (window, sinks, rows)
+
+
+def _check_cached_scaled(att, compute, pos, q, k, v, got):
+    """One sample of one query row against the oracle; the bound has no term that does not
+    follow the scales of V, and stays well below the outputs."""
+    u, rep, m = half_step(compute), att.n_heads // att.n_kv_heads, pos + 1
+    (kc, ks, kl), (vc, vs, vl), kk, vv = cached_rows(k[:m], v[:m], compute)
+    ref = oa.attention(f64(q), kk, vv, oa.visible([pos], m, att.window, att.sinks), att.scale)
+    r = lambda x: np.repeat(x, rep, axis=1).transpose(1, 0, 2)                  # [A][m][d]
+    over = lambda x: (ref["p"] @ r(x)).transpose(1, 0, 2)
+    wide = lambda x: np.repeat(x, oa.GROUP, -1)
+    p, size = ref["p"].transpose(0, 2, 1), float(np.sqrt((ref["out"] ** 2).mean()))
+    # P s is rounded to fp16 (2^-11 of it) with the largest scale brought to [2^14, 2^15) and
+    # half of the positions 16 times lower: below fp16's normal range half a step is 2^-25 of
+    # at least 2^14 / 16 for the largest scale.  What that takes is put back for code 7.5, so
+    # each meets a code within 7.5 of that
+    top = vs.max((0, 2))[None, :, None] + 0 * wide(vs)
+    each = 7.5 * (2.0 ** -11 * (1 + 2.0 ** -10) * p * r(wide(vs)) + 2.0 ** -35 * r(top))
+    # a weight is off by its score's error: s q . c + lo sum(q) in float32, d + 16 roundings
+    de = (att.head_dim + 16) * U32 * att.scale * \
+        (r(wide(np.abs(kl)) + wide(ks) * kc) @ np.abs(f64(q)).transpose(1, 2, 0))  # [A][m][1]
+    part = 3 * de * p * r(wide(np.abs(vl)) + wide(vs) * vc)
+    # either is independent from position to position and of either sign: over 8 times the root
+    # of the squares' sum with a probability of 2 exp(-32) (Hoeffding).  The power and what the
+    # positions share 2^-20; sums: a lane adds some m / 16 terms, the joins 64 more
+    root = lambda x: 8 * np.sqrt((x ** 2).sum(1))[None]
+    tol = u * np.abs(ref["out"]) + root(each) + root(part) + 3 * 2.0 ** -20 * over(np.abs(vv)) + \
+        (m / 16 + 64) * U32 * over(wide(np.abs(vl)) + wide(vs) * vc) + (2.0 ** -25 if compute == "f16" else 0.0)
+    assert np.median(tol) < 0.25 * size, (np.median(tol), size)       # the bound can fail
+    ratio = worst(np.abs(f64(got) - ref["out"]), tol)
+    print("  error / bound:", round(ratio, 3), "bound / size:", float(np.median(tol) / size), flush=True)
+    assert ratio <= 1.0
+
+
+@pytest.mark.parametrize("compute", COMPUTES)
+@pytest.mark.parametrize("n,spread,score,sink", [(300, 1e-4, 1.0, 0.0), (300, 1e-4, 4.0, 0.0), (300, 3e-3, 1.0, 9.0),
+                                                 (4096, 1.0, 0.5, 14.0), (8192, 1.0, 1.0, 12.0), (20000, 0.01, 1.0, 14.0)])
+def test_small_values_and_small_weights(n, spread, score, sink, compute):
+    """Small V, peaky softmax, and long contexts behind a first position of value 0 that
+    takes almost all of the weight: what the others add is all there is."""
+    A, H, d = 4, 2, 128
+    att = svl.make_attention(A, H, d, compute=compute)
+    gen = _gen(n)
+    k, v = draw(gen, (n, H, d), compute), draw(gen, (n, H, d), compute, spread)
+    q = draw(gen, (1, A, d), compute, score)
+    if sink:
+        # the first key is along the query, its score `sink` above what the others reach on average
+        unit = q[0, ::2].float()
+        k[0] = (unit * (sink * d ** 0.5 / (unit ** 2).sum(-1, keepdim=True))).to(k.dtype)
+        q[0, 1::2] = q[0, ::2]
+        v[0] = 0
+    cache = svl.alloc_kv4_cache(att, 1, n)
+    svl.svl_kv4_append(att, [0, n], [0], k, v, cache, n)
+    out = torch.full_like(q, float("nan"))
+    svl.svl_kv4_attention(att, [0, 1], [n - 1], q, cache, n, out, svl.alloc_kv4_workspace(att))
+    _check_cached_scaled(att, compute, n - 1, q, k, v, out)
+
+
+@pytest.mark.parametrize("compute", COMPUTES)
+@pytest.mark.parametrize("n,sink,down,up", [(300, 0.0, 8, 4), (300, 10.0, 5, 8), (5000, 12.0, 4, 8)])
+def test_powers_of_two_of_v_come_out_as_they_are(n, sink, down, up, compute):
+    """V times 2^x has the same codes and scales and minima of 2^x: so has the output, to the
+    bit where it is a normal number."""
+    A, H, d = 4, 2, 64
+    att = svl.make_attention(A, H, d, compute=compute)
+    gen = _gen(n)
+    k, v, q = draw(gen, (n, H, d), compute), draw(gen, (n, H, d), compute), draw(gen, (1, A, d), compute)
+    if sink:
+        unit = q[0, ::2].float()
+        k[0] = (unit * (sink * d ** 0.5 / (unit ** 2).sum(-1, keepdim=True))).to(k.dtype)
+        q[0, 1::2] = q[0, ::2]
+    # multiples of 2^-6: exact at every power below
+    v = torch.round(v.float() * 64).div(64).to(v.dtype)
+    outs = []
+    for x in (0, -down, up):
+        cache = svl.alloc_kv4_cache(att, 1, n)
+        svl.svl_kv4_append(att, [0, n], [0], k, (v.float() * 2.0 ** x).to(v.dtype), cache, n)
+        out = torch.full_like(q, float("nan"))
+        svl.svl_kv4_attention(att, [0, 1], [n - 1], q, cache, n, out, svl.alloc_kv4_workspace(att))
+        outs.append(out.double() * 2.0 ** -x)
+    normal = outs[0].abs() >= 2.0 ** (down - 14)
+    assert normal.float().mean() > (0.3 if compute == "f16" else 0.8)
+    for x in outs[1:]:
+        assert torch.equal(x[normal], outs[0][normal])
