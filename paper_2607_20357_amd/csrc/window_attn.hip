@@ -111,6 +111,10 @@ __global__ __launch_bounds__(256, 2) void window_attn_kernel(WinArgs a) {
 #pragma unroll
     for (int r = 0; r < 16; ++r) o[b][r] = 0.f;
   const float sl2 = a.scale * 1.4426950408889634f;   // scores in log2 units
+  // fp16: weights are held 2^7 times larger (2^15 at most, see the maximum below), so that
+  // those of a long tail behind a first key are seldom subnormal: half a step of those is
+  // 2^-32 of the row's largest weight
+  constexpr float UP = F16 ? 7.f : 0.f;
 
   const int fr = lds_frag<D>(lane), tr = lds_tr<D>(lane);
   const int wlim = a.window > 0 ? a.window : 1 << 30;   // (positions are below 2^30)
@@ -188,7 +192,7 @@ __global__ __launch_bounds__(256, 2) void window_attn_kernel(WinArgs a) {
         for (int c = 0; c < NB; ++c) o[c] *= alpha;
         m = mn;
       }
-      const float mu = m == -__builtin_inff() ? 0.f : m;   // nothing above -inf yet
+      const float mu = m == -__builtin_inff() ? 0.f : m - UP;   // nothing above -inf yet: 0
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
         st[r] = exp2_raw(fmaf(st[r], sl2, -mu));
@@ -253,7 +257,7 @@ __global__ __launch_bounds__(256, 2) void window_attn_kernel(WinArgs a) {
       *reinterpret_cast<uint2*>(out + (a.packed ? packed_index(row, col, a.ldo) : row * a.ldo + col)) = w;
     }
   if (a.lse && half == 0)
-    a.lse[row * a.n_heads + h] = l == 0.f ? -__builtin_inff() : m * 0.6931471805599453f + logf(l);
+    a.lse[row * a.n_heads + h] = l == 0.f ? -__builtin_inff() : (m - UP) * 0.6931471805599453f + logf(l);
 }
 
 template <int D, bool F16>

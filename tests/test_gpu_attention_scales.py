@@ -5,7 +5,8 @@ import pytest
 import torch
 
 import paper_2607_20357_amd as svl
-from attention_helpers import U32, cached_rows, check_window, draw, f64, half_step, offsets, run_window, worst
+from attention_helpers import (U32, cached_rows, check_window, draw, dtype_of, f64, half_step, offsets, run_window,
+                               score_error, worst)
 from oracle import attention as oa
 
 pytestmark = pytest.mark.gpu
@@ -141,3 +142,43 @@ def test_powers_of_two_of_v_come_out_as_they_are(n, sink, down, up, compute):
     assert normal.float().mean() > (0.3 if compute == "f16" else 0.8)
     for x in outs[1:]:
         assert torch.equal(x[normal], outs[0][normal])
+
+
+# ------------------------------------------------------------------ small weights
+def _behind_a_sink(heads, n, compute, above, seed=0):
+    """Rows whose first key has a score `above` over all the others' 0 and a value of 0, so
+    that out, and the gradients of the others, come from weights of e^-above."""
+    A, H, d = heads
+    gen = _gen(seed)
+    q = torch.ones((n, A, d), device="cuda")
+    k = torch.zeros((n, H, d), device="cuda")
+    k[0] = above * d ** -0.5
+    v = draw(gen, (n, H, d), compute)
+    v[0] = 0
+    # with signs of either kind in the other keys the scores stay 0
+    k[1:, :, 0::2], k[1:, :, 1::2] = 0.5, -0.5
+    dt = dtype_of(compute)
+    return q.to(dt), k.to(dt), v, draw(gen, (n, A, d), compute)
+
+
+@pytest.mark.parametrize("compute", COMPUTES)
+@pytest.mark.parametrize("n,above", [(40, 13.0), (300, 14.0), (300, 16.0), (700, 15.0)])
+def test_outputs_of_small_weights(n, above, compute):
+    heads = (2, 1, 128)
+    att = svl.make_attention(*heads, compute=compute)
+    q, k, v, _ = _behind_a_sink(heads, n, compute, above)
+    cu, u = offsets([n]), half_step(compute)
+    v = v * (1000.0 if compute == "f16" else 1.0)
+    out, lse = run_window(att, cu, None, q, k, v)
+    Q, K, V = f64(q), f64(k), f64(v)
+    ref = oa.attention(Q, K, V, oa.visible(np.arange(n), n, 0, 0), att.scale)
+    pav = (ref["p"] @ np.repeat(np.abs(V), 2, axis=1).transpose(1, 0, 2)).transpose(1, 0, 2)
+    # P is rounded once; fp16: the row's largest is held at 2^7 to 2^15, half a subnormal
+    # step is 2^-25 of that
+    de = score_error(Q, K, att.scale)
+    low = 2.0 ** -32 * np.cumsum(np.abs(V), 0) if compute == "f16" else 0.0
+    tol = u * (np.abs(ref["out"]) + pav) * (1 + 2 * u) + 3 * de * pav + low + (2.0 ** -25 if compute == "f16" else 0.0)
+    ratio = worst(np.abs(f64(out) - ref["out"]), tol)
+    print("  error / bound:", round(ratio, 3), "bound / size:", float(np.median(tol[5:]) / np.abs(ref["out"][5:]).mean()), flush=True)
+    assert ratio <= 1.0
+    assert worst(np.abs(f64(lse) - ref["lse"]), de + (n + 8) * U32 + 4 * U32 * np.abs(ref["lse"])) <= 1.0
