@@ -335,6 +335,11 @@ __global__ __launch_bounds__(DKV_NT, 2) void window_dkv_kernel(WinBwdArgs a) {
     for (int r = 0; r < 16; ++r) sum[b][r] = 0.f;
   const float sl2 = a.scale * kLog2e;
   int ex = -126;                         // fp16: dS 2^-ex, the same in every lane of the wave
+  // fp16: P is held 2^12 times larger, so that small weights keep their digits as an operand
+  // (weights are 1 at most, but for the log-sum's rounding: the next 2^3 are for scores of
+  // millions); dP - D takes it back: fac = 2^(-ex - UP)
+  constexpr int UP = F16 ? 12 : 0;
+  const float back = pow2f(-UP);
   float fac = 1.f;
 
   static_assert(STEP % 16 == 0, "a thread's pieces of a tile");
@@ -387,7 +392,7 @@ __global__ __launch_bounds__(DKV_NT, 2) void window_dkv_kernel(WinBwdArgs a) {
       *reinterpret_cast<u32x4*>(&dst[WIN_DQ * D + at]) = gr[i];
     }
     if (tid < WIN_DQ) {
-      s_lse[buf][tid] = lse_r * kLog2e;
+      s_lse[buf][tid] = lse_r * kLog2e - UP;
       s_delta[buf][tid] = delta_r;
       if constexpr (F16) s_expo[buf][tid] = expo_r;
     }
@@ -477,7 +482,7 @@ __global__ __launch_bounds__(DKV_NT, 2) void window_dkv_kernel(WinBwdArgs a) {
         if (e > ex) {
           const float f = ldexpf(1.f, ex - e);
           ex = e;
-          fac = pow2f(-ex);
+          fac = pow2f(-ex) * back;
 #pragma unroll
           for (int b = 0; b < NB; ++b) sum[b] *= f;
         }
@@ -526,7 +531,7 @@ __global__ __launch_bounds__(DKV_NT, 2) void window_dkv_kernel(WinBwdArgs a) {
     }
   }
   const float f = for_k ? a.scale : 1.f;
-  if (!F16 || !for_k) ex = 0;
+  if (!F16 || !for_k) ex = -UP;
   if (it.part >= 0) {
     // float32 blocks [dk, dv][key][dim], the keys past the sample too (not read)
     float* pb = a.partial + it.part * (2 * WIN_DK * D) + (for_k ? 0 : WIN_DK * D) + (int64_t)(32 * kg + lk) * D;

@@ -182,3 +182,30 @@ def test_outputs_of_small_weights(n, above, compute):
     print("  error / bound:", round(ratio, 3), "bound / size:", float(np.median(tol[5:]) / np.abs(ref["out"][5:]).mean()), flush=True)
     assert ratio <= 1.0
     assert worst(np.abs(f64(lse) - ref["lse"]), de + (n + 8) * U32 + 4 * U32 * np.abs(ref["lse"])) <= 1.0
+
+
+@pytest.mark.parametrize("compute", COMPUTES)
+@pytest.mark.parametrize("n,above,window", [(40, 12.0, 0), (300, 13.0, 0), (300, 15.0, 0), (700, 14.0, 300)])
+def test_value_gradients_of_small_weights(n, above, window, compute):
+    """Keys that every row gives a weight near e^-above."""
+    heads = (2, 1, 128)
+    att = svl.make_attention(*heads, window=window, sinks=1, compute=compute)
+    q, k, v, grad = _behind_a_sink(heads, n, compute, above)
+    cu, u = offsets([n]), half_step(compute)
+    grad = grad * (1000.0 if compute == "f16" else 1.0)
+    dv = run_window(att, cu, None, q, k, v, None, grad)[4]
+    ok = oa.visible(np.arange(n), n, window, 1)
+    ref = oa.attention(f64(q), f64(k), f64(v), ok, att.scale, f64(grad))
+    ag = np.abs(f64(grad)).transpose(1, 0, 2)
+    # P (from a log-sum with float32's error) rounded once; fp16: held 2^12 times larger, half a
+    # subnormal step is 2^-37.  The sums over rows and heads are float32
+    dw = score_error(f64(q), f64(k), att.scale) + (n + 8) * U32 + 4 * U32 * np.abs(ref["lse"]).max()
+    pe = ref["p"] * (u * (1 + 2 * u) + 3 * dw + 2 * n * U32) + np.where(ok[None], 2.0 ** -37 if compute == "f16" else 0.0, 0.0)
+    tol = (pe.transpose(0, 2, 1) @ ag).sum(0)[:, None] + u * np.abs(ref["dv"]) + (2.0 ** -25 if compute == "f16" else 0.0)
+    # (a sum past fp16's largest value is inf)
+    over = np.abs(ref["dv"]) > (65500.0 if compute == "f16" else np.inf)
+    err = np.where(over, 0.0, np.abs(f64(dv) - ref["dv"]))
+    assert (np.abs(f64(dv))[over] >= 65408).all()
+    print("  error / bound:", round(worst(err, tol), 3), "bound / size:",
+          float(np.median(tol[1:]) / np.abs(ref["dv"][1:]).mean()), flush=True)
+    assert worst(err, tol) <= 1.0
