@@ -11,9 +11,10 @@
 // the query gradient by tiles of query rows, the key and value gradients by
 // tiles of keys; S and dP are formed in both.
 //
-// fp16: dS is scaled by a power of two into fp16's range, from the largest
-// gradient of the row (dQ) or of the rows so far (dK), and further down where
-// that does not hold it; the factor is taken out in float32.
+// fp16: dS is scaled by a power of two that brings the largest gradient of the row
+// (dQ) or of the rows so far (dK) into [2^10, 2^11), and further down where dS
+// passes 2^15: rows that give almost all of their weight to one key have dS far
+// below their gradient.  The factor is taken out in float32.
 //
 // An inf or NaN of a row or key must not reach those that it is masked from (0
 // times inf): in tiles that are partly masked, such values are 0 in the operands
@@ -82,11 +83,11 @@ __global__ __launch_bounds__(NT, 2) void window_dq_kernel(WinBwdArgs a) {
   // (a lane past the sample has the operands of row 0: no weights, or those of keys that
   // row 0 does not see would set the wave's scale)
   const float lse2 = on ? a.lse[row * a.n_heads + h] * kLog2e : __builtin_inff();
-  // fp16: dS 2^-ex, which brings the row's largest gradient into [1, 2) (a row of
+  // fp16: dS 2^-ex, which brings the row's largest gradient into [2^10, 2^11) (a row of
   // zeros, or with an inf or NaN, asks for nothing: fp16's smallest exponent)
   int ex = 0;
   if constexpr (F16)
-    ex = top > 0 && top < kNonfinite<true> ? (int)(__float_as_uint(act_bits_to_f32<true>(top)) >> 23) - 127 : -24;
+    ex = (top > 0 && top < kNonfinite<true> ? (int)(__float_as_uint(act_bits_to_f32<true>(top)) >> 23) - 127 : -24) - 10;
   if constexpr (F16)
     if (on && half == 0) a.expo[row * a.n_heads + h] = ex;
   float off_d = 0.f;             // sum(dS), times fac

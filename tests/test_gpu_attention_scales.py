@@ -209,3 +209,41 @@ def test_value_gradients_of_small_weights(n, above, window, compute):
     print("  error / bound:", round(worst(err, tol), 3), "bound / size:",
           float(np.median(tol[1:]) / np.abs(ref["dv"][1:]).mean()), flush=True)
     assert worst(err, tol) <= 1.0
+
+
+@pytest.mark.parametrize("compute", COMPUTES)
+@pytest.mark.parametrize("n,above,window", [(40, 9.0, 0), (300, 11.0, 0), (300, 13.0, 0), (700, 12.0, 300)])
+def test_query_and_key_gradients_of_small_weights(n, above, window, compute):
+    """Rows that give almost all of their weight to one key: dS is small everywhere."""
+    heads = (2, 1, 128)
+    att = svl.make_attention(*heads, window=window, sinks=1, compute=compute)
+    q, k, v, grad = _behind_a_sink(heads, n, compute, above)
+    cu, u, d = offsets([n]), half_step(compute), 128
+    grad = grad * (4096.0 if compute == "f16" else 1.0)
+    _, _, dq, dk, _ = run_window(att, cu, None, q, k, v, None, grad)
+    ok = oa.visible(np.arange(n), n, window, 1)
+    ref = oa.attention(f64(q), f64(k), f64(v), ok, att.scale, f64(grad))
+    ag, ak, aq = (np.abs(f64(x)).transpose(1, 0, 2) for x in (grad, k, q))
+    av, g = np.abs(f64(v)).transpose(1, 0, 2), np.abs(f64(grad))
+    dw = score_error(f64(q), f64(k), att.scale) + (n + 8) * U32 + 4 * U32 * np.abs(ref["lse"]).max()
+    # dP and D: float32 sums of d terms, and D's part of out's rounding (taken off again for dk,
+    # and for dq by the second term of dS: to the error of that sum)
+    out_err = u * np.abs(ref["out"]) + (2.0 ** -25 if compute == "f16" else 0.0)
+    pav = (ref["p"] @ np.repeat(av, 2, axis=0)).transpose(1, 0, 2)
+    out_err = out_err + (u + 3 * dw) * pav + (2.0 ** -31 * np.cumsum(np.abs(f64(v)), 0) if compute == "f16" else 0.0)
+    delta = (g * out_err).sum(-1).T[..., None]                                   # [A][n][1]
+    sums = (d + 8) * U32 * (ag @ np.repeat(av, 2, axis=0).transpose(0, 2, 1))    # [A][n][m]
+    es = ref["p"] * (delta + sums) + (u * (1 + 2 * u) + 3 * dw) * np.abs(ref["ds"])
+    if compute == "f16":
+        # held with the row's (dk: the rows') largest gradient in [2^10, 2^11), or where that
+        # overflows the largest dS there: half a subnormal step of either
+        es = es + np.where(ok[None], 2.0 ** -35 * max(g.max(), 2 * np.abs(ref["ds"]).max()), 0.0)
+    tq = att.scale * (es @ np.repeat(ak, 2, axis=0)).transpose(1, 0, 2) + u * np.abs(ref["dq"])
+    tk = att.scale * (es.transpose(0, 2, 1) @ aq).sum(0)[:, None] + u * np.abs(ref["dk"])
+    tk = tk + 2 * n * U32 * att.scale * (np.abs(ref["ds"]).transpose(0, 2, 1) @ aq).sum(0)[:, None]
+    tiny = 2.0 ** -25 if compute == "f16" else 0.0
+    for name, got, t in (("dq", dq, tq + tiny), ("dk", dk, tk + tiny)):
+        err = np.abs(f64(got) - ref[name])
+        print(" ", name, "error / bound:", round(worst(err, t), 3), "bound / size:",
+              float(np.median(t[5:]) / np.abs(ref[name][5:]).mean()), flush=True)
+        assert worst(err, t) <= 1.0, name
