@@ -85,9 +85,6 @@ hipError_t timed(int cls, hipStream_t st, F&& f) {
   return r;
 }
 
-enum KClass { K_SELECT = 0, K_GATHER, K_NORM, K_QKV, K_ATTN, K_O, K_GU, K_DOWN, K_ROPE, K_FINISH,
-              K_KV_APPEND, K_CTRL };
-
 // ------------------------------------------------------------------ validation
 svl_status check_config(const svl_config* c, bool for_kernels = true) {
   if (!c) return fail(SVL_E_NULL, "config is NULL");

@@ -17,8 +17,6 @@
 namespace svl {
 namespace {
 
-constexpr int K_ATTN = 4, K_KV_APPEND = 10;   // kernel classes of svl_timing_read
-
 bool is_aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 int64_t round256(int64_t x) { return (x + 255) & ~int64_t(255); }
 int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }

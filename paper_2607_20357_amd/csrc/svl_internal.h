@@ -230,6 +230,9 @@ hipError_t launch_nonfinite(const float* x, int64_t n, uint32_t* flag, hipStream
 // and returns st; validates a config as every entry point does.
 svl_status set_error(svl_status st, const char* msg);
 svl_status validate_config(const svl_config* c);
+// Kernel classes of svl_timing_read.
+enum KClass { K_SELECT = 0, K_GATHER, K_NORM, K_QKV, K_ATTN, K_O, K_GU, K_DOWN, K_ROPE, K_FINISH,
+              K_KV_APPEND, K_CTRL };
 // Runs f(arg), bracketed by events of a kernel class while timing is on.
 hipError_t timed_call(int kernel_class, hipStream_t st, hipError_t (*f)(const void*), const void* arg);
 
