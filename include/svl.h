@@ -547,6 +547,7 @@ svl_status svl_decode_step_noalloc(const svl_config *cfg, const svl_layer_weight
  * the device, and a captured call keeps the lengths it was made with.  Rows
  * outside the samples are neither read nor written.  Samples of one call do not
  * share rows, and nothing that a call writes may be part of another of its arrays.
+ * Calls that write one cache are made one after the other: positions share words.
  * No call needs another workspace state than its own: two captured graphs may
  * share one as long as they do not run at once. */
 typedef struct {
@@ -602,7 +603,9 @@ size_t svl_kv4_workspace_bytes(const svl_attention *att);
  * hold its keys.  One row per sample is a decode step; several are a prompt's
  * next chunk or proposed tokens.  The products use the codes themselves: K and V
  * are not rounded on the way; the softmax weights times s are rounded to 16 bits
- * once. */
+ * once, under a power of two from the largest s of V seen (weights down to 2^-24 of
+ * the largest keep their digits there).  What the window or the causal order hides
+ * may hold anything. */
 svl_status svl_kv4_attention(const svl_attention *att, int32_t batch, const int32_t *cu_rows,
                              const int32_t *pos, const void *q, int64_t ld_q, const void *cache,
                              int32_t max_len, void *out, int64_t ld_out, void *ws, size_t ws_bytes,
@@ -633,7 +636,11 @@ size_t svl_window_workspace_bytes(const svl_attention *att, int32_t batch, const
  * gets a gradient (zero where no query sees it), summed over its query heads and
  * rows in a fixed order: the same bits on every call.  With fp16 rows dS is scaled
  * by powers of two on the way, so small or loss-scaled gradients keep their
- * digits.  What the rounding of out changes in rowsum(grad_out * out) is put back
+ * digits: grad_q's by the row's largest gradient, grad_k's by the largest of the
+ * head group's rows so far, taken by blocks of 32 rows, so beside a row whose
+ * gradient is over 2^20 times as large a key's may lose digits.  A key seen by a row
+ * whose out or gradient is not finite may get a gradient that is not finite, in
+ * grad_v too.  What the rounding of out changes in rowsum(grad_out * out) is put back
  * for grad_k; in grad_q it stays. */
 svl_status svl_window_attention_backward(
     const svl_attention *att, int32_t batch, const int32_t *cu_q, const int32_t *cu_k,
