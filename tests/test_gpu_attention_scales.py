@@ -247,3 +247,31 @@ def test_query_and_key_gradients_of_small_weights(n, above, window, compute):
         print(" ", name, "error / bound:", round(worst(err, t), 3), "bound / size:",
               float(np.median(t[5:]) / np.abs(ref[name][5:]).mean()), flush=True)
         assert worst(err, t) <= 1.0, name
+
+
+# ------------------------------------------------------------------ distance
+@pytest.mark.parametrize("ld,n", [(1 << 22, [290, 33]), (1 << 23, [130, 140])])
+def test_rows_far_apart(ld, n):
+    """Samples whose rows span more than 2 GiB: the same bits as rows side by side."""
+    A, H, d = 4, 2, 128
+    att = svl.make_attention(A, H, d, window=70, sinks=3)
+    gen, cu = _gen(len(n)), offsets(n)
+    total = int(cu[-1])
+    heads = (A, H, H, A, A, A, H, H)                    # q, k, v, out, grad, dq, dk, dv
+    wide, at, far = torch.empty((total, ld), dtype=torch.float16, device="cuda"), 0, []
+    for h in heads:
+        far.append(wide[:, at:at + h * d].unflatten(1, (h, d)))
+        at += h * d
+    near = [draw(gen, (total, h, d), "f16") for h in heads]
+    for x, y in zip(far, near):
+        x.copy_(y)
+    sums = []
+    for q, k, v, out, grad, dq, dk, dv in (near, far):
+        lse = torch.empty((total, A), device="cuda")
+        svl.svl_window_attention(att, cu, None, q, k, v, out, lse=lse)
+        svl.svl_window_attention_backward(att, cu, None, q, k, v, out, lse, grad, dq, dk, dv,
+                                          svl.alloc_window_workspace(att, cu))
+        sums.append(lse)
+    assert torch.equal(*sums)
+    for x, y in zip(far, near):
+        assert torch.equal(x, y)
