@@ -9,7 +9,8 @@ Kinds of case:
   norm     svl_norm_forward, and with a gradient svl_norm_backward: RMS or layer
            norm of rows, and the gradients of the rows, the gain and the bias
   loss     svl_lm_loss: the language-model head's softmax cross entropy against
-           each row's label, and the gradients of the rows and of the head
+           each row's label, and the gradients of the rows and of the head; a row
+           without a label (an image position) has neither loss nor gradient
   adamw    svl_adamw_step over a list of tensors, states in 32 bits or in 8, and
            for 8 bits svl_adamw_read_state: the moments that the codes stand for
 
@@ -72,7 +73,7 @@ def listed():
         _norm("norm_train_layer", 2885, 1024, "layer", "f16", "f16", "f32", True, bias=True),
         # serving: log-probabilities of given tokens, one row of each of eight requests
         _loss("score_step_b8", 8, 4096, 32000, "f16", False, False, 0.0),
-        # one image and question: image positions carry no label
+        # a few questions, half of the positions without a label
         _loss("loss_prompt", 640, 4096, 32000, "bf16", True, True, 0.5),
         # the controllers learn through a frozen decoder: the rows' gradient only, odd sizes, a scaled loss
         _loss("loss_frozen_head", 3001, 3584, 65537, "f16", True, False, 0.25, 1024.0),
@@ -110,7 +111,7 @@ def draw(rng):
         top = int(8192 * 4096 * 32000 * 0.6 / (width * vocab))
         compute = rng.choice(["bf16", "f16"])
         return _loss(None, log_int(1, min(top, 8000)), width, vocab, compute, "x" in both, "w" in both,
-                     rng.choice([0.0, 0.1, 0.6]), 1024.0 if compute == "f16" else 1.0,
+                     rng.choice([0.0, 0.1, 0.6, 0.9]), 1024.0 if compute == "f16" else 1.0,
                      "w" in both and rng.random() < 0.3)
     sizes = [log_int(1, 3000000) for _ in range(log_int(1, 90))]
     return _adamw(None, sizes, any_type(), any_type(), rng.choice([8, 32]), rng.random() < 0.5)
@@ -273,7 +274,7 @@ def _plain_loss(st):
     total = e.sum(-1, keepdim=True)
     lse = top + torch.log(total)
     loss = torch.where(there, (lse - s.gather(1, at)).squeeze(1), torch.zeros_like(st["row_weight"]))
-    out = [loss, lse.squeeze(1)]
+    out = [loss, torch.where(there, lse.squeeze(1), torch.zeros_like(loss))]
     if not (case["grad_x"] or case["grad_w"]):
         return tuple(out)
     del s
@@ -487,11 +488,12 @@ def work(case):
             moved += n * d * (x + y + x) + d * g + (8 if case["bias"] else 4) * d
         return {"bytes": moved, "flops": 0}
     if kind == "loss":
-        n, d, v = case["rows"], case["width"], case["vocab"]
-        moved = 2 * (n * d + v * d) + 12 * n
+        d, v = case["width"], case["vocab"]
+        n = case["rows"] * (1.0 - case["ignored"])      # rows with a label
+        moved = 2 * (n * d + v * d) + 12 * case["rows"]
         products = 1 + case["grad_x"] + case["grad_w"]
         if case["grad_x"]:
-            moved += 2 * n * d
+            moved += 2 * case["rows"] * d
         if case["grad_w"]:
             moved += 2 * v * d * (2 if case["accumulate"] else 1)
         return {"bytes": moved, "flops": 2 * products * n * d * v}
@@ -571,7 +573,8 @@ def _exact_loss(case, st):
             if case["grad_w"]:
                 dw += p.t().contiguous() @ x[a:z]
         del s
-    out = [loss, lse]
+    has = (st["labels"] >= 0) & (st["labels"] < v)
+    out = [loss, torch.where(has, lse, torch.zeros_like(lse))]
     if case["grad_x"]:
         out.append(dx)
     if case["grad_w"]:
