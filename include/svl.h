@@ -677,6 +677,171 @@ svl_status svl_decode_step4(const svl_config *cfg, const svl_layer_weights *laye
                             int32_t sinks, void *cache, int32_t max_len, void *ws,
                             size_t ws_bytes, void *stream);
 
+/* ---- embedding, row norm, language-model loss, optimizer step -------------
+ * What surrounds the decoder where it learns and answers: the rows of its input
+ * tokens, the norm after its last layer, the loss of its head against the next
+ * tokens (whose gradient is what svl_train_step takes as grad_hidden, through the
+ * norm's backward), and the step of the parameters that learn.
+ *
+ * Rows are [row][width] with a stride ld in elements, at least width, at most 2^23
+ * and a multiple of 8; widths are multiples of 8.  Arrays are 16-byte aligned unless
+ * said otherwise.  rows = 0 is a call without work (gradients of weights that are not
+ * accumulated are then zero).  At most 2^24 rows.  Sums, statistics and moments are
+ * float32, in an order that depends on the sizes alone: the same bits on every call.
+ * Nothing that a call writes may be part of another of its arrays, but where it is
+ * said.  A workspace needs no state: two captured graphs may share one as long as
+ * they do not run at once.  Lengths are host values and stay in a captured call. */
+typedef enum { SVL_TYPE_F32 = 0, SVL_TYPE_BF16 = 1, SVL_TYPE_F16 = 2 } svl_type;
+
+typedef struct {
+  int32_t width, vocab;   /* table [vocab][width]; width <= 65536, vocab < 2^24 */
+  int32_t table_type;     /* svl_type of the table and of its gradient */
+  int32_t row_type;       /* svl_type of the rows and of their gradient */
+  float scale;            /* finite; 1 for a plain lookup */
+} svl_embedding;
+
+/* out[r] = scale * table[tokens[r]], rounded once; a row of zeros where the token
+ * (dev int32 [rows], 4-byte aligned) is outside [0, vocab). */
+svl_status svl_embed(const svl_embedding *emb, int32_t rows, const int32_t *tokens,
+                     const void *table, int64_t ld_table, void *out, int64_t ld_out, void *stream);
+
+/* Workspace bytes of svl_embed_backward (0 on bad arguments). */
+size_t svl_embed_workspace_bytes(const svl_embedding *emb, int32_t rows);
+
+/* The table's gradient: G[v] = scale * (sum of grad_rows[r] over the rows whose token
+ * is v, ascending in pieces), rounded once.  accumulate = 0: every row of grad_table is
+ * written, zeros where no token is; 1: G is added to the rows that have tokens, others
+ * are not touched.  Rows whose token is outside the table take no part and may hold
+ * anything. */
+svl_status svl_embed_backward(const svl_embedding *emb, int32_t rows, const int32_t *tokens,
+                              const void *grad_rows, int64_t ld_grad_rows, void *grad_table,
+                              int64_t ld_grad_table, int32_t accumulate, void *ws, size_t ws_bytes,
+                              void *stream);
+
+typedef enum { SVL_NORM_RMS = 0, SVL_NORM_LAYER = 1 } svl_norm_kind;
+#define SVL_NORM_MAX_WIDTH 16384
+
+typedef struct {
+  int32_t width;          /* at most SVL_NORM_MAX_WIDTH */
+  int32_t kind;           /* svl_norm_kind */
+  int32_t x_type, y_type; /* svl_type of the rows and of the normed rows */
+  int32_t gain_type;      /* svl_type of gain and bias */
+  float eps;              /* finite, >= 0 */
+} svl_norm;
+
+/* y = (x - m) r gain + bias, r = 1 / sqrt(mean (x - m)^2 + eps), with m = 0 (RMS) or
+ * the row's mean (layer norm).
+ *   gain   dev [width] or NULL (1);  bias dev [width] or NULL (0)
+ *   y      may be x where types and strides are the same
+ *   stats  dev float [rows][2] or NULL: (m, r), which the backward reads. */
+svl_status svl_norm_forward(const svl_norm *norm, int32_t rows, const void *x, int64_t ld_x,
+                            const void *gain, const void *bias, void *y, int64_t ld_y, float *stats,
+                            void *stream);
+
+/* Workspace bytes of svl_norm_backward (0 on bad arguments). */
+size_t svl_norm_workspace_bytes(const svl_norm *norm, int32_t rows);
+
+/* Gradients from x, gain, stats and grad_y (y_type).
+ *   grad_x     x_type [rows][width] or NULL; may be grad_y where types and strides are
+ *              the same
+ *   grad_gain, grad_bias  dev float [width] or NULL: sums over the rows, written, or
+ *              added to what is there (accumulate = 1). */
+svl_status svl_norm_backward(const svl_norm *norm, int32_t rows, const void *x, int64_t ld_x,
+                             const void *gain, const float *stats, const void *grad_y,
+                             int64_t ld_grad_y, void *grad_x, int64_t ld_grad_x, float *grad_gain,
+                             float *grad_bias, int32_t accumulate, void *ws, size_t ws_bytes,
+                             void *stream);
+
+typedef struct {
+  int32_t d_model;        /* a multiple of 64, at most 65536 */
+  int32_t vocab;          /* 1 .. 2^20 */
+  int32_t compute;        /* svl_compute: fp16 or bf16 rows and weights */
+} svl_lm_head;
+
+/* Workspace bytes of svl_lm_loss with the gradients named (0 on bad arguments).  With
+ * gradients it holds 16 bits for each of the vocabulary of at most a piece of the rows
+ * (about 1 GiB of them), never the logits. */
+size_t svl_lm_loss_workspace_bytes(const svl_lm_head *head, int32_t rows, int32_t want_grad_x,
+                                   int32_t want_grad_w);
+
+/* Softmax cross entropy of the rows' logits s = x w^T against their labels:
+ *   lse[r] = log sum_v exp(s[r][v]),  loss[r] = lse[r] - s[r][labels[r]]
+ * and the gradients of sum_r row_weight[r] loss[r]:
+ *   grad_x = P w,  grad_w = P^T x,  P[r][v] = row_weight[r] (softmax(s[r])[v] - [v = label]).
+ * A row whose label is outside [0, vocab) takes no part: its loss, lse and grad_x are
+ * 0, and its x may hold anything.  Rows without a label cost next to nothing.
+ *   x          dev [rows][d_model];  w dev [vocab][d_model] (compute's type)
+ *   labels     dev int32 [rows] (4-byte aligned)
+ *   row_weight dev float [rows] or NULL (1): 1 / n for a mean; with fp16 a loss scale
+ *              belongs here too
+ *   loss       dev float [rows];  lse dev float [rows] or NULL (all three 4-byte aligned)
+ *   grad_x     dev [rows][d_model] or NULL;  grad_w dev [vocab][d_model] or NULL, written,
+ *              or added to what is there (accumulate = 1)
+ * Row strides here are at most 2^21.  Logits and sums are float32.  P is rounded to 16 bits once more than softmax itself
+ * was held in (fp16 digits), in fp16 under 2^14 over the largest weight, so weights down
+ * to 2^-20 of the largest keep their digits. */
+svl_status svl_lm_loss(const svl_lm_head *head, int32_t rows, const void *x, int64_t ld_x,
+                       const void *w, int64_t ld_w, const int32_t *labels, const float *row_weight,
+                       float *loss, float *lse, void *grad_x, int64_t ld_grad_x, void *grad_w,
+                       int64_t ld_grad_w, int32_t accumulate, void *ws, size_t ws_bytes,
+                       void *stream);
+
+typedef struct {
+  double lr, beta1, beta2, eps, weight_decay;  /* finite; betas in [0, 1), eps and decay >= 0 */
+  int32_t state_bits;                          /* 32 or 8 */
+} svl_adamw;
+
+/* One tensor of an optimizer step: n elements, each array contiguous.  m and v are
+ * float [n], or with state_bits = 8 codes uint8 [n] with a scale (float, 4-byte aligned)
+ * for each 256 elements, [ceil(n / 256)]; zeros are the state before the first step.
+ * master: float [n] or NULL; where given, the step works on it and param becomes its
+ * rounding.  No two tensors of a call share elements. */
+typedef struct {
+  int64_t n;                        /* 0 .. 2^40 */
+  int32_t param_type, grad_type;    /* svl_type */
+  void *param;
+  const void *grad;
+  float *master;
+  void *m, *v;
+  float *m_scale, *v_scale;         /* state_bits = 8; otherwise NULL */
+} svl_adamw_tensor;
+
+/* What changes from step to step, read on the device: a captured step follows it. */
+typedef struct {
+  float lr;
+  float correction1, correction2;   /* 1 - beta1^step, 1 - beta2^step */
+  float grad_scale;
+  uint32_t seed;
+} svl_adamw_dev;
+
+/* One AdamW step of a host array of tensors, which is read before the call returns and
+ * travels with the launches:
+ *   g = grad_scale grad;  m' = beta1 m + (1 - beta1) g;  v' = beta2 v + (1 - beta2) g g,
+ *   p' = p - lr weight_decay p - lr (m' / (1 - beta1^step)) / (sqrt(v' / (1 - beta2^step)) + eps),
+ * float32, the factors too (1 - beta in float64 first); each product and each sum of m'
+ * and v' is rounded once, in the order written ((1 - beta2) g first).  p' goes by m' and v' before they are coded.
+ *   step  from 1;  dev NULL or the above, which then stands for lr, step, grad_scale, seed
+ * 8-bit states: a block of 256 holds scale = 2^floor(log2 max |value|) (at least 2^-90, 0
+ * where all are 0) and codes of m' and of sqrt(v'):
+ *   m  sign, 4 bits e, 3 bits f:  +-scale (1 + f / 8) 2^(e - 14), e = 0: +-scale (f / 8) 2^-13
+ *   v  5 bits e, 3 bits f: the square, as float32, of  scale (1 + f / 8) 2^(e - 30), e = 0:
+ *      scale (f / 8) 2^-29
+ * rounded up or down by chance, so that many small changes are not lost: with y = |value| /
+ * scale, u = the place of y between the neighbours in units of 2^-20 rounded down, it is the upper
+ * one where u + 16 h >= 2^20, h the low (m) or high (v) 16 bits of
+ *   mix(i 0x9E3779B9 + mix(seed + 0x9E3779B9 (t + 1) + 0xBB67AE85 (i >> 32))),
+ *   mix(x): x ^= x >> 16, x *= 0x6A09E667, x ^= x >> 15, x *= 0xBB67AE85, x ^= x >> 16
+ * modulo 2^32, for element i of tensor t of the call: give each step another seed.  A
+ * block with an inf or NaN has a NaN scale and reads as NaN. */
+svl_status svl_adamw_step(const svl_adamw *adam, int32_t n_tensors, const svl_adamw_tensor *tensors,
+                          int64_t step, uint32_t seed, float grad_scale, const svl_adamw_dev *dev,
+                          void *stream);
+
+/* The values that 8-bit states stand for: n codes of m (second = 0) or of v (second = 1)
+ * and their scales to float [n]. */
+svl_status svl_adamw_read_state(int32_t second, int64_t n, const void *codes, const float *scales,
+                                float *out, void *stream);
+
 /* Message for the last non-OK status returned on this thread. */
 const char *svl_last_error(void);
 
@@ -693,8 +858,9 @@ int32_t svl_abi_version(void);
  * (prefill and decode), 5 o-proj gemm, 6 gate/up gemm, 7 down gemm, 8 rope
  * table, 9 split-K finish (QKV and gate/up launches whose K was split),
  * 10 KV-cache append, 11 compute controller (statistics, encodings, its
- * matrix-vector products, budget rows and row compaction) and the
- * training-time budget term. */
+ * matrix-vector products, budget rows and row compaction), the
+ * training-time budget term, the language-model loss and the optimizer step.
+ * Embedding rows and their gradient count as 1, row norms as 2. */
 #define SVL_KCLASS_COUNT 12
 svl_status svl_timing_enable(int32_t on);
 svl_status svl_timing_read(int32_t kernel_class, double *total_ms, int64_t *launches);

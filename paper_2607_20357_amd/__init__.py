@@ -18,4 +18,9 @@ from .binding import (  # noqa: F401
     svl_kv4_append, svl_kv4_attention, svl_kv4_cache_bytes, svl_kv4_read, svl_kv4_workspace_bytes,
     svl_window_attention, svl_window_attention_backward, svl_window_workspace_bytes,
     alloc_cache4, alloc_decode4_workspace, svl_cache4_bytes, svl_decode_step4, svl_prefill_cache4,
+    SVL_NORM_LAYER, SVL_NORM_RMS, SVL_TYPE_BF16, SVL_TYPE_F16, SVL_TYPE_F32, AdamwTensors,
+    alloc_embed_workspace, alloc_lm_loss_workspace, alloc_norm_workspace, make_adamw, make_embedding,
+    make_lm_head, make_norm, svl_adamw, svl_adamw_read_state, svl_adamw_step, svl_adamw_tensor, svl_embed,
+    svl_embed_backward, svl_embed_workspace_bytes, svl_embedding, svl_lm_head, svl_lm_loss,
+    svl_lm_loss_workspace_bytes, svl_norm, svl_norm_backward, svl_norm_forward, svl_norm_workspace_bytes,
 )

@@ -21,6 +21,8 @@ LIB_PATH = os.path.join(_HERE, "libsvl.so")
 
 SVL_F32, SVL_BF16 = 0, 1
 SVL_COMPUTE_F16, SVL_COMPUTE_BF16 = 0, 1
+SVL_TYPE_F32, SVL_TYPE_BF16, SVL_TYPE_F16 = 0, 1, 2
+SVL_NORM_RMS, SVL_NORM_LAYER = 0, 1
 SVL_NOALLOC_SCRATCH_BYTES = 64 << 20   # include/svl.h
 KCLASS = {"select": 0, "gather": 1, "rmsnorm": 2, "gemm_qkv": 3, "attention": 4, "gemm_o": 5,
           "gemm_gate_up": 6, "gemm_down": 7, "rope_table": 8, "finish": 9, "kv_append": 10,
@@ -79,6 +81,30 @@ class svl_attention(ctypes.Structure):
     _fields_ = [("n_heads", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32),
                 ("head_dim", ctypes.c_int32), ("compute", ctypes.c_int32),
                 ("window", ctypes.c_int32), ("sinks", ctypes.c_int32), ("scale", ctypes.c_float)]
+
+
+class svl_embedding(ctypes.Structure):
+    _fields_ = [("width", ctypes.c_int32), ("vocab", ctypes.c_int32), ("table_type", ctypes.c_int32),
+                ("row_type", ctypes.c_int32), ("scale", ctypes.c_float)]
+
+
+class svl_norm(ctypes.Structure):
+    _fields_ = [("width", ctypes.c_int32), ("kind", ctypes.c_int32), ("x_type", ctypes.c_int32),
+                ("y_type", ctypes.c_int32), ("gain_type", ctypes.c_int32), ("eps", ctypes.c_float)]
+
+
+class svl_lm_head(ctypes.Structure):
+    _fields_ = [("d_model", ctypes.c_int32), ("vocab", ctypes.c_int32), ("compute", ctypes.c_int32)]
+
+
+class svl_adamw(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_double) for n in ("lr", "beta1", "beta2", "eps", "weight_decay")] + [
+        ("state_bits", ctypes.c_int32)]
+
+
+class svl_adamw_tensor(ctypes.Structure):
+    _fields_ = [("n", ctypes.c_int64), ("param_type", ctypes.c_int32), ("grad_type", ctypes.c_int32)] + [
+        (n, ctypes.c_void_p) for n in ("param", "grad", "master", "m", "v", "m_scale", "v_scale")]
 
 
 class svl_flops(ctypes.Structure):
@@ -169,6 +195,24 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.svl_window_attention.argtypes = [attp, i32, P, P, P, i64, P, i64, P, i64, P, P, i64, P, P]
     lib.svl_window_attention_backward.argtypes = [attp, i32, P, P, P, i64, P, i64, P, i64, P, P, i64,
                                                   P, P, i64, P, i64, P, i64, P, i64, P, sz, P]
+    embp, normp, headp = (ctypes.POINTER(t) for t in (svl_embedding, svl_norm, svl_lm_head))
+    lib.svl_embed.argtypes = [embp, i32, P, P, i64, P, i64, P]
+    lib.svl_embed_workspace_bytes.argtypes = [embp, i32]
+    lib.svl_embed_workspace_bytes.restype = sz
+    lib.svl_embed_backward.argtypes = [embp, i32, P, P, i64, P, i64, i32, P, sz, P]
+    lib.svl_norm_forward.argtypes = [normp, i32, P, i64, P, P, P, i64, P, P]
+    lib.svl_norm_workspace_bytes.argtypes = [normp, i32]
+    lib.svl_norm_workspace_bytes.restype = sz
+    lib.svl_norm_backward.argtypes = [normp, i32, P, i64, P, P, P, i64, P, i64, P, P, i32, P, sz, P]
+    lib.svl_lm_loss_workspace_bytes.argtypes = [headp, i32, i32, i32]
+    lib.svl_lm_loss_workspace_bytes.restype = sz
+    lib.svl_lm_loss.argtypes = [headp, i32, P, i64, P, i64, P, P, P, P, P, i64, P, i64, i32, P, sz, P]
+    lib.svl_adamw_step.argtypes = [ctypes.POINTER(svl_adamw), i32, ctypes.POINTER(svl_adamw_tensor), i64,
+                                   ctypes.c_uint32, ctypes.c_float, P, P]
+    lib.svl_adamw_read_state.argtypes = [i32, i64, P, P, P, P]
+    for f in ("svl_embed", "svl_embed_backward", "svl_norm_forward", "svl_norm_backward", "svl_lm_loss",
+              "svl_adamw_step", "svl_adamw_read_state"):
+        getattr(lib, f).restype = i32
     for f in ("svl_select_tokens", "svl_layer_forward", "svl_prefill", "svl_count_flops",
               "svl_timing_enable", "svl_timing_read", "svl_count_positive", "svl_budget_project",
               "svl_prefill_cache", "svl_decode_step", "svl_decode_step_noalloc",
@@ -1127,3 +1171,325 @@ def svl_decode_step4(cfg: svl_config, layers, x: torch.Tensor, cache_len, layer_
     _check(load_library().svl_decode_step4(
         ctypes.byref(cfg), table.array, B, _dev(x, "x"), clp, lmp, hmp, fmp, int(window), int(sinks),
         _dev(cache, "cache"), int(max_len), _dev(ws, "ws"), _nbytes(ws), _launch_stream(stream)))
+
+
+# ------------------------------------------------------------------ embedding, norm, loss, optimizer
+_TYPES = {"f32": (SVL_TYPE_F32, torch.float32), "bf16": (SVL_TYPE_BF16, torch.bfloat16),
+          "f16": (SVL_TYPE_F16, torch.float16)}
+_TYPE_DTYPE = {v: t for v, t in _TYPES.values()}
+_DTYPE_TYPE = {t: v for v, t in _TYPES.values()}
+
+
+def _type(name) -> int:
+    if name not in _TYPES:
+        raise ValueError(f"unknown type {name!r}: one of {sorted(_TYPES)}")
+    return _TYPES[name][0]
+
+
+def _on_gpu(t: torch.Tensor, name: str) -> int:
+    """Address of a tensor on the current GPU."""
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a GPU tensor (no CPU path exists)")
+    if t.get_device() != torch.cuda.current_device():
+        raise ValueError(f"{name} is on {t.device}, the library launches on cuda:{torch.cuda.current_device()}")
+    return t.data_ptr()
+
+
+def _matrix(t, name: str, dtype: Optional[torch.dtype], rows: int, width: int):
+    """Checks [>= rows][width] values, contiguous along a row; returns the row stride."""
+    if not isinstance(t, torch.Tensor):
+        raise ValueError(f"{name} must be a torch tensor")
+    if t.dtype != dtype:
+        raise ValueError(f"{name} has dtype {t.dtype}, expected {dtype}")
+    shape = t.shape
+    if len(shape) != 2 or shape[1] != width:
+        raise ValueError(f"{name} has shape {tuple(shape)}, expected (rows, {width})")
+    if shape[0] < rows:
+        raise ValueError(f"{name} holds {shape[0]} rows, needs at least {rows}")
+    if shape[0] == 0:
+        return width
+    strides = t.stride()
+    if strides[1] != 1:
+        raise ValueError(f"{name}: rows must be contiguous, strides are {strides}")
+    ld = strides[0] if shape[0] > 1 else width
+    if ld < width or ld % 8:
+        raise ValueError(f"{name}: row stride {ld} must be at least {width} and a multiple of 8")
+    return ld
+
+
+def _vector(t, name: str, dtype: torch.dtype, n: int, required: bool = True) -> None:
+    if t is None and not required:
+        return
+    if not isinstance(t, torch.Tensor):
+        raise ValueError(f"{name} must be a torch tensor")
+    if t.dtype != dtype:
+        raise ValueError(f"{name} has dtype {t.dtype}, expected {dtype}")
+    if t.dim() != 1 or t.shape[0] < n:
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected at least ({n},)")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+
+
+def _place(t, name: str):
+    """Address of a checked tensor, None for a missing or empty one."""
+    return None if t is None or t.numel() == 0 else _on_gpu(t, name)
+
+
+def _rows_of(t, name: str) -> int:
+    if not isinstance(t, torch.Tensor) or t.dim() not in (1, 2):
+        raise ValueError(f"{name} must be a torch tensor of rows")
+    return int(t.shape[0])
+
+
+def _bytes_of(call: str, *args) -> int:
+    n = getattr(load_library(), call)(*args)
+    if n == 0:
+        raise SvlError(2, f"{call}: " + load_library().svl_last_error().decode())
+    return int(n)
+
+
+def make_embedding(width: int, vocab: int, table: str = "bf16", rows: str = "bf16",
+                   scale: float = 1.0) -> svl_embedding:
+    """svl_embedding; types are "f32", "bf16" or "f16"."""
+    return svl_embedding(int(width), int(vocab), _type(table), _type(rows), float(scale))
+
+
+def svl_embed(emb: svl_embedding, tokens: torch.Tensor, table: torch.Tensor, out: torch.Tensor,
+              stream=None) -> None:
+    """out[r] = scale * table[tokens[r]] for tokens int32 [rows]; zeros for a token outside the table."""
+    n = _rows_of(tokens, "tokens")
+    _vector(tokens, "tokens", torch.int32, n)
+    ldt = _matrix(table, "table", _TYPE_DTYPE.get(emb.table_type), emb.vocab, emb.width)
+    ldo = _matrix(out, "out", _TYPE_DTYPE.get(emb.row_type), n, emb.width)
+    _check(load_library().svl_embed(ctypes.byref(emb), n, _place(tokens, "tokens"), _place(table, "table"), ldt,
+                                    _place(out, "out"), ldo, _launch_stream(stream)))
+
+
+def svl_embed_workspace_bytes(emb: svl_embedding, rows: int) -> int:
+    return _bytes_of("svl_embed_workspace_bytes", ctypes.byref(emb), int(rows))
+
+
+def alloc_embed_workspace(emb: svl_embedding, rows: int, device="cuda") -> torch.Tensor:
+    return torch.empty(svl_embed_workspace_bytes(emb, rows), dtype=torch.uint8, device=device)
+
+
+def svl_embed_backward(emb: svl_embedding, tokens: torch.Tensor, grad_rows: torch.Tensor,
+                       grad_table: torch.Tensor, ws: torch.Tensor, accumulate: bool = False,
+                       stream=None) -> None:
+    """The table's gradient from the rows' gradient, written, or added to grad_table."""
+    n = _rows_of(tokens, "tokens")
+    _vector(tokens, "tokens", torch.int32, n)
+    ldr = _matrix(grad_rows, "grad_rows", _TYPE_DTYPE.get(emb.row_type), n, emb.width)
+    ldt = _matrix(grad_table, "grad_table", _TYPE_DTYPE.get(emb.table_type), emb.vocab, emb.width)
+    _expect(ws, "ws", torch.uint8, 1)
+    _check(load_library().svl_embed_backward(
+        ctypes.byref(emb), n, _place(tokens, "tokens"), _place(grad_rows, "grad_rows"), ldr,
+        _place(grad_table, "grad_table"), ldt, int(accumulate), _dev(ws, "ws"), _nbytes(ws),
+        _launch_stream(stream)))
+
+
+def make_norm(width: int, kind: str = "rms", x: str = "f32", y: str = "bf16", gain: str = "bf16",
+              eps: float = 1e-6) -> svl_norm:
+    """svl_norm of kind "rms" or "layer"; types are "f32", "bf16" or "f16"."""
+    kinds = {"rms": SVL_NORM_RMS, "layer": SVL_NORM_LAYER}
+    if kind not in kinds:
+        raise ValueError(f"unknown norm kind {kind!r}")
+    return svl_norm(int(width), kinds[kind], _type(x), _type(y), _type(gain), float(eps))
+
+
+def _norm_weights(norm: svl_norm, gain, bias=None) -> None:
+    dt = _TYPE_DTYPE.get(norm.gain_type)
+    _vector(gain, "gain", dt, norm.width, required=False)
+    _vector(bias, "bias", dt, norm.width, required=False)
+
+
+def _norm_stats(stats, rows: int) -> None:
+    if stats is None:
+        return
+    _expect(stats, "stats", torch.float32, 2 * rows)
+    if stats.dim() != 2 or stats.shape[1] != 2 or not stats.is_contiguous():
+        raise ValueError(f"stats has shape {tuple(stats.shape)}, expected (rows, 2), contiguous")
+
+
+def svl_norm_forward(norm: svl_norm, x: torch.Tensor, gain: Optional[torch.Tensor], y: torch.Tensor,
+                     bias: Optional[torch.Tensor] = None, stats: Optional[torch.Tensor] = None,
+                     stream=None) -> None:
+    """RMS or layer norm of the rows of x into y; stats, if given, gets what the backward reads."""
+    n = _rows_of(x, "x")
+    ldx = _matrix(x, "x", _TYPE_DTYPE.get(norm.x_type), n, norm.width)
+    ldy = _matrix(y, "y", _TYPE_DTYPE.get(norm.y_type), n, norm.width)
+    _norm_weights(norm, gain, bias)
+    _norm_stats(stats, n)
+    _check(load_library().svl_norm_forward(
+        ctypes.byref(norm), n, _place(x, "x"), ldx, _place(gain, "gain"), _place(bias, "bias"), _place(y, "y"), ldy,
+        _place(stats, "stats"), _launch_stream(stream)))
+
+
+def svl_norm_workspace_bytes(norm: svl_norm, rows: int) -> int:
+    return _bytes_of("svl_norm_workspace_bytes", ctypes.byref(norm), int(rows))
+
+
+def alloc_norm_workspace(norm: svl_norm, rows: int, device="cuda") -> torch.Tensor:
+    return torch.empty(svl_norm_workspace_bytes(norm, rows), dtype=torch.uint8, device=device)
+
+
+def svl_norm_backward(norm: svl_norm, x: torch.Tensor, gain: Optional[torch.Tensor], stats: torch.Tensor,
+                      grad_y: torch.Tensor, grad_x: Optional[torch.Tensor], ws: Optional[torch.Tensor] = None,
+                      grad_gain: Optional[torch.Tensor] = None, grad_bias: Optional[torch.Tensor] = None,
+                      accumulate: bool = False, stream=None) -> None:
+    """Gradients of svl_norm_forward: of the rows, and of gain and bias (float32 [width], written, or
+    added to).  ws is needed for the latter two."""
+    n = _rows_of(x, "x")
+    ldx = _matrix(x, "x", _TYPE_DTYPE.get(norm.x_type), n, norm.width)
+    ldy = _matrix(grad_y, "grad_y", _TYPE_DTYPE.get(norm.y_type), n, norm.width)
+    ldg = 0 if grad_x is None else _matrix(grad_x, "grad_x", _TYPE_DTYPE.get(norm.x_type), n, norm.width)
+    _norm_weights(norm, gain)
+    if stats is None:
+        raise ValueError("stats is required")
+    _norm_stats(stats, n)
+    _vector(grad_gain, "grad_gain", torch.float32, norm.width, required=False)
+    _vector(grad_bias, "grad_bias", torch.float32, norm.width, required=False)
+    if ws is not None:
+        _expect(ws, "ws", torch.uint8, 1)
+    _check(load_library().svl_norm_backward(
+        ctypes.byref(norm), n, _place(x, "x"), ldx, _place(gain, "gain"), _place(stats, "stats"),
+        _place(grad_y, "grad_y"), ldy, _place(grad_x, "grad_x"), ldg, _place(grad_gain, "grad_gain"),
+        _place(grad_bias, "grad_bias"), int(accumulate), None if ws is None else _dev(ws, "ws"),
+        0 if ws is None else _nbytes(ws), _launch_stream(stream)))
+
+
+def make_lm_head(d_model: int, vocab: int, compute: str = "bf16") -> svl_lm_head:
+    """svl_lm_head with "f16" or "bf16" rows and weights."""
+    kinds = {"f16": SVL_COMPUTE_F16, "bf16": SVL_COMPUTE_BF16}
+    if compute not in kinds:
+        raise ValueError(f"unknown compute type {compute!r}")
+    return svl_lm_head(int(d_model), int(vocab), kinds[compute])
+
+
+def svl_lm_loss_workspace_bytes(head: svl_lm_head, rows: int, grad_x: bool = False, grad_w: bool = False) -> int:
+    return _bytes_of("svl_lm_loss_workspace_bytes", ctypes.byref(head), int(rows), int(grad_x), int(grad_w))
+
+
+def alloc_lm_loss_workspace(head: svl_lm_head, rows: int, grad_x: bool = False, grad_w: bool = False,
+                            device="cuda") -> torch.Tensor:
+    """Workspace of svl_lm_loss for at most `rows` rows with the gradients named."""
+    return torch.empty(svl_lm_loss_workspace_bytes(head, rows, grad_x, grad_w), dtype=torch.uint8, device=device)
+
+
+def svl_lm_loss(head: svl_lm_head, x: torch.Tensor, w: torch.Tensor, labels: torch.Tensor, loss: torch.Tensor,
+                ws: torch.Tensor, lse: Optional[torch.Tensor] = None, row_weight: Optional[torch.Tensor] = None,
+                grad_x: Optional[torch.Tensor] = None, grad_w: Optional[torch.Tensor] = None,
+                accumulate: bool = False, stream=None) -> None:
+    """Cross entropy of rows x [rows][D] under the head w [vocab][D] against labels int32 [rows] (outside
+    the vocabulary: none) into loss (float32 [rows]); lse, if given, gets the log-sums.  grad_x and grad_w
+    get the gradients of sum(row_weight * loss); grad_w is written, or added to."""
+    n, D, V = _rows_of(x, "x"), head.d_model, head.vocab
+    dt = torch.bfloat16 if head.compute == SVL_COMPUTE_BF16 else torch.float16
+    ldx = _matrix(x, "x", dt, n, D)
+    ldw = _matrix(w, "w", dt, V, D)
+    _vector(labels, "labels", torch.int32, n)
+    _vector(loss, "loss", torch.float32, n)
+    _vector(lse, "lse", torch.float32, n, required=False)
+    _vector(row_weight, "row_weight", torch.float32, n, required=False)
+    ldgx = 0 if grad_x is None else _matrix(grad_x, "grad_x", dt, n, D)
+    ldgw = 0 if grad_w is None else _matrix(grad_w, "grad_w", dt, V, D)
+    _expect(ws, "ws", torch.uint8, 1)
+    _check(load_library().svl_lm_loss(
+        ctypes.byref(head), n, _place(x, "x"), ldx, _place(w, "w"), ldw, _place(labels, "labels"),
+        _place(row_weight, "row_weight"), _place(loss, "loss"), _place(lse, "lse"), _place(grad_x, "grad_x"), ldgx,
+        _place(grad_w, "grad_w"), ldgw, int(accumulate), _dev(ws, "ws"), _nbytes(ws), _launch_stream(stream)))
+
+
+def make_adamw(lr: float, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8, weight_decay: float = 0.0,
+               state_bits: int = 32) -> svl_adamw:
+    """svl_adamw with states of 32 or of 8 bits."""
+    return svl_adamw(float(lr), float(beta1), float(beta2), float(eps), float(weight_decay), int(state_bits))
+
+
+class AdamwTensors:
+    """The tensors of an optimizer step, marshalled once: dicts of param, grad, m and v, where wanted
+    master, and for 8-bit states m_scale and v_scale.  It keeps references, not copies."""
+
+    FIELDS = ("param", "grad", "master", "m", "v", "m_scale", "v_scale")
+
+    def __init__(self, tensors: Sequence[Dict[str, torch.Tensor]]):
+        self.tensors = [dict(t) for t in tensors]
+        eight = None
+        for i, t in enumerate(self.tensors):
+            unknown = set(t) - set(self.FIELDS)
+            if unknown:
+                raise ValueError(f"tensor {i}: unknown entries {sorted(unknown)}")
+            for k in ("param", "grad", "m", "v"):
+                if t.get(k) is None:
+                    raise ValueError(f"tensor {i}: {k} is missing")
+            n = t["param"].numel()
+            this = t["m"].dtype == torch.uint8
+            if eight is not None and this != eight:
+                raise ValueError(f"tensor {i}: states of 8 and of 32 bits in one list")
+            eight = this
+            if not this and (t.get("m_scale") is not None or t.get("v_scale") is not None):
+                raise ValueError(f"tensor {i}: scales belong to 8-bit states")
+            state = torch.uint8 if this else torch.float32
+            expect = {"param": None, "grad": None, "m": state, "v": state}
+            if t.get("master") is not None:
+                expect["master"] = torch.float32
+            for k, dt in expect.items():
+                x = t[k]
+                if dt is None and x.dtype not in _DTYPE_TYPE or dt is not None and x.dtype != dt:
+                    raise ValueError(f"tensor {i}: {k} has dtype {x.dtype}")
+                if x.numel() != n:
+                    raise ValueError(f"tensor {i}: {k} holds {x.numel()} elements, param {n}")
+            if this:
+                for k in ("m_scale", "v_scale"):
+                    x = t.get(k)
+                    if x is None or x.dtype != torch.float32 or x.numel() < -(-n // 256):
+                        raise ValueError(f"tensor {i}: {k} must hold {-(-n // 256)} float32 scales")
+            for k, x in t.items():
+                if x is not None and not x.is_contiguous():
+                    raise ValueError(f"tensor {i}: {k} must be contiguous")
+        self.state_bits = 8 if eight else 32
+        self.device = None
+        self.array = (svl_adamw_tensor * max(len(self.tensors), 1))()
+        for i, t in enumerate(self.tensors):
+            place = {}
+            for k in self.FIELDS:
+                x = t.get(k)
+                if x is None or x.numel() == 0:
+                    continue
+                place[k] = _on_gpu(x, f"{k} of tensor {i}")
+                self.device = x.get_device()
+            self.array[i] = svl_adamw_tensor(n=t["param"].numel(), param_type=_DTYPE_TYPE[t["param"].dtype],
+                                             grad_type=_DTYPE_TYPE[t["grad"].dtype], **place)
+
+
+def svl_adamw_step(adam: svl_adamw, tensors, step: int = 1, seed: int = 0, grad_scale: float = 1.0,
+                   dev: Optional[torch.Tensor] = None, stream=None) -> None:
+    """One AdamW step of an AdamwTensors (or a list of its dicts).  dev: 5 32-bit words on the GPU (lr,
+    1 - beta1^step, 1 - beta2^step, grad_scale as float32, the seed as uint32) in place of lr, step,
+    grad_scale and seed; a captured step reads them at each replay."""
+    if not isinstance(tensors, AdamwTensors):
+        tensors = AdamwTensors(tensors)
+    if tensors.tensors and tensors.state_bits != adam.state_bits:
+        raise ValueError(f"states of {tensors.state_bits} bits, the description says {adam.state_bits}")
+    if tensors.device is not None and tensors.device != torch.cuda.current_device():
+        raise ValueError(f"the tensors are on cuda:{tensors.device}, the library launches on "
+                         f"cuda:{torch.cuda.current_device()}")
+    if dev is not None and (not isinstance(dev, torch.Tensor) or dev.element_size() != 4 or dev.numel() < 5):
+        raise ValueError("dev must hold 5 words of 32 bits")
+    _check(load_library().svl_adamw_step(
+        ctypes.byref(adam), len(tensors.tensors), tensors.array, int(step), int(seed) & 0xFFFFFFFF,
+        float(grad_scale), None if dev is None else _dev(dev, "dev"), _launch_stream(stream)))
+
+
+def svl_adamw_read_state(which: str, codes: torch.Tensor, scales: torch.Tensor, out: torch.Tensor,
+                         stream=None) -> None:
+    """The float32 values that 8-bit codes of "m" or "v" stand for, into out."""
+    if which not in ("m", "v"):
+        raise ValueError(f"unknown state {which!r}")
+    n = codes.numel() if isinstance(codes, torch.Tensor) else 0
+    _expect(codes, "codes", torch.uint8, n)
+    _expect(scales, "scales", torch.float32, -(-n // 256))
+    _expect(out, "out", torch.float32, n)
+    _check(load_library().svl_adamw_read_state(int(which == "v"), n, _dev(codes, "codes") or None,
+                                               _dev(scales, "scales") or None, _dev(out, "out") or None,
+                                               _launch_stream(stream)))

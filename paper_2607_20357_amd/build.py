@@ -23,7 +23,8 @@ SOURCES = ["abi.cpp", "plan.cpp", "select_gather.hip", "norm_misc.hip", "gemm_mf
            "attn_mfma.hip", "fp32_path.hip", "finish.hip", "budget.cpp", "attn_decode.hip",
            "controller.hip", "budget_loss.hip", "gemv_decode.hip", "train_abi.cpp",
            "train.hip", "train_gemm3.hip", "attn_abi.cpp", "kv4.hip", "window_attn.hip",
-           "window_attn_bwd.hip"]
+           "window_attn_bwd.hip", "learn_abi.cpp", "row_norm.hip", "embed.hip", "adamw.hip", "lm_loss.hip",
+           "lm_gemm.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 COMMON = ["--offload-arch=gfx950", "-O3", "-std=c++20", "-fPIC",

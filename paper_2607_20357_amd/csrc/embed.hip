@@ -1,0 +1,311 @@
+// Rows of an embedding table by token, and the table's gradient.
+//
+// The gradient is a sum over the rows of each token.  Rows are put in the order
+// of their tokens by a radix sort that keeps the order of equal ones, then a
+// workgroup per table row sums its run of rows in that order, so the result has
+// the same bits on every call and no atomic touches a value.  A run's whole
+// aligned pieces of 32 and of 1024 rows are summed before, side by side, so that a
+// token that fills the batch costs no more than one that is rare.  Memory bounds
+// it: every gradient row is read once, every table row written once.
+#include "learn_ops.h"
+#include "svl_internal.h"
+
+namespace svl {
+namespace {
+
+constexpr int NT = 256;
+constexpr int SLAB = NT * 8;   // columns of a workgroup
+
+__global__ __launch_bounds__(NT) void embed_kernel(EmbedArgs a) {
+  const int64_t row = blockIdx.x;
+  const int col = blockIdx.y * SLAB + threadIdx.x * 8;
+  if (col >= a.width) return;
+  const int32_t tok = a.tokens[row];
+  float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+  if (tok >= 0 && tok < a.vocab) {
+    widen8(load_raw8(a.table, a.table_type, (int64_t)tok * a.ldt + col), a.table_type, v);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] *= a.scale;
+  }
+  store8(a.out, a.row_type, row * a.ldr + col, v);
+}
+
+// ------------------------------------------------------------------ order
+// A token outside the table counts as one behind it.
+__device__ __forceinline__ uint32_t token_key(const SortArgs& s, int i) {
+  const int32_t t = s.tokens[i];
+  return t >= 0 && t < s.vocab ? (uint32_t)t : (uint32_t)s.vocab;
+}
+
+__device__ __forceinline__ void sort_source(const SortArgs& s, int pass, int i, uint32_t* key, uint32_t* at) {
+  if (pass == 0) {
+    *key = token_key(s, i);
+    *at = (uint32_t)i;
+  } else {
+    *key = s.key[(pass - 1) & 1][i];
+    *at = s.at[(pass - 1) & 1][i];
+  }
+}
+
+// Counts of a wave's digits of rows [i0, i1) into cnt[256] (LDS, cleared before).
+__device__ __forceinline__ void count_unit(const SortArgs& s, int pass, int i0, int i1, uint32_t* cnt) {
+  for (int i = i0 + (int)(threadIdx.x & 63); i < i1; i += 64) {
+    uint32_t key, at;
+    sort_source(s, pass, i, &key, &at);
+    atomicAdd(&cnt[(key >> (8 * pass)) & 255u], 1u);   // whole numbers: any order
+  }
+}
+
+// Moves a wave's rows to where their digit's next place is (cnt: first places).
+__device__ __forceinline__ void move_unit(const SortArgs& s, int pass, int i0, int i1, uint32_t* cnt) {
+  const int lane = threadIdx.x & 63;
+  const uint64_t below = ((uint64_t)1 << lane) - 1;
+  for (int b = i0; b < i1; b += 64) {
+    const int i = b + lane;
+    uint32_t key = 0, at = 0;
+    if (i < i1) sort_source(s, pass, i, &key, &at);
+    const uint32_t digit = (key >> (8 * pass)) & 255u;
+    uint64_t same = __ballot(i < i1);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const uint64_t one = __ballot((digit >> k) & 1u);
+      same &= (digit >> k) & 1u ? one : ~one;
+    }
+    if (i < i1) {
+      const uint32_t to = cnt[digit] + (uint32_t)__popcll(same & below);
+      s.key[pass & 1][to] = key;
+      s.at[pass & 1][to] = at;
+    }
+    wave_lds_handoff();
+    if (i < i1 && (same & below) == 0) cnt[digit] += (uint32_t)__popcll(same);
+    wave_lds_handoff();
+  }
+}
+
+// Exclusive sums of v over the workgroup's threads (at most 16 waves).
+__device__ __forceinline__ uint32_t block_before(uint32_t v, uint32_t* s, uint32_t* total) {
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, nw = blockDim.x >> 6;
+  uint32_t x = v;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const uint32_t y = __shfl_up(x, o, 64);
+    if (lane >= o) x += y;
+  }
+  __syncthreads();
+  if (lane == 63) s[w] = x;
+  __syncthreads();
+  uint32_t before = 0, all = 0;
+  for (int i = 0; i < nw; ++i) {
+    if (i < w) before += s[i];
+    all += s[i];
+  }
+  *total = all;
+  return before + x - v;
+}
+
+__global__ __launch_bounds__(1024) void sort_alone_kernel(SortArgs s) {
+  __shared__ uint32_t cnt[16][256];
+  __shared__ uint32_t sums[16];
+  const int tid = threadIdx.x, w = tid >> 6;
+  const int seg = ((s.rows + 1023) / 1024) * 64;
+  const int i0 = w * seg < s.rows ? w * seg : s.rows;
+  const int i1 = i0 + seg < s.rows ? i0 + seg : s.rows;
+  for (int pass = 0; pass < s.passes; ++pass) {
+    for (int i = tid; i < 16 * 256; i += 1024) (&cnt[0][0])[i] = 0;
+    __syncthreads();
+    count_unit(s, pass, i0, i1, cnt[w]);
+    __syncthreads();
+    uint32_t n = 0, all;
+    if (tid < 256)
+      for (int k = 0; k < 16; ++k) n += cnt[k][tid];
+    uint32_t first = block_before(n, sums, &all);
+    if (tid < 256)
+      for (int k = 0; k < 16; ++k) {
+        const uint32_t c = cnt[k][tid];
+        cnt[k][tid] = first;
+        first += c;
+      }
+    __syncthreads();
+    move_unit(s, pass, i0, i1, cnt[w]);
+    __syncthreads();   // the pass's rows are written before the next one reads them
+  }
+}
+
+__global__ __launch_bounds__(NT) void sort_count_kernel(SortArgs s, int pass) {
+  __shared__ uint32_t cnt[4][256];
+  const int tid = threadIdx.x, w = tid >> 6, unit = blockIdx.x * 4 + w;
+  for (int i = tid; i < 4 * 256; i += NT) (&cnt[0][0])[i] = 0;
+  __syncthreads();
+  if (unit < s.units) {
+    const int i0 = unit * SORT_UNIT;
+    count_unit(s, pass, i0, i0 + SORT_UNIT < s.rows ? i0 + SORT_UNIT : s.rows, cnt[w]);
+  }
+  __syncthreads();
+  for (int i = tid; i < 4 * 256; i += NT) {
+    const int u = blockIdx.x * 4 + i / 256;
+    if (u < s.units) s.count[(int64_t)(i % 256) * s.units + u] = cnt[i / 256][i % 256];
+  }
+}
+
+// Counts [digit][unit] to first places.
+__global__ __launch_bounds__(1024) void sort_scan_kernel(SortArgs s) {
+  __shared__ uint32_t sums[16];
+  const int64_t n = 256 * (int64_t)s.units;
+  uint32_t carry = 0;
+  for (int64_t b = 0; b < n; b += 4096) {
+    const int64_t i = b + threadIdx.x * 4;   // (n is a multiple of 256)
+    uint4 c = make_uint4(0, 0, 0, 0);
+    if (i < n) c = *reinterpret_cast<const uint4*>(s.count + i);
+    uint32_t all;
+    uint32_t first = carry + block_before(c.x + c.y + c.z + c.w, sums, &all);
+    if (i < n)
+      *reinterpret_cast<uint4*>(s.count + i) =
+          make_uint4(first, first + c.x, first + c.x + c.y, first + c.x + c.y + c.z);
+    carry += all;
+  }
+}
+
+__global__ __launch_bounds__(NT) void sort_move_kernel(SortArgs s, int pass) {
+  __shared__ uint32_t cnt[4][256];
+  const int tid = threadIdx.x, w = tid >> 6, unit = blockIdx.x * 4 + w;
+  for (int i = tid; i < 4 * 256; i += NT) {
+    const int u = blockIdx.x * 4 + i / 256;
+    cnt[i / 256][i % 256] = u < s.units ? s.count[(int64_t)(i % 256) * s.units + u] : 0;
+  }
+  __syncthreads();
+  if (unit >= s.units) return;
+  const int i0 = unit * SORT_UNIT;
+  move_unit(s, pass, i0, i0 + SORT_UNIT < s.rows ? i0 + SORT_UNIT : s.rows, cnt[w]);
+}
+
+// ------------------------------------------------------------------ sums
+// First place whose key is at least `key`, by the wave together: 64 probes a step.
+__device__ __forceinline__ int first_at_least(const uint32_t* k, int n, uint32_t key) {
+  const int lane = threadIdx.x & 63;
+  int lo = 0, hi = n;                    // k[i] < key for i < lo, >= key for i >= hi
+  while (hi > lo) {
+    const int step = (hi - lo + 63) / 64;
+    const int i = lo + lane * step;
+    const uint64_t less = __ballot(i < hi && k[i < hi ? i : lo] < key);
+    const int c = __popcll(less);        // the first c probes are smaller
+    if (c == 0) return lo;
+    const int from = lo + (c - 1) * step + 1, to = lo + c * step;
+    lo = from;
+    hi = to < hi ? to : hi;
+  }
+  return lo;
+}
+
+__device__ __forceinline__ void add_rows(const EmbedArgs& a, int i0, int i1, int col, float* sum) {
+#pragma unroll 4
+  for (int i = i0; i < i1; ++i) {
+    float v[8];
+    widen8(load_raw8(a.grad_rows, a.row_type, (int64_t)a.at[i] * a.ldr + col), a.row_type, v);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) sum[k] += v[k];
+  }
+}
+
+__device__ __forceinline__ void add_pieces(const float* piece, int width, int i0, int i1, int col, float* sum) {
+#pragma unroll 4
+  for (int i = i0; i < i1; ++i) {
+    const float4* p = reinterpret_cast<const float4*>(piece + (int64_t)i * width + col);
+    const float4 x = p[0], y = p[1];
+    sum[0] += x.x; sum[1] += x.y; sum[2] += x.z; sum[3] += x.w;
+    sum[4] += y.x; sum[5] += y.y; sum[6] += y.z; sum[7] += y.w;
+  }
+}
+
+// Sums of the aligned pieces of N places that lie inside one run (N = 32: of rows; 1024: of pieces of 32).
+template <int N>
+__global__ __launch_bounds__(NT) void embed_pieces_kernel(EmbedArgs a) {
+  const int p = blockIdx.x;
+  const int col = blockIdx.y * SLAB + threadIdx.x * 8;
+  const uint32_t key = a.key[p * N];
+  if (key >= (uint32_t)a.vocab || a.key[p * N + N - 1] != key || col >= a.width) return;
+  float sum[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+  if constexpr (N == 32) add_rows(a, p * N, p * N + N, col, sum);
+  else add_pieces(a.sum32, a.width, p * 32, p * 32 + 32, col, sum);
+  store8((N == 32 ? a.sum32 : a.sum1024) + (int64_t)p * a.width, SVL_TYPE_F32, col, sum);
+}
+
+// One table row a workgroup (BY_PLACE: a place of the order that begins a run).
+template <bool BY_PLACE>
+__global__ __launch_bounds__(NT) void embed_sum_kernel(EmbedArgs a) {
+  const int64_t b = blockIdx.x;
+  const int col = blockIdx.y * SLAB + threadIdx.x * 8;
+  int lo, hi;
+  uint32_t key;
+  if constexpr (BY_PLACE) {
+    lo = (int)b;
+    key = a.key[lo];
+    if (key >= (uint32_t)a.vocab || (lo > 0 && a.key[lo - 1] == key)) return;
+    hi = lo + first_at_least(a.key + lo, a.rows - lo, key + 1);
+  } else {
+    key = (uint32_t)b;
+    lo = first_at_least(a.key, a.rows, key);
+    hi = lo < a.rows && a.key[lo] == key ? lo + first_at_least(a.key + lo, a.rows - lo, key + 1) : lo;
+  }
+  if (col >= a.width) return;
+  float sum[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+  const int p0 = (lo + 31) / 32, p1 = hi / 32;           // whole pieces of 32
+  if (!a.sum32 || p0 >= p1) {
+    add_rows(a, lo, hi, col, sum);
+  } else {
+    add_rows(a, lo, p0 * 32, col, sum);
+    const int q0 = (p0 + 31) / 32, q1 = p1 / 32;         // whole pieces of 1024
+    if (!a.sum1024 || q0 >= q1) {
+      add_pieces(a.sum32, a.width, p0, p1, col, sum);
+    } else {
+      add_pieces(a.sum32, a.width, p0, q0 * 32, col, sum);
+      add_pieces(a.sum1024, a.width, q0, q1, col, sum);
+      add_pieces(a.sum32, a.width, q1 * 32, p1, col, sum);
+    }
+    add_rows(a, p1 * 32, hi, col, sum);
+  }
+  const int64_t to = (int64_t)key * a.ldt + col;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) sum[i] *= a.scale;
+  if (BY_PLACE) {
+    float old[8];
+    widen8(load_raw8(a.out, a.table_type, to), a.table_type, old);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) sum[i] += old[i];
+  }
+  store8(a.out, a.table_type, to, sum);
+}
+
+}  // namespace
+
+// A column slab is a grid's second dimension: the first times 256 stays under 2^32.
+hipError_t launch_embed(const EmbedArgs& a, hipStream_t st) {
+  embed_kernel<<<dim3(a.rows, (a.width + SLAB - 1) / SLAB), NT, 0, st>>>(a);
+  return hipGetLastError();
+}
+
+hipError_t launch_sort_tokens(const SortArgs& s, hipStream_t st) {
+  if (s.rows <= SORT_ALONE) {
+    sort_alone_kernel<<<1, 1024, 0, st>>>(s);
+    return hipGetLastError();
+  }
+  const int blocks = (s.units + 3) / 4;
+  for (int pass = 0; pass < s.passes; ++pass) {
+    sort_count_kernel<<<blocks, NT, 0, st>>>(s, pass);
+    sort_scan_kernel<<<1, 1024, 0, st>>>(s);
+    sort_move_kernel<<<blocks, NT, 0, st>>>(s, pass);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
+hipError_t launch_embed_backward(const EmbedArgs& a, hipStream_t st) {
+  const uint32_t slabs = (a.width + SLAB - 1) / SLAB;
+  if (a.sum32) embed_pieces_kernel<32><<<dim3(a.rows / 32, slabs), NT, 0, st>>>(a);
+  if (a.sum1024) embed_pieces_kernel<1024><<<dim3(a.rows / 1024, slabs), NT, 0, st>>>(a);
+  if (a.accumulate) embed_sum_kernel<true><<<dim3(a.rows, slabs), NT, 0, st>>>(a);
+  else embed_sum_kernel<false><<<dim3(a.vocab, slabs), NT, 0, st>>>(a);
+  return hipGetLastError();
+}
+
+}  // namespace svl

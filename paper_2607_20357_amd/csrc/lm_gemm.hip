@@ -1,0 +1,342 @@
+// The three matrix products of the language-model loss:
+//   logits  s = x w^T, whose tiles leave as exponentials and their slabs' maxima and sums
+//   grad_x  P w        grad_w  P^T x
+//
+// C[n][m] = sum_k A[m][k] B[n][k] in tiles of 256 x 256, 64 of the sum at a time.  Each
+// operand comes as its memory has it: rows along k (fragments by 16-byte LDS
+// reads), or rows along m or n (transposed LDS reads), so neither w, x nor P is
+// ever laid out a second time.  Both go from memory to LDS without passing
+// registers; the places of a tile's 16-byte pieces are exchanged on the way (the
+// lane asks for another piece, since its place in LDS is fixed), so that both
+// kinds of fragment read are free of bank conflicts.
+#include "device_util.h"
+#include "lm_loss.h"
+#include "svl_internal.h"
+#include "window_attn.h"
+
+namespace svl {
+namespace {
+
+constexpr int NT = 512;              // 8 waves: 2 along m of 128, 4 along n of 64
+constexpr int TILE_ELEMS = LM_TILE * LM_BK;
+
+typedef __attribute__((address_space(3))) void lds_void;
+
+__device__ __forceinline__ int wave_id() { return __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6); }
+
+// One operand's tiles.  TR: rows along the sum.
+template <bool TR>
+struct Operand {
+  const uint16_t* p;      // of the tile's first row (TR: first column), first k
+  int64_t ld;
+  int32_t k;              // length of the sum, where rows along it end (TR)
+  uint32_t voff[4];
+
+  __device__ __forceinline__ void init(const uint16_t* base, int64_t ld_, int32_t first, int32_t count,
+                                       int32_t k0, int32_t k_) {
+    const int w = wave_id(), lane = threadIdx.x & 63;
+    ld = ld_;
+    k = k_;
+    if constexpr (TR) {
+      p = base + (int64_t)k0 * ld + first;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int r = (i * 8 + w) * 2 + (lane >> 5), at = lane & 31;
+        const int f = (r & 3) | (((r >> 3) & 3) << 2);
+        int piece = (((at >> 1) ^ f) << 1) | (at & 1);
+        const int most = (count - first) / 8 - 1;     // (widths are multiples of 8)
+        piece = piece < most ? piece : most;
+        voff[i] = (uint32_t)r * ((uint32_t)ld * 2) + piece * 16;
+      }
+    } else {
+      p = base + (int64_t)first * ld + k0;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        int r = (i * 8 + w) * 8 + (lane >> 3);
+        const int piece = (lane & 7) ^ (((r >> 2) & 3) << 1);
+        r = r < count - first ? r : count - first - 1;
+        voff[i] = (uint32_t)r * ((uint32_t)ld * 2) + piece * 16;
+      }
+    }
+  }
+
+  // Tile kt of the sum (from k0 on; `left` of the sum from there) on its way to LDS.
+  __device__ __forceinline__ void fetch(int kt, int left, uint16_t* lds) const {
+    const int w = wave_id();
+    const uint16_t* q = TR ? p + (int64_t)kt * LM_BK * ld : p + kt * LM_BK;
+    const __amdgpu_buffer_rsrc_t rs = make_rsrc(q, 0x7fffffffu);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      uint32_t v = voff[i];
+      if (TR && left < LM_BK) {       // the last rows of the sum: P is 0 behind them
+        const int over = (i * 8 + w) * 2 + (int)((threadIdx.x & 63) >> 5) - (left - 1);
+        v -= over > 0 ? (uint32_t)over * ((uint32_t)ld * 2) : 0u;
+      }
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_void*)(lds + (i * 8 + w) * 512), 16, v, 0, 0, 0);
+    }
+  }
+};
+
+// Fragments of 16 rows (or columns) of a tile, from `first` on, 32 of the sum from 32 kk on.
+template <bool TR>
+struct Fragments {
+  uint32_t at;          // in elements
+  __device__ __forceinline__ void init(int first) {
+    const int lane = threadIdx.x & 63, g = lane >> 4, l = lane & 15;
+    if constexpr (TR) at = (uint32_t)((8 * g + l / 4) * LM_TILE + (((first / 16) ^ (l / 4 | g << 2)) * 16) + (l & 3) * 4);
+    else at = (uint32_t)((first + l) * LM_BK + ((g ^ ((l >> 2) << 1)) * 8));
+  }
+  __device__ __forceinline__ u32x4 read(const uint16_t* lds, int block, int kk) const {
+    if constexpr (TR) {
+      const uint16_t* q = lds + (at ^ (block * 16)) + kk * 32 * LM_TILE;
+      const uint2 a = lds_read_tr(q), b = lds_read_tr(q + 4 * LM_TILE);
+      return u32x4{a.x, a.y, b.x, b.y};
+    } else {
+      return *reinterpret_cast<const u32x4*>(lds + (at ^ (kk * 32)) + block * 16 * LM_BK);
+    }
+  }
+};
+
+template <bool F16>
+__device__ __forceinline__ floatx4 mfma(const u32x4& a, const u32x4& b, const floatx4& c) {
+  return mfma16x16x32<F16>(__builtin_bit_cast(uint4, a), __builtin_bit_cast(uint4, b), c);
+}
+
+struct Tile {
+  int m, n, piece, pieces, tiles, id;
+};
+
+// Workgroup -> tile: consecutive workgroups of an XCD take blocks of 8 x 4 tiles.
+__device__ __forceinline__ bool tile_of(int mt, int nt, int nk, bool cut, Tile* t) {
+  t->tiles = mt * nt;
+  t->pieces = cut ? lm_pieces(t->tiles, nk) : 1;
+  const int total = t->tiles * t->pieces, per = (total + 7) / 8;
+  const int i = (int)(blockIdx.x & 7) * per + (int)(blockIdx.x >> 3);
+  if ((int)(blockIdx.x >> 3) >= per || i >= total) return false;
+  t->piece = i / t->tiles;
+  t->id = i;
+  const int j = i % t->tiles, group = j / (8 * nt), in = j % (8 * nt);
+  const int gm = mt - group * 8 < 8 ? mt - group * 8 : 8;
+  t->m = group * 8 + in % gm;
+  t->n = in / gm;
+  return true;
+}
+
+// Sizes of a product: m, n, k, and k's steps.
+struct Sizes {
+  int m, n, k, nk;
+};
+__device__ __forceinline__ Sizes sizes_of(const LmArgs& a, LmProduct p) {
+  int rows = a.head->rows - a.chunk0;
+  rows = rows < 0 ? 0 : rows < a.chunk ? rows : a.chunk;
+  Sizes s;
+  s.m = p == LM_LOGITS ? a.vocab : a.d;
+  s.n = p == LM_GRAD_W ? a.vocab : rows;
+  s.k = p == LM_LOGITS ? a.d : p == LM_GRAD_X ? a.vocab : rows;
+  s.nk = (s.k + LM_BK - 1) / LM_BK;
+  return s;
+}
+
+// What an element of a gradient becomes, four along d: grad_x or grad_w.
+template <bool F16>
+__device__ __forceinline__ void store_grad(const LmArgs& a, LmProduct p, int n, int m, floatx4 v) {
+  const float scale = a.head->weight * (F16 ? 1.f / LM_E_SCALE : 1.f);
+  if (p == LM_GRAD_X) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] *= scale;
+    const int64_t row = a.row_of[a.chunk0 + n];
+    *reinterpret_cast<uint2*>(a.grad_x + row * a.ldgx + m) =
+        make_uint2(pack_act2<F16>(v[0], v[1]), pack_act2<F16>(v[2], v[3]));
+    return;
+  }
+  float4* sum = a.sum_w ? reinterpret_cast<float4*>(a.sum_w + (int64_t)n * a.d + m) : nullptr;
+  if (sum && !a.first) {
+    const float4 s = *sum;
+    v[0] += s.x; v[1] += s.y; v[2] += s.z; v[3] += s.w;
+  }
+  if (!a.last) {
+    *sum = make_float4(v[0], v[1], v[2], v[3]);
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v[i] *= scale;
+  uint2* out = reinterpret_cast<uint2*>(a.grad_w + (int64_t)n * a.ldgw + m);
+  if (a.accumulate) {
+    const uint2 o = *out;
+    v[0] += act_bits_to_f32<F16>(o.x & 0xffffu);
+    v[1] += act_bits_to_f32<F16>(o.x >> 16);
+    v[2] += act_bits_to_f32<F16>(o.y & 0xffffu);
+    v[3] += act_bits_to_f32<F16>(o.y >> 16);
+  }
+  *out = make_uint2(pack_act2<F16>(v[0], v[1]), pack_act2<F16>(v[2], v[3]));
+}
+
+// Logits of 128 entries of the vocabulary (a wave's) become exponentials under their
+// row's largest; a lane holds 32 of the row's, three others the rest.
+template <bool F16>
+__device__ __forceinline__ void store_logits(const LmArgs& a, int m0, int n, bool there, floatx4 (&acc)[8]) {
+  const int g = (threadIdx.x & 63) >> 4;
+  float top = -INFINITY;
+  if (m0 + LM_SLAB > a.vocab) {
+#pragma unroll
+    for (int b = 0; b < 8; ++b)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (m0 + b * 16 + g * 4 + i >= a.vocab) acc[b][i] = -INFINITY;
+  }
+#pragma unroll
+  for (int b = 0; b < 8; ++b)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) top = fmaxf(top, acc[b][i]);
+  top = fmaxf(top, __shfl_xor(top, 16, 64));
+  top = fmaxf(top, __shfl_xor(top, 32, 64));
+  const int label = there ? a.label[a.chunk0 + n] - m0 : -1;
+  float sum = 0.f, mine = 0.f;
+  const bool none = top == -INFINITY;    // nothing of the vocabulary here, or no probability
+#pragma unroll
+  for (int b = 0; b < 8; ++b)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if (b * 16 + g * 4 + i == label) mine = acc[b][i];
+      acc[b][i] = none && !(acc[b][i] != acc[b][i]) ? 0.f : exp2_raw((acc[b][i] - top) * 1.44269504088896340736f);
+      sum += acc[b][i];
+    }
+  sum += __shfl_xor(sum, 16, 64);
+  sum += __shfl_xor(sum, 32, 64);
+  if (!there) return;
+  if (label >= 0 && label < LM_SLAB && (label >> 2 & 3) == g) a.label_logit[n] = mine;
+  if (g == 0) a.stats[(int64_t)n * (a.vp / LM_SLAB) + m0 / LM_SLAB] = make_float2(top, sum);
+  if (!a.e) return;
+#pragma unroll
+  for (int b = 0; b < 8; ++b)
+    *reinterpret_cast<uint2*>(a.e + (int64_t)n * a.vp + m0 + b * 16 + g * 4) =
+        make_uint2(pack_act2<true>(acc[b][0] * LM_E_SCALE, acc[b][1] * LM_E_SCALE),
+                   pack_act2<true>(acc[b][2] * LM_E_SCALE, acc[b][3] * LM_E_SCALE));
+}
+
+template <LmProduct P, bool F16>
+__global__ __launch_bounds__(NT) void lm_product_kernel(LmArgs a) {
+  constexpr bool TA = P != LM_LOGITS, TB = P == LM_GRAD_W;
+  // (two objects: reads of one do not wait for what is on its way to the other)
+  __shared__ __attribute__((aligned(16))) uint16_t lds0[2 * TILE_ELEMS];
+  __shared__ __attribute__((aligned(16))) uint16_t lds1[2 * TILE_ELEMS];
+  const Sizes s = sizes_of(a, P);
+  Tile t;
+  if (!tile_of((s.m + LM_TILE - 1) / LM_TILE, (s.n + LM_TILE - 1) / LM_TILE, s.nk, P != LM_LOGITS, &t)) return;
+  const int m0 = t.m * LM_TILE, n0 = t.n * LM_TILE;
+  const int kt0 = (int)((int64_t)s.nk * t.piece / t.pieces), kt1 = (int)((int64_t)s.nk * (t.piece + 1) / t.pieces);
+
+  const uint16_t* xc = a.xc + (int64_t)a.chunk0 * a.d;
+  Operand<TA> A;
+  Operand<TB> B;
+  if constexpr (P == LM_LOGITS) {
+    A.init(a.w, a.ldw, m0, a.vocab, 0, a.d);
+    B.init(xc, a.d, n0, s.n, 0, a.d);
+  } else if constexpr (P == LM_GRAD_X) {
+    A.init(a.w, a.ldw, m0, a.d, 0, a.vocab);
+    B.init(a.e, a.vp, n0, s.n, 0, a.vp);
+  } else {
+    A.init(xc, a.d, m0, a.d, 0, s.nk * LM_BK);
+    B.init(a.e, a.vp, n0, a.vp, 0, s.nk * LM_BK);
+  }
+  const int w = wave_id(), wm = w & 1, wn = w >> 1;
+  Fragments<TA> fa;
+  Fragments<TB> fb;
+  fa.init(wm * 128);
+  fb.init(wn * 64);
+
+  floatx4 acc[4][8];
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) acc[i][j] = floatx4{0.f, 0.f, 0.f, 0.f};
+
+  const auto fetch = [&](int kt, uint16_t* lds) {
+    A.fetch(kt, A.k - kt * LM_BK, lds);
+    B.fetch(kt, B.k - kt * LM_BK, lds + TILE_ELEMS);
+  };
+  const auto multiply = [&](const uint16_t* lds) {
+#pragma unroll
+    for (int kk = 0; kk < 2; ++kk) {
+      u32x4 af[8], bf[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) bf[i] = fb.read(lds + TILE_ELEMS, i, kk);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) af[j] = fa.read(lds, j, kk);
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc[i][j] = mfma<F16>(af[j], bf[i], acc[i][j]);
+    }
+  };
+  if (kt0 < kt1) fetch(kt0, lds0);
+  for (int kt = kt0; kt < kt1; kt += 2) {
+    __syncthreads();                       // tile kt is there, and lds1 is free
+    if (kt + 1 < kt1) fetch(kt + 1, lds1);
+    multiply(lds0);
+    if (kt + 1 >= kt1) break;
+    __syncthreads();
+    if (kt + 2 < kt1) fetch(kt + 2, lds0);
+    multiply(lds1);
+  }
+
+  const int lane = threadIdx.x & 63, g = lane >> 4, l = lane & 15;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int n = n0 + wn * 64 + i * 16 + l, m = m0 + wm * 128;
+    if constexpr (P == LM_LOGITS) {
+      store_logits<F16>(a, m, n, n < s.n, acc[i]);
+    } else if (t.pieces > 1) {
+      float* part = a.parts + (int64_t)t.id * LM_TILE * LM_TILE + (int64_t)(n - n0) * LM_TILE + wm * 128 + g * 4;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) *reinterpret_cast<floatx4*>(part + j * 16) = acc[i][j];
+    } else if (n < s.n) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if (m + j * 16 < s.m) store_grad<F16>(a, P, n, m + j * 16 + g * 4, acc[i][j]);
+    }
+  }
+}
+
+// Joins the pieces of a cut product: 4 of a tile's rows a workgroup, 64 lanes a row.
+template <LmProduct P, bool F16>
+__global__ __launch_bounds__(256) void lm_join_kernel(LmArgs a) {
+  const Sizes s = sizes_of(a, P);
+  const int mt = (s.m + LM_TILE - 1) / LM_TILE, nt = (s.n + LM_TILE - 1) / LM_TILE, tiles = mt * nt;
+  const int pieces = lm_pieces(tiles, s.nk), j = blockIdx.x / 64;
+  if (pieces <= 1 || j >= tiles) return;
+  const int group = j / (8 * nt), in = j % (8 * nt), gm = mt - group * 8 < 8 ? mt - group * 8 : 8;
+  const int r = (blockIdx.x % 64) * 4 + (threadIdx.x >> 6), c = (threadIdx.x & 63) * 4;
+  const int m = (group * 8 + in % gm) * LM_TILE + c, n = in / gm * LM_TILE + r;
+  if (n >= s.n || m >= s.m) return;
+  const float* p = a.parts + ((int64_t)j * LM_TILE + r) * LM_TILE + c;
+  floatx4 v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+  for (int i = 0; i < pieces; ++i) v += *reinterpret_cast<const floatx4*>(p + (int64_t)i * tiles * LM_TILE * LM_TILE);
+  store_grad<F16>(a, P, n, m, v);
+}
+
+template <LmProduct P, bool F16>
+hipError_t launch(const LmArgs& a, hipStream_t st) {
+  // the most tiles that the rows with a label can need; workgroups without one end at once
+  const int64_t m = P == LM_LOGITS ? a.vocab : a.d, n = P == LM_GRAD_W ? a.vocab : a.chunk;
+  const int64_t tiles = ((m + LM_TILE - 1) / LM_TILE) * ((n + LM_TILE - 1) / LM_TILE);
+  const int64_t grid = P == LM_LOGITS || tiles > LM_PARTS ? tiles : (int64_t)LM_PARTS;
+  lm_product_kernel<P, F16><<<(uint32_t)((grid + 7) / 8 * 8), NT, 0, st>>>(a);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || P == LM_LOGITS) return e;
+  if (P == LM_GRAD_W && tiles > LM_PARTS / 2) return hipSuccess;      // never cut
+  const int64_t cut = tiles < LM_PARTS / 2 ? tiles : LM_PARTS / 2;   // tiles that may be
+  lm_join_kernel<P, F16><<<(uint32_t)(cut * 64), 256, 0, st>>>(a);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_lm_product(const LmArgs& a, LmProduct p, bool f16, hipStream_t st) {
+  if (p == LM_LOGITS) return f16 ? launch<LM_LOGITS, true>(a, st) : launch<LM_LOGITS, false>(a, st);
+  if (p == LM_GRAD_X) return f16 ? launch<LM_GRAD_X, true>(a, st) : launch<LM_GRAD_X, false>(a, st);
+  return f16 ? launch<LM_GRAD_W, true>(a, st) : launch<LM_GRAD_W, false>(a, st);
+}
+
+}  // namespace svl
