@@ -24,8 +24,8 @@ typedef __attribute__((address_space(3))) void lds_void;
 
 __device__ __forceinline__ int wave_id() { return __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6); }
 
-// One operand's tiles.  TR: rows along the sum.
-template <bool TR>
+// One operand's tiles.  TR: rows along the sum; ENDS: they end inside a tile.
+template <bool TR, bool ENDS>
 struct Operand {
   const uint16_t* p;      // of the tile's first row (TR: first column), first k
   int64_t ld;
@@ -60,20 +60,23 @@ struct Operand {
     }
   }
 
-  // Tile kt of the sum (from k0 on; `left` of the sum from there) on its way to LDS.
-  __device__ __forceinline__ void fetch(int kt, int left, uint16_t* lds) const {
+  // Tile kt of the sum on its way to LDS, tiles in ascending order.  Rows behind the last of
+  // the sum are taken to be the last: P is 0 there.
+  __device__ __forceinline__ void fetch(int kt, uint16_t* lds) {
     const int w = wave_id();
     const uint16_t* q = TR ? p + (int64_t)kt * LM_BK * ld : p + kt * LM_BK;
     const __amdgpu_buffer_rsrc_t rs = make_rsrc(q, 0x7fffffffu);
+    const int left = k - kt * LM_BK;
+    if (ENDS && left < LM_BK) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      uint32_t v = voff[i];
-      if (TR && left < LM_BK) {       // the last rows of the sum: P is 0 behind them
+      for (int i = 0; i < 4; ++i) {
         const int over = (i * 8 + w) * 2 + (int)((threadIdx.x & 63) >> 5) - (left - 1);
-        v -= over > 0 ? (uint32_t)over * ((uint32_t)ld * 2) : 0u;
+        voff[i] -= over > 0 ? (uint32_t)over * ((uint32_t)ld * 2) : 0u;
       }
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_void*)(lds + (i * 8 + w) * 512), 16, v, 0, 0, 0);
     }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_void*)(lds + (i * 8 + w) * 512), 16, voff[i], 0, 0, 0);
   }
 };
 
@@ -86,14 +89,25 @@ struct Fragments {
     if constexpr (TR) at = (uint32_t)((8 * g + l / 4) * LM_TILE + (((first / 16) ^ (l / 4 | g << 2)) * 16) + (l & 3) * 4);
     else at = (uint32_t)((first + l) * LM_BK + ((g ^ ((l >> 2) << 1)) * 8));
   }
-  __device__ __forceinline__ u32x4 read(const uint16_t* lds, int block, int kk) const {
+  // The lane's place in the tile at `lds`.  (Opaque: the compiler would otherwise keep every block's
+  // place of both buffers in registers, which the products need.)
+  __device__ __forceinline__ uint32_t place(const uint16_t* lds) const {
+    uint32_t p = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const uint16_t*)lds + 2 * at;
+    asm volatile("" : "+v"(p));
+    return p;
+  }
+  static __device__ __forceinline__ u32x4 read(uint32_t place, int block, int kk) {
     if constexpr (TR) {
-      const uint16_t* q = lds + (at ^ (block * 16)) + kk * 32 * LM_TILE;
-      const uint2 a = lds_read_tr(q), b = lds_read_tr(q + 4 * LM_TILE);
+      const uint32_t q = (place ^ (block * 32)) + kk * 64 * LM_TILE;
+      const uint2 a = read_tr(q), b = read_tr(q + 8 * LM_TILE);
       return u32x4{a.x, a.y, b.x, b.y};
     } else {
-      return *reinterpret_cast<const u32x4*>(lds + (at ^ (kk * 32)) + block * 16 * LM_BK);
+      return *(__attribute__((address_space(3))) const u32x4*)(uintptr_t)((place ^ (kk * 64)) + block * 32 * LM_BK);
     }
+  }
+  static __device__ __forceinline__ uint2 read_tr(uint32_t at) {
+    return __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+        (__attribute__((address_space(3))) shortx4*)(uintptr_t)at));
   }
 };
 
@@ -227,8 +241,8 @@ __global__ __launch_bounds__(NT) void lm_product_kernel(LmArgs a) {
   const int kt0 = (int)((int64_t)s.nk * t.piece / t.pieces), kt1 = (int)((int64_t)s.nk * (t.piece + 1) / t.pieces);
 
   const uint16_t* xc = a.xc + (int64_t)a.chunk0 * a.d;
-  Operand<TA> A;
-  Operand<TB> B;
+  Operand<TA, P == LM_GRAD_X> A;
+  Operand<TB, false> B;
   if constexpr (P == LM_LOGITS) {
     A.init(a.w, a.ldw, m0, a.vocab, 0, a.d);
     B.init(xc, a.d, n0, s.n, 0, a.d);
@@ -252,32 +266,38 @@ __global__ __launch_bounds__(NT) void lm_product_kernel(LmArgs a) {
     for (int j = 0; j < 8; ++j) acc[i][j] = floatx4{0.f, 0.f, 0.f, 0.f};
 
   const auto fetch = [&](int kt, uint16_t* lds) {
-    A.fetch(kt, A.k - kt * LM_BK, lds);
-    B.fetch(kt, B.k - kt * LM_BK, lds + TILE_ELEMS);
+    A.fetch(kt, lds);
+    B.fetch(kt, lds + TILE_ELEMS);
   };
   const auto multiply = [&](const uint16_t* lds) {
+    const uint32_t pa = fa.place(lds), pb = fb.place(lds + TILE_ELEMS);
 #pragma unroll
     for (int kk = 0; kk < 2; ++kk) {
+      __builtin_amdgcn_sched_barrier(0);
       u32x4 af[8], bf[4];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) bf[i] = fb.read(lds + TILE_ELEMS, i, kk);
+      for (int i = 0; i < 4; ++i) bf[i] = fb.read(pb, i, kk);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) af[j] = fa.read(lds, j, kk);
+      for (int j = 0; j < 8; ++j) af[j] = fa.read(pa, j, kk);
 #pragma unroll
       for (int j = 0; j < 8; ++j)
 #pragma unroll
         for (int i = 0; i < 4; ++i) acc[i][j] = mfma<F16>(af[j], bf[i], acc[i][j]);
     }
   };
-  if (kt0 < kt1) fetch(kt0, lds0);
-  for (int kt = kt0; kt < kt1; kt += 2) {
+  int kt = kt0;
+  if (kt < kt1) fetch(kt, lds0);
+  for (; kt + 1 < kt1; kt += 2) {
     __syncthreads();                       // tile kt is there, and lds1 is free
-    if (kt + 1 < kt1) fetch(kt + 1, lds1);
+    fetch(kt + 1, lds1);
     multiply(lds0);
-    if (kt + 1 >= kt1) break;
     __syncthreads();
     if (kt + 2 < kt1) fetch(kt + 2, lds0);
     multiply(lds1);
+  }
+  if (kt < kt1) {
+    __syncthreads();
+    multiply(lds0);
   }
 
   const int lane = threadIdx.x & 63, g = lane >> 4, l = lane & 15;
