@@ -231,9 +231,7 @@ __device__ __forceinline__ void store_logits(const LmArgs& a, int m0, int n, boo
 template <LmProduct P, bool F16>
 __global__ __launch_bounds__(NT) void lm_product_kernel(LmArgs a) {
   constexpr bool TA = P != LM_LOGITS, TB = P == LM_GRAD_W;
-  // (two objects: reads of one do not wait for what is on its way to the other)
-  __shared__ __attribute__((aligned(16))) uint16_t lds0[2 * TILE_ELEMS];
-  __shared__ __attribute__((aligned(16))) uint16_t lds1[2 * TILE_ELEMS];
+  __shared__ __attribute__((aligned(1024))) uint16_t lds[4 * TILE_ELEMS];   // two buffers of A's and B's tiles
   const Sizes s = sizes_of(a, P);
   Tile t;
   if (!tile_of((s.m + LM_TILE - 1) / LM_TILE, (s.n + LM_TILE - 1) / LM_TILE, s.nk, P != LM_LOGITS, &t)) return;
@@ -265,15 +263,14 @@ __global__ __launch_bounds__(NT) void lm_product_kernel(LmArgs a) {
 #pragma unroll
     for (int j = 0; j < 8; ++j) acc[i][j] = floatx4{0.f, 0.f, 0.f, 0.f};
 
-  const auto fetch = [&](int kt, uint16_t* lds) {
-    A.fetch(kt, lds);
-    B.fetch(kt, lds + TILE_ELEMS);
+  const auto fetch = [&](int kt, uint16_t* to) {
+    A.fetch(kt, to);
+    B.fetch(kt, to + TILE_ELEMS);
   };
-  const auto multiply = [&](const uint16_t* lds) {
-    const uint32_t pa = fa.place(lds), pb = fb.place(lds + TILE_ELEMS);
+  const auto multiply = [&](const uint16_t* at) {
+    const uint32_t pa = fa.place(at), pb = fb.place(at + TILE_ELEMS);
 #pragma unroll
     for (int kk = 0; kk < 2; ++kk) {
-      __builtin_amdgcn_sched_barrier(0);
       u32x4 af[8], bf[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) bf[i] = fb.read(pb, i, kk);
@@ -285,19 +282,11 @@ __global__ __launch_bounds__(NT) void lm_product_kernel(LmArgs a) {
         for (int i = 0; i < 4; ++i) acc[i][j] = mfma<F16>(af[j], bf[i], acc[i][j]);
     }
   };
-  int kt = kt0;
-  if (kt < kt1) fetch(kt, lds0);
-  for (; kt + 1 < kt1; kt += 2) {
-    __syncthreads();                       // tile kt is there, and lds1 is free
-    fetch(kt + 1, lds1);
-    multiply(lds0);
-    __syncthreads();
-    if (kt + 2 < kt1) fetch(kt + 2, lds0);
-    multiply(lds1);
-  }
-  if (kt < kt1) {
-    __syncthreads();
-    multiply(lds0);
+  if (kt0 < kt1) fetch(kt0, lds);
+  for (int kt = kt0, at = 0; kt < kt1; ++kt, at ^= 2 * TILE_ELEMS) {
+    __syncthreads();                       // tile kt is there, and the other buffer is free
+    if (kt + 1 < kt1) fetch(kt + 1, lds + (at ^ 2 * TILE_ELEMS));
+    multiply(lds + at);
   }
 
   const int lane = threadIdx.x & 63, g = lane >> 4, l = lane & 15;
