@@ -20,7 +20,13 @@ namespace {
 constexpr int NT = 512;              // 8 waves: 2 along m of 128, 4 along n of 64
 constexpr int TILE_ELEMS = LM_TILE * LM_BK;
 
-typedef __attribute__((address_space(3))) void lds_void;
+// 16 bytes a lane from memory to LDS, from `to` on in lane order.  (The builtin would do, but
+// for the compiler every transposed LDS read after it may be of what it brings: it waits
+// for memory before each.  Here the waits are the turns' own, wait_loads().)
+__device__ __forceinline__ void load_to_lds(const u32x4& rsrc, uint32_t voff, uint32_t to) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
+               :: "s"(to), "v"(voff), "s"(rsrc) : "memory");   // (nothing else here uses m0)
+}
 
 __device__ __forceinline__ int wave_id() { return __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6); }
 
@@ -65,7 +71,11 @@ struct Operand {
   __device__ __forceinline__ void fetch(int kt, uint16_t* lds) {
     const int w = wave_id();
     const uint16_t* q = TR ? p + (int64_t)kt * LM_BK * ld : p + kt * LM_BK;
-    const __amdgpu_buffer_rsrc_t rs = make_rsrc(q, 0x7fffffffu);
+    const uint64_t a = reinterpret_cast<uint64_t>(q);
+    const u32x4 rs = {(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)a),
+                      (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(a >> 32)) & 0xffffu, 0x7fffffffu,
+                      0x00020000u};
+    const uint32_t first = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint16_t*)lds + w * 1024;
     const int left = k - kt * LM_BK;
     if (ENDS && left < LM_BK) {
 #pragma unroll
@@ -76,7 +86,7 @@ struct Operand {
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i)
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_void*)(lds + (i * 8 + w) * 512), 16, voff[i], 0, 0, 0);
+      load_to_lds(rs, voff[i], __builtin_amdgcn_readfirstlane((int)first) + i * 8192);
   }
 };
 
@@ -115,6 +125,17 @@ template <bool F16>
 __device__ __forceinline__ floatx4 mfma(const u32x4& a, const u32x4& b, const floatx4& c) {
   return mfma16x16x32<F16>(__builtin_bit_cast(uint4, a), __builtin_bit_cast(uint4, b), c);
 }
+
+// Ends a turn: nothing moves over it, and all waves have come here.
+__device__ __forceinline__ void turn() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_sched_barrier(0);
+  __builtin_amdgcn_s_barrier();
+  __builtin_amdgcn_sched_barrier(0);
+  asm volatile("" ::: "memory");
+}
+__device__ __forceinline__ void wait_lds() { __builtin_amdgcn_s_waitcnt(0xc07f); }     // lgkmcnt(0)
+__device__ __forceinline__ void wait_loads() { __builtin_amdgcn_s_waitcnt(0x0f70); }   // vmcnt(0)
 
 struct Tile {
   int m, n, piece, pieces, tiles, id;
@@ -267,27 +288,50 @@ __global__ __launch_bounds__(NT) void lm_product_kernel(LmArgs a) {
     A.fetch(kt, to);
     B.fetch(kt, to + TILE_ELEMS);
   };
-  const auto multiply = [&](const uint16_t* at) {
-    const uint32_t pa = fa.place(at), pb = fb.place(at + TILE_ELEMS);
+  // The two waves of a SIMD take turns: while one multiplies, the other reads its next
+  // fragments, and a barrier ends each turn.  The second group is a turn behind.
+  const int group = w >> 2;
+  u32x4 af[8], bf[4];
+  const auto read = [&](uint32_t pa, uint32_t pb, int kk) {
 #pragma unroll
-    for (int kk = 0; kk < 2; ++kk) {
-      u32x4 af[8], bf[4];
+    for (int i = 0; i < 4; ++i) bf[i] = fb.read(pb, i, kk);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) bf[i] = fb.read(pb, i, kk);
+    for (int j = 0; j < 8; ++j) af[j] = fa.read(pa, j, kk);
+  };
+  const auto multiply = [&] {
+    __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) af[j] = fa.read(pa, j, kk);
+    for (int j = 0; j < 8; ++j)
 #pragma unroll
-      for (int j = 0; j < 8; ++j)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) acc[i][j] = mfma<F16>(af[j], bf[i], acc[i][j]);
-    }
+      for (int i = 0; i < 4; ++i) acc[i][j] = mfma<F16>(af[j], bf[i], acc[i][j]);
+    __builtin_amdgcn_s_setprio(0);
   };
   if (kt0 < kt1) fetch(kt0, lds);
-  for (int kt = kt0, at = 0; kt < kt1; ++kt, at ^= 2 * TILE_ELEMS) {
-    __syncthreads();                       // tile kt is there, and the other buffer is free
-    if (kt + 1 < kt1) fetch(kt + 1, lds + (at ^ 2 * TILE_ELEMS));
-    multiply(lds + at);
+  wait_loads();
+  turn();
+  if (group == 1) {
+    if (kt0 + 1 < kt1) fetch(kt0 + 1, lds + 2 * TILE_ELEMS);
+    turn();
   }
+  for (int kt = kt0, at = 0; kt < kt1; ++kt, at ^= 2 * TILE_ELEMS) {
+    const uint32_t pa = fa.place(lds + at), pb = fb.place(lds + at + TILE_ELEMS);
+    // the other buffer is free: its last readers, group 1, were done a turn ago
+    if (group == 0 && kt + 1 < kt1) fetch(kt + 1, lds + (at ^ 2 * TILE_ELEMS));
+    read(pa, pb, 0);
+    wait_lds();
+    turn();
+    multiply();
+    turn();
+    read(pa, pb, 1);
+    wait_lds();
+    if (group == 1) wait_loads();          // its part of tile kt + 1, which group 0 reads next
+    turn();
+    if (group == 1 && kt + 2 < kt1) fetch(kt + 2, lds + at);   // all have read tile kt
+    multiply();
+    if (group == 0) wait_loads();
+    turn();
+  }
+  if (group == 0) turn();
 
   const int lane = threadIdx.x & 63, g = lane >> 4, l = lane & 15;
 #pragma unroll
