@@ -210,7 +210,7 @@ int64_t lm_layout(const svl_lm_head& h, int32_t rows, bool want_x, bool want_w, 
   a->row_of = l.take<int32_t>(rows);
   a->label = l.take<int32_t>(rows);
   a->weight = l.take<float>(rows);
-  a->xc = l.take<uint16_t>(cdiv(rows, LM_BK) * LM_BK * h.d_model);
+  a->xc = l.take<uint16_t>(cdiv(rows, LM_ROWS) * LM_ROWS * h.d_model);
   a->label_logit = l.take<float>(a->chunk);
   a->log_sum = l.take<float>(a->chunk);
   a->stats = l.take<float2>((int64_t)a->chunk * (a->vp / LM_SLAB));

@@ -2,13 +2,13 @@
 //   logits  s = x w^T, whose tiles leave as exponentials and their slabs' maxima and sums
 //   grad_x  P w        grad_w  P^T x
 //
-// C[n][m] = sum_k A[m][k] B[n][k] in tiles of 256 x 256, 64 of the sum at a time.  Each
+// C[n][m] = sum_k A[m][k] B[n][k] in tiles of 256 x 256, stages of 32 of the sum.  Each
 // operand comes as its memory has it: rows along k (fragments by 16-byte LDS
 // reads), or rows along m or n (transposed LDS reads), so neither w, x nor P is
 // ever laid out a second time.  Both go from memory to LDS without passing
-// registers; the places of a tile's 16-byte pieces are exchanged on the way (the
-// lane asks for another piece, since its place in LDS is fixed), so that both
-// kinds of fragment read are free of bank conflicts.
+// registers, three stages ahead; the places of a stage's 16-byte pieces are exchanged
+// on the way (the lane asks for another piece, since its place in LDS is fixed), so
+// that both kinds of fragment read are free of bank conflicts.
 #include "device_util.h"
 #include "lm_loss.h"
 #include "svl_internal.h"
@@ -18,7 +18,7 @@ namespace svl {
 namespace {
 
 constexpr int NT = 512;              // 8 waves: 2 along m of 128, 4 along n of 64
-constexpr int TILE_ELEMS = LM_TILE * LM_BK;
+constexpr int STAGE = LM_TILE * LM_BK;   // elements of an operand's stage
 
 // 16 bytes a lane from memory to LDS, from `to` on in lane order.  (The builtin would do, but
 // for the compiler every transposed LDS read after it may be of what it brings: it waits
@@ -30,89 +30,85 @@ __device__ __forceinline__ void load_to_lds(const u32x4& rsrc, uint32_t voff, ui
 
 __device__ __forceinline__ int wave_id() { return __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6); }
 
-// One operand's tiles.  TR: rows along the sum; ENDS: they end inside a tile.
+// One operand's stages.  TR: rows along the sum; ENDS: they end inside a stage.
 template <bool TR, bool ENDS>
 struct Operand {
   const uint16_t* p;      // of the tile's first row (TR: first column), first k
   int64_t ld;
   int32_t k;              // length of the sum, where rows along it end (TR)
-  uint32_t voff[4];
+  uint32_t voff[2];
 
-  __device__ __forceinline__ void init(const uint16_t* base, int64_t ld_, int32_t first, int32_t count,
-                                       int32_t k0, int32_t k_) {
+  __device__ __forceinline__ void init(const uint16_t* base, int64_t ld_, int32_t first, int32_t count, int32_t k_) {
     const int w = wave_id(), lane = threadIdx.x & 63;
     ld = ld_;
     k = k_;
-    if constexpr (TR) {
-      p = base + (int64_t)k0 * ld + first;
+    p = base + (TR ? (int64_t)first : (int64_t)first * ld);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < 2; ++i) {
+      if constexpr (TR) {
+        // two rows of 256 columns; pairs of pieces change places by the row
         const int r = (i * 8 + w) * 2 + (lane >> 5), at = lane & 31;
-        const int f = (r & 3) | (((r >> 3) & 3) << 2);
+        const int f = (r & 3) | ((r >> 3) << 2);
         int piece = (((at >> 1) ^ f) << 1) | (at & 1);
         const int most = (count - first) / 8 - 1;     // (widths are multiples of 8)
         piece = piece < most ? piece : most;
         voff[i] = (uint32_t)r * ((uint32_t)ld * 2) + piece * 16;
-      }
-    } else {
-      p = base + (int64_t)first * ld + k0;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        int r = (i * 8 + w) * 8 + (lane >> 3);
-        const int piece = (lane & 7) ^ (((r >> 2) & 3) << 1);
+      } else {
+        // 16 rows of 32: pieces change places by the row's quad
+        int r = (i * 8 + w) * 16 + (lane >> 2);
+        const int piece = (lane & 3) ^ (lane >> 4);
         r = r < count - first ? r : count - first - 1;
         voff[i] = (uint32_t)r * ((uint32_t)ld * 2) + piece * 16;
       }
     }
   }
 
-  // Tile kt of the sum on its way to LDS, tiles in ascending order.  Rows behind the last of
-  // the sum are taken to be the last: P is 0 there.
-  __device__ __forceinline__ void fetch(int kt, uint16_t* lds) {
+  // Stage s of the sum on its way to LDS, stages in ascending order.  Rows behind the last
+  // of the sum are taken to be the last: P is 0 there.
+  __device__ __forceinline__ void fetch(int s, uint16_t* lds) {
     const int w = wave_id();
-    const uint16_t* q = TR ? p + (int64_t)kt * LM_BK * ld : p + kt * LM_BK;
-    const uint64_t a = reinterpret_cast<uint64_t>(q);
+    const uint64_t a = reinterpret_cast<uint64_t>(TR ? p + (int64_t)s * LM_BK * ld : p + s * LM_BK);
     const u32x4 rs = {(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)a),
                       (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(a >> 32)) & 0xffffu, 0x7fffffffu,
                       0x00020000u};
     const uint32_t first = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint16_t*)lds + w * 1024;
-    const int left = k - kt * LM_BK;
+    const int left = k - s * LM_BK;
     if (ENDS && left < LM_BK) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
+      for (int i = 0; i < 2; ++i) {
         const int over = (i * 8 + w) * 2 + (int)((threadIdx.x & 63) >> 5) - (left - 1);
         voff[i] -= over > 0 ? (uint32_t)over * ((uint32_t)ld * 2) : 0u;
       }
     }
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+    for (int i = 0; i < 2; ++i)
       load_to_lds(rs, voff[i], __builtin_amdgcn_readfirstlane((int)first) + i * 8192);
   }
 };
 
-// Fragments of 16 rows (or columns) of a tile, from `first` on, 32 of the sum from 32 kk on.
+// Fragments of 16 rows (or columns) of a stage, from `first` on.
 template <bool TR>
 struct Fragments {
-  uint32_t at;          // in elements
+  uint32_t at;          // bytes
   __device__ __forceinline__ void init(int first) {
     const int lane = threadIdx.x & 63, g = lane >> 4, l = lane & 15;
-    if constexpr (TR) at = (uint32_t)((8 * g + l / 4) * LM_TILE + (((first / 16) ^ (l / 4 | g << 2)) * 16) + (l & 3) * 4);
-    else at = (uint32_t)((first + l) * LM_BK + ((g ^ ((l >> 2) << 1)) * 8));
+    if constexpr (TR) at = (uint32_t)((8 * g + l / 4) * LM_TILE * 2 + (((first / 16) ^ (l / 4 | g << 2)) * 32) + (l & 3) * 8);
+    else at = (uint32_t)((first + l) * LM_BK * 2 + ((g ^ (l >> 2)) * 16));
   }
-  // The lane's place in the tile at `lds`.  (Opaque: the compiler would otherwise keep every block's
-  // place of both buffers in registers, which the products need.)
+  // The lane's place in the stage at `lds`.  (Opaque: the compiler would otherwise keep every block's
+  // place of every buffer in registers, which the products need.)
   __device__ __forceinline__ uint32_t place(const uint16_t* lds) const {
-    uint32_t p = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const uint16_t*)lds + 2 * at;
+    uint32_t p = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const uint16_t*)lds + at;
     asm volatile("" : "+v"(p));
     return p;
   }
-  static __device__ __forceinline__ u32x4 read(uint32_t place, int block, int kk) {
+  static __device__ __forceinline__ u32x4 read(uint32_t place, int block) {
     if constexpr (TR) {
-      const uint32_t q = (place ^ (block * 32)) + kk * 64 * LM_TILE;
+      const uint32_t q = place ^ (block * 32);
       const uint2 a = read_tr(q), b = read_tr(q + 8 * LM_TILE);
       return u32x4{a.x, a.y, b.x, b.y};
     } else {
-      return *(__attribute__((address_space(3))) const u32x4*)(uintptr_t)((place ^ (kk * 64)) + block * 32 * LM_BK);
+      return *(__attribute__((address_space(3))) const u32x4*)(uintptr_t)(place + block * 32 * LM_BK);
     }
   }
   static __device__ __forceinline__ uint2 read_tr(uint32_t at) {
@@ -135,7 +131,9 @@ __device__ __forceinline__ void turn() {
   asm volatile("" ::: "memory");
 }
 __device__ __forceinline__ void wait_lds() { __builtin_amdgcn_s_waitcnt(0xc07f); }     // lgkmcnt(0)
-__device__ __forceinline__ void wait_loads() { __builtin_amdgcn_s_waitcnt(0x0f70); }   // vmcnt(0)
+// Until at most N of the wave's loads are on their way (vmcnt).
+template <int N>
+__device__ __forceinline__ void wait_loads() { __builtin_amdgcn_s_waitcnt(0x0f70 | N); }
 
 struct Tile {
   int m, n, piece, pieces, tiles, id;
@@ -252,7 +250,7 @@ __device__ __forceinline__ void store_logits(const LmArgs& a, int m0, int n, boo
 template <LmProduct P, bool F16>
 __global__ __launch_bounds__(NT) void lm_product_kernel(LmArgs a) {
   constexpr bool TA = P != LM_LOGITS, TB = P == LM_GRAD_W;
-  __shared__ __attribute__((aligned(1024))) uint16_t lds[4 * TILE_ELEMS];   // two buffers of A's and B's tiles
+  __shared__ __attribute__((aligned(1024))) uint16_t lds[4 * 2 * STAGE];   // four buffers of A's and B's stages
   const Sizes s = sizes_of(a, P);
   Tile t;
   if (!tile_of((s.m + LM_TILE - 1) / LM_TILE, (s.n + LM_TILE - 1) / LM_TILE, s.nk, P != LM_LOGITS, &t)) return;
@@ -263,14 +261,14 @@ __global__ __launch_bounds__(NT) void lm_product_kernel(LmArgs a) {
   Operand<TA, P == LM_GRAD_X> A;
   Operand<TB, false> B;
   if constexpr (P == LM_LOGITS) {
-    A.init(a.w, a.ldw, m0, a.vocab, 0, a.d);
-    B.init(xc, a.d, n0, s.n, 0, a.d);
+    A.init(a.w, a.ldw, m0, a.vocab, a.d);
+    B.init(xc, a.d, n0, s.n, a.d);
   } else if constexpr (P == LM_GRAD_X) {
-    A.init(a.w, a.ldw, m0, a.d, 0, a.vocab);
-    B.init(a.e, a.vp, n0, s.n, 0, a.vp);
+    A.init(a.w, a.ldw, m0, a.d, a.vocab);
+    B.init(a.e, a.vp, n0, s.n, a.vp);
   } else {
-    A.init(xc, a.d, m0, a.d, 0, s.nk * LM_BK);
-    B.init(a.e, a.vp, n0, a.vp, 0, s.nk * LM_BK);
+    A.init(xc, a.d, m0, a.d, s.nk * LM_BK);
+    B.init(a.e, a.vp, n0, a.vp, s.nk * LM_BK);
   }
   const int w = wave_id(), wm = w & 1, wn = w >> 1;
   Fragments<TA> fa;
@@ -284,51 +282,54 @@ __global__ __launch_bounds__(NT) void lm_product_kernel(LmArgs a) {
 #pragma unroll
     for (int j = 0; j < 8; ++j) acc[i][j] = floatx4{0.f, 0.f, 0.f, 0.f};
 
-  const auto fetch = [&](int kt, uint16_t* to) {
-    A.fetch(kt, to);
-    B.fetch(kt, to + TILE_ELEMS);
-  };
-  // The two waves of a SIMD take turns: while one multiplies, the other reads its next
-  // fragments, and a barrier ends each turn.  The second group is a turn behind.
+  // The two waves of a SIMD take turns: while one multiplies a stage, the other reads its
+  // fragments of one, and a barrier ends each turn.  The second group is a turn behind:
+  //   turn 2s     group 0 reads s         group 1 multiplies s - 1
+  //   turn 2s + 1 group 0 multiplies s    group 1 reads s
+  // Stage s's buffer is free from turn 2s + 2 on.  Each wave asks for half of its part of stage
+  // s + 3 (the buffer of s - 1) in either turn of its stage s, and before turn 2s + 2 all have
+  // waited for their part of stage s + 1: a load has five turns to come.
   const int group = w >> 2;
+  const auto buffer = [&](int i) { return lds + ((i - kt0) & 3) * 2 * STAGE; };
   u32x4 af[8], bf[4];
-  const auto read = [&](uint32_t pa, uint32_t pb, int kk) {
+#pragma unroll 1
+  for (int i = kt0; i < kt0 + 3; ++i)
+    if (i < kt1) {
+      A.fetch(i, buffer(i));
+      B.fetch(i, buffer(i) + STAGE);
+    }
+  if (kt0 + 2 < kt1) wait_loads<8>(); else wait_loads<0>();   // stage kt0
+  turn();
+  if (group == 1) turn();
+#pragma unroll 1
+  for (int i = kt0; i < kt1; ++i) {
+    const bool more = i + 3 < kt1;
+    const uint32_t pa = fa.place(buffer(i)), pb = fb.place(buffer(i) + STAGE);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) bf[i] = fb.read(pb, i, kk);
+    for (int j = 0; j < 4; ++j) bf[j] = fb.read(pb, j);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) af[j] = fa.read(pa, j, kk);
-  };
-  const auto multiply = [&] {
+    for (int j = 0; j < 8; ++j) af[j] = fa.read(pa, j);
+    if (more) A.fetch(i + 3, buffer(i + 3));
+    wait_lds();
+    if (group == 1) {
+      if (more) wait_loads<6>(); else wait_loads<0>();
+    }
+    turn();
     __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-    for (int j = 0; j < 8; ++j)
+    for (int j = 0; j < 8; ++j) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) acc[i][j] = mfma<F16>(af[j], bf[i], acc[i][j]);
+      for (int n = 0; n < 4; ++n) acc[n][j] = mfma<F16>(af[j], bf[n], acc[n][j]);
+      if (j == 1) {
+        __builtin_amdgcn_sched_barrier(0);
+        if (more) B.fetch(i + 3, buffer(i + 3) + STAGE);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
     __builtin_amdgcn_s_setprio(0);
-  };
-  if (kt0 < kt1) fetch(kt0, lds);
-  wait_loads();
-  turn();
-  if (group == 1) {
-    if (kt0 + 1 < kt1) fetch(kt0 + 1, lds + 2 * TILE_ELEMS);
-    turn();
-  }
-  for (int kt = kt0, at = 0; kt < kt1; ++kt, at ^= 2 * TILE_ELEMS) {
-    const uint32_t pa = fa.place(lds + at), pb = fb.place(lds + at + TILE_ELEMS);
-    // the other buffer is free: its last readers, group 1, were done a turn ago
-    if (group == 0 && kt + 1 < kt1) fetch(kt + 1, lds + (at ^ 2 * TILE_ELEMS));
-    read(pa, pb, 0);
-    wait_lds();
-    turn();
-    multiply();
-    turn();
-    read(pa, pb, 1);
-    wait_lds();
-    if (group == 1) wait_loads();          // its part of tile kt + 1, which group 0 reads next
-    turn();
-    if (group == 1 && kt + 2 < kt1) fetch(kt + 2, lds + at);   // all have read tile kt
-    multiply();
-    if (group == 0) wait_loads();
+    if (group == 0) {
+      if (more) wait_loads<8>(); else wait_loads<0>();
+    }
     turn();
   }
   if (group == 0) turn();

@@ -8,10 +8,11 @@
 namespace svl {
 
 constexpr int32_t LM_TILE = 256;     // rows and columns of a product's tile
-constexpr int32_t LM_BK = 64;        // of its sum at a time
+constexpr int32_t LM_BK = 32;        // of its sum at a time
+constexpr int32_t LM_ROWS = 64;      // labelled rows are filled up with zeros to a multiple
 constexpr int32_t LM_SLAB = 128;     // vocabulary entries whose exponentials share a maximum
 constexpr int32_t LM_PARTS = 256;    // most workgroups (tiles x pieces) of a product whose sum is cut
-constexpr int32_t LM_CUT = 8;        // least steps of LM_BK of a piece of a sum
+constexpr int32_t LM_CUT = 16;       // least steps of LM_BK of a piece of a sum
 // Exponentials are held as fp16 under 2^14 (normal down to 2^-28 of their slab's largest), P
 // in fp16 likewise (of the largest weight).
 constexpr float LM_E_SCALE = 16384.f;
@@ -44,7 +45,7 @@ struct LmArgs {
   int32_t* row_of;              // [rows] the row it is
   int32_t* label;               // [rows]
   float* weight;                // [rows]
-  uint16_t* xc;                 // [rows to a multiple of 64][d]
+  uint16_t* xc;                 // [rows to a multiple of LM_ROWS][d]
   float* label_logit;           // [chunk]
   float* log_sum;               // [chunk]
   float2* stats;                // [chunk][vp / LM_SLAB] (maximum, sum of exponentials)

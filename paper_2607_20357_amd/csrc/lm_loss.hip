@@ -61,7 +61,7 @@ __global__ __launch_bounds__(NT) void lm_pack_kernel(LmArgs a, int packed) {
   const uint4 zero = make_uint4(0, 0, 0, 0);
   if ((int)blockIdx.x < packed) {
     const int i = blockIdx.x, n = a.head->rows;
-    if (i >= (n + LM_BK - 1) / LM_BK * LM_BK) return;
+    if (i >= (n + LM_ROWS - 1) / LM_ROWS * LM_ROWS) return;
     const uint16_t* from = i < n ? a.x + (int64_t)a.row_of[i] * a.ldx : nullptr;
     for (int c = threadIdx.x * 8; c < a.d; c += NT * 8)
       *reinterpret_cast<uint4*>(a.xc + (int64_t)i * a.d + c) = from ? *reinterpret_cast<const uint4*>(from + c) : zero;
@@ -107,7 +107,7 @@ template <bool F16>
 __global__ __launch_bounds__(NT) void lm_softmax_kernel(LmArgs a) {
   const int i = blockIdx.x, n = a.head->rows - a.chunk0;
   const int col = blockIdx.y * (NT * 8) + threadIdx.x * 8;
-  if (i >= (n + LM_BK - 1) / LM_BK * LM_BK || col >= a.vp) return;
+  if (i >= (n + LM_ROWS - 1) / LM_ROWS * LM_ROWS || col >= a.vp) return;
   uint16_t* p = a.e + (int64_t)i * a.vp + col;
   if (i >= n) {
     *reinterpret_cast<uint4*>(p) = make_uint4(0, 0, 0, 0);
@@ -139,7 +139,7 @@ __global__ __launch_bounds__(NT) void lm_zero_w_kernel(uint16_t* w, int64_t ld, 
 
 hipError_t launch_lm_rows(const LmArgs& a, hipStream_t st) {
   lm_count_kernel<<<1, 1024, 0, st>>>(a);
-  const int packed = (a.rows + LM_BK - 1) / LM_BK * LM_BK;
+  const int packed = (a.rows + LM_ROWS - 1) / LM_ROWS * LM_ROWS;
   lm_pack_kernel<<<packed + a.rows, NT, 0, st>>>(a, packed);
   return hipGetLastError();
 }
@@ -150,7 +150,7 @@ hipError_t launch_lm_stats(const LmArgs& a, hipStream_t st) {
 }
 
 hipError_t launch_lm_softmax(const LmArgs& a, bool f16, hipStream_t st) {
-  const dim3 grid((a.chunk + LM_BK - 1) / LM_BK * LM_BK, (a.vp + NT * 8 - 1) / (NT * 8));
+  const dim3 grid((a.chunk + LM_ROWS - 1) / LM_ROWS * LM_ROWS, (a.vp + NT * 8 - 1) / (NT * 8));
   if (f16) lm_softmax_kernel<true><<<grid, NT, 0, st>>>(a);
   else lm_softmax_kernel<false><<<grid, NT, 0, st>>>(a);
   return hipGetLastError();
