@@ -56,7 +56,7 @@ struct Operand {
       } else {
         // 16 rows of 32: pieces change places by the row's quad
         int r = (i * 8 + w) * 16 + (lane >> 2);
-        const int piece = (lane & 3) ^ (lane >> 4);
+        const int piece = (lane & 3) ^ (-(lane >> 4) & 3);
         r = r < count - first ? r : count - first - 1;
         voff[i] = (uint32_t)r * ((uint32_t)ld * 2) + piece * 16;
       }
@@ -93,7 +93,7 @@ struct Fragments {
   __device__ __forceinline__ void init(int first) {
     const int lane = threadIdx.x & 63, g = lane >> 4, l = lane & 15;
     if constexpr (TR) at = (uint32_t)((8 * g + l / 4) * LM_TILE * 2 + (((first / 16) ^ (l / 4 | g << 2)) * 32) + (l & 3) * 8);
-    else at = (uint32_t)((first + l) * LM_BK * 2 + ((g ^ (l >> 2)) * 16));
+    else at = (uint32_t)((first + l) * LM_BK * 2 + ((g ^ (-(l >> 2) & 3)) * 16));
   }
   // The lane's place in the stage at `lds`.  (Opaque: the compiler would otherwise keep every block's
   // place of every buffer in registers, which the products need.)
