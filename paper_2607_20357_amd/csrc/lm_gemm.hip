@@ -48,7 +48,7 @@ struct Operand {
       if constexpr (TR) {
         // two rows of 256 columns; pairs of pieces change places by the row
         const int r = (i * 8 + w) * 2 + (lane >> 5), at = lane & 31;
-        const int f = (r & 3) | ((r >> 3) << 2);
+        const int f = 2 * (r & 3);
         int piece = (((at >> 1) ^ f) << 1) | (at & 1);
         const int most = (count - first) / 8 - 1;     // (widths are multiples of 8)
         piece = piece < most ? piece : most;
@@ -56,7 +56,7 @@ struct Operand {
       } else {
         // 16 rows of 32: pieces change places by the row's quad
         int r = (i * 8 + w) * 16 + (lane >> 2);
-        const int piece = (lane & 3) ^ (-(lane >> 4) & 3);
+        const int piece = (lane & 3) ^ (lane >> 4);
         r = r < count - first ? r : count - first - 1;
         voff[i] = (uint32_t)r * ((uint32_t)ld * 2) + piece * 16;
       }
@@ -86,14 +86,16 @@ struct Operand {
   }
 };
 
-// Fragments of 16 rows (or columns) of a stage, from `first` on.
+// Fragments of 32 rows (or columns) of a stage, from `first` on, 16 of the sum each.
 template <bool TR>
 struct Fragments {
   uint32_t at;          // bytes
   __device__ __forceinline__ void init(int first) {
-    const int lane = threadIdx.x & 63, g = lane >> 4, l = lane & 15;
-    if constexpr (TR) at = (uint32_t)((8 * g + l / 4) * LM_TILE * 2 + (((first / 16) ^ (l / 4 | g << 2)) * 32) + (l & 3) * 8);
-    else at = (uint32_t)((first + l) * LM_BK * 2 + ((g ^ (-(l >> 2) & 3)) * 16));
+    const int lane = threadIdx.x & 63, h = lane >> 5, l = lane & 15;
+    if constexpr (TR)
+      at = (uint32_t)((8 * h + l / 4) * LM_TILE * 2 + (((first / 16 + ((lane >> 4) & 1)) ^ (2 * (l / 4))) * 32) + (l & 3) * 8);
+    else
+      at = (uint32_t)((first + (lane & 31)) * LM_BK * 2 + ((h ^ ((lane >> 2) & 3)) * 16));
   }
   // The lane's place in the stage at `lds`.  (Opaque: the compiler would otherwise keep every block's
   // place of every buffer in registers, which the products need.)
@@ -102,13 +104,13 @@ struct Fragments {
     asm volatile("" : "+v"(p));
     return p;
   }
-  static __device__ __forceinline__ u32x4 read(uint32_t place, int block) {
+  static __device__ __forceinline__ u32x4 read(uint32_t place, int block, int kk) {
     if constexpr (TR) {
-      const uint32_t q = place ^ (block * 32);
+      const uint32_t q = (place ^ (block * 64)) + kk * 32 * LM_TILE;
       const uint2 a = read_tr(q), b = read_tr(q + 8 * LM_TILE);
       return u32x4{a.x, a.y, b.x, b.y};
     } else {
-      return *(__attribute__((address_space(3))) const u32x4*)(uintptr_t)(place + block * 32 * LM_BK);
+      return *(__attribute__((address_space(3))) const u32x4*)(uintptr_t)((place ^ (kk * 32)) + block * 64 * LM_BK);
     }
   }
   static __device__ __forceinline__ uint2 read_tr(uint32_t at) {
@@ -116,11 +118,6 @@ struct Fragments {
         (__attribute__((address_space(3))) shortx4*)(uintptr_t)at));
   }
 };
-
-template <bool F16>
-__device__ __forceinline__ floatx4 mfma(const u32x4& a, const u32x4& b, const floatx4& c) {
-  return mfma16x16x32<F16>(__builtin_bit_cast(uint4, a), __builtin_bit_cast(uint4, b), c);
-}
 
 // Ends a turn: nothing moves over it, and all waves have come here.
 __device__ __forceinline__ void turn() {
@@ -204,47 +201,52 @@ __device__ __forceinline__ void store_grad(const LmArgs& a, LmProduct p, int n, 
   *out = make_uint2(pack_act2<F16>(v[0], v[1]), pack_act2<F16>(v[2], v[3]));
 }
 
+// Element 4 q + i of a 32 x 32 block's lane is 8 q + 4 (lane / 32) + i along m.
+__device__ __forceinline__ floatx4 quad(const floatx16& v, int q) {
+  return floatx4{v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]};
+}
+
 // Logits of 128 entries of the vocabulary (a wave's) become exponentials under their
-// row's largest; a lane holds 32 of the row's, three others the rest.
+// row's largest; a lane holds 64 of the row's, another the rest.
 template <bool F16>
-__device__ __forceinline__ void store_logits(const LmArgs& a, int m0, int n, bool there, floatx4 (&acc)[8]) {
-  const int g = (threadIdx.x & 63) >> 4;
+__device__ __forceinline__ void store_logits(const LmArgs& a, int m0, int n, bool there, floatx16 (&acc)[4]) {
+  const int h = (threadIdx.x & 63) >> 5;
   float top = -INFINITY;
   if (m0 + LM_SLAB > a.vocab) {
 #pragma unroll
-    for (int b = 0; b < 8; ++b)
+    for (int b = 0; b < 4; ++b)
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (m0 + b * 16 + g * 4 + i >= a.vocab) acc[b][i] = -INFINITY;
+      for (int i = 0; i < 16; ++i)
+        if (m0 + b * 32 + 8 * (i / 4) + 4 * h + i % 4 >= a.vocab) acc[b][i] = -INFINITY;
   }
 #pragma unroll
-  for (int b = 0; b < 8; ++b)
+  for (int b = 0; b < 4; ++b)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) top = fmaxf(top, acc[b][i]);
-  top = fmaxf(top, __shfl_xor(top, 16, 64));
+    for (int i = 0; i < 16; ++i) top = fmaxf(top, acc[b][i]);
   top = fmaxf(top, __shfl_xor(top, 32, 64));
-  const int label = there ? a.label[a.chunk0 + n] - m0 : -1;
+  const int label = there ? a.label[a.chunk0 + n] - m0 - 4 * h : -1;
   float sum = 0.f, mine = 0.f;
   const bool none = top == -INFINITY;    // nothing of the vocabulary here, or no probability
 #pragma unroll
-  for (int b = 0; b < 8; ++b)
+  for (int b = 0; b < 4; ++b)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      if (b * 16 + g * 4 + i == label) mine = acc[b][i];
+    for (int i = 0; i < 16; ++i) {
+      if (b * 32 + 8 * (i / 4) + i % 4 == label) mine = acc[b][i];
       acc[b][i] = none && !(acc[b][i] != acc[b][i]) ? 0.f : exp2_raw((acc[b][i] - top) * 1.44269504088896340736f);
       sum += acc[b][i];
     }
-  sum += __shfl_xor(sum, 16, 64);
   sum += __shfl_xor(sum, 32, 64);
   if (!there) return;
-  if (label >= 0 && label < LM_SLAB && (label >> 2 & 3) == g) a.label_logit[n] = mine;
-  if (g == 0) a.stats[(int64_t)n * (a.vp / LM_SLAB) + m0 / LM_SLAB] = make_float2(top, sum);
+  if (label >= 0 && label < LM_SLAB && (label & 4) == 0) a.label_logit[n] = mine;
+  if (h == 0) a.stats[(int64_t)n * (a.vp / LM_SLAB) + m0 / LM_SLAB] = make_float2(top, sum);
   if (!a.e) return;
 #pragma unroll
-  for (int b = 0; b < 8; ++b)
-    *reinterpret_cast<uint2*>(a.e + (int64_t)n * a.vp + m0 + b * 16 + g * 4) =
-        make_uint2(pack_act2<true>(acc[b][0] * LM_E_SCALE, acc[b][1] * LM_E_SCALE),
-                   pack_act2<true>(acc[b][2] * LM_E_SCALE, acc[b][3] * LM_E_SCALE));
+  for (int b = 0; b < 4; ++b)
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      *reinterpret_cast<uint2*>(a.e + (int64_t)n * a.vp + m0 + b * 32 + 8 * q + 4 * h) =
+          make_uint2(pack_act2<true>(acc[b][4 * q] * LM_E_SCALE, acc[b][4 * q + 1] * LM_E_SCALE),
+                     pack_act2<true>(acc[b][4 * q + 2] * LM_E_SCALE, acc[b][4 * q + 3] * LM_E_SCALE));
 }
 
 template <LmProduct P, bool F16>
@@ -276,11 +278,11 @@ __global__ __launch_bounds__(NT) void lm_product_kernel(LmArgs a) {
   fa.init(wm * 128);
   fb.init(wn * 64);
 
-  floatx4 acc[4][8];
+  floatx16 acc[2][4];
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
+  for (int i = 0; i < 2; ++i)
 #pragma unroll
-    for (int j = 0; j < 8; ++j) acc[i][j] = floatx4{0.f, 0.f, 0.f, 0.f};
+    for (int j = 0; j < 4; ++j) acc[i][j] = floatx16{};
 
   // The two waves of a SIMD take turns: while one multiplies a stage, the other reads its
   // fragments of one, and a barrier ends each turn.  The second group is a turn behind:
@@ -291,7 +293,7 @@ __global__ __launch_bounds__(NT) void lm_product_kernel(LmArgs a) {
   // waited for their part of stage s + 1: a load has five turns to come.
   const int group = w >> 2;
   const auto buffer = [&](int i) { return lds + ((i - kt0) & 3) * 2 * STAGE; };
-  u32x4 af[8], bf[4];
+  u32x4 af[2][4], bf[2][2];
 #pragma unroll 1
   for (int i = kt0; i < kt0 + 3; ++i)
     if (i < kt1) {
@@ -306,9 +308,12 @@ __global__ __launch_bounds__(NT) void lm_product_kernel(LmArgs a) {
     const bool more = i + 3 < kt1;
     const uint32_t pa = fa.place(buffer(i)), pb = fb.place(buffer(i) + STAGE);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) bf[j] = fb.read(pb, j);
+    for (int kk = 0; kk < 2; ++kk) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) af[j] = fa.read(pa, j);
+      for (int j = 0; j < 2; ++j) bf[kk][j] = fb.read(pb, j, kk);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) af[kk][j] = fa.read(pa, j, kk);
+    }
     if (more) A.fetch(i + 3, buffer(i + 3));
     wait_lds();
     if (group == 1) {
@@ -317,15 +322,17 @@ __global__ __launch_bounds__(NT) void lm_product_kernel(LmArgs a) {
     turn();
     __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
+    for (int kk = 0; kk < 2; ++kk)
 #pragma unroll
-      for (int n = 0; n < 4; ++n) acc[n][j] = mfma<F16>(af[j], bf[n], acc[n][j]);
-      if (j == 1) {
-        __builtin_amdgcn_sched_barrier(0);
-        if (more) B.fetch(i + 3, buffer(i + 3) + STAGE);
-        __builtin_amdgcn_sched_barrier(0);
+      for (int j = 0; j < 4; ++j) {
+#pragma unroll
+        for (int n = 0; n < 2; ++n) acc[n][j] = mfma32x32x16<F16>(af[kk][j], bf[kk][n], acc[n][j]);
+        if (kk == 0 && j == 1) {
+          __builtin_amdgcn_sched_barrier(0);
+          if (more) B.fetch(i + 3, buffer(i + 3) + STAGE);
+          __builtin_amdgcn_sched_barrier(0);
+        }
       }
-    }
     __builtin_amdgcn_s_setprio(0);
     if (group == 0) {
       if (more) wait_loads<8>(); else wait_loads<0>();
@@ -334,20 +341,25 @@ __global__ __launch_bounds__(NT) void lm_product_kernel(LmArgs a) {
   }
   if (group == 0) turn();
 
-  const int lane = threadIdx.x & 63, g = lane >> 4, l = lane & 15;
+  const int lane = threadIdx.x & 63, h = lane >> 5;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int n = n0 + wn * 64 + i * 16 + l, m = m0 + wm * 128;
+  for (int i = 0; i < 2; ++i) {
+    const int n = n0 + wn * 64 + i * 32 + (lane & 31), m = m0 + wm * 128;
     if constexpr (P == LM_LOGITS) {
       store_logits<F16>(a, m, n, n < s.n, acc[i]);
     } else if (t.pieces > 1) {
-      float* part = a.parts + (int64_t)t.id * LM_TILE * LM_TILE + (int64_t)(n - n0) * LM_TILE + wm * 128 + g * 4;
+      float* part = a.parts + (int64_t)t.id * LM_TILE * LM_TILE + (int64_t)(n - n0) * LM_TILE + wm * 128 + h * 4;
 #pragma unroll
-      for (int j = 0; j < 8; ++j) *reinterpret_cast<floatx4*>(part + j * 16) = acc[i][j];
+      for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) *reinterpret_cast<floatx4*>(part + j * 32 + q * 8) = quad(acc[i][j], q);
     } else if (n < s.n) {
 #pragma unroll
-      for (int j = 0; j < 8; ++j)
-        if (m + j * 16 < s.m) store_grad<F16>(a, P, n, m + j * 16 + g * 4, acc[i][j]);
+      for (int j = 0; j < 4; ++j) {
+        if (m + j * 32 >= s.m) continue;                     // (d is a multiple of 64)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) store_grad<F16>(a, P, n, m + j * 32 + q * 8 + h * 4, quad(acc[i][j], q));
+      }
     }
   }
 }
