@@ -6,7 +6,7 @@
 // operand comes as its memory has it: rows along k (fragments by 16-byte LDS
 // reads), or rows along m or n (transposed LDS reads), so neither w, x nor P is
 // ever laid out a second time.  Both go from memory to LDS without passing
-// registers, three stages ahead; the places of a stage's 16-byte pieces are exchanged
+// registers, four stages ahead; the places of a stage's 16-byte pieces are exchanged
 // on the way (the lane asks for another piece, since its place in LDS is fixed), so
 // that both kinds of fragment read are free of bank conflicts.
 #include "device_util.h"
@@ -17,8 +17,9 @@
 namespace svl {
 namespace {
 
-constexpr int NT = 512;              // 8 waves: 2 along m of 128, 4 along n of 64
-constexpr int STAGE = LM_TILE * LM_BK;   // elements of an operand's stage
+constexpr int NT = 256;              // 4 waves of 128 x 128
+constexpr int BS = LM_BK / 2;        // of the sum a stage
+constexpr int STAGE = LM_TILE * BS;   // elements of an operand's stage
 
 // 16 bytes a lane from memory to LDS, from `to` on in lane order.  (The builtin would do, but
 // for the compiler every transposed LDS read after it may be of what it brings: it waits
@@ -36,7 +37,9 @@ struct Operand {
   const uint16_t* p;      // of the tile's first row (TR: first column), first k
   int64_t ld;
   int32_t k;              // length of the sum, where rows along it end (TR)
-  uint32_t voff[2];
+  uint32_t voff[4];
+  u32x4 rs;
+  int left;
 
   __device__ __forceinline__ void init(const uint16_t* base, int64_t ld_, int32_t first, int32_t count, int32_t k_) {
     const int w = wave_id(), lane = threadIdx.x & 63;
@@ -44,10 +47,10 @@ struct Operand {
     k = k_;
     p = base + (TR ? (int64_t)first : (int64_t)first * ld);
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
+    for (int i = 0; i < 4; ++i) {
       if constexpr (TR) {
         // two rows of 256 columns; pairs of pieces change places by the row
-        const int r = (i * 8 + w) * 2 + (lane >> 5), at = lane & 31;
+        const int r = (i * 4 + w) * 2 + (lane >> 5), at = lane & 31;
         const int f = 2 * (r & 3);
         int piece = (((at >> 1) ^ f) << 1) | (at & 1);
         const int most = (count - first) / 8 - 1;     // (widths are multiples of 8)
@@ -55,7 +58,7 @@ struct Operand {
         voff[i] = (uint32_t)r * ((uint32_t)ld * 2) + piece * 16;
       } else {
         // 16 rows of 32: pieces change places by the row's quad
-        int r = (i * 8 + w) * 16 + (lane >> 2);
+        int r = (i * 4 + w) * 16 + (lane >> 2);
         const int piece = (lane & 3) ^ (lane >> 4);
         r = r < count - first ? r : count - first - 1;
         voff[i] = (uint32_t)r * ((uint32_t)ld * 2) + piece * 16;
@@ -63,26 +66,26 @@ struct Operand {
     }
   }
 
-  // Stage s of the sum on its way to LDS, stages in ascending order.  Rows behind the last
-  // of the sum are taken to be the last: P is 0 there.
-  __device__ __forceinline__ void fetch(int s, uint16_t* lds) {
-    const int w = wave_id();
-    const uint64_t a = reinterpret_cast<uint64_t>(TR ? p + (int64_t)s * LM_BK * ld : p + s * LM_BK);
-    const u32x4 rs = {(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)a),
-                      (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(a >> 32)) & 0xffffu, 0x7fffffffu,
-                      0x00020000u};
-    const uint32_t first = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint16_t*)lds + w * 1024;
-    const int left = k - s * LM_BK;
-    if (ENDS && left < LM_BK) {
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const int over = (i * 8 + w) * 2 + (int)((threadIdx.x & 63) >> 5) - (left - 1);
-        voff[i] -= over > 0 ? (uint32_t)over * ((uint32_t)ld * 2) : 0u;
-      }
+  // From here on the wave's loads are of stage s.
+  __device__ __forceinline__ void at_stage(int s) {
+    left = k - s * BS;
+    int64_t row = (int64_t)s * BS;
+    if (ENDS && left < 1) {     // (a step's second stage may lie behind the sum)
+      row = k - 1;
+      left = 1;
     }
-#pragma unroll
-    for (int i = 0; i < 2; ++i)
-      load_to_lds(rs, voff[i], __builtin_amdgcn_readfirstlane((int)first) + i * 8192);
+    const uint64_t a = reinterpret_cast<uint64_t>(TR ? p + row * ld : p + s * BS);
+    rs = u32x4{(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)a),
+               (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(a >> 32)) & 0xffffu, 0x7fffffffu, 0x00020000u};
+  }
+  // The wave's load i of 4.  Rows behind the last of the sum are taken to be the last: P is 0 there.
+  __device__ __forceinline__ void fetch(int i, uint32_t lds) const {
+    uint32_t v = voff[i];
+    if (ENDS && left < BS) {
+      const int over = (i * 4 + wave_id()) * 2 + (int)((threadIdx.x & 63) >> 5) - (left - 1);
+      v -= over > 0 ? (uint32_t)over * ((uint32_t)ld * 2) : 0u;
+    }
+    load_to_lds(rs, v, lds + i * 4096);
   }
 };
 
@@ -95,12 +98,12 @@ struct Fragments {
     if constexpr (TR)
       at = (uint32_t)((8 * h + l / 4) * LM_TILE * 2 + (((first / 16 + ((lane >> 4) & 1)) ^ (2 * (l / 4))) * 32) + (l & 3) * 8);
     else
-      at = (uint32_t)((first + (lane & 31)) * LM_BK * 2 + ((h ^ ((lane >> 2) & 3)) * 16));
+      at = (uint32_t)((first + (lane & 31)) * BS * 2 + ((h ^ ((lane >> 2) & 3)) * 16));
   }
-  // The lane's place in the stage at `lds`.  (Opaque: the compiler would otherwise keep every block's
-  // place of every buffer in registers, which the products need.)
-  __device__ __forceinline__ uint32_t place(const uint16_t* lds) const {
-    uint32_t p = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const uint16_t*)lds + at;
+  // The lane's place in the stage at LDS address `lds`.  (Opaque: the compiler would otherwise keep every
+  // block's place of every buffer in registers.)
+  __device__ __forceinline__ uint32_t place(uint32_t lds) const {
+    uint32_t p = lds + at;
     asm volatile("" : "+v"(p));
     return p;
   }
@@ -110,7 +113,7 @@ struct Fragments {
       const uint2 a = read_tr(q), b = read_tr(q + 8 * LM_TILE);
       return u32x4{a.x, a.y, b.x, b.y};
     } else {
-      return *(__attribute__((address_space(3))) const u32x4*)(uintptr_t)((place ^ (kk * 32)) + block * 64 * LM_BK);
+      return *(__attribute__((address_space(3))) const u32x4*)(uintptr_t)((place ^ (kk * 32)) + block * 64 * BS);
     }
   }
   static __device__ __forceinline__ uint2 read_tr(uint32_t at) {
@@ -130,7 +133,7 @@ __device__ __forceinline__ void turn() {
 __device__ __forceinline__ void wait_lds() { __builtin_amdgcn_s_waitcnt(0xc07f); }     // lgkmcnt(0)
 // Until at most N of the wave's loads are on their way (vmcnt).
 template <int N>
-__device__ __forceinline__ void wait_loads() { __builtin_amdgcn_s_waitcnt(0x0f70 | N); }
+__device__ __forceinline__ void wait_loads() { __builtin_amdgcn_s_waitcnt(0x0f70 | (N & 15) | (N >> 4) << 14); }
 
 struct Tile {
   int m, n, piece, pieces, tiles, id;
@@ -250,7 +253,7 @@ __device__ __forceinline__ void store_logits(const LmArgs& a, int m0, int n, boo
 }
 
 template <LmProduct P, bool F16>
-__global__ __launch_bounds__(NT) void lm_product_kernel(LmArgs a) {
+__global__ __launch_bounds__(NT, 1) void lm_product_kernel(LmArgs a) {
   constexpr bool TA = P != LM_LOGITS, TB = P == LM_GRAD_W;
   __shared__ __attribute__((aligned(1024))) uint16_t lds[4 * 2 * STAGE];   // four buffers of A's and B's stages
   const Sizes s = sizes_of(a, P);
@@ -272,79 +275,89 @@ __global__ __launch_bounds__(NT) void lm_product_kernel(LmArgs a) {
     A.init(xc, a.d, m0, a.d, s.nk * LM_BK);
     B.init(a.e, a.vp, n0, a.vp, s.nk * LM_BK);
   }
-  const int w = wave_id(), wm = w & 1, wn = w >> 1;
+  const int w = wave_id(), wm = w & 1, wn = w >> 1;   // (128 x 128: 2 fragments read for 4 x 4 products)
   Fragments<TA> fa;
   Fragments<TB> fb;
   fa.init(wm * 128);
-  fb.init(wn * 64);
+  fb.init(wn * 128);
 
-  floatx16 acc[2][4];
+  floatx16 acc[4][4];
 #pragma unroll
-  for (int i = 0; i < 2; ++i)
+  for (int i = 0; i < 4; ++i)
 #pragma unroll
     for (int j = 0; j < 4; ++j) acc[i][j] = floatx16{};
 
-  // The two waves of a SIMD take turns: while one multiplies a stage, the other reads its
-  // fragments of one, and a barrier ends each turn.  The second group is a turn behind:
-  //   turn 2s     group 0 reads s         group 1 multiplies s - 1
-  //   turn 2s + 1 group 0 multiplies s    group 1 reads s
-  // Stage s's buffer is free from turn 2s + 2 on.  Each wave asks for half of its part of stage
-  // s + 3 (the buffer of s - 1) in either turn of its stage s, and before turn 2s + 2 all have
-  // waited for their part of stage s + 1: a load has five turns to come.
-  const int group = w >> 2;
-  const auto buffer = [&](int i) { return lds + ((i - kt0) & 3) * 2 * STAGE; };
-  u32x4 af[2][4], bf[2][2];
-#pragma unroll 1
-  for (int i = kt0; i < kt0 + 3; ++i)
-    if (i < kt1) {
-      A.fetch(i, buffer(i));
-      B.fetch(i, buffer(i) + STAGE);
+  // Four buffers of stages.  While a stage's fragments, in registers, are multiplied, the next
+  // stage's are read and the loads of the stage after three others go out into the buffer that
+  // the multiplied one has left: one barrier a stage, and nothing waits at it for longer than the
+  // slowest wave.  The sum's last stages ask for its last once more, so that all stages are alike.
+  const uint32_t base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint16_t*)lds;
+  const uint32_t mine = __builtin_amdgcn_readfirstlane((int)(base + w * 1024));
+  const int s0 = 2 * kt0, s1 = 2 * kt1;
+  const auto buffer = [&](int s) { return (uint32_t)((s - s0) & 3) * (4u * STAGE); };
+  struct Frags {
+    u32x4 a[2][4], b[2][4];
+  };
+  const auto at_stage = [&](int s) {
+    const int t = s < s1 ? s : s1 - 1;
+    A.at_stage(t);
+    B.at_stage(t);
+  };
+  const auto fetch = [&](int i, uint32_t buf) {
+    if (i < 4) A.fetch(i, mine + buf);
+    else B.fetch(i - 4, mine + buf + 2 * STAGE);
+  };
+  // Fragment i of 16, in the order in which the products take them.
+  const auto read = [&](Frags& f, int i, uint32_t pa, uint32_t pb) {
+    const int kk = i / 8, j = i % 8;
+    if (j % 2 == 0) f.b[kk][j / 2] = fb.read(pb, j / 2, kk);
+    else f.a[kk][j / 2] = fa.read(pa, j / 2, kk);
+  };
+  // Products of `f`, with the reads of `next` from stage s + 1 and the loads of stage s + 4 between them.
+  const auto step = [&](const Frags& f, Frags& next, int s) {
+    const uint32_t pa = fa.place(base + buffer(s + 1)), pb = fb.place(base + buffer(s + 1) + 2 * STAGE);
+    const uint32_t to = buffer(s);
+    at_stage(s + 4);
+#pragma unroll
+    for (int i = 0; i < 32; ++i) {
+      const int kk = i / 16, m = i / 4 % 4, n = i % 4;
+      acc[n][m] = mfma32x32x16<F16>(f.a[kk][m], f.b[kk][n], acc[n][m]);
+      if (i % 2 == 0) read(next, i / 2, pa, pb);
+      if (i % 4 == 1) fetch(i / 4, to);
+      __builtin_amdgcn_sched_barrier(0);
     }
-  if (kt0 + 2 < kt1) wait_loads<8>(); else wait_loads<0>();   // stage kt0
-  turn();
-  if (group == 1) turn();
-#pragma unroll 1
-  for (int i = kt0; i < kt1; ++i) {
-    const bool more = i + 3 < kt1;
-    const uint32_t pa = fa.place(buffer(i)), pb = fb.place(buffer(i) + STAGE);
-#pragma unroll
-    for (int kk = 0; kk < 2; ++kk) {
-#pragma unroll
-      for (int j = 0; j < 2; ++j) bf[kk][j] = fb.read(pb, j, kk);
-#pragma unroll
-      for (int j = 0; j < 4; ++j) af[kk][j] = fa.read(pa, j, kk);
-    }
-    if (more) A.fetch(i + 3, buffer(i + 3));
     wait_lds();
-    if (group == 1) {
-      if (more) wait_loads<6>(); else wait_loads<0>();
+  };
+  Frags f0, f1;
+  if (kt0 < kt1) {
+#pragma unroll 1
+    for (int s = s0; s < s0 + 4; ++s) {
+      at_stage(s);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) fetch(i, buffer(s));
     }
+    wait_loads<24>();
     turn();
-    __builtin_amdgcn_s_setprio(1);
+    const uint32_t pa = fa.place(base), pb = fb.place(base + 2 * STAGE);
 #pragma unroll
-    for (int kk = 0; kk < 2; ++kk)
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-#pragma unroll
-        for (int n = 0; n < 2; ++n) acc[n][j] = mfma32x32x16<F16>(af[kk][j], bf[kk][n], acc[n][j]);
-        if (kk == 0 && j == 1) {
-          __builtin_amdgcn_sched_barrier(0);
-          if (more) B.fetch(i + 3, buffer(i + 3) + STAGE);
-          __builtin_amdgcn_sched_barrier(0);
-        }
-      }
-    __builtin_amdgcn_s_setprio(0);
-    if (group == 0) {
-      if (more) wait_loads<8>(); else wait_loads<0>();
+    for (int i = 0; i < 16; ++i) read(f0, i, pa, pb);
+    wait_lds();
+#pragma unroll 1
+    for (int s = s0; s < s1; s += 2) {
+      wait_loads<16>();      // stage s + 1
+      turn();
+      step(f0, f1, s);
+      wait_loads<16>();
+      turn();
+      step(f1, f0, s + 1);   // (behind the last stage: what is read is not used)
     }
-    turn();
+    wait_loads<0>();         // nothing may come into LDS that is another's by then
   }
-  if (group == 0) turn();
 
   const int lane = threadIdx.x & 63, h = lane >> 5;
 #pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const int n = n0 + wn * 64 + i * 32 + (lane & 31), m = m0 + wm * 128;
+  for (int i = 0; i < 4; ++i) {
+    const int n = n0 + wn * 128 + i * 32 + (lane & 31), m = m0 + wm * 128;
     if constexpr (P == LM_LOGITS) {
       store_logits<F16>(a, m, n, n < s.n, acc[i]);
     } else if (t.pieces > 1) {

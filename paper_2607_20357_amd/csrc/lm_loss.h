@@ -8,11 +8,11 @@
 namespace svl {
 
 constexpr int32_t LM_TILE = 256;     // rows and columns of a product's tile
-constexpr int32_t LM_BK = 32;        // of its sum at a time
+constexpr int32_t LM_BK = 64;        // of its sum a step
 constexpr int32_t LM_ROWS = 64;      // labelled rows are filled up with zeros to a multiple
 constexpr int32_t LM_SLAB = 128;     // vocabulary entries whose exponentials share a maximum
 constexpr int32_t LM_PARTS = 256;    // most workgroups (tiles x pieces) of a product whose sum is cut
-constexpr int32_t LM_CUT = 16;       // least steps of LM_BK of a piece of a sum
+constexpr int32_t LM_CUT = 8;        // least steps of LM_BK of a piece of a sum
 // Exponentials are held as fp16 under 2^14 (normal down to 2^-28 of their slab's largest), P
 // in fp16 likewise (of the largest weight).
 constexpr float LM_E_SCALE = 16384.f;
