@@ -170,38 +170,44 @@ __device__ __forceinline__ Sizes sizes_of(const LmArgs& a, LmProduct p) {
   return s;
 }
 
-// What an element of a gradient becomes, four along d: grad_x or grad_w.
+// Four elements of a gradient along d, from float32 to where they go: grad_x or grad_w.
 template <bool F16>
-__device__ __forceinline__ void store_grad(const LmArgs& a, LmProduct p, int n, int m, floatx4 v) {
-  const float scale = a.head->weight * (F16 ? 1.f / LM_E_SCALE : 1.f);
-  if (p == LM_GRAD_X) {
+__device__ __forceinline__ uint2 round_grad(floatx4 v, uint2 old, bool add) {
+  if (add) {
+    v[0] += act_bits_to_f32<F16>(old.x & 0xffffu);
+    v[1] += act_bits_to_f32<F16>(old.x >> 16);
+    v[2] += act_bits_to_f32<F16>(old.y & 0xffffu);
+    v[3] += act_bits_to_f32<F16>(old.y >> 16);
+  }
+  return make_uint2(pack_act2<F16>(v[0], v[1]), pack_act2<F16>(v[2], v[3]));
+}
+template <bool F16>
+__device__ __forceinline__ float grad_scale(const LmArgs& a) { return a.head->weight * (F16 ? 1.f / LM_E_SCALE : 1.f); }
+
+// N quads along d of one row of grad_w, 8 apart: sums of passes, and what is there already.
+template <bool F16, int N>
+__device__ __forceinline__ void add_grad_w(const LmArgs& a, int n, int m, float scale, floatx4 (&v)[N]) {
+  if (a.sum_w) {
+    float4* sum = reinterpret_cast<float4*>(a.sum_w + (int64_t)n * a.d + m);
+    if (!a.first) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] *= scale;
-    const int64_t row = a.row_of[a.chunk0 + n];
-    *reinterpret_cast<uint2*>(a.grad_x + row * a.ldgx + m) =
-        make_uint2(pack_act2<F16>(v[0], v[1]), pack_act2<F16>(v[2], v[3]));
-    return;
-  }
-  float4* sum = a.sum_w ? reinterpret_cast<float4*>(a.sum_w + (int64_t)n * a.d + m) : nullptr;
-  if (sum && !a.first) {
-    const float4 s = *sum;
-    v[0] += s.x; v[1] += s.y; v[2] += s.z; v[3] += s.w;
-  }
-  if (!a.last) {
-    *sum = make_float4(v[0], v[1], v[2], v[3]);
-    return;
-  }
+      for (int i = 0; i < N; ++i) {
+        const float4 s = sum[2 * i];
+        v[i][0] += s.x; v[i][1] += s.y; v[i][2] += s.z; v[i][3] += s.w;
+      }
+    }
+    if (!a.last) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) v[i] *= scale;
+      for (int i = 0; i < N; ++i) sum[2 * i] = make_float4(v[i][0], v[i][1], v[i][2], v[i][3]);
+      return;
+    }
+  }
   uint2* out = reinterpret_cast<uint2*>(a.grad_w + (int64_t)n * a.ldgw + m);
-  if (a.accumulate) {
-    const uint2 o = *out;
-    v[0] += act_bits_to_f32<F16>(o.x & 0xffffu);
-    v[1] += act_bits_to_f32<F16>(o.x >> 16);
-    v[2] += act_bits_to_f32<F16>(o.y & 0xffffu);
-    v[3] += act_bits_to_f32<F16>(o.y >> 16);
-  }
-  *out = make_uint2(pack_act2<F16>(v[0], v[1]), pack_act2<F16>(v[2], v[3]));
+  uint2 old[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) old[i] = a.accumulate ? out[2 * i] : make_uint2(0, 0);
+#pragma unroll
+  for (int i = 0; i < N; ++i) out[2 * i] = round_grad<F16>(v[i] * scale, old[i], a.accumulate);
 }
 
 // Element 4 q + i of a 32 x 32 block's lane is 8 q + 4 (lane / 32) + i along m.
@@ -209,10 +215,21 @@ __device__ __forceinline__ floatx4 quad(const floatx16& v, int q) {
   return floatx4{v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]};
 }
 
+// A wave's 128 rows of 128 16-bit results pass through its quarter of LDS, so that they leave in
+// whole lines: 8 bytes (half h of the 16-byte piece) in, 16 bytes of 4 rows out; pieces change
+// places by the row against bank conflicts.
+__device__ __forceinline__ void put(uint16_t* own, int row, int piece, int h, uint2 v) {
+  *reinterpret_cast<uint2*>(own + row * 128 + (piece ^ (row & 15)) * 8 + h * 4) = v;
+}
+__device__ __forceinline__ u32x4 get(const uint16_t* own, int row, int piece) {
+  return *reinterpret_cast<const u32x4*>(own + row * 128 + (piece ^ (row & 15)) * 8);
+}
+
 // Logits of 128 entries of the vocabulary (a wave's) become exponentials under their
 // row's largest; a lane holds 64 of the row's, another the rest.
 template <bool F16>
-__device__ __forceinline__ void store_logits(const LmArgs& a, int m0, int n, bool there, floatx16 (&acc)[4]) {
+__device__ __forceinline__ void store_logits(const LmArgs& a, int m0, int n, bool there, uint16_t* own, int row,
+                                             floatx16 (&acc)[4]) {
   const int h = (threadIdx.x & 63) >> 5;
   float top = -INFINITY;
   if (m0 + LM_SLAB > a.vocab) {
@@ -239,17 +256,18 @@ __device__ __forceinline__ void store_logits(const LmArgs& a, int m0, int n, boo
       sum += acc[b][i];
     }
   sum += __shfl_xor(sum, 32, 64);
-  if (!there) return;
-  if (label >= 0 && label < LM_SLAB && (label & 4) == 0) a.label_logit[n] = mine;
-  if (h == 0) a.stats[(int64_t)n * (a.vp / LM_SLAB) + m0 / LM_SLAB] = make_float2(top, sum);
+  if (there) {
+    if (label >= 0 && label < LM_SLAB && (label & 4) == 0) a.label_logit[n] = mine;
+    if (h == 0) a.stats[(int64_t)n * (a.vp / LM_SLAB) + m0 / LM_SLAB] = make_float2(top, sum);
+  }
   if (!a.e) return;
 #pragma unroll
   for (int b = 0; b < 4; ++b)
 #pragma unroll
     for (int q = 0; q < 4; ++q)
-      *reinterpret_cast<uint2*>(a.e + (int64_t)n * a.vp + m0 + b * 32 + 8 * q + 4 * h) =
+      put(own, row, b * 4 + q, h,
           make_uint2(pack_act2<true>(acc[b][4 * q] * LM_E_SCALE, acc[b][4 * q + 1] * LM_E_SCALE),
-                     pack_act2<true>(acc[b][4 * q + 2] * LM_E_SCALE, acc[b][4 * q + 3] * LM_E_SCALE));
+                     pack_act2<true>(acc[b][4 * q + 2] * LM_E_SCALE, acc[b][4 * q + 3] * LM_E_SCALE)));
 }
 
 template <LmProduct P, bool F16>
@@ -354,26 +372,64 @@ __global__ __launch_bounds__(NT, 1) void lm_product_kernel(LmArgs a) {
     wait_loads<0>();         // nothing may come into LDS that is another's by then
   }
 
-  const int lane = threadIdx.x & 63, h = lane >> 5;
+  const int lane = threadIdx.x & 63, h = lane >> 5, m = m0 + wm * 128;
+  if (P != LM_LOGITS && t.pieces > 1) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int n = n0 + wn * 128 + i * 32 + (lane & 31), m = m0 + wm * 128;
-    if constexpr (P == LM_LOGITS) {
-      store_logits<F16>(a, m, n, n < s.n, acc[i]);
-    } else if (t.pieces > 1) {
-      float* part = a.parts + (int64_t)t.id * LM_TILE * LM_TILE + (int64_t)(n - n0) * LM_TILE + wm * 128 + h * 4;
+    for (int i = 0; i < 4; ++i) {
+      float* part = a.parts + (int64_t)t.id * LM_TILE * LM_TILE + (int64_t)(wn * 128 + i * 32 + (lane & 31)) * LM_TILE +
+                    wm * 128 + h * 4;
 #pragma unroll
       for (int j = 0; j < 4; ++j)
 #pragma unroll
         for (int q = 0; q < 4; ++q) *reinterpret_cast<floatx4*>(part + j * 32 + q * 8) = quad(acc[i][j], q);
-    } else if (n < s.n) {
+    }
+    return;
+  }
+  const float scale = P == LM_LOGITS ? 1.f : grad_scale<F16>(a);
+  if (P == LM_GRAD_W && (a.accumulate || a.sum_w)) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int n = n0 + wn * 128 + i * 32 + (lane & 31);
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        if (m + j * 32 >= s.m) continue;                     // (d is a multiple of 64)
+        if (n >= s.n || m + j * 32 >= s.m) continue;         // (d is a multiple of 64)
+        floatx4 v[4];
 #pragma unroll
-        for (int q = 0; q < 4; ++q) store_grad<F16>(a, P, n, m + j * 32 + q * 8 + h * 4, quad(acc[i][j], q));
+        for (int q = 0; q < 4; ++q) v[q] = quad(acc[i][j], q);
+        add_grad_w<F16>(a, n, m + j * 32 + h * 4, scale, v);
       }
     }
+    return;
+  }
+  turn();                                  // all are done with the stages
+  uint16_t* own = lds + w * (128 * 128);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int row = i * 32 + (lane & 31), n = n0 + wn * 128 + row;
+    if constexpr (P == LM_LOGITS) {
+      store_logits<F16>(a, m, n, n < s.n, own, row, acc[i]);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+          put(own, row, j * 4 + q, h, round_grad<F16>(quad(acc[i][j], q) * scale, make_uint2(0, 0), false));
+    }
+  }
+  if (P == LM_LOGITS && !a.e) return;
+  wave_lds_handoff();
+  const int piece = lane & 15, col = m + piece * 8;
+  if (P != LM_LOGITS && col >= s.m) return;
+#pragma unroll 8
+  for (int i = 0; i < 32; ++i) {
+    const int row = i * 4 + (lane >> 4), n = n0 + wn * 128 + row;
+    if (n >= s.n) break;
+    const u32x4 v = get(own, row, piece);
+    uint16_t* to;
+    if constexpr (P == LM_LOGITS) to = a.e + (int64_t)n * a.vp + col;
+    else if constexpr (P == LM_GRAD_X) to = a.grad_x + (int64_t)a.row_of[a.chunk0 + n] * a.ldgx + col;
+    else to = a.grad_w + (int64_t)n * a.ldgw + col;
+    *reinterpret_cast<u32x4*>(to) = v;
   }
 }
 
@@ -392,7 +448,14 @@ __global__ __launch_bounds__(256) void lm_join_kernel(LmArgs a) {
   floatx4 v = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
   for (int i = 0; i < pieces; ++i) v += *reinterpret_cast<const floatx4*>(p + (int64_t)i * tiles * LM_TILE * LM_TILE);
-  store_grad<F16>(a, P, n, m, v);
+  const float scale = grad_scale<F16>(a);
+  if constexpr (P == LM_GRAD_X) {
+    *reinterpret_cast<uint2*>(a.grad_x + (int64_t)a.row_of[a.chunk0 + n] * a.ldgx + m) =
+        round_grad<F16>(v * scale, make_uint2(0, 0), false);
+  } else {
+    floatx4 one[1] = {v};
+    add_grad_w<F16>(a, n, m, scale, one);
+  }
 }
 
 template <LmProduct P, bool F16>
