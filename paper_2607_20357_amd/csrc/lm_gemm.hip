@@ -2,13 +2,14 @@
 //   logits  s = x w^T, whose tiles leave as exponentials and their slabs' maxima and sums
 //   grad_x  P w        grad_w  P^T x
 //
-// C[n][m] = sum_k A[m][k] B[n][k] in tiles of 256 x 256, stages of 32 of the sum.  Each
+// C[n][m] = sum_k A[m][k] B[n][k] in tiles of 256 x 256, 64 of the sum a step.  Each
 // operand comes as its memory has it: rows along k (fragments by 16-byte LDS
 // reads), or rows along m or n (transposed LDS reads), so neither w, x nor P is
 // ever laid out a second time.  Both go from memory to LDS without passing
-// registers, four stages ahead; the places of a stage's 16-byte pieces are exchanged
-// on the way (the lane asks for another piece, since its place in LDS is fixed), so
-// that both kinds of fragment read are free of bank conflicts.
+// registers, two and three steps ahead, a whole line of memory at a time; the places of
+// a step's 16-byte pieces are exchanged on the way (the lane asks for another piece,
+// since its place in LDS is fixed), so that both kinds of fragment read are free of
+// bank conflicts.
 #include "device_util.h"
 #include "lm_loss.h"
 #include "svl_internal.h"
@@ -18,8 +19,7 @@ namespace svl {
 namespace {
 
 constexpr int NT = 256;              // 4 waves of 128 x 128
-constexpr int BS = LM_BK / 2;        // of the sum a stage
-constexpr int STAGE = LM_TILE * BS;   // elements of an operand's stage
+constexpr int STEP = LM_TILE * LM_BK;   // elements of an operand's step
 
 // 16 bytes a lane from memory to LDS, from `to` on in lane order.  (The builtin would do, but
 // for the compiler every transposed LDS read after it may be of what it brings: it waits
@@ -31,13 +31,13 @@ __device__ __forceinline__ void load_to_lds(const u32x4& rsrc, uint32_t voff, ui
 
 __device__ __forceinline__ int wave_id() { return __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6); }
 
-// One operand's stages.  TR: rows along the sum; ENDS: they end inside a stage.
+// One operand's steps.  TR: rows along the sum; ENDS: they end inside a step.
 template <bool TR, bool ENDS>
 struct Operand {
   const uint16_t* p;      // of the tile's first row (TR: first column), first k
   int64_t ld;
   int32_t k;              // length of the sum, where rows along it end (TR)
-  uint32_t voff[4];
+  uint32_t voff[8];
   u32x4 rs;
   int left;
 
@@ -47,41 +47,35 @@ struct Operand {
     k = k_;
     p = base + (TR ? (int64_t)first : (int64_t)first * ld);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < 8; ++i) {
       if constexpr (TR) {
         // two rows of 256 columns; pairs of pieces change places by the row
         const int r = (i * 4 + w) * 2 + (lane >> 5), at = lane & 31;
-        const int f = 2 * (r & 3);
-        int piece = (((at >> 1) ^ f) << 1) | (at & 1);
+        int piece = (((at >> 1) ^ (2 * (r & 3))) << 1) | (at & 1);
         const int most = (count - first) / 8 - 1;     // (widths are multiples of 8)
         piece = piece < most ? piece : most;
         voff[i] = (uint32_t)r * ((uint32_t)ld * 2) + piece * 16;
       } else {
-        // 16 rows of 32: pieces change places by the row's quad
-        int r = (i * 4 + w) * 16 + (lane >> 2);
-        const int piece = (lane & 3) ^ (lane >> 4);
+        // 8 rows of 64: pieces change places by the pair of rows
+        int r = (i * 4 + w) * 8 + (lane >> 3);
+        const int piece = (lane & 7) ^ ((r >> 1) & 7);
         r = r < count - first ? r : count - first - 1;
         voff[i] = (uint32_t)r * ((uint32_t)ld * 2) + piece * 16;
       }
     }
   }
 
-  // From here on the wave's loads are of stage s.
-  __device__ __forceinline__ void at_stage(int s) {
-    left = k - s * BS;
-    int64_t row = (int64_t)s * BS;
-    if (ENDS && left < 1) {     // (a step's second stage may lie behind the sum)
-      row = k - 1;
-      left = 1;
-    }
-    const uint64_t a = reinterpret_cast<uint64_t>(TR ? p + row * ld : p + s * BS);
+  // From here on the wave's loads are of step t.
+  __device__ __forceinline__ void at_step(int t) {
+    left = k - t * LM_BK;
+    const uint64_t a = reinterpret_cast<uint64_t>(TR ? p + (int64_t)t * LM_BK * ld : p + t * LM_BK);
     rs = u32x4{(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)a),
                (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(a >> 32)) & 0xffffu, 0x7fffffffu, 0x00020000u};
   }
-  // The wave's load i of 4.  Rows behind the last of the sum are taken to be the last: P is 0 there.
+  // The wave's load i of 8.  Rows behind the last of the sum are taken to be the last: P is 0 there.
   __device__ __forceinline__ void fetch(int i, uint32_t lds) const {
     uint32_t v = voff[i];
-    if (ENDS && left < BS) {
+    if (ENDS && left < LM_BK) {
       const int over = (i * 4 + wave_id()) * 2 + (int)((threadIdx.x & 63) >> 5) - (left - 1);
       v -= over > 0 ? (uint32_t)over * ((uint32_t)ld * 2) : 0u;
     }
@@ -89,7 +83,7 @@ struct Operand {
   }
 };
 
-// Fragments of 32 rows (or columns) of a stage, from `first` on, 16 of the sum each.
+// Fragments of 32 rows (or columns) of a step, from `first` on, 16 of the sum each.
 template <bool TR>
 struct Fragments {
   uint32_t at;          // bytes
@@ -98,22 +92,23 @@ struct Fragments {
     if constexpr (TR)
       at = (uint32_t)((8 * h + l / 4) * LM_TILE * 2 + (((first / 16 + ((lane >> 4) & 1)) ^ (2 * (l / 4))) * 32) + (l & 3) * 8);
     else
-      at = (uint32_t)((first + (lane & 31)) * BS * 2 + ((h ^ ((lane >> 2) & 3)) * 16));
+      at = (uint32_t)((first + (lane & 31)) * LM_BK * 2 + ((h ^ ((lane >> 1) & 7)) * 16));
   }
-  // The lane's place in the stage at LDS address `lds`.  (Opaque: the compiler would otherwise keep every
+  // The lane's place in the step at LDS address `lds`.  (Opaque: the compiler would otherwise keep every
   // block's place of every buffer in registers.)
   __device__ __forceinline__ uint32_t place(uint32_t lds) const {
     uint32_t p = lds + at;
     asm volatile("" : "+v"(p));
     return p;
   }
+  // kk: which 16 of the step's 64
   static __device__ __forceinline__ u32x4 read(uint32_t place, int block, int kk) {
     if constexpr (TR) {
       const uint32_t q = (place ^ (block * 64)) + kk * 32 * LM_TILE;
       const uint2 a = read_tr(q), b = read_tr(q + 8 * LM_TILE);
       return u32x4{a.x, a.y, b.x, b.y};
     } else {
-      return *(__attribute__((address_space(3))) const u32x4*)(uintptr_t)((place ^ (kk * 32)) + block * 64 * BS);
+      return *(__attribute__((address_space(3))) const u32x4*)(uintptr_t)((place ^ (kk * 32)) + block * 64 * LM_BK);
     }
   }
   static __device__ __forceinline__ uint2 read_tr(uint32_t at) {
@@ -233,11 +228,12 @@ __device__ __forceinline__ void store_logits(const LmArgs& a, int m0, int n, boo
   const int h = (threadIdx.x & 63) >> 5;
   float top = -INFINITY;
   if (m0 + LM_SLAB > a.vocab) {
+    const int end = a.vocab - m0 - 4 * h;
 #pragma unroll
     for (int b = 0; b < 4; ++b)
 #pragma unroll
       for (int i = 0; i < 16; ++i)
-        if (m0 + b * 32 + 8 * (i / 4) + 4 * h + i % 4 >= a.vocab) acc[b][i] = -INFINITY;
+        if (b * 32 + 8 * (i / 4) + i % 4 >= end) acc[b][i] = -INFINITY;
   }
 #pragma unroll
   for (int b = 0; b < 4; ++b)
@@ -246,19 +242,27 @@ __device__ __forceinline__ void store_logits(const LmArgs& a, int m0, int n, boo
   top = fmaxf(top, __shfl_xor(top, 32, 64));
   const int label = there ? a.label[a.chunk0 + n] - m0 - 4 * h : -1;
   float sum = 0.f, mine = 0.f;
-  const bool none = top == -INFINITY;    // nothing of the vocabulary here, or no probability
+  if (__any(label >= 0 && label < LM_SLAB)) {
+#pragma unroll
+    for (int b = 0; b < 4; ++b)
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        if (b * 32 + 8 * (i / 4) + i % 4 == label) mine = acc[b][i];
+  }
+  // 2^(log2(e) (s - top) + 14): what is kept.  (top -inf: nothing of the vocabulary here, or no probability)
+  constexpr float LOG2E = 1.44269504088896340736f;
+  const float from = 14.f - (top == -INFINITY ? 0.f : top * LOG2E);
 #pragma unroll
   for (int b = 0; b < 4; ++b)
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
-      if (b * 32 + 8 * (i / 4) + i % 4 == label) mine = acc[b][i];
-      acc[b][i] = none && !(acc[b][i] != acc[b][i]) ? 0.f : exp2_raw((acc[b][i] - top) * 1.44269504088896340736f);
+      acc[b][i] = exp2_raw(fmaf(acc[b][i], LOG2E, from));
       sum += acc[b][i];
     }
   sum += __shfl_xor(sum, 32, 64);
   if (there) {
     if (label >= 0 && label < LM_SLAB && (label & 4) == 0) a.label_logit[n] = mine;
-    if (h == 0) a.stats[(int64_t)n * (a.vp / LM_SLAB) + m0 / LM_SLAB] = make_float2(top, sum);
+    if (h == 0) a.stats[(int64_t)n * (a.vp / LM_SLAB) + m0 / LM_SLAB] = make_float2(top, sum * (1.f / LM_E_SCALE));
   }
   if (!a.e) return;
 #pragma unroll
@@ -266,14 +270,14 @@ __device__ __forceinline__ void store_logits(const LmArgs& a, int m0, int n, boo
 #pragma unroll
     for (int q = 0; q < 4; ++q)
       put(own, row, b * 4 + q, h,
-          make_uint2(pack_act2<true>(acc[b][4 * q] * LM_E_SCALE, acc[b][4 * q + 1] * LM_E_SCALE),
-                     pack_act2<true>(acc[b][4 * q + 2] * LM_E_SCALE, acc[b][4 * q + 3] * LM_E_SCALE)));
+          make_uint2(pack_act2<true>(acc[b][4 * q], acc[b][4 * q + 1]),
+                     pack_act2<true>(acc[b][4 * q + 2], acc[b][4 * q + 3])));
 }
 
 template <LmProduct P, bool F16>
 __global__ __launch_bounds__(NT, 1) void lm_product_kernel(LmArgs a) {
   constexpr bool TA = P != LM_LOGITS, TB = P == LM_GRAD_W;
-  __shared__ __attribute__((aligned(1024))) uint16_t lds[4 * 2 * STAGE];   // four buffers of A's and B's stages
+  __shared__ __attribute__((aligned(1024))) uint16_t lds[5 * STEP];   // all 160 KB: three steps of one operand, two of the other
   const Sizes s = sizes_of(a, P);
   Tile t;
   if (!tile_of((s.m + LM_TILE - 1) / LM_TILE, (s.n + LM_TILE - 1) / LM_TILE, s.nk, P != LM_LOGITS, &t)) return;
@@ -305,69 +309,78 @@ __global__ __launch_bounds__(NT, 1) void lm_product_kernel(LmArgs a) {
 #pragma unroll
     for (int j = 0; j < 4; ++j) acc[i][j] = floatx16{};
 
-  // Four buffers of stages.  While a stage's fragments, in registers, are multiplied, the next
-  // stage's are read and the loads of the stage after three others go out into the buffer that
-  // the multiplied one has left: one barrier a stage, and nothing waits at it for longer than the
-  // slowest wave.  The sum's last stages ask for its last once more, so that all stages are alike.
+  // While half a step's fragments, in registers, are multiplied, the next half's are read and loads of
+  // a later step go out: in the first half the deep operand's of two steps on, in the second the other's
+  // of two steps on, into the buffer whose last fragments the first half has read.  One barrier a step.
+  // The deep operand has three buffers: what streams from memory (w, P) in place of what the tiles of an
+  // XCD share (x).  The sum's last steps ask for its last once more, so that all are alike.
+  constexpr bool DEEP_A = P != LM_GRAD_W;
   const uint32_t base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint16_t*)lds;
+  const uint32_t other = 3 * 2 * STEP;     // the other operand's buffers are behind the deep one's
   const uint32_t mine = __builtin_amdgcn_readfirstlane((int)(base + w * 1024));
-  const int s0 = 2 * kt0, s1 = 2 * kt1;
-  const auto buffer = [&](int s) { return (uint32_t)((s - s0) & 3) * (4u * STAGE); };
   struct Frags {
     u32x4 a[2][4], b[2][4];
   };
-  const auto at_stage = [&](int s) {
-    const int t = s < s1 ? s : s1 - 1;
-    A.at_stage(t);
-    B.at_stage(t);
+  const auto at_step = [&](bool deep, int t) {
+    t = t < kt1 ? t : kt1 - 1;
+    if (deep == DEEP_A) A.at_step(t); else B.at_step(t);
   };
-  const auto fetch = [&](int i, uint32_t buf) {
-    if (i < 4) A.fetch(i, mine + buf);
-    else B.fetch(i - 4, mine + buf + 2 * STAGE);
+  const auto fetch = [&](bool deep, int i, uint32_t buf) {
+    if (deep == DEEP_A) A.fetch(i, mine + buf); else B.fetch(i, mine + buf);
   };
-  // Fragment i of 16, in the order in which the products take them.
-  const auto read = [&](Frags& f, int i, uint32_t pa, uint32_t pb) {
+  // Fragment i of 16 of a half, in the order in which the products take them.
+  const auto read = [&](Frags& f, int i, uint32_t pa, uint32_t pb, int half) {
     const int kk = i / 8, j = i % 8;
-    if (j % 2 == 0) f.b[kk][j / 2] = fb.read(pb, j / 2, kk);
-    else f.a[kk][j / 2] = fa.read(pa, j / 2, kk);
+    if (j % 2 == 0) f.b[kk][j / 2] = fb.read(pb, j / 2, 2 * half + kk);
+    else f.a[kk][j / 2] = fa.read(pa, j / 2, 2 * half + kk);
   };
-  // Products of `f`, with the reads of `next` from stage s + 1 and the loads of stage s + 4 between them.
-  const auto step = [&](const Frags& f, Frags& next, int s) {
-    const uint32_t pa = fa.place(base + buffer(s + 1)), pb = fb.place(base + buffer(s + 1) + 2 * STAGE);
-    const uint32_t to = buffer(s);
-    at_stage(s + 4);
+  // Products of `f`, with the reads of half `half` of the step at pa, pb and the loads into `to` between them.
+  const auto multiply = [&](const Frags& f, Frags& next, uint32_t pa, uint32_t pb, int half, bool deep, uint32_t to) {
 #pragma unroll
     for (int i = 0; i < 32; ++i) {
       const int kk = i / 16, m = i / 4 % 4, n = i % 4;
       acc[n][m] = mfma32x32x16<F16>(f.a[kk][m], f.b[kk][n], acc[n][m]);
-      if (i % 2 == 0) read(next, i / 2, pa, pb);
-      if (i % 4 == 1) fetch(i / 4, to);
+      if (i % 2 == 0) read(next, i / 2, pa, pb, half);
+      if (i % 4 == 1) fetch(deep, i / 4, to);
       __builtin_amdgcn_sched_barrier(0);
     }
     wait_lds();
   };
+  const auto places = [&](uint32_t deep, uint32_t shallow, uint32_t& pa, uint32_t& pb) {
+    pa = fa.place(base + (DEEP_A ? deep : other + shallow));
+    pb = fb.place(base + (DEEP_A ? other + shallow : deep));
+  };
   Frags f0, f1;
   if (kt0 < kt1) {
-#pragma unroll 1
-    for (int s = s0; s < s0 + 4; ++s) {
-      at_stage(s);
+    uint32_t pa, pb;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) fetch(i, buffer(s));
+    for (int i = 0; i < 2; ++i) {
+      at_step(true, kt0 + i);
+      at_step(false, kt0 + i);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) fetch(true, j, i * 2 * STEP);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) fetch(false, j, other + i * 2 * STEP);
     }
-    wait_loads<24>();
+    wait_loads<16>();
     turn();
-    const uint32_t pa = fa.place(base), pb = fb.place(base + 2 * STAGE);
+    places(0, 0, pa, pb);
 #pragma unroll
-    for (int i = 0; i < 16; ++i) read(f0, i, pa, pb);
+    for (int i = 0; i < 16; ++i) read(f0, i, pa, pb, 0);
     wait_lds();
+    uint32_t deep = 0, shallow = 0;      // buffers of step t
 #pragma unroll 1
-    for (int s = s0; s < s1; s += 2) {
-      wait_loads<16>();      // stage s + 1
+    for (int t = kt0; t < kt1; ++t) {
+      const uint32_t deep1 = deep == 4 * STEP ? 0 : deep + 2 * STEP, deep2 = deep1 == 4 * STEP ? 0 : deep1 + 2 * STEP;
+      at_step(true, t + 2);
+      multiply(f0, f1, pa, pb, 1, true, deep2);
+      wait_loads<8>();                   // step t + 1 of both; what is on its way is of step t + 2
       turn();
-      step(f0, f1, s);
-      wait_loads<16>();
-      turn();
-      step(f1, f0, s + 1);   // (behind the last stage: what is read is not used)
+      places(deep1, shallow ^ 2 * STEP, pa, pb);
+      at_step(false, t + 2);
+      multiply(f1, f0, pa, pb, 0, false, other + shallow);   // (behind the last step: reads that nothing uses)
+      deep = deep1;
+      shallow ^= 2 * STEP;
     }
     wait_loads<0>();         // nothing may come into LDS that is another's by then
   }
