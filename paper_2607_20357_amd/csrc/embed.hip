@@ -47,37 +47,50 @@ __device__ __forceinline__ void sort_source(const SortArgs& s, int pass, int i, 
   }
 }
 
-// Counts of a wave's digits of rows [i0, i1) into cnt[256] (LDS, cleared before).
-__device__ __forceinline__ void count_unit(const SortArgs& s, int pass, int i0, int i1, uint32_t* cnt) {
-  for (int i = i0 + (int)(threadIdx.x & 63); i < i1; i += 64) {
-    uint32_t key, at;
-    sort_source(s, pass, i, &key, &at);
-    atomicAdd(&cnt[(key >> (8 * pass)) & 255u], 1u);   // whole numbers: any order
+// A wave's rows [i0, i1), at most SORT_UNIT, in registers: all loads at once, then LDS alone.
+constexpr int EACH = SORT_UNIT / 64;
+struct Unit {
+  uint32_t key[EACH], at[EACH];
+};
+__device__ __forceinline__ void load_unit(const SortArgs& s, int pass, int i0, int i1, Unit& u) {
+#pragma unroll
+  for (int k = 0; k < EACH; ++k) {
+    const int i = i0 + k * 64 + (int)(threadIdx.x & 63);
+    u.key[k] = u.at[k] = 0;
+    if (i < i1) sort_source(s, pass, i, &u.key[k], &u.at[k]);
   }
 }
 
-// Moves a wave's rows to where their digit's next place is (cnt: first places).
-__device__ __forceinline__ void move_unit(const SortArgs& s, int pass, int i0, int i1, uint32_t* cnt) {
+// Counts of the unit's digits into cnt[256] (LDS, cleared before).
+__device__ __forceinline__ void count_unit(int pass, int i0, int i1, const Unit& u, uint32_t* cnt) {
+#pragma unroll
+  for (int k = 0; k < EACH; ++k)
+    if (i0 + k * 64 + (int)(threadIdx.x & 63) < i1)
+      atomicAdd(&cnt[(u.key[k] >> (8 * pass)) & 255u], 1u);   // whole numbers: any order
+}
+
+// Moves the unit's rows to where their digit's next place is (cnt: first places).
+__device__ __forceinline__ void move_unit(const SortArgs& s, int pass, int i0, int i1, const Unit& u, uint32_t* cnt) {
   const int lane = threadIdx.x & 63;
   const uint64_t below = ((uint64_t)1 << lane) - 1;
-  for (int b = i0; b < i1; b += 64) {
-    const int i = b + lane;
-    uint32_t key = 0, at = 0;
-    if (i < i1) sort_source(s, pass, i, &key, &at);
-    const uint32_t digit = (key >> (8 * pass)) & 255u;
-    uint64_t same = __ballot(i < i1);
+#pragma unroll
+  for (int b = 0; b < EACH; ++b) {
+    if (i0 + b * 64 >= i1) break;
+    const bool there = i0 + b * 64 + lane < i1;
+    const uint32_t digit = (u.key[b] >> (8 * pass)) & 255u;
+    uint64_t same = __ballot(there);
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
       const uint64_t one = __ballot((digit >> k) & 1u);
       same &= (digit >> k) & 1u ? one : ~one;
     }
-    if (i < i1) {
+    if (there) {
       const uint32_t to = cnt[digit] + (uint32_t)__popcll(same & below);
-      s.key[pass & 1][to] = key;
-      s.at[pass & 1][to] = at;
+      s.key[pass & 1][to] = u.key[b];
+      s.at[pass & 1][to] = u.at[b];
     }
     wave_lds_handoff();
-    if (i < i1 && (same & below) == 0) cnt[digit] += (uint32_t)__popcll(same);
+    if (there && (same & below) == 0) cnt[digit] += (uint32_t)__popcll(same);
     wave_lds_handoff();
   }
 }
@@ -112,8 +125,10 @@ __global__ __launch_bounds__(1024) void sort_alone_kernel(SortArgs s) {
   const int i1 = i0 + seg < s.rows ? i0 + seg : s.rows;
   for (int pass = 0; pass < s.passes; ++pass) {
     for (int i = tid; i < 16 * 256; i += 1024) (&cnt[0][0])[i] = 0;
+    Unit u;
+    load_unit(s, pass, i0, i1, u);
     __syncthreads();
-    count_unit(s, pass, i0, i1, cnt[w]);
+    count_unit(pass, i0, i1, u, cnt[w]);
     __syncthreads();
     uint32_t n = 0, all;
     if (tid < 256)
@@ -126,7 +141,7 @@ __global__ __launch_bounds__(1024) void sort_alone_kernel(SortArgs s) {
         first += c;
       }
     __syncthreads();
-    move_unit(s, pass, i0, i1, cnt[w]);
+    move_unit(s, pass, i0, i1, u, cnt[w]);
     __syncthreads();   // the pass's rows are written before the next one reads them
   }
 }
@@ -137,8 +152,10 @@ __global__ __launch_bounds__(NT) void sort_count_kernel(SortArgs s, int pass) {
   for (int i = tid; i < 4 * 256; i += NT) (&cnt[0][0])[i] = 0;
   __syncthreads();
   if (unit < s.units) {
-    const int i0 = unit * SORT_UNIT;
-    count_unit(s, pass, i0, i0 + SORT_UNIT < s.rows ? i0 + SORT_UNIT : s.rows, cnt[w]);
+    const int i0 = unit * SORT_UNIT, i1 = i0 + SORT_UNIT < s.rows ? i0 + SORT_UNIT : s.rows;
+    Unit u;
+    load_unit(s, pass, i0, i1, u);
+    count_unit(pass, i0, i1, u, cnt[w]);
   }
   __syncthreads();
   for (int i = tid; i < 4 * 256; i += NT) {
@@ -174,35 +191,49 @@ __global__ __launch_bounds__(NT) void sort_move_kernel(SortArgs s, int pass) {
   }
   __syncthreads();
   if (unit >= s.units) return;
-  const int i0 = unit * SORT_UNIT;
-  move_unit(s, pass, i0, i0 + SORT_UNIT < s.rows ? i0 + SORT_UNIT : s.rows, cnt[w]);
+  const int i0 = unit * SORT_UNIT, i1 = i0 + SORT_UNIT < s.rows ? i0 + SORT_UNIT : s.rows;
+  Unit u;
+  load_unit(s, pass, i0, i1, u);
+  move_unit(s, pass, i0, i1, u, cnt[w]);
 }
 
 // ------------------------------------------------------------------ sums
-// First place whose key is at least `key`, by the wave together: 64 probes a step.
-__device__ __forceinline__ int first_at_least(const uint32_t* k, int n, uint32_t key) {
-  const int lane = threadIdx.x & 63;
-  int lo = 0, hi = n;                    // k[i] < key for i < lo, >= key for i >= hi
-  while (hi > lo) {
-    const int step = (hi - lo + 63) / 64;
-    const int i = lo + lane * step;
-    const uint64_t less = __ballot(i < hi && k[i < hi ? i : lo] < key);
-    const int c = __popcll(less);        // the first c probes are smaller
-    if (c == 0) return lo;
-    const int from = lo + (c - 1) * step + 1, to = lo + c * step;
-    lo = from;
-    hi = to < hi ? to : hi;
+// Where each token's run begins: the first place whose key is at least v, for v = 0 .. vocab.
+__global__ __launch_bounds__(NT) void embed_runs_kernel(EmbedArgs a) {
+  const int v = blockIdx.x * NT + threadIdx.x;
+  if (v > a.vocab) return;
+  int lo = 0, hi = a.rows;
+  while (lo < hi) {
+    const int mid = (lo + hi) >> 1;
+    if (a.key[mid] < (uint32_t)v) lo = mid + 1; else hi = mid;
   }
-  return lo;
+  a.run[v] = lo;
 }
 
+// Rows of places [i0, i1): their numbers by the wave together, then eight rows in flight.
 __device__ __forceinline__ void add_rows(const EmbedArgs& a, int i0, int i1, int col, float* sum) {
-#pragma unroll 4
-  for (int i = i0; i < i1; ++i) {
-    float v[8];
-    widen8(load_raw8(a.grad_rows, a.row_type, (int64_t)a.at[i] * a.ldr + col), a.row_type, v);
+  const int lane = threadIdx.x & 63;
+  for (int b = i0; b < i1; b += 64) {
+    const int n = i1 - b < 64 ? i1 - b : 64;
+    const uint32_t at = lane < n ? a.at[b + lane] : 0;
+#pragma unroll 1
+    for (int i = 0; i < n; i += 8) {
+      Raw8 raw[8];
 #pragma unroll
-    for (int k = 0; k < 8; ++k) sum[k] += v[k];
+      for (int k = 0; k < 8; ++k) {
+        const int j = i + k < n ? i + k : n - 1;
+        const int64_t row = __builtin_amdgcn_readlane((int)at, j);
+        if (i + k < n) raw[k] = load_raw8(a.grad_rows, a.row_type, row * a.ldr + col);
+      }
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        if (i + k >= n) break;
+        float v[8];
+        widen8(raw[k], a.row_type, v);
+#pragma unroll
+        for (int c = 0; c < 8; ++c) sum[c] += v[c];
+      }
+    }
   }
 }
 
@@ -222,47 +253,43 @@ __global__ __launch_bounds__(NT) void embed_pieces_kernel(EmbedArgs a) {
   const int p = blockIdx.x;
   const int col = blockIdx.y * SLAB + threadIdx.x * 8;
   const uint32_t key = a.key[p * N];
-  if (key >= (uint32_t)a.vocab || a.key[p * N + N - 1] != key || col >= a.width) return;
+  // (columns behind the last load the last: their wave reads places together)
+  if (key >= (uint32_t)a.vocab || a.key[p * N + N - 1] != key) return;
+  const int from = col < a.width ? col : a.width - 8;
   float sum[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-  if constexpr (N == 32) add_rows(a, p * N, p * N + N, col, sum);
-  else add_pieces(a.sum32, a.width, p * 32, p * 32 + 32, col, sum);
-  store8((N == 32 ? a.sum32 : a.sum1024) + (int64_t)p * a.width, SVL_TYPE_F32, col, sum);
+  if constexpr (N == 32) add_rows(a, p * N, p * N + N, from, sum);
+  else add_pieces(a.sum32, a.width, p * 32, p * 32 + 32, from, sum);
+  if (col < a.width) store8((N == 32 ? a.sum32 : a.sum1024) + (int64_t)p * a.width, SVL_TYPE_F32, col, sum);
 }
 
 // One table row a workgroup (BY_PLACE: a place of the order that begins a run).
 template <bool BY_PLACE>
 __global__ __launch_bounds__(NT) void embed_sum_kernel(EmbedArgs a) {
-  const int64_t b = blockIdx.x;
-  const int col = blockIdx.y * SLAB + threadIdx.x * 8;
-  int lo, hi;
-  uint32_t key;
+  const int col = blockIdx.y * SLAB + threadIdx.x * 8, from = col < a.width ? col : a.width - 8;
+  uint32_t key = blockIdx.x;
   if constexpr (BY_PLACE) {
-    lo = (int)b;
-    key = a.key[lo];
-    if (key >= (uint32_t)a.vocab || (lo > 0 && a.key[lo - 1] == key)) return;
-    hi = lo + first_at_least(a.key + lo, a.rows - lo, key + 1);
-  } else {
-    key = (uint32_t)b;
-    lo = first_at_least(a.key, a.rows, key);
-    hi = lo < a.rows && a.key[lo] == key ? lo + first_at_least(a.key + lo, a.rows - lo, key + 1) : lo;
+    const int i = blockIdx.x;
+    key = a.key[i];
+    if (key >= (uint32_t)a.vocab || (i > 0 && a.key[i - 1] == key)) return;
   }
-  if (col >= a.width) return;
+  const int lo = a.run[key], hi = a.run[key + 1];
   float sum[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
   const int p0 = (lo + 31) / 32, p1 = hi / 32;           // whole pieces of 32
   if (!a.sum32 || p0 >= p1) {
-    add_rows(a, lo, hi, col, sum);
+    add_rows(a, lo, hi, from, sum);
   } else {
-    add_rows(a, lo, p0 * 32, col, sum);
+    add_rows(a, lo, p0 * 32, from, sum);
     const int q0 = (p0 + 31) / 32, q1 = p1 / 32;         // whole pieces of 1024
     if (!a.sum1024 || q0 >= q1) {
-      add_pieces(a.sum32, a.width, p0, p1, col, sum);
+      add_pieces(a.sum32, a.width, p0, p1, from, sum);
     } else {
-      add_pieces(a.sum32, a.width, p0, q0 * 32, col, sum);
-      add_pieces(a.sum1024, a.width, q0, q1, col, sum);
-      add_pieces(a.sum32, a.width, q1 * 32, p1, col, sum);
+      add_pieces(a.sum32, a.width, p0, q0 * 32, from, sum);
+      add_pieces(a.sum1024, a.width, q0, q1, from, sum);
+      add_pieces(a.sum32, a.width, q1 * 32, p1, from, sum);
     }
-    add_rows(a, p1 * 32, hi, col, sum);
+    add_rows(a, p1 * 32, hi, from, sum);
   }
+  if (col >= a.width) return;
   const int64_t to = (int64_t)key * a.ldt + col;
 #pragma unroll
   for (int i = 0; i < 8; ++i) sum[i] *= a.scale;
@@ -301,6 +328,7 @@ hipError_t launch_sort_tokens(const SortArgs& s, hipStream_t st) {
 
 hipError_t launch_embed_backward(const EmbedArgs& a, hipStream_t st) {
   const uint32_t slabs = (a.width + SLAB - 1) / SLAB;
+  embed_runs_kernel<<<a.vocab / NT + 1, NT, 0, st>>>(a);
   if (a.sum32) embed_pieces_kernel<32><<<dim3(a.rows / 32, slabs), NT, 0, st>>>(a);
   if (a.sum1024) embed_pieces_kernel<1024><<<dim3(a.rows / 1024, slabs), NT, 0, st>>>(a);
   if (a.accumulate) embed_sum_kernel<true><<<dim3(a.rows, slabs), NT, 0, st>>>(a);

@@ -139,6 +139,7 @@ int64_t embed_layout(const svl_embedding& e, int32_t rows, char* base, SortArgs*
     s->key[i] = l.take<uint32_t>(rows);
     s->at[i] = l.take<uint32_t>(rows);
   }
+  a->run = l.take<int32_t>((int64_t)e.vocab + 1);
   if (rows > SORT_ALONE) s->count = l.take<uint32_t>(256 * (int64_t)s->units);
   if (rows > EMBED_PIECES_FROM) a->sum32 = l.take<float>((int64_t)(rows / 32) * e.width);
   if (rows >= 1024) a->sum1024 = l.take<float>((int64_t)(rows / 1024) * e.width);
@@ -292,11 +293,12 @@ svl_status svl_embed_backward(const svl_embedding* emb, int32_t rows, const int3
   SVL_TRY(check_row_count(rows));
   SVL_TRY(check_flag(accumulate, "accumulate"));
   SVL_TRY(check_array(grad_table, ld_grad_table, emb->width, "grad_table"));
+  if (rows == 0 && accumulate) return SVL_OK;
   if (rows > 0) {
     SVL_TRY(check_pointer(tokens, "tokens", 4));
     SVL_TRY(check_array(grad_rows, ld_grad_rows, emb->width, "grad_rows"));
-    SVL_TRY(check_workspace(ws, ws_bytes, svl_embed_workspace_bytes(emb, rows)));
   }
+  SVL_TRY(check_workspace(ws, ws_bytes, svl_embed_workspace_bytes(emb, rows)));
   EmbedArgs a = embed_args(*emb, rows, tokens);
   SortArgs s{};
   embed_layout(*emb, rows, static_cast<char*>(ws), &s, &a);
@@ -304,7 +306,6 @@ svl_status svl_embed_backward(const svl_embedding* emb, int32_t rows, const int3
   a.grad_rows = grad_rows; a.ldr = ld_grad_rows;
   a.out = grad_table; a.ldt = ld_grad_table;
   a.accumulate = accumulate != 0;
-  if (rows == 0 && a.accumulate) return SVL_OK;
   const hipStream_t st = (hipStream_t)stream;
   return hip_status(timed_launch(K_GATHER, st, [&] {
     if (rows > 0) {
@@ -368,15 +369,11 @@ svl_status svl_norm_backward(const svl_norm* norm, int32_t rows, const void* x, 
   a.want_bias = grad_bias != nullptr;
   a.partial = static_cast<float*>(ws);
   const hipStream_t st = (hipStream_t)stream;
-  const int32_t pieces = std::min(rows, NORM_PIECES);
-  const int64_t stride = (int64_t)(a.want_gain + a.want_bias) * norm->width;
   return hip_status(timed_launch(K_NORM, st, [&] {
     hipError_t e = rows > 0 ? launch_row_norm_backward(a, st) : hipSuccess;
-    if (e == hipSuccess && grad_gain)
-      e = launch_norm_join(a.partial, stride, pieces, norm->width, grad_gain, accumulate != 0, st);
-    if (e == hipSuccess && grad_bias)
-      e = launch_norm_join(a.partial + (grad_gain ? norm->width : 0), stride, pieces, norm->width, grad_bias,
-                           accumulate != 0, st);
+    if (e == hipSuccess && weights)
+      e = launch_norm_join(a.partial, norm_pieces(rows, norm->width), norm->width, grad_gain ? grad_gain : grad_bias,
+                           grad_gain ? grad_bias : nullptr, accumulate != 0, st);
     return e;
   }), "row norm gradient");
 }

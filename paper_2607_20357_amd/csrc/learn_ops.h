@@ -93,14 +93,15 @@ struct RowNormArgs {
   float eps;
 };
 
-// Pieces of the rows whose weight gradients are summed apart, one workgroup (or a
-// wave of one) each.  8192 rows of 4096: see row_norm.hip.
+// Pieces of the rows whose weight gradients are summed apart, a workgroup each.
 constexpr int32_t NORM_PIECES = 512;
+int32_t norm_pieces(int32_t rows, int32_t width);
 
 hipError_t launch_row_norm(const RowNormArgs& a, hipStream_t st);
 hipError_t launch_row_norm_backward(const RowNormArgs& a, hipStream_t st);
-// grad[c] = (accumulate ? grad[c] : 0) + sum over pieces of partial[piece * stride + c]
-hipError_t launch_norm_join(const float* partial, int64_t stride, int32_t pieces, int32_t width, float* grad,
+// grad0[c] (and grad1[c], where given) = (accumulate ? what it is : 0) + sum over pieces of
+// partial[piece][vector][c]
+hipError_t launch_norm_join(const float* partial, int32_t pieces, int32_t width, float* grad0, float* grad1,
                             bool accumulate, hipStream_t st);
 
 // ------------------------------------------------------------------ embedding
@@ -117,6 +118,7 @@ struct EmbedArgs {
   // backward: rows ordered by token, and sums of 32 and of 1024 of them
   const uint32_t* key;
   const uint32_t* at;
+  int32_t* run;            // [vocab + 1] first places of the tokens' runs
   float* sum32;            // [rows / 32][width], or nullptr
   float* sum1024;          // [rows / 1024][width], or nullptr
 };

@@ -5,8 +5,8 @@
 //   grad_bias = sum grad_y.
 //
 // Memory bounds both: a row is read once, kept in registers between the sums
-// over it and the result, and written once.  In the backward a workgroup (or,
-// for narrow rows, a wave) takes every NORM_PIECES-th row and keeps its sums
+// over it and the result, and written once.  In the backward a workgroup takes
+// every NORM_PIECES-th row (four rows at once where they are narrow) and keeps its sums
 // of the weight gradients in registers; the pieces' sums are joined in order.
 #include "learn_ops.h"
 #include "svl_internal.h"
@@ -98,13 +98,13 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void row_norm_kernel(RowNormArgs
   }
 }
 
+// A workgroup takes every pieces-th group of PER rows; where PER > 1 its waves' sums of the weight
+// gradients meet in LDS, so that narrow rows leave no more of them than wide ones.
 template <int T, int C>
 __global__ __launch_bounds__(T < 256 ? 256 : T) void row_norm_backward_kernel(RowNormArgs a, int32_t pieces) {
   constexpr int PER = T < 256 ? 256 / T : 1;
   __shared__ float2 s[2][T / 64];
   const int t = threadIdx.x % T;
-  const int piece = blockIdx.x * PER + threadIdx.x / T;
-  if (piece >= pieces) return;
   int col[C];
   float g[C][8], dg[C][8], db[C][8];
 #pragma unroll
@@ -122,7 +122,7 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void row_norm_backward_kernel(Ro
   }
   const float inv = 1.f / (float)a.width;
   int slot = 0;
-  for (int64_t row = piece; row < a.rows; row += pieces, slot ^= 1) {
+  for (int64_t row = (int64_t)blockIdx.x * PER + threadIdx.x / T; row < a.rows; row += (int64_t)pieces * PER, slot ^= 1) {
     Raw8 xr[C], yr[C];
     load_row<C>(a.x, a.x_type, row * a.ldx, col, a.width, xr);
     load_row<C>(a.grad_y, a.y_type, row * a.ldgy, col, a.width, yr);
@@ -154,7 +154,30 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void row_norm_backward_kernel(Ro
       store8(a.grad_x, a.x_type, row * a.ldgx + col[c], h[c]);
     }
   }
-  float* part = a.partial + (int64_t)piece * (a.want_gain + a.want_bias) * a.width;
+  if (!a.want_gain && !a.want_bias) return;
+  if constexpr (PER > 1) {
+    __shared__ float w[PER - 1][2 * C * 8][T];
+    const int r = threadIdx.x / T;
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (r > 0) {
+          w[r - 1][(c * 8 + i) * 2][t] = dg[c][i];
+          w[r - 1][(c * 8 + i) * 2 + 1][t] = db[c][i];
+        }
+    __syncthreads();
+    if (r > 0) return;
+    for (int k = 0; k < PER - 1; ++k)
+#pragma unroll
+      for (int c = 0; c < C; ++c)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          dg[c][i] += w[k][(c * 8 + i) * 2][t];
+          db[c][i] += w[k][(c * 8 + i) * 2 + 1][t];
+        }
+  }
+  float* part = a.partial + (int64_t)blockIdx.x * (a.want_gain + a.want_bias) * a.width;
 #pragma unroll
   for (int c = 0; c < C; ++c) {
     if (col[c] >= a.width) continue;
@@ -163,13 +186,17 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void row_norm_backward_kernel(Ro
   }
 }
 
-// 16 columns a workgroup, 64 groups of pieces.
-__global__ __launch_bounds__(1024) void norm_join_kernel(const float* partial, int64_t stride, int32_t pieces,
-                                                         int32_t width, float* grad, bool accumulate) {
+// 16 columns a workgroup, 64 groups of pieces; a vector of the partial sums each grid row.
+__global__ __launch_bounds__(1024) void norm_join_kernel(const float* partial, int32_t pieces, int32_t width,
+                                                         float* grad0, float* grad1, bool accumulate) {
   __shared__ float s[64][17];
   const int c = blockIdx.x * 16 + threadIdx.x % 16, g = threadIdx.x / 16;
+  const int64_t stride = (int64_t)gridDim.y * width;
+  partial += (int64_t)blockIdx.y * width;
+  float* grad = blockIdx.y ? grad1 : grad0;
   float sum = 0.f;
   if (c < width)
+#pragma unroll 4
     for (int p = g; p < pieces; p += 64) sum += partial[(int64_t)p * stride + c];
   s[g][threadIdx.x % 16] = sum;
   __syncthreads();
@@ -203,18 +230,24 @@ hipError_t launch_row_norm(const RowNormArgs& a, hipStream_t st) {
   });
 }
 
+int32_t norm_pieces(int32_t rows, int32_t width) {
+  const int32_t per = width <= 1024 ? 4 : 1, groups = (rows + per - 1) / per;
+  return groups < NORM_PIECES ? groups : NORM_PIECES;
+}
+
 hipError_t launch_row_norm_backward(const RowNormArgs& a, hipStream_t st) {
-  const int32_t pieces = a.rows < NORM_PIECES ? a.rows : NORM_PIECES;
+  const int32_t pieces = norm_pieces(a.rows, a.width);
   return by_width(a.width, [&](auto t, auto c) {
     constexpr int T = decltype(t)::value, C = decltype(c)::value, PER = T < 256 ? 256 / T : 1;
-    row_norm_backward_kernel<T, C><<<(pieces + PER - 1) / PER, T * PER, 0, st>>>(a, pieces);
+    row_norm_backward_kernel<T, C><<<pieces, T * PER, 0, st>>>(a, pieces);
     return hipGetLastError();
   });
 }
 
-hipError_t launch_norm_join(const float* partial, int64_t stride, int32_t pieces, int32_t width, float* grad,
+hipError_t launch_norm_join(const float* partial, int32_t pieces, int32_t width, float* grad0, float* grad1,
                             bool accumulate, hipStream_t st) {
-  norm_join_kernel<<<(width + 15) / 16, 1024, 0, st>>>(partial, stride, pieces, width, grad, accumulate);
+  norm_join_kernel<<<dim3((width + 15) / 16, grad1 ? 2 : 1), 1024, 0, st>>>(partial, pieces, width, grad0, grad1,
+                                                                          accumulate);
   return hipGetLastError();
 }
 
