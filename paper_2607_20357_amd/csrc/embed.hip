@@ -69,8 +69,9 @@ __device__ __forceinline__ void count_unit(int pass, int i0, int i1, const Unit&
       atomicAdd(&cnt[(u.key[k] >> (8 * pass)) & 255u], 1u);   // whole numbers: any order
 }
 
-// Moves the unit's rows to where their digit's next place is (cnt: first places).
-__device__ __forceinline__ void move_unit(const SortArgs& s, int pass, int i0, int i1, const Unit& u, uint32_t* cnt) {
+// Moves the unit's rows to where their digit's next place is (cnt: first places): put(place, key, at).
+template <class Put>
+__device__ __forceinline__ void move_unit(int pass, int i0, int i1, const Unit& u, uint32_t* cnt, const Put& put) {
   const int lane = threadIdx.x & 63;
   const uint64_t below = ((uint64_t)1 << lane) - 1;
 #pragma unroll
@@ -84,11 +85,7 @@ __device__ __forceinline__ void move_unit(const SortArgs& s, int pass, int i0, i
       const uint64_t one = __ballot((digit >> k) & 1u);
       same &= (digit >> k) & 1u ? one : ~one;
     }
-    if (there) {
-      const uint32_t to = cnt[digit] + (uint32_t)__popcll(same & below);
-      s.key[pass & 1][to] = u.key[b];
-      s.at[pass & 1][to] = u.at[b];
-    }
+    if (there) put(cnt[digit] + (uint32_t)__popcll(same & below), u.key[b], u.at[b]);
     wave_lds_handoff();
     if (there && (same & below) == 0) cnt[digit] += (uint32_t)__popcll(same);
     wave_lds_handoff();
@@ -116,17 +113,30 @@ __device__ __forceinline__ uint32_t block_before(uint32_t v, uint32_t* s, uint32
   return before + x - v;
 }
 
+// One workgroup, the rows in LDS between the passes: 16384 rows of a vocabulary of 32000 37 us (8192 21,
+// 1024 8), most of it the ballots of move_unit; several workgroups take six launches for it.
 __global__ __launch_bounds__(1024) void sort_alone_kernel(SortArgs s) {
   __shared__ uint32_t cnt[16][256];
   __shared__ uint32_t sums[16];
-  const int tid = threadIdx.x, w = tid >> 6;
+  __shared__ uint32_t key[SORT_ALONE];
+  __shared__ uint16_t at[SORT_ALONE];
+  const int tid = threadIdx.x, w = tid >> 6, lane = tid & 63;
   const int seg = ((s.rows + 1023) / 1024) * 64;
   const int i0 = w * seg < s.rows ? w * seg : s.rows;
   const int i1 = i0 + seg < s.rows ? i0 + seg : s.rows;
   for (int pass = 0; pass < s.passes; ++pass) {
     for (int i = tid; i < 16 * 256; i += 1024) (&cnt[0][0])[i] = 0;
     Unit u;
-    load_unit(s, pass, i0, i1, u);
+    if (pass == 0) {
+      load_unit(s, 0, i0, i1, u);
+    } else {
+#pragma unroll
+      for (int k = 0; k < EACH; ++k) {
+        const int i = i0 + k * 64 + lane;
+        u.key[k] = i < i1 ? key[i] : 0;
+        u.at[k] = i < i1 ? at[i] : 0;
+      }
+    }
     __syncthreads();
     count_unit(pass, i0, i1, u, cnt[w]);
     __syncthreads();
@@ -141,8 +151,17 @@ __global__ __launch_bounds__(1024) void sort_alone_kernel(SortArgs s) {
         first += c;
       }
     __syncthreads();
-    move_unit(s, pass, i0, i1, u, cnt[w]);
-    __syncthreads();   // the pass's rows are written before the next one reads them
+    move_unit(pass, i0, i1, u, cnt[w], [&](uint32_t to, uint32_t k, uint32_t a) {
+      key[to] = k;
+      at[to] = (uint16_t)a;
+    });
+    __syncthreads();   // the pass's rows are there before the next one reads them
+  }
+  uint32_t* to_key = s.key[(s.passes - 1) & 1];
+  uint32_t* to_at = s.at[(s.passes - 1) & 1];
+  for (int i = tid; i < s.rows; i += 1024) {
+    to_key[i] = key[i];
+    to_at[i] = at[i];
   }
 }
 
@@ -194,7 +213,10 @@ __global__ __launch_bounds__(NT) void sort_move_kernel(SortArgs s, int pass) {
   const int i0 = unit * SORT_UNIT, i1 = i0 + SORT_UNIT < s.rows ? i0 + SORT_UNIT : s.rows;
   Unit u;
   load_unit(s, pass, i0, i1, u);
-  move_unit(s, pass, i0, i1, u, cnt[w]);
+  move_unit(pass, i0, i1, u, cnt[w], [&](uint32_t to, uint32_t k, uint32_t a) {
+    s.key[pass & 1][to] = k;
+    s.at[pass & 1][to] = a;
+  });
 }
 
 // ------------------------------------------------------------------ sums
@@ -210,31 +232,38 @@ __global__ __launch_bounds__(NT) void embed_runs_kernel(EmbedArgs a) {
   a.run[v] = lo;
 }
 
-// Rows of places [i0, i1): their numbers by the wave together, then eight rows in flight.
-__device__ __forceinline__ void add_rows(const EmbedArgs& a, int i0, int i1, int col, float* sum) {
+// Rows of places [i0, i1): their numbers by the wave together, then FLIGHT rows at a time
+// (behind the last one the last again, which is not added).
+constexpr int FLIGHT = 8;
+template <bool WIDE>
+__device__ __forceinline__ void add_rows_of(const EmbedArgs& a, int i0, int i1, int col, float* sum) {
   const int lane = threadIdx.x & 63;
+  const int32_t type = WIDE ? (int32_t)SVL_TYPE_F32 : a.row_type == SVL_TYPE_BF16 ? SVL_TYPE_BF16 : SVL_TYPE_F16;
   for (int b = i0; b < i1; b += 64) {
     const int n = i1 - b < 64 ? i1 - b : 64;
     const uint32_t at = lane < n ? a.at[b + lane] : 0;
 #pragma unroll 1
-    for (int i = 0; i < n; i += 8) {
-      Raw8 raw[8];
+    for (int i = 0; i < n; i += FLIGHT) {
+      Raw8 raw[FLIGHT];
 #pragma unroll
-      for (int k = 0; k < 8; ++k) {
+      for (int k = 0; k < FLIGHT; ++k) {
         const int j = i + k < n ? i + k : n - 1;
-        const int64_t row = __builtin_amdgcn_readlane((int)at, j);
-        if (i + k < n) raw[k] = load_raw8(a.grad_rows, a.row_type, row * a.ldr + col);
+        raw[k] = load_raw8(a.grad_rows, type, (int64_t)__builtin_amdgcn_readlane((int)at, j) * a.ldr + col);
       }
 #pragma unroll
-      for (int k = 0; k < 8; ++k) {
+      for (int k = 0; k < FLIGHT; ++k) {
         if (i + k >= n) break;
         float v[8];
-        widen8(raw[k], a.row_type, v);
+        widen8(raw[k], type, v);
 #pragma unroll
         for (int c = 0; c < 8; ++c) sum[c] += v[c];
       }
     }
   }
+}
+__device__ __forceinline__ void add_rows(const EmbedArgs& a, int i0, int i1, int col, float* sum) {
+  if (a.row_type == SVL_TYPE_F32) add_rows_of<true>(a, i0, i1, col, sum);
+  else add_rows_of<false>(a, i0, i1, col, sum);
 }
 
 __device__ __forceinline__ void add_pieces(const float* piece, int width, int i0, int i1, int col, float* sum) {
