@@ -51,7 +51,7 @@ struct Operand {
       if constexpr (TR) {
         // two rows of 256 columns; pairs of pieces change places by the row
         const int r = (i * 4 + w) * 2 + (lane >> 5), at = lane & 31;
-        int piece = (((at >> 1) ^ (2 * (r & 3))) << 1) | (at & 1);
+        int piece = (((at >> 1) ^ ((r & 3) | ((r >> 3 & 3) << 2))) << 1) | (at & 1);
         const int most = (count - first) / 8 - 1;     // (widths are multiples of 8)
         piece = piece < most ? piece : most;
         voff[i] = (uint32_t)r * ((uint32_t)ld * 2) + piece * 16;
@@ -83,16 +83,16 @@ struct Operand {
   }
 };
 
-// Fragments of 32 rows (or columns) of a step, from `first` on, 16 of the sum each.
+// Fragments of 16 rows (or columns) of a step, from `first` on, 32 of the sum each.
 template <bool TR>
 struct Fragments {
   uint32_t at;          // bytes
   __device__ __forceinline__ void init(int first) {
-    const int lane = threadIdx.x & 63, h = lane >> 5, l = lane & 15;
+    const int lane = threadIdx.x & 63, g = lane >> 4, l = lane & 15;
     if constexpr (TR)
-      at = (uint32_t)((8 * h + l / 4) * LM_TILE * 2 + (((first / 16 + ((lane >> 4) & 1)) ^ (2 * (l / 4))) * 32) + (l & 3) * 8);
+      at = (uint32_t)((8 * g + l / 4) * LM_TILE * 2 + (((first / 16) ^ (l / 4 | g << 2)) * 32) + (l & 3) * 8);
     else
-      at = (uint32_t)((first + (lane & 31)) * LM_BK * 2 + ((h ^ ((lane >> 1) & 7)) * 16));
+      at = (uint32_t)((first + l) * LM_BK * 2 + ((g ^ (l >> 1)) * 16));
   }
   // The lane's place in the step at LDS address `lds`.  (Opaque: the compiler would otherwise keep every
   // block's place of every buffer in registers.)
@@ -101,14 +101,13 @@ struct Fragments {
     asm volatile("" : "+v"(p));
     return p;
   }
-  // kk: which 16 of the step's 64
-  static __device__ __forceinline__ u32x4 read(uint32_t place, int block, int kk) {
+  static __device__ __forceinline__ u32x4 read(uint32_t place, int block, int half) {
     if constexpr (TR) {
-      const uint32_t q = (place ^ (block * 64)) + kk * 32 * LM_TILE;
+      const uint32_t q = (place ^ (block * 32)) + half * 64 * LM_TILE;
       const uint2 a = read_tr(q), b = read_tr(q + 8 * LM_TILE);
       return u32x4{a.x, a.y, b.x, b.y};
     } else {
-      return *(__attribute__((address_space(3))) const u32x4*)(uintptr_t)((place ^ (kk * 32)) + block * 64 * LM_BK);
+      return *(__attribute__((address_space(3))) const u32x4*)(uintptr_t)((place ^ (half * 64)) + block * 32 * LM_BK);
     }
   }
   static __device__ __forceinline__ uint2 read_tr(uint32_t at) {
@@ -116,6 +115,16 @@ struct Fragments {
         (__attribute__((address_space(3))) shortx4*)(uintptr_t)at));
   }
 };
+
+// c += a b.  (In assembly so that all sums stay where they are, in the accumulation registers: the
+// compiler moves some of 64 blocks of 4 to and fro.  What the hardware does not wait for by itself is
+// kept apart: a sum is used again 64 products later, and read after settle().)
+template <bool F16>
+__device__ __forceinline__ void mfma(const u32x4& a, const u32x4& b, floatx4& c) {
+  if constexpr (F16) asm volatile("v_mfma_f32_16x16x32_f16 %0, %1, %2, %0" : "+a"(c) : "v"(a), "v"(b));
+  else asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(c) : "v"(a), "v"(b));
+}
+__device__ __forceinline__ void settle() { asm volatile("s_nop 15\n\ts_nop 15" ::: "memory"); }
 
 // Ends a turn: nothing moves over it, and all waves have come here.
 __device__ __forceinline__ void turn() {
@@ -179,7 +188,7 @@ __device__ __forceinline__ uint2 round_grad(floatx4 v, uint2 old, bool add) {
 template <bool F16>
 __device__ __forceinline__ float grad_scale(const LmArgs& a) { return a.head->weight * (F16 ? 1.f / LM_E_SCALE : 1.f); }
 
-// N quads along d of one row of grad_w, 8 apart: sums of passes, and what is there already.
+// N quads along d of one row of grad_w, 16 apart: sums of passes, and what is there already.
 template <bool F16, int N>
 __device__ __forceinline__ void add_grad_w(const LmArgs& a, int n, int m, float scale, floatx4 (&v)[N]) {
   if (a.sum_w) {
@@ -187,91 +196,86 @@ __device__ __forceinline__ void add_grad_w(const LmArgs& a, int n, int m, float 
     if (!a.first) {
 #pragma unroll
       for (int i = 0; i < N; ++i) {
-        const float4 s = sum[2 * i];
+        const float4 s = sum[4 * i];
         v[i][0] += s.x; v[i][1] += s.y; v[i][2] += s.z; v[i][3] += s.w;
       }
     }
     if (!a.last) {
 #pragma unroll
-      for (int i = 0; i < N; ++i) sum[2 * i] = make_float4(v[i][0], v[i][1], v[i][2], v[i][3]);
+      for (int i = 0; i < N; ++i) sum[4 * i] = make_float4(v[i][0], v[i][1], v[i][2], v[i][3]);
       return;
     }
   }
   uint2* out = reinterpret_cast<uint2*>(a.grad_w + (int64_t)n * a.ldgw + m);
   uint2 old[N];
 #pragma unroll
-  for (int i = 0; i < N; ++i) old[i] = a.accumulate ? out[2 * i] : make_uint2(0, 0);
+  for (int i = 0; i < N; ++i) old[i] = a.accumulate ? out[4 * i] : make_uint2(0, 0);
 #pragma unroll
-  for (int i = 0; i < N; ++i) out[2 * i] = round_grad<F16>(v[i] * scale, old[i], a.accumulate);
-}
-
-// Element 4 q + i of a 32 x 32 block's lane is 8 q + 4 (lane / 32) + i along m.
-__device__ __forceinline__ floatx4 quad(const floatx16& v, int q) {
-  return floatx4{v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]};
+  for (int i = 0; i < N; ++i) out[4 * i] = round_grad<F16>(v[i] * scale, old[i], a.accumulate);
 }
 
 // A wave's 128 rows of 128 16-bit results pass through its quarter of LDS, so that they leave in
-// whole lines: 8 bytes (half h of the 16-byte piece) in, 16 bytes of 4 rows out; pieces change
+// whole lines: 8 bytes (a half of the 16-byte piece) in, 16 bytes of 4 rows out; pieces change
 // places by the row against bank conflicts.
-__device__ __forceinline__ void put(uint16_t* own, int row, int piece, int h, uint2 v) {
-  *reinterpret_cast<uint2*>(own + row * 128 + (piece ^ (row & 15)) * 8 + h * 4) = v;
+__device__ __forceinline__ void put(uint16_t* own, int row, int piece, int half, uint2 v) {
+  *reinterpret_cast<uint2*>(own + row * 128 + (piece ^ (row & 15)) * 8 + half * 4) = v;
 }
 __device__ __forceinline__ u32x4 get(const uint16_t* own, int row, int piece) {
   return *reinterpret_cast<const u32x4*>(own + row * 128 + (piece ^ (row & 15)) * 8);
 }
 
 // Logits of 128 entries of the vocabulary (a wave's) become exponentials under their
-// row's largest; a lane holds 64 of the row's, another the rest.
+// row's largest; a lane holds 32 of the row's, three others the rest.
 template <bool F16>
 __device__ __forceinline__ void store_logits(const LmArgs& a, int m0, int n, bool there, uint16_t* own, int row,
-                                             floatx16 (&acc)[4]) {
-  const int h = (threadIdx.x & 63) >> 5;
+                                             floatx4 (&acc)[8]) {
+  const int g = (threadIdx.x & 63) >> 4;
   float top = -INFINITY;
   if (m0 + LM_SLAB > a.vocab) {
-    const int end = a.vocab - m0 - 4 * h;
+    const int end = a.vocab - m0 - 4 * g;
 #pragma unroll
-    for (int b = 0; b < 4; ++b)
+    for (int b = 0; b < 8; ++b)
 #pragma unroll
-      for (int i = 0; i < 16; ++i)
-        if (b * 32 + 8 * (i / 4) + i % 4 >= end) acc[b][i] = -INFINITY;
+      for (int i = 0; i < 4; ++i)
+        if (b * 16 + i >= end) acc[b][i] = -INFINITY;
   }
 #pragma unroll
-  for (int b = 0; b < 4; ++b)
+  for (int b = 0; b < 8; ++b)
 #pragma unroll
-    for (int i = 0; i < 16; ++i) top = fmaxf(top, acc[b][i]);
+    for (int i = 0; i < 4; ++i) top = fmaxf(top, acc[b][i]);
+  top = fmaxf(top, __shfl_xor(top, 16, 64));
   top = fmaxf(top, __shfl_xor(top, 32, 64));
-  const int label = there ? a.label[a.chunk0 + n] - m0 - 4 * h : -1;
-  float sum = 0.f, mine = 0.f;
-  if (__any(label >= 0 && label < LM_SLAB)) {
+  const int label = there ? a.label[a.chunk0 + n] - m0 : -1;
+  const bool here = label >= 0 && label < LM_SLAB && (label >> 2 & 3) == g;
+  float sum = 0.f;
+  if (__any(here)) {
+    float mine = 0.f;
 #pragma unroll
-    for (int b = 0; b < 4; ++b)
+    for (int b = 0; b < 8; ++b)
 #pragma unroll
-      for (int i = 0; i < 16; ++i)
-        if (b * 32 + 8 * (i / 4) + i % 4 == label) mine = acc[b][i];
+      for (int i = 0; i < 4; ++i)
+        if (b * 16 + i == label - 4 * g) mine = acc[b][i];
+    if (here) a.label_logit[n] = mine;
   }
   // 2^(log2(e) (s - top) + 14): what is kept.  (top -inf: nothing of the vocabulary here, or no probability)
   constexpr float LOG2E = 1.44269504088896340736f;
   const float from = 14.f - (top == -INFINITY ? 0.f : top * LOG2E);
 #pragma unroll
-  for (int b = 0; b < 4; ++b)
+  for (int b = 0; b < 8; ++b)
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
+    for (int i = 0; i < 4; ++i) {
       acc[b][i] = exp2_raw(fmaf(acc[b][i], LOG2E, from));
       sum += acc[b][i];
     }
+  sum += __shfl_xor(sum, 16, 64);
   sum += __shfl_xor(sum, 32, 64);
-  if (there) {
-    if (label >= 0 && label < LM_SLAB && (label & 4) == 0) a.label_logit[n] = mine;
-    if (h == 0) a.stats[(int64_t)n * (a.vp / LM_SLAB) + m0 / LM_SLAB] = make_float2(top, sum * (1.f / LM_E_SCALE));
-  }
+  if (there && g == 0)
+    a.stats[(int64_t)n * (a.vp / LM_SLAB) + m0 / LM_SLAB] = make_float2(top, sum * (1.f / LM_E_SCALE));
   if (!a.e) return;
 #pragma unroll
-  for (int b = 0; b < 4; ++b)
-#pragma unroll
-    for (int q = 0; q < 4; ++q)
-      put(own, row, b * 4 + q, h,
-          make_uint2(pack_act2<true>(acc[b][4 * q], acc[b][4 * q + 1]),
-                     pack_act2<true>(acc[b][4 * q + 2], acc[b][4 * q + 3])));
+  for (int b = 0; b < 8; ++b)
+    put(own, row, 2 * b + (g >> 1), g & 1,
+        make_uint2(pack_act2<true>(acc[b][0], acc[b][1]), pack_act2<true>(acc[b][2], acc[b][3])));
 }
 
 template <LmProduct P, bool F16>
@@ -303,11 +307,11 @@ __global__ __launch_bounds__(NT, 1) void lm_product_kernel(LmArgs a) {
   fa.init(wm * 128);
   fb.init(wn * 128);
 
-  floatx16 acc[4][4];
+  floatx4 acc[8][8];
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
+  for (int i = 0; i < 8; ++i)
 #pragma unroll
-    for (int j = 0; j < 4; ++j) acc[i][j] = floatx16{};
+    for (int j = 0; j < 8; ++j) acc[i][j] = floatx4{0.f, 0.f, 0.f, 0.f};
 
   // While half a step's fragments, in registers, are multiplied, the next half's are read and loads of
   // a later step go out: in the first half the deep operand's of two steps on, in the second the other's
@@ -319,7 +323,7 @@ __global__ __launch_bounds__(NT, 1) void lm_product_kernel(LmArgs a) {
   const uint32_t other = 3 * 2 * STEP;     // the other operand's buffers are behind the deep one's
   const uint32_t mine = __builtin_amdgcn_readfirstlane((int)(base + w * 1024));
   struct Frags {
-    u32x4 a[2][4], b[2][4];
+    u32x4 a[8], b[8];
   };
   const auto at_step = [&](bool deep, int t) {
     t = t < kt1 ? t : kt1 - 1;
@@ -330,18 +334,16 @@ __global__ __launch_bounds__(NT, 1) void lm_product_kernel(LmArgs a) {
   };
   // Fragment i of 16 of a half, in the order in which the products take them.
   const auto read = [&](Frags& f, int i, uint32_t pa, uint32_t pb, int half) {
-    const int kk = i / 8, j = i % 8;
-    if (j % 2 == 0) f.b[kk][j / 2] = fb.read(pb, j / 2, 2 * half + kk);
-    else f.a[kk][j / 2] = fa.read(pa, j / 2, 2 * half + kk);
+    if (i % 2 == 0) f.b[i / 2] = fb.read(pb, i / 2, half);
+    else f.a[i / 2] = fa.read(pa, i / 2, half);
   };
   // Products of `f`, with the reads of half `half` of the step at pa, pb and the loads into `to` between them.
   const auto multiply = [&](const Frags& f, Frags& next, uint32_t pa, uint32_t pb, int half, bool deep, uint32_t to) {
 #pragma unroll
-    for (int i = 0; i < 32; ++i) {
-      const int kk = i / 16, m = i / 4 % 4, n = i % 4;
-      acc[n][m] = mfma32x32x16<F16>(f.a[kk][m], f.b[kk][n], acc[n][m]);
-      if (i % 2 == 0) read(next, i / 2, pa, pb, half);
-      if (i % 4 == 1) fetch(deep, i / 4, to);
+    for (int i = 0; i < 64; ++i) {
+      mfma<F16>(f.a[i / 8], f.b[i % 8], acc[i % 8][i / 8]);
+      if (i % 4 == 0) read(next, i / 4, pa, pb, half);
+      if (i % 8 == 3) fetch(deep, i / 8, to);
       __builtin_amdgcn_sched_barrier(0);
     }
     wait_lds();
@@ -381,52 +383,48 @@ __global__ __launch_bounds__(NT, 1) void lm_product_kernel(LmArgs a) {
       multiply(f1, f0, pa, pb, 0, false, other + shallow);   // (behind the last step: reads that nothing uses)
       deep = deep1;
       shallow ^= 2 * STEP;
+      if (t + 1 == kt1) settle();        // (in the loop: whatever leaves it finds the sums done)
     }
     wait_loads<0>();         // nothing may come into LDS that is another's by then
   }
 
-  const int lane = threadIdx.x & 63, h = lane >> 5, m = m0 + wm * 128;
+  // Element i of a block's lane is 4 (lane / 16) + i along m, lane % 16 along n.
+  const int lane = threadIdx.x & 63, g = lane >> 4, m = m0 + wm * 128;
   if (P != LM_LOGITS && t.pieces > 1) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      float* part = a.parts + (int64_t)t.id * LM_TILE * LM_TILE + (int64_t)(wn * 128 + i * 32 + (lane & 31)) * LM_TILE +
-                    wm * 128 + h * 4;
+    for (int i = 0; i < 8; ++i) {
+      float* part = a.parts + (int64_t)t.id * LM_TILE * LM_TILE + (int64_t)(wn * 128 + i * 16 + (lane & 15)) * LM_TILE +
+                    wm * 128 + g * 4;
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
-#pragma unroll
-        for (int q = 0; q < 4; ++q) *reinterpret_cast<floatx4*>(part + j * 32 + q * 8) = quad(acc[i][j], q);
+      for (int j = 0; j < 8; ++j) *reinterpret_cast<floatx4*>(part + j * 16) = acc[i][j];
     }
     return;
   }
   const float scale = P == LM_LOGITS ? 1.f : grad_scale<F16>(a);
   if (P == LM_GRAD_W && (a.accumulate || a.sum_w)) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int n = n0 + wn * 128 + i * 32 + (lane & 31);
+    for (int i = 0; i < 8; ++i) {
+      const int n = n0 + wn * 128 + i * 16 + (lane & 15);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        if (n >= s.n || m + j * 32 >= s.m) continue;         // (d is a multiple of 64)
-        floatx4 v[4];
-#pragma unroll
-        for (int q = 0; q < 4; ++q) v[q] = quad(acc[i][j], q);
-        add_grad_w<F16>(a, n, m + j * 32 + h * 4, scale, v);
+      for (int j = 0; j < 8; j += 4) {
+        if (n >= s.n || m + j * 16 >= s.m) continue;         // (d is a multiple of 64)
+        floatx4 v[4] = {acc[i][j], acc[i][j + 1], acc[i][j + 2], acc[i][j + 3]};
+        add_grad_w<F16>(a, n, m + j * 16 + g * 4, scale, v);
       }
     }
     return;
   }
-  turn();                                  // all are done with the stages
+  turn();                                  // all are done with the steps
   uint16_t* own = lds + w * (128 * 128);
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int row = i * 32 + (lane & 31), n = n0 + wn * 128 + row;
+  for (int i = 0; i < 8; ++i) {
+    const int row = i * 16 + (lane & 15), n = n0 + wn * 128 + row;
     if constexpr (P == LM_LOGITS) {
       store_logits<F16>(a, m, n, n < s.n, own, row, acc[i]);
     } else {
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
-#pragma unroll
-        for (int q = 0; q < 4; ++q)
-          put(own, row, j * 4 + q, h, round_grad<F16>(quad(acc[i][j], q) * scale, make_uint2(0, 0), false));
+      for (int j = 0; j < 8; ++j)
+        put(own, row, 2 * j + (g >> 1), g & 1, round_grad<F16>(acc[i][j] * scale, make_uint2(0, 0), false));
     }
   }
   if (P == LM_LOGITS && !a.e) return;
