@@ -1186,12 +1186,17 @@ def _type(name) -> int:
     return _TYPES[name][0]
 
 
-def _on_gpu(t: torch.Tensor, name: str) -> int:
-    """Address of a tensor on the current GPU."""
-    if not t.is_cuda:
-        raise ValueError(f"{name} must be a GPU tensor (no CPU path exists)")
-    if t.get_device() != torch.cuda.current_device():
-        raise ValueError(f"{name} is on {t.device}, the library launches on cuda:{torch.cuda.current_device()}")
+def _here() -> int:
+    """The GPU that calls launch on."""
+    return torch._C._cuda_getDevice() if torch.cuda.is_initialized() else torch.cuda.current_device()
+
+
+def _on_gpu(t: torch.Tensor, name: str, here: int) -> int:
+    """Address of a tensor on the GPU that calls launch on."""
+    if t.get_device() != here:
+        if not t.is_cuda:
+            raise ValueError(f"{name} must be a GPU tensor (no CPU path exists)")
+        raise ValueError(f"{name} is on {t.device}, the library launches on cuda:{here}")
     return t.data_ptr()
 
 
@@ -1230,9 +1235,25 @@ def _vector(t, name: str, dtype: torch.dtype, n: int, required: bool = True) -> 
         raise ValueError(f"{name} must be contiguous")
 
 
-def _place(t, name: str):
-    """Address of a checked tensor, None for a missing or empty one."""
-    return None if t is None or t.numel() == 0 else _on_gpu(t, name)
+def _places(*pairs):
+    """Addresses of checked tensors, given as (tensor, name); None for a missing or empty one."""
+    here, out = None, []
+    for t, name in pairs:
+        if t is None or t.numel() == 0:
+            out.append(None)
+            continue
+        if here is None:
+            if not t.is_cuda:
+                raise ValueError(f"{name} must be a GPU tensor (no CPU path exists)")
+            here = _here()
+        out.append(_on_gpu(t, name, here))
+    return out
+
+
+def _workspace(ws: Optional[torch.Tensor]) -> None:
+    _expect(ws, "ws", torch.uint8, 1)
+    if not ws.is_contiguous():
+        raise ValueError("ws must be contiguous")
 
 
 def _rows_of(t, name: str) -> int:
@@ -1261,8 +1282,8 @@ def svl_embed(emb: svl_embedding, tokens: torch.Tensor, table: torch.Tensor, out
     _vector(tokens, "tokens", torch.int32, n)
     ldt = _matrix(table, "table", _TYPE_DTYPE.get(emb.table_type), emb.vocab, emb.width)
     ldo = _matrix(out, "out", _TYPE_DTYPE.get(emb.row_type), n, emb.width)
-    _check(load_library().svl_embed(ctypes.byref(emb), n, _place(tokens, "tokens"), _place(table, "table"), ldt,
-                                    _place(out, "out"), ldo, _launch_stream(stream)))
+    pt, pw, po = _places((tokens, "tokens"), (table, "table"), (out, "out"))
+    _check(load_library().svl_embed(ctypes.byref(emb), n, pt, pw, ldt, po, ldo, _launch_stream(stream)))
 
 
 def svl_embed_workspace_bytes(emb: svl_embedding, rows: int) -> int:
@@ -1281,11 +1302,10 @@ def svl_embed_backward(emb: svl_embedding, tokens: torch.Tensor, grad_rows: torc
     _vector(tokens, "tokens", torch.int32, n)
     ldr = _matrix(grad_rows, "grad_rows", _TYPE_DTYPE.get(emb.row_type), n, emb.width)
     ldt = _matrix(grad_table, "grad_table", _TYPE_DTYPE.get(emb.table_type), emb.vocab, emb.width)
-    _expect(ws, "ws", torch.uint8, 1)
-    _check(load_library().svl_embed_backward(
-        ctypes.byref(emb), n, _place(tokens, "tokens"), _place(grad_rows, "grad_rows"), ldr,
-        _place(grad_table, "grad_table"), ldt, int(accumulate), _dev(ws, "ws"), _nbytes(ws),
-        _launch_stream(stream)))
+    _workspace(ws)
+    pt, pr, pg, pw = _places((tokens, "tokens"), (grad_rows, "grad_rows"), (grad_table, "grad_table"), (ws, "ws"))
+    _check(load_library().svl_embed_backward(ctypes.byref(emb), n, pt, pr, ldr, pg, ldt, int(accumulate), pw,
+                                             _nbytes(ws), _launch_stream(stream)))
 
 
 def make_norm(width: int, kind: str = "rms", x: str = "f32", y: str = "bf16", gain: str = "bf16",
@@ -1320,9 +1340,9 @@ def svl_norm_forward(norm: svl_norm, x: torch.Tensor, gain: Optional[torch.Tenso
     ldy = _matrix(y, "y", _TYPE_DTYPE.get(norm.y_type), n, norm.width)
     _norm_weights(norm, gain, bias)
     _norm_stats(stats, n)
-    _check(load_library().svl_norm_forward(
-        ctypes.byref(norm), n, _place(x, "x"), ldx, _place(gain, "gain"), _place(bias, "bias"), _place(y, "y"), ldy,
-        _place(stats, "stats"), _launch_stream(stream)))
+    px, pg, pb, py, ps = _places((x, "x"), (gain, "gain"), (bias, "bias"), (y, "y"), (stats, "stats"))
+    _check(load_library().svl_norm_forward(ctypes.byref(norm), n, px, ldx, pg, pb, py, ldy, ps,
+                                           _launch_stream(stream)))
 
 
 def svl_norm_workspace_bytes(norm: svl_norm, rows: int) -> int:
@@ -1350,11 +1370,12 @@ def svl_norm_backward(norm: svl_norm, x: torch.Tensor, gain: Optional[torch.Tens
     _vector(grad_gain, "grad_gain", torch.float32, norm.width, required=False)
     _vector(grad_bias, "grad_bias", torch.float32, norm.width, required=False)
     if ws is not None:
-        _expect(ws, "ws", torch.uint8, 1)
+        _workspace(ws)
+    px, pg, ps, py, pdx, pdg, pdb, pw = _places(
+        (x, "x"), (gain, "gain"), (stats, "stats"), (grad_y, "grad_y"), (grad_x, "grad_x"), (grad_gain, "grad_gain"),
+        (grad_bias, "grad_bias"), (ws, "ws"))
     _check(load_library().svl_norm_backward(
-        ctypes.byref(norm), n, _place(x, "x"), ldx, _place(gain, "gain"), _place(stats, "stats"),
-        _place(grad_y, "grad_y"), ldy, _place(grad_x, "grad_x"), ldg, _place(grad_gain, "grad_gain"),
-        _place(grad_bias, "grad_bias"), int(accumulate), None if ws is None else _dev(ws, "ws"),
+        ctypes.byref(norm), n, px, ldx, pg, ps, py, ldy, pdx, ldg, pdg, pdb, int(accumulate), pw,
         0 if ws is None else _nbytes(ws), _launch_stream(stream)))
 
 
@@ -1393,11 +1414,12 @@ def svl_lm_loss(head: svl_lm_head, x: torch.Tensor, w: torch.Tensor, labels: tor
     _vector(row_weight, "row_weight", torch.float32, n, required=False)
     ldgx = 0 if grad_x is None else _matrix(grad_x, "grad_x", dt, n, D)
     ldgw = 0 if grad_w is None else _matrix(grad_w, "grad_w", dt, V, D)
-    _expect(ws, "ws", torch.uint8, 1)
-    _check(load_library().svl_lm_loss(
-        ctypes.byref(head), n, _place(x, "x"), ldx, _place(w, "w"), ldw, _place(labels, "labels"),
-        _place(row_weight, "row_weight"), _place(loss, "loss"), _place(lse, "lse"), _place(grad_x, "grad_x"), ldgx,
-        _place(grad_w, "grad_w"), ldgw, int(accumulate), _dev(ws, "ws"), _nbytes(ws), _launch_stream(stream)))
+    _workspace(ws)
+    px, pw, pl, pr, po, ps, pdx, pdw, pws = _places(
+        (x, "x"), (w, "w"), (labels, "labels"), (row_weight, "row_weight"), (loss, "loss"), (lse, "lse"),
+        (grad_x, "grad_x"), (grad_w, "grad_w"), (ws, "ws"))
+    _check(load_library().svl_lm_loss(ctypes.byref(head), n, px, ldx, pw, ldw, pl, pr, po, ps, pdx, ldgx, pdw, ldgw,
+                                      int(accumulate), pws, _nbytes(ws), _launch_stream(stream)))
 
 
 def make_adamw(lr: float, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8, weight_decay: float = 0.0,
@@ -1456,7 +1478,9 @@ class AdamwTensors:
                 x = t.get(k)
                 if x is None or x.numel() == 0:
                     continue
-                place[k] = _on_gpu(x, f"{k} of tensor {i}")
+                if not x.is_cuda:
+                    raise ValueError(f"{k} of tensor {i} must be a GPU tensor (no CPU path exists)")
+                place[k] = _on_gpu(x, f"{k} of tensor {i}", _here())
                 self.device = x.get_device()
             self.array[i] = svl_adamw_tensor(n=t["param"].numel(), param_type=_DTYPE_TYPE[t["param"].dtype],
                                              grad_type=_DTYPE_TYPE[t["grad"].dtype], **place)
@@ -1471,9 +1495,8 @@ def svl_adamw_step(adam: svl_adamw, tensors, step: int = 1, seed: int = 0, grad_
         tensors = AdamwTensors(tensors)
     if tensors.tensors and tensors.state_bits != adam.state_bits:
         raise ValueError(f"states of {tensors.state_bits} bits, the description says {adam.state_bits}")
-    if tensors.device is not None and tensors.device != torch.cuda.current_device():
-        raise ValueError(f"the tensors are on cuda:{tensors.device}, the library launches on "
-                         f"cuda:{torch.cuda.current_device()}")
+    if tensors.device is not None and tensors.device != _here():
+        raise ValueError(f"the tensors are on cuda:{tensors.device}, the library launches on cuda:{_here()}")
     if dev is not None and (not isinstance(dev, torch.Tensor) or dev.element_size() != 4 or dev.numel() < 5):
         raise ValueError("dev must hold 5 words of 32 bits")
     _check(load_library().svl_adamw_step(

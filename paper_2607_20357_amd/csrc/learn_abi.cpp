@@ -423,7 +423,7 @@ svl_status svl_lm_loss(const svl_lm_head* head, int32_t rows, const void* x, int
     for (a.chunk0 = 0; e == hipSuccess && a.chunk0 < rows; a.chunk0 += a.chunk) {
       a.first = a.chunk0 == 0;
       a.last = a.chunk0 + a.chunk >= rows;
-      if (e == hipSuccess) e = launch_lm_product(a, LM_LOGITS, f16, st);
+      if (e == hipSuccess) e = rows <= LM_FEW ? launch_lm_few_logits(a, f16, st) : launch_lm_product(a, LM_LOGITS, f16, st);
       if (e == hipSuccess) e = launch_lm_stats(a, st);
       if (e == hipSuccess && a.e) e = launch_lm_softmax(a, f16, st);
       if (e == hipSuccess && grad_x) e = launch_lm_product(a, LM_GRAD_X, f16, st);

@@ -11,6 +11,8 @@ constexpr int32_t LM_TILE = 256;     // rows and columns of a product's tile
 constexpr int32_t LM_BK = 64;        // of its sum a step
 constexpr int32_t LM_ROWS = 64;      // labelled rows are filled up with zeros to a multiple
 constexpr int32_t LM_SLAB = 128;     // vocabulary entries whose exponentials share a maximum
+constexpr int32_t LM_FEW = 64;       // rows of a call whose logits a wave's products take straight from memory
+constexpr int32_t LM_PACK = 1024;    // rows of a call that are packed in one launch
 constexpr int32_t LM_PARTS = 256;    // most workgroups (tiles x pieces) of a product whose sum is cut
 constexpr int32_t LM_CUT = 8;        // least steps of LM_BK of a piece of a sum
 // Exponentials are held as fp16 under 2^14 (normal down to 2^-28 of their slab's largest), P
@@ -68,6 +70,7 @@ hipError_t launch_lm_rows(const LmArgs& a, hipStream_t st);                 // l
 hipError_t launch_lm_stats(const LmArgs& a, hipStream_t st);                // log-sums and losses
 hipError_t launch_lm_softmax(const LmArgs& a, bool f16, hipStream_t st);    // exponentials to P
 hipError_t launch_lm_product(const LmArgs& a, LmProduct p, bool f16, hipStream_t st);
+hipError_t launch_lm_few_logits(const LmArgs& a, bool f16, hipStream_t st); // logits of at most LM_FEW rows
 hipError_t launch_lm_zero_w(const LmArgs& a, hipStream_t st);               // a call without rows
 
 }  // namespace svl

@@ -78,6 +78,156 @@ __global__ __launch_bounds__(NT) void lm_pack_kernel(LmArgs a, int packed) {
       *reinterpret_cast<uint4*>(a.grad_x + (int64_t)i * a.ldgx + c) = zero;
 }
 
+// Both at once for a call of few rows: each workgroup counts the labels before its row by itself.
+__global__ __launch_bounds__(NT) void lm_pack_few_kernel(LmArgs a) {
+  __shared__ int s_n[NT / 64][2];
+  __shared__ float s_w[NT / 64];
+  const int i = blockIdx.x, tid = threadIdx.x, lane = tid & 63;
+  int before = 0, all = 0;
+  float top = 0.f;
+  for (int b = 0; b < a.rows; b += NT) {
+    const int r = b + tid, label = r < a.rows ? a.labels[r] : -1;
+    const bool has = label >= 0 && label < a.vocab;
+    if (has && i == 0) top = fmaxf(top, a.row_weight ? fabsf(a.row_weight[r]) : 1.f);
+    all += __popcll(__ballot(has));
+    before += __popcll(__ballot(has && r < i));
+  }
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
+  if (lane == 0) {
+    s_n[tid >> 6][0] = before;
+    s_n[tid >> 6][1] = all;
+    s_w[tid >> 6] = top;
+  }
+  __syncthreads();
+  before = all = 0;
+#pragma unroll
+  for (int k = 0; k < NT / 64; ++k) {
+    before += s_n[k][0];
+    all += s_n[k][1];
+    top = fmaxf(top, s_w[k]);
+  }
+  if (i == 0 && tid == 0) *a.head = LmHead{all, top};
+  const uint4 zero = make_uint4(0, 0, 0, 0);
+  if (i >= a.rows) {      // rows of zeros behind the last
+    const int to = all + i - a.rows;
+    if (to < (all + LM_ROWS - 1) / LM_ROWS * LM_ROWS)
+      for (int c = tid * 8; c < a.d; c += NT * 8) *reinterpret_cast<uint4*>(a.xc + (int64_t)to * a.d + c) = zero;
+    return;
+  }
+  const int label = a.labels[i];
+  if (label >= 0 && label < a.vocab) {
+    if (tid == 0) {
+      a.row_of[before] = i;
+      a.label[before] = label;
+      a.weight[before] = a.row_weight ? a.row_weight[i] : 1.f;
+    }
+    for (int c = tid * 8; c < a.d; c += NT * 8)
+      *reinterpret_cast<uint4*>(a.xc + (int64_t)before * a.d + c) =
+          *reinterpret_cast<const uint4*>(a.x + (int64_t)i * a.ldx + c);
+    return;
+  }
+  if (tid == 0) {
+    a.loss[i] = 0.f;
+    if (a.lse) a.lse[i] = 0.f;
+  }
+  if (a.grad_x)
+    for (int c = tid * 8; c < a.d; c += NT * 8)
+      *reinterpret_cast<uint4*>(a.grad_x + (int64_t)i * a.ldgx + c) = zero;
+}
+
+// Logits of at most 16 NB rows: w is what there is to read, and is read once.  A workgroup takes a slab of
+// the vocabulary, a wave 16 entries of it and their whole rows, straight into the products' registers;
+// the rows of x come from the caches.  Results as lm_gemm.hip's.
+template <int NB, bool F16>
+__global__ __launch_bounds__(512) void lm_few_logits_kernel(LmArgs a) {
+  __shared__ float s_top[8][NB * 16], s_sum[8][NB * 16];
+  const int rows = a.head->rows;
+  if (rows == 0) return;
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, g = lane >> 4, l = lane & 15;
+  const int m0 = blockIdx.x * LM_SLAB + w * 16;
+  const int v = m0 + l < a.vocab ? m0 + l : a.vocab - 1;
+  const uint16_t* pw = a.w + (int64_t)v * a.ldw + g * 8;
+  const uint16_t* px[NB];
+#pragma unroll
+  for (int b = 0; b < NB; ++b) {
+    const int r = b * 16 + l < rows ? b * 16 + l : rows - 1;
+    px[b] = a.xc + (int64_t)r * a.d + g * 8;
+  }
+  typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+  const auto load = [](const uint16_t* p) { return *reinterpret_cast<const uint4*>(p); };
+  const auto once = [](const uint16_t* p) {
+    return __builtin_bit_cast(uint4, __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p)));
+  };
+  floatx4 acc[NB];
+#pragma unroll
+  for (int b = 0; b < NB; ++b) acc[b] = floatx4{0.f, 0.f, 0.f, 0.f};
+  constexpr int DEEP = NB == 4 ? 4 : 8;     // loads of w in flight, 1 KB each a wave
+  int k = 0;
+  for (; k + 32 * DEEP <= a.d; k += 32 * DEEP) {
+    uint4 wf[DEEP], xf[DEEP][NB];
+#pragma unroll
+    for (int i = 0; i < DEEP; ++i) wf[i] = once(pw + k + 32 * i);
+#pragma unroll
+    for (int i = 0; i < DEEP; ++i)
+#pragma unroll
+      for (int b = 0; b < NB; ++b) xf[i][b] = load(px[b] + k + 32 * i);
+#pragma unroll
+    for (int i = 0; i < DEEP; ++i)
+#pragma unroll
+      for (int b = 0; b < NB; ++b) acc[b] = mfma16x16x32<F16>(wf[i], xf[i][b], acc[b]);
+  }
+  for (; k < a.d; k += 32) {
+    const uint4 wf = once(pw + k);
+#pragma unroll
+    for (int b = 0; b < NB; ++b) acc[b] = mfma16x16x32<F16>(wf, load(px[b] + k), acc[b]);
+  }
+  float top[NB];
+#pragma unroll
+  for (int b = 0; b < NB; ++b) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (m0 + 4 * g + i >= a.vocab) acc[b][i] = -INFINITY;
+    top[b] = fmaxf(fmaxf(acc[b][0], acc[b][1]), fmaxf(acc[b][2], acc[b][3]));
+    top[b] = fmaxf(top[b], __shfl_xor(top[b], 16, 64));
+    top[b] = fmaxf(top[b], __shfl_xor(top[b], 32, 64));
+    if (g == 0) s_top[w][b * 16 + l] = top[b];
+  }
+  __syncthreads();
+#pragma unroll
+  for (int b = 0; b < NB; ++b) {
+    const int n = b * 16 + l;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) top[b] = fmaxf(top[b], s_top[i][n]);
+    const int label = n < rows ? a.label[n] - m0 - 4 * g : -1;
+    const float from = top[b] == -INFINITY ? 0.f : top[b];
+    float sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if (i == label) a.label_logit[n] = acc[b][i];
+      acc[b][i] = expf(acc[b][i] - from);
+      sum += acc[b][i];
+    }
+    sum += __shfl_xor(sum, 16, 64);
+    sum += __shfl_xor(sum, 32, 64);
+    if (g == 0) s_sum[w][n] = sum;
+    if (a.e && n < rows)
+      *reinterpret_cast<uint2*>(a.e + (int64_t)n * a.vp + m0 + 4 * g) =
+          make_uint2(pack_act2<true>(acc[b][0] * LM_E_SCALE, acc[b][1] * LM_E_SCALE),
+                     pack_act2<true>(acc[b][2] * LM_E_SCALE, acc[b][3] * LM_E_SCALE));
+  }
+  __syncthreads();
+  const int n = threadIdx.x;
+  if (n >= NB * 16 || n >= rows) return;
+  float sum = 0.f, most = -INFINITY;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    sum += s_sum[i][n];
+    most = fmaxf(most, s_top[i][n]);
+  }
+  a.stats[(int64_t)n * (a.vp / LM_SLAB) + blockIdx.x] = make_float2(most, sum);
+}
+
 // A row a wave.
 __global__ __launch_bounds__(NT) void lm_stats_kernel(LmArgs a) {
   const int i = blockIdx.x * (NT / 64) + (threadIdx.x >> 6), lane = threadIdx.x & 63;
@@ -138,6 +288,10 @@ __global__ __launch_bounds__(NT) void lm_zero_w_kernel(uint16_t* w, int64_t ld, 
 }  // namespace
 
 hipError_t launch_lm_rows(const LmArgs& a, hipStream_t st) {
+  if (a.rows <= LM_PACK) {
+    lm_pack_few_kernel<<<a.rows + LM_ROWS, NT, 0, st>>>(a);
+    return hipGetLastError();
+  }
   lm_count_kernel<<<1, 1024, 0, st>>>(a);
   const int packed = (a.rows + LM_ROWS - 1) / LM_ROWS * LM_ROWS;
   lm_pack_kernel<<<packed + a.rows, NT, 0, st>>>(a, packed);
@@ -153,6 +307,21 @@ hipError_t launch_lm_softmax(const LmArgs& a, bool f16, hipStream_t st) {
   const dim3 grid((a.chunk + LM_ROWS - 1) / LM_ROWS * LM_ROWS, (a.vp + NT * 8 - 1) / (NT * 8));
   if (f16) lm_softmax_kernel<true><<<grid, NT, 0, st>>>(a);
   else lm_softmax_kernel<false><<<grid, NT, 0, st>>>(a);
+  return hipGetLastError();
+}
+
+hipError_t launch_lm_few_logits(const LmArgs& a, bool f16, hipStream_t st) {
+  const uint32_t slabs = a.vp / LM_SLAB;
+  if (a.rows <= 16) {
+    if (f16) lm_few_logits_kernel<1, true><<<slabs, 512, 0, st>>>(a);
+    else lm_few_logits_kernel<1, false><<<slabs, 512, 0, st>>>(a);
+  } else if (a.rows <= 32) {
+    if (f16) lm_few_logits_kernel<2, true><<<slabs, 512, 0, st>>>(a);
+    else lm_few_logits_kernel<2, false><<<slabs, 512, 0, st>>>(a);
+  } else {
+    if (f16) lm_few_logits_kernel<4, true><<<slabs, 512, 0, st>>>(a);
+    else lm_few_logits_kernel<4, false><<<slabs, 512, 0, st>>>(a);
+  }
   return hipGetLastError();
 }
 
