@@ -147,14 +147,16 @@ __global__ __launch_bounds__(512) void lm_few_logits_kernel(LmArgs a) {
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, g = lane >> 4, l = lane & 15;
   const int m0 = blockIdx.x * LM_SLAB + w * 16;
   const int v = m0 + l < a.vocab ? m0 + l : a.vocab - 1;
-  const uint16_t* pw = a.w + (int64_t)v * a.ldw + g * 8;
+  const uint16_t* pw = a.w + (int64_t)v * a.ldw + g * 16;
   const uint16_t* px[NB];
 #pragma unroll
   for (int b = 0; b < NB; ++b) {
     const int r = b * 16 + l < rows ? b * 16 + l : rows - 1;
-    px[b] = a.xc + (int64_t)r * a.d + g * 8;
+    px[b] = a.xc + (int64_t)r * a.d + g * 16;
   }
+  // Of 64 of the sum a lane takes 16 in a row, 8 for each of two products: a line is asked for whole.
   typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+  const auto at = [](int i) { return 64 * (i / 2) + 8 * (i & 1); };
   const auto load = [](const uint16_t* p) { return *reinterpret_cast<const uint4*>(p); };
   const auto once = [](const uint16_t* p) {
     return __builtin_bit_cast(uint4, __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p)));
@@ -162,26 +164,37 @@ __global__ __launch_bounds__(512) void lm_few_logits_kernel(LmArgs a) {
   floatx4 acc[NB];
 #pragma unroll
   for (int b = 0; b < NB; ++b) acc[b] = floatx4{0.f, 0.f, 0.f, 0.f};
-  constexpr int DEEP = NB == 4 ? 4 : 8;     // loads of w in flight, 1 KB each a wave
+  constexpr int DEEP = NB == 4 ? 4 : 8;     // loads of w ahead, 1 KB each a wave, beside as many in use
   int k = 0;
-  for (; k + 32 * DEEP <= a.d; k += 32 * DEEP) {
-    uint4 wf[DEEP], xf[DEEP][NB];
+  if (a.d >= 32 * DEEP) {
+    uint4 next[DEEP];
 #pragma unroll
-    for (int i = 0; i < DEEP; ++i) wf[i] = once(pw + k + 32 * i);
+    for (int i = 0; i < DEEP; ++i) next[i] = once(pw + at(i));
+    for (; k + 32 * DEEP <= a.d; k += 32 * DEEP) {
+      uint4 wf[DEEP], xf[DEEP][NB];
 #pragma unroll
-    for (int i = 0; i < DEEP; ++i)
+      for (int i = 0; i < DEEP; ++i)
 #pragma unroll
-      for (int b = 0; b < NB; ++b) xf[i][b] = load(px[b] + k + 32 * i);
+        for (int b = 0; b < NB; ++b) xf[i][b] = load(px[b] + k + at(i));
 #pragma unroll
-    for (int i = 0; i < DEEP; ++i)
+      for (int i = 0; i < DEEP; ++i) wf[i] = next[i];
+      const int ahead = k + 64 * DEEP <= a.d ? k + 32 * DEEP : k;    // (the last ones once more)
 #pragma unroll
-      for (int b = 0; b < NB; ++b) acc[b] = mfma16x16x32<F16>(wf[i], xf[i][b], acc[b]);
+      for (int i = 0; i < DEEP; ++i) next[i] = once(pw + ahead + at(i));
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int i = 0; i < DEEP; ++i)
+#pragma unroll
+        for (int b = 0; b < NB; ++b) acc[b] = mfma16x16x32<F16>(wf[i], xf[i][b], acc[b]);
+    }
   }
-  for (; k < a.d; k += 32) {
-    const uint4 wf = once(pw + k);
+  for (; k < a.d; k += 64)
 #pragma unroll
-    for (int b = 0; b < NB; ++b) acc[b] = mfma16x16x32<F16>(wf, load(px[b] + k), acc[b]);
-  }
+    for (int i = 0; i < 2; ++i) {
+      const uint4 wf = once(pw + k + at(i));
+#pragma unroll
+      for (int b = 0; b < NB; ++b) acc[b] = mfma16x16x32<F16>(wf, load(px[b] + k + at(i)), acc[b]);
+    }
   float top[NB];
 #pragma unroll
   for (int b = 0; b < NB; ++b) {
