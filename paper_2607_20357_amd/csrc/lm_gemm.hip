@@ -18,8 +18,7 @@
 namespace svl {
 namespace {
 
-constexpr int NT = 256;              // 4 waves of 128 x 128
-constexpr int STEP = LM_TILE * LM_BK;   // elements of an operand's step
+constexpr int NT = 256;              // 4 waves, 2 along m and 2 along n, of W x W: tiles of 2 W x 2 W
 
 // 16 bytes a lane from memory to LDS, from `to` on in lane order.  (The builtin would do, but
 // for the compiler every transposed LDS read after it may be of what it brings: it waits
@@ -31,13 +30,15 @@ __device__ __forceinline__ void load_to_lds(const u32x4& rsrc, uint32_t voff, ui
 
 __device__ __forceinline__ int wave_id() { return __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6); }
 
-// One operand's steps.  TR: rows along the sum; ENDS: they end inside a step.
-template <bool TR, bool ENDS>
+// One operand's steps of T rows (or columns).  TR: rows along the sum; ENDS: they end inside a step.
+template <bool TR, bool ENDS, int T>
 struct Operand {
+  static constexpr int LOADS = T / 32;      // of a wave a step
+  static constexpr int PER = T == 256 ? 2 : 4;   // TR: rows of a load
   const uint16_t* p;      // of the tile's first row (TR: first column), first k
   int64_t ld;
   int32_t k;              // length of the sum, where rows along it end (TR)
-  uint32_t voff[8];
+  uint32_t voff[LOADS];
   u32x4 rs;
   int left;
 
@@ -47,11 +48,11 @@ struct Operand {
     k = k_;
     p = base + (TR ? (int64_t)first : (int64_t)first * ld);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
+    for (int i = 0; i < LOADS; ++i) {
       if constexpr (TR) {
-        // two rows of 256 columns; pairs of pieces change places by the row
-        const int r = (i * 4 + w) * 2 + (lane >> 5), at = lane & 31;
-        int piece = (((at >> 1) ^ ((r & 3) | ((r >> 3 & 3) << 2))) << 1) | (at & 1);
+        // PER rows of T columns; pairs of pieces change places by the row
+        const int r = (i * 4 + w) * PER + lane / (64 / PER), at = lane % (64 / PER);
+        int piece = (((at >> 1) ^ ((r & 3) | ((r >> 3 & (T / 64 - 1)) << 2))) << 1) | (at & 1);
         const int most = (count - first) / 8 - 1;     // (widths are multiples of 8)
         piece = piece < most ? piece : most;
         voff[i] = (uint32_t)r * ((uint32_t)ld * 2) + piece * 16;
@@ -72,11 +73,11 @@ struct Operand {
     rs = u32x4{(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)a),
                (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(a >> 32)) & 0xffffu, 0x7fffffffu, 0x00020000u};
   }
-  // The wave's load i of 8.  Rows behind the last of the sum are taken to be the last: P is 0 there.
+  // The wave's load i.  Rows behind the last of the sum are taken to be the last: P is 0 there.
   __device__ __forceinline__ void fetch(int i, uint32_t lds) const {
     uint32_t v = voff[i];
     if (ENDS && left < LM_BK) {
-      const int over = (i * 4 + wave_id()) * 2 + (int)((threadIdx.x & 63) >> 5) - (left - 1);
+      const int over = (i * 4 + wave_id()) * PER + (int)(threadIdx.x & 63) / (64 / PER) - (left - 1);
       v -= over > 0 ? (uint32_t)over * ((uint32_t)ld * 2) : 0u;
     }
     load_to_lds(rs, v, lds + i * 4096);
@@ -84,13 +85,13 @@ struct Operand {
 };
 
 // Fragments of 16 rows (or columns) of a step, from `first` on, 32 of the sum each.
-template <bool TR>
+template <bool TR, int T>
 struct Fragments {
   uint32_t at;          // bytes
   __device__ __forceinline__ void init(int first) {
     const int lane = threadIdx.x & 63, g = lane >> 4, l = lane & 15;
     if constexpr (TR)
-      at = (uint32_t)((8 * g + l / 4) * LM_TILE * 2 + (((first / 16) ^ (l / 4 | g << 2)) * 32) + (l & 3) * 8);
+      at = (uint32_t)((8 * g + l / 4) * T * 2 + (((first / 16) ^ (l / 4 | (g & (T / 64 - 1)) << 2)) * 32) + (l & 3) * 8);
     else
       at = (uint32_t)((first + l) * LM_BK * 2 + ((g ^ (l >> 1)) * 16));
   }
@@ -103,8 +104,8 @@ struct Fragments {
   }
   static __device__ __forceinline__ u32x4 read(uint32_t place, int block, int half) {
     if constexpr (TR) {
-      const uint32_t q = (place ^ (block * 32)) + half * 64 * LM_TILE;
-      const uint2 a = read_tr(q), b = read_tr(q + 8 * LM_TILE);
+      const uint32_t q = (place ^ (block * 32)) + half * 64 * T;
+      const uint2 a = read_tr(q), b = read_tr(q + 8 * T);
       return u32x4{a.x, a.y, b.x, b.y};
     } else {
       return *(__attribute__((address_space(3))) const u32x4*)(uintptr_t)((place ^ (half * 64)) + block * 32 * LM_BK);
@@ -214,14 +215,16 @@ __device__ __forceinline__ void add_grad_w(const LmArgs& a, int n, int m, float 
   for (int i = 0; i < N; ++i) out[4 * i] = round_grad<F16>(v[i] * scale, old[i], a.accumulate);
 }
 
-// A wave's 128 rows of 128 16-bit results pass through its quarter of LDS, so that they leave in
-// whole lines: 8 bytes (a half of the 16-byte piece) in, 16 bytes of 4 rows out; pieces change
+// A wave's W rows of W 16-bit results pass through its part of LDS, so that they leave in
+// whole lines: 8 bytes (a half of the 16-byte piece) in, 16 bytes of a few rows out; pieces change
 // places by the row against bank conflicts.
+template <int W>
 __device__ __forceinline__ void put(uint16_t* own, int row, int piece, int half, uint2 v) {
-  *reinterpret_cast<uint2*>(own + row * 128 + (piece ^ (row & 15)) * 8 + half * 4) = v;
+  *reinterpret_cast<uint2*>(own + row * W + (piece ^ (row & (W / 8 - 1))) * 8 + half * 4) = v;
 }
+template <int W>
 __device__ __forceinline__ u32x4 get(const uint16_t* own, int row, int piece) {
-  return *reinterpret_cast<const u32x4*>(own + row * 128 + (piece ^ (row & 15)) * 8);
+  return *reinterpret_cast<const u32x4*>(own + row * W + (piece ^ (row & (W / 8 - 1))) * 8);
 }
 
 // Logits of 128 entries of the vocabulary (a wave's) become exponentials under their
@@ -274,23 +277,26 @@ __device__ __forceinline__ void store_logits(const LmArgs& a, int m0, int n, boo
   if (!a.e) return;
 #pragma unroll
   for (int b = 0; b < 8; ++b)
-    put(own, row, 2 * b + (g >> 1), g & 1,
+    put<LM_SLAB>(own, row, 2 * b + (g >> 1), g & 1,
         make_uint2(pack_act2<true>(acc[b][0], acc[b][1]), pack_act2<true>(acc[b][2], acc[b][3])));
 }
 
-template <LmProduct P, bool F16>
-__global__ __launch_bounds__(NT, 1) void lm_product_kernel(LmArgs a) {
+template <LmProduct P, bool F16, int W>
+__global__ __launch_bounds__(NT, W == 128 ? 1 : 2) void lm_product_kernel(LmArgs a) {
+  constexpr int T = 2 * W, NB = W / 16, STEP = T * LM_BK;   // tile, a wave's blocks a side, elements of an operand's step
+  static_assert(P == LM_GRAD_W || W == 128, "");            // (a slab is a wave's; sums are cut in tiles of LM_TILE)
   constexpr bool TA = P != LM_LOGITS, TB = P == LM_GRAD_W;
-  __shared__ __attribute__((aligned(1024))) uint16_t lds[5 * STEP];   // all 160 KB: three steps of one operand, two of the other
+  __shared__ __attribute__((aligned(1024))) uint16_t lds[5 * STEP];   // three steps of one operand, two of the other: 160 or 80 KB
   const Sizes s = sizes_of(a, P);
   Tile t;
-  if (!tile_of((s.m + LM_TILE - 1) / LM_TILE, (s.n + LM_TILE - 1) / LM_TILE, s.nk, P != LM_LOGITS, &t)) return;
-  const int m0 = t.m * LM_TILE, n0 = t.n * LM_TILE;
+  if (!tile_of((s.m + T - 1) / T, (s.n + T - 1) / T, s.nk, P != LM_LOGITS && T == LM_TILE, &t)) return;
+  const int m0 = t.m * T, n0 = t.n * T;
   const int kt0 = (int)((int64_t)s.nk * t.piece / t.pieces), kt1 = (int)((int64_t)s.nk * (t.piece + 1) / t.pieces);
 
   const uint16_t* xc = a.xc + (int64_t)a.chunk0 * a.d;
-  Operand<TA, P == LM_GRAD_X> A;
-  Operand<TB, false> B;
+  Operand<TA, P == LM_GRAD_X, T> A;
+  Operand<TB, false, T> B;
+  constexpr int LOADS = Operand<TA, false, T>::LOADS;
   if constexpr (P == LM_LOGITS) {
     A.init(a.w, a.ldw, m0, a.vocab, a.d);
     B.init(xc, a.d, n0, s.n, a.d);
@@ -301,17 +307,17 @@ __global__ __launch_bounds__(NT, 1) void lm_product_kernel(LmArgs a) {
     A.init(xc, a.d, m0, a.d, s.nk * LM_BK);
     B.init(a.e, a.vp, n0, a.vp, s.nk * LM_BK);
   }
-  const int w = wave_id(), wm = w & 1, wn = w >> 1;   // (128 x 128: 2 fragments read for 4 x 4 products)
-  Fragments<TA> fa;
-  Fragments<TB> fb;
-  fa.init(wm * 128);
-  fb.init(wn * 128);
+  const int w = wave_id(), wm = w & 1, wn = w >> 1;
+  Fragments<TA, T> fa;
+  Fragments<TB, T> fb;
+  fa.init(wm * W);
+  fb.init(wn * W);
 
-  floatx4 acc[8][8];
+  floatx4 acc[NB][NB];
 #pragma unroll
-  for (int i = 0; i < 8; ++i)
+  for (int i = 0; i < NB; ++i)
 #pragma unroll
-    for (int j = 0; j < 8; ++j) acc[i][j] = floatx4{0.f, 0.f, 0.f, 0.f};
+    for (int j = 0; j < NB; ++j) acc[i][j] = floatx4{0.f, 0.f, 0.f, 0.f};
 
   // While half a step's fragments, in registers, are multiplied, the next half's are read and loads of
   // a later step go out: in the first half the deep operand's of two steps on, in the second the other's
@@ -323,7 +329,7 @@ __global__ __launch_bounds__(NT, 1) void lm_product_kernel(LmArgs a) {
   const uint32_t other = 3 * 2 * STEP;     // the other operand's buffers are behind the deep one's
   const uint32_t mine = __builtin_amdgcn_readfirstlane((int)(base + w * 1024));
   struct Frags {
-    u32x4 a[8], b[8];
+    u32x4 a[NB], b[NB];
   };
   const auto at_step = [&](bool deep, int t) {
     t = t < kt1 ? t : kt1 - 1;
@@ -332,7 +338,7 @@ __global__ __launch_bounds__(NT, 1) void lm_product_kernel(LmArgs a) {
   const auto fetch = [&](bool deep, int i, uint32_t buf) {
     if (deep == DEEP_A) A.fetch(i, mine + buf); else B.fetch(i, mine + buf);
   };
-  // Fragment i of 16 of a half, in the order in which the products take them.
+  // Fragment i of a half, in the order in which the products take them.
   const auto read = [&](Frags& f, int i, uint32_t pa, uint32_t pb, int half) {
     if (i % 2 == 0) f.b[i / 2] = fb.read(pb, i / 2, half);
     else f.a[i / 2] = fa.read(pa, i / 2, half);
@@ -340,10 +346,10 @@ __global__ __launch_bounds__(NT, 1) void lm_product_kernel(LmArgs a) {
   // Products of `f`, with the reads of half `half` of the step at pa, pb and the loads into `to` between them.
   const auto multiply = [&](const Frags& f, Frags& next, uint32_t pa, uint32_t pb, int half, bool deep, uint32_t to) {
 #pragma unroll
-    for (int i = 0; i < 64; ++i) {
-      mfma<F16>(f.a[i / 8], f.b[i % 8], acc[i % 8][i / 8]);
-      if (i % 4 == 0) read(next, i / 4, pa, pb, half);
-      if (i % 8 == 3) fetch(deep, i / 8, to);
+    for (int i = 0; i < NB * NB; ++i) {
+      mfma<F16>(f.a[i / NB], f.b[i % NB], acc[i % NB][i / NB]);
+      if (i % (NB / 2) == 0) read(next, i / (NB / 2), pa, pb, half);
+      if (i % NB == NB / 2 - 1) fetch(deep, i / NB, to);
       __builtin_amdgcn_sched_barrier(0);
     }
     wait_lds();
@@ -360,15 +366,15 @@ __global__ __launch_bounds__(NT, 1) void lm_product_kernel(LmArgs a) {
       at_step(true, kt0 + i);
       at_step(false, kt0 + i);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) fetch(true, j, i * 2 * STEP);
+      for (int j = 0; j < LOADS; ++j) fetch(true, j, i * 2 * STEP);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) fetch(false, j, other + i * 2 * STEP);
+      for (int j = 0; j < LOADS; ++j) fetch(false, j, other + i * 2 * STEP);
     }
-    wait_loads<16>();
+    wait_loads<2 * LOADS>();
     turn();
     places(0, 0, pa, pb);
 #pragma unroll
-    for (int i = 0; i < 16; ++i) read(f0, i, pa, pb, 0);
+    for (int i = 0; i < 2 * NB; ++i) read(f0, i, pa, pb, 0);
     wait_lds();
     uint32_t deep = 0, shallow = 0;      // buffers of step t
 #pragma unroll 1
@@ -376,7 +382,7 @@ __global__ __launch_bounds__(NT, 1) void lm_product_kernel(LmArgs a) {
       const uint32_t deep1 = deep == 4 * STEP ? 0 : deep + 2 * STEP, deep2 = deep1 == 4 * STEP ? 0 : deep1 + 2 * STEP;
       at_step(true, t + 2);
       multiply(f0, f1, pa, pb, 1, true, deep2);
-      wait_loads<8>();                   // step t + 1 of both; what is on its way is of step t + 2
+      wait_loads<LOADS>();               // step t + 1 of both; what is on its way is of step t + 2
       turn();
       places(deep1, shallow ^ 2 * STEP, pa, pb);
       at_step(false, t + 2);
@@ -389,24 +395,23 @@ __global__ __launch_bounds__(NT, 1) void lm_product_kernel(LmArgs a) {
   }
 
   // Element i of a block's lane is 4 (lane / 16) + i along m, lane % 16 along n.
-  const int lane = threadIdx.x & 63, g = lane >> 4, m = m0 + wm * 128;
+  const int lane = threadIdx.x & 63, g = lane >> 4, m = m0 + wm * W;
   if (P != LM_LOGITS && t.pieces > 1) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      float* part = a.parts + (int64_t)t.id * LM_TILE * LM_TILE + (int64_t)(wn * 128 + i * 16 + (lane & 15)) * LM_TILE +
-                    wm * 128 + g * 4;
+    for (int i = 0; i < NB; ++i) {
+      float* part = a.parts + (int64_t)t.id * T * T + (int64_t)(wn * W + i * 16 + (lane & 15)) * T + wm * W + g * 4;
 #pragma unroll
-      for (int j = 0; j < 8; ++j) *reinterpret_cast<floatx4*>(part + j * 16) = acc[i][j];
+      for (int j = 0; j < NB; ++j) *reinterpret_cast<floatx4*>(part + j * 16) = acc[i][j];
     }
     return;
   }
   const float scale = P == LM_LOGITS ? 1.f : grad_scale<F16>(a);
   if (P == LM_GRAD_W && (a.accumulate || a.sum_w)) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const int n = n0 + wn * 128 + i * 16 + (lane & 15);
+    for (int i = 0; i < NB; ++i) {
+      const int n = n0 + wn * W + i * 16 + (lane & 15);
 #pragma unroll
-      for (int j = 0; j < 8; j += 4) {
+      for (int j = 0; j < NB; j += 4) {
         if (n >= s.n || m + j * 16 >= s.m) continue;         // (d is a multiple of 64)
         floatx4 v[4] = {acc[i][j], acc[i][j + 1], acc[i][j + 2], acc[i][j + 3]};
         add_grad_w<F16>(a, n, m + j * 16 + g * 4, scale, v);
@@ -415,27 +420,28 @@ __global__ __launch_bounds__(NT, 1) void lm_product_kernel(LmArgs a) {
     return;
   }
   turn();                                  // all are done with the steps
-  uint16_t* own = lds + w * (128 * 128);
+  uint16_t* own = lds + w * (W * W);
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const int row = i * 16 + (lane & 15), n = n0 + wn * 128 + row;
+  for (int i = 0; i < NB; ++i) {
+    const int row = i * 16 + (lane & 15), n = n0 + wn * W + row;
     if constexpr (P == LM_LOGITS) {
       store_logits<F16>(a, m, n, n < s.n, own, row, acc[i]);
     } else {
 #pragma unroll
-      for (int j = 0; j < 8; ++j)
-        put(own, row, 2 * j + (g >> 1), g & 1, round_grad<F16>(acc[i][j] * scale, make_uint2(0, 0), false));
+      for (int j = 0; j < NB; ++j)
+        put<W>(own, row, 2 * j + (g >> 1), g & 1, round_grad<F16>(acc[i][j] * scale, make_uint2(0, 0), false));
     }
   }
   if (P == LM_LOGITS && !a.e) return;
   wave_lds_handoff();
-  const int piece = lane & 15, col = m + piece * 8;
+  constexpr int ROWS = 512 / W;            // of a wave's store
+  const int piece = lane % (W / 8), col = m + piece * 8;
   if (P != LM_LOGITS && col >= s.m) return;
 #pragma unroll 8
-  for (int i = 0; i < 32; ++i) {
-    const int row = i * 4 + (lane >> 4), n = n0 + wn * 128 + row;
+  for (int i = 0; i < W / ROWS; ++i) {
+    const int row = i * ROWS + lane / (W / 8), n = n0 + wn * W + row;
     if (n >= s.n) break;
-    const u32x4 v = get(own, row, piece);
+    const u32x4 v = get<W>(own, row, piece);
     uint16_t* to;
     if constexpr (P == LM_LOGITS) to = a.e + (int64_t)n * a.vp + col;
     else if constexpr (P == LM_GRAD_X) to = a.grad_x + (int64_t)a.row_of[a.chunk0 + n] * a.ldgx + col;
@@ -469,15 +475,16 @@ __global__ __launch_bounds__(256) void lm_join_kernel(LmArgs a) {
   }
 }
 
-template <LmProduct P, bool F16>
+template <LmProduct P, bool F16, int W>
 hipError_t launch(const LmArgs& a, hipStream_t st) {
   // the most tiles that the rows with a label can need; workgroups without one end at once
+  constexpr int T = 2 * W;
   const int64_t m = P == LM_LOGITS ? a.vocab : a.d, n = P == LM_GRAD_W ? a.vocab : a.chunk;
-  const int64_t tiles = ((m + LM_TILE - 1) / LM_TILE) * ((n + LM_TILE - 1) / LM_TILE);
-  const int64_t grid = P == LM_LOGITS || tiles > LM_PARTS ? tiles : (int64_t)LM_PARTS;
-  lm_product_kernel<P, F16><<<(uint32_t)((grid + 7) / 8 * 8), NT, 0, st>>>(a);
+  const int64_t tiles = ((m + T - 1) / T) * ((n + T - 1) / T);
+  const int64_t grid = P == LM_LOGITS || T != LM_TILE || tiles > LM_PARTS ? tiles : (int64_t)LM_PARTS;
+  lm_product_kernel<P, F16, W><<<(uint32_t)((grid + 7) / 8 * 8), NT, 0, st>>>(a);
   hipError_t e = hipGetLastError();
-  if (e != hipSuccess || P == LM_LOGITS) return e;
+  if (e != hipSuccess || P == LM_LOGITS || T != LM_TILE) return e;
   if (P == LM_GRAD_W && tiles > LM_PARTS / 2) return hipSuccess;      // never cut
   const int64_t cut = tiles < LM_PARTS / 2 ? tiles : LM_PARTS / 2;   // tiles that may be
   lm_join_kernel<P, F16><<<(uint32_t)(cut * 64), 256, 0, st>>>(a);
@@ -487,9 +494,14 @@ hipError_t launch(const LmArgs& a, hipStream_t st) {
 }  // namespace
 
 hipError_t launch_lm_product(const LmArgs& a, LmProduct p, bool f16, hipStream_t st) {
-  if (p == LM_LOGITS) return f16 ? launch<LM_LOGITS, true>(a, st) : launch<LM_LOGITS, false>(a, st);
-  if (p == LM_GRAD_X) return f16 ? launch<LM_GRAD_X, true>(a, st) : launch<LM_GRAD_X, false>(a, st);
-  return f16 ? launch<LM_GRAD_W, true>(a, st) : launch<LM_GRAD_W, false>(a, st);
+  if (p == LM_LOGITS) return f16 ? launch<LM_LOGITS, true, 128>(a, st) : launch<LM_LOGITS, false, 128>(a, st);
+  if (p == LM_GRAD_X) return f16 ? launch<LM_GRAD_X, true, 128>(a, st) : launch<LM_GRAD_X, false, 128>(a, st);
+  // Of a short sum the head's gradient is what costs, all of it written at once: two workgroups a CU, one
+  // writing while the other multiplies
+  const int64_t tiles = (int64_t)((a.d + LM_TILE - 1) / LM_TILE) * ((a.vocab + LM_TILE - 1) / LM_TILE);
+  if (a.chunk <= LM_SHORT && tiles > LM_PARTS / 2)
+    return f16 ? launch<LM_GRAD_W, true, 64>(a, st) : launch<LM_GRAD_W, false, 64>(a, st);
+  return f16 ? launch<LM_GRAD_W, true, 128>(a, st) : launch<LM_GRAD_W, false, 128>(a, st);
 }
 
 }  // namespace svl

@@ -12,6 +12,7 @@ constexpr int32_t LM_BK = 64;        // of its sum a step
 constexpr int32_t LM_ROWS = 64;      // labelled rows are filled up with zeros to a multiple
 constexpr int32_t LM_SLAB = 128;     // vocabulary entries whose exponentials share a maximum
 constexpr int32_t LM_FEW = 64;       // rows of a call whose logits a wave's products take straight from memory
+constexpr int32_t LM_SHORT = 1024;   // rows up to which the head's gradient comes in tiles of a quarter the size
 constexpr int32_t LM_PACK = 1024;    // rows of a call that are packed in one launch
 constexpr int32_t LM_PARTS = 256;    // most workgroups (tiles x pieces) of a product whose sum is cut
 constexpr int32_t LM_CUT = 8;        // least steps of LM_BK of a piece of a sum
