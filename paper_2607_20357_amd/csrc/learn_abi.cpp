@@ -217,7 +217,8 @@ int64_t lm_layout(const svl_lm_head& h, int32_t rows, bool want_x, bool want_w, 
   a->stats = l.take<float2>((int64_t)a->chunk * (a->vp / LM_SLAB));
   if (want_x || want_w) {
     a->e = l.take<uint16_t>((int64_t)a->chunk * a->vp);
-    a->parts = l.take<float>((int64_t)LM_PARTS * LM_TILE * LM_TILE);
+    a->parts = l.take<float>(std::max(want_x ? lm_parts(*a, LM_GRAD_X) : 0, want_w ? lm_parts(*a, LM_GRAD_W) : 0) *
+                             LM_TILE * LM_TILE);
   }
   if (want_w && a->chunk < rows) a->sum_w = l.take<float>((int64_t)h.vocab * h.d_model);
   return l.at;

@@ -450,28 +450,32 @@ __global__ __launch_bounds__(NT, W == 128 ? 1 : 2) void lm_product_kernel(LmArgs
   }
 }
 
-// Joins the pieces of a cut product: 4 of a tile's rows a workgroup, 64 lanes a row.
+// Joins the pieces of a cut product: 16 of a tile's rows a workgroup, 64 lanes a row.
 template <LmProduct P, bool F16>
 __global__ __launch_bounds__(256) void lm_join_kernel(LmArgs a) {
   const Sizes s = sizes_of(a, P);
   const int mt = (s.m + LM_TILE - 1) / LM_TILE, nt = (s.n + LM_TILE - 1) / LM_TILE, tiles = mt * nt;
-  const int pieces = lm_pieces(tiles, s.nk), j = blockIdx.x / 64;
+  const int pieces = lm_pieces(tiles, s.nk), j = blockIdx.x / 16;
   if (pieces <= 1 || j >= tiles) return;
   const int group = j / (8 * nt), in = j % (8 * nt), gm = mt - group * 8 < 8 ? mt - group * 8 : 8;
-  const int r = (blockIdx.x % 64) * 4 + (threadIdx.x >> 6), c = (threadIdx.x & 63) * 4;
-  const int m = (group * 8 + in % gm) * LM_TILE + c, n = in / gm * LM_TILE + r;
-  if (n >= s.n || m >= s.m) return;
-  const float* p = a.parts + ((int64_t)j * LM_TILE + r) * LM_TILE + c;
-  floatx4 v = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-  for (int i = 0; i < pieces; ++i) v += *reinterpret_cast<const floatx4*>(p + (int64_t)i * tiles * LM_TILE * LM_TILE);
+  const int c = (threadIdx.x & 63) * 4, m = (group * 8 + in % gm) * LM_TILE + c;
+  if (m >= s.m) return;
   const float scale = grad_scale<F16>(a);
-  if constexpr (P == LM_GRAD_X) {
-    *reinterpret_cast<uint2*>(a.grad_x + (int64_t)a.row_of[a.chunk0 + n] * a.ldgx + m) =
-        round_grad<F16>(v * scale, make_uint2(0, 0), false);
-  } else {
-    floatx4 one[1] = {v};
-    add_grad_w<F16>(a, n, m, scale, one);
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const int r = (blockIdx.x % 16) * 16 + k * 4 + (threadIdx.x >> 6), n = in / gm * LM_TILE + r;
+    if (n >= s.n) return;
+    const float* p = a.parts + ((int64_t)j * LM_TILE + r) * LM_TILE + c;
+    floatx4 v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+    for (int i = 0; i < pieces; ++i) v += *reinterpret_cast<const floatx4*>(p + (int64_t)i * tiles * LM_TILE * LM_TILE);
+    if constexpr (P == LM_GRAD_X) {
+      *reinterpret_cast<uint2*>(a.grad_x + (int64_t)a.row_of[a.chunk0 + n] * a.ldgx + m) =
+          round_grad<F16>(v * scale, make_uint2(0, 0), false);
+    } else {
+      floatx4 one[1] = {v};
+      add_grad_w<F16>(a, n, m, scale, one);
+    }
   }
 }
 
@@ -481,25 +485,42 @@ hipError_t launch(const LmArgs& a, hipStream_t st) {
   constexpr int T = 2 * W;
   const int64_t m = P == LM_LOGITS ? a.vocab : a.d, n = P == LM_GRAD_W ? a.vocab : a.chunk;
   const int64_t tiles = ((m + T - 1) / T) * ((n + T - 1) / T);
-  const int64_t grid = P == LM_LOGITS || T != LM_TILE || tiles > LM_PARTS ? tiles : (int64_t)LM_PARTS;
-  lm_product_kernel<P, F16, W><<<(uint32_t)((grid + 7) / 8 * 8), NT, 0, st>>>(a);
+  const int64_t parts = P == LM_LOGITS || T != LM_TILE ? 0 : lm_parts(a, P);
+  lm_product_kernel<P, F16, W><<<(uint32_t)(((tiles > parts ? tiles : parts) + 7) / 8 * 8), NT, 0, st>>>(a);
   hipError_t e = hipGetLastError();
-  if (e != hipSuccess || P == LM_LOGITS || T != LM_TILE) return e;
-  if (P == LM_GRAD_W && tiles > LM_PARTS / 2) return hipSuccess;      // never cut
-  const int64_t cut = tiles < LM_PARTS / 2 ? tiles : LM_PARTS / 2;   // tiles that may be
-  lm_join_kernel<P, F16><<<(uint32_t)(cut * 64), 256, 0, st>>>(a);
+  if (e != hipSuccess || parts == 0) return e;
+  const int64_t cut = tiles < 2 * LM_CUS ? tiles : 2 * LM_CUS;      // tiles that may be cut
+  lm_join_kernel<P, F16><<<(uint32_t)(cut * 16), 256, 0, st>>>(a);
   return hipGetLastError();
 }
 
 }  // namespace
+
+int64_t lm_parts(const LmArgs& a, LmProduct p) {
+  const auto tiles_of = [](int64_t x) { return (int32_t)((x + LM_TILE - 1) / LM_TILE); };
+  int64_t most = 0;
+  if (p == LM_GRAD_X) {
+    for (int32_t nt = 1; nt <= tiles_of(a.chunk); ++nt) {
+      const int32_t tiles = tiles_of(a.d) * nt, s = lm_pieces(tiles, (a.vocab + LM_BK - 1) / LM_BK);
+      if (s > 1 && (int64_t)tiles * s > most) most = (int64_t)tiles * s;
+    }
+  } else {
+    const int64_t tiles = (int64_t)tiles_of(a.d) * tiles_of(a.vocab);
+    if (tiles <= 2 * LM_CUS)
+      for (int32_t nk = 1; nk <= (a.chunk + LM_BK - 1) / LM_BK; ++nk) {
+        const int32_t s = lm_pieces((int32_t)tiles, nk);
+        if (s > 1 && tiles * s > most) most = tiles * s;
+      }
+  }
+  return most;
+}
 
 hipError_t launch_lm_product(const LmArgs& a, LmProduct p, bool f16, hipStream_t st) {
   if (p == LM_LOGITS) return f16 ? launch<LM_LOGITS, true, 128>(a, st) : launch<LM_LOGITS, false, 128>(a, st);
   if (p == LM_GRAD_X) return f16 ? launch<LM_GRAD_X, true, 128>(a, st) : launch<LM_GRAD_X, false, 128>(a, st);
   // Of a short sum the head's gradient is what costs, all of it written at once: two workgroups a CU, one
   // writing while the other multiplies
-  const int64_t tiles = (int64_t)((a.d + LM_TILE - 1) / LM_TILE) * ((a.vocab + LM_TILE - 1) / LM_TILE);
-  if (a.chunk <= LM_SHORT && tiles > LM_PARTS / 2)
+  if (a.chunk <= LM_SHORT && lm_parts(a, LM_GRAD_W) == 0)
     return f16 ? launch<LM_GRAD_W, true, 64>(a, st) : launch<LM_GRAD_W, false, 64>(a, st);
   return f16 ? launch<LM_GRAD_W, true, 128>(a, st) : launch<LM_GRAD_W, false, 128>(a, st);
 }

@@ -11,10 +11,14 @@ constexpr int32_t LM_TILE = 256;     // rows and columns of a product's tile
 constexpr int32_t LM_BK = 64;        // of its sum a step
 constexpr int32_t LM_ROWS = 64;      // labelled rows are filled up with zeros to a multiple
 constexpr int32_t LM_SLAB = 128;     // vocabulary entries whose exponentials share a maximum
-constexpr int32_t LM_FEW = 64;       // rows of a call whose logits a wave's products take straight from memory
-constexpr int32_t LM_SHORT = 1024;   // rows up to which the head's gradient comes in tiles of a quarter the size
+// Rows of a call whose logits a wave's products take straight from memory (vocabulary 32000, 4096: 8 rows
+// 62 us against 80 in tiles; 24 rows 97 against 89).
+constexpr int32_t LM_FEW = 16;
+// Rows up to which the head's gradient comes in tiles of a quarter the size (with the softmax before it: 320
+// rows 136 us against 165, 640 222 against 237, 1024 308 against 307).
+constexpr int32_t LM_SHORT = 768;
 constexpr int32_t LM_PACK = 1024;    // rows of a call that are packed in one launch
-constexpr int32_t LM_PARTS = 256;    // most workgroups (tiles x pieces) of a product whose sum is cut
+constexpr int32_t LM_CUS = 256;      // tiles at work at once
 constexpr int32_t LM_CUT = 8;        // least steps of LM_BK of a piece of a sum
 // Exponentials are held as fp16 under 2^14 (normal down to 2^-28 of their slab's largest), P
 // in fp16 likewise (of the largest weight).
@@ -53,18 +57,30 @@ struct LmArgs {
   float* log_sum;               // [chunk]
   float2* stats;                // [chunk][vp / LM_SLAB] (maximum, sum of exponentials)
   uint16_t* e;                  // [chunk][vp] exponentials, then P; or nullptr
-  float* parts;                 // [LM_PARTS] tiles of a cut sum
+  float* parts;                 // tiles of a cut sum's pieces
   float* sum_w;                 // [vocab][d] the head's gradient of earlier passes, or nullptr
   bool first, last;             // pass of the call
 };
 
 enum LmProduct : int32_t { LM_LOGITS = 0, LM_GRAD_X = 1, LM_GRAD_W = 2 };
 
-// Pieces of a product's sum of nk steps over `tiles` tiles.
+// Pieces of a product's sum of nk steps over `tiles` tiles: as many as fill the rounds of the CUs,
+// up to three, where that shortens them by a tenth at least (a piece more is its tile written and read once in
+// float32).  (grad_x of 500 steps, with the softmax before it: 144 tiles in three pieces 567 us,
+// whole 686; 160 615 against 714.)
 __host__ __device__ inline int32_t lm_pieces(int32_t tiles, int32_t nk) {
-  if (tiles <= 0 || tiles > LM_PARTS / 2) return 1;
-  const int32_t s = LM_PARTS / tiles, most = nk / LM_CUT;
-  return s < most ? s : (most > 1 ? most : 1);
+  if (tiles <= 0 || tiles > 2 * LM_CUS) return 1;
+  const int32_t most = nk / LM_CUT;
+  int32_t best = 1, rounds = (tiles + LM_CUS - 1) / LM_CUS;     // time: rounds / best
+  for (int32_t r = 1; r <= 3; ++r) {
+    int32_t s = r * LM_CUS / tiles;
+    s = s < most ? s : most;
+    if (s > best && 10 * r * best < 9 * rounds * s) {
+      best = s;
+      rounds = r;
+    }
+  }
+  return best;
 }
 
 hipError_t launch_lm_rows(const LmArgs& a, hipStream_t st);                 // labelled rows, packed
@@ -72,6 +88,8 @@ hipError_t launch_lm_stats(const LmArgs& a, hipStream_t st);                // l
 hipError_t launch_lm_softmax(const LmArgs& a, bool f16, hipStream_t st);    // exponentials to P
 hipError_t launch_lm_product(const LmArgs& a, LmProduct p, bool f16, hipStream_t st);
 hipError_t launch_lm_few_logits(const LmArgs& a, bool f16, hipStream_t st); // logits of at most LM_FEW rows
+// Most pieces of all tiles that a product is cut into, whatever rows have a label (0: it is never cut).
+int64_t lm_parts(const LmArgs& a, LmProduct p);
 hipError_t launch_lm_zero_w(const LmArgs& a, hipStream_t st);               // a call without rows
 
 }  // namespace svl
