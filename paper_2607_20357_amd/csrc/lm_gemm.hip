@@ -119,7 +119,9 @@ struct Fragments {
 
 // c += a b.  (In assembly so that all sums stay where they are, in the accumulation registers: the
 // compiler moves some of 64 blocks of 4 to and fro.  What the hardware does not wait for by itself is
-// kept apart: a sum is used again 64 products later, and read after settle().)
+// kept apart: the fragments come from LDS, whose arrival is waited for, and no instruction of the vector
+// unit writes an operand shortly before; a sum is used again by the product NB^2 later, and read after
+// settle().  tests/test_lm_products_cpu.py looks at what the compiler makes of it.)
 template <bool F16>
 __device__ __forceinline__ void mfma(const u32x4& a, const u32x4& b, floatx4& c) {
   if constexpr (F16) asm volatile("v_mfma_f32_16x16x32_f16 %0, %1, %2, %0" : "+a"(c) : "v"(a), "v"(b));
@@ -376,6 +378,11 @@ __global__ __launch_bounds__(NT, W == 128 ? 1 : 2) void lm_product_kernel(LmArgs
 #pragma unroll
     for (int i = 0; i < 2 * NB; ++i) read(f0, i, pa, pb, 0);
     wait_lds();
+#pragma unroll
+    for (int i = 0; i < NB; ++i)
+#pragma unroll
+      for (int j = 0; j < NB; ++j) asm volatile("" : "+a"(acc[i][j]));   // the zeros are written before
+    settle();
     uint32_t deep = 0, shallow = 0;      // buffers of step t
 #pragma unroll 1
     for (int t = kt0; t < kt1; ++t) {
