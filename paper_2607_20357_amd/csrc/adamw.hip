@@ -196,22 +196,35 @@ __global__ __launch_bounds__(NT) void adamw_kernel(AdamwArgs a) {
   }
 }
 
+// READS pieces of 4 a thread, a wave's in a row: what it writes leaves in whole lines.
+constexpr int READS = 4;
 __global__ __launch_bounds__(NT) void adamw_read_kernel(bool second, int64_t n, const uint8_t* codes,
                                                         const float* scales, float* out) {
 #pragma clang fp contract(off)
-  const int64_t i = ((int64_t)blockIdx.x * NT + threadIdx.x) * 8;
-  if (i >= n) return;
-  const int valid = n - i >= 8 ? 8 : (int)(n - i);
-  uint32_t c[8];
-  load_codes(codes, i, valid, c);
-  const float s = scales[i / ADAMW_BLOCK];
-  float v[8];
-#pragma unroll
-  for (int k = 0; k < 8; ++k) {
-    const float x = s * code_value(second ? c[k] : c[k] & 127u, second ? LOW_V : LOW_M);
-    v[k] = second ? x * x : c[k] & 128u ? -x : x;
+  const int64_t i0 = ((int64_t)blockIdx.x * READS * NT + threadIdx.x) * 4;
+  const auto value = [&](uint32_t c, float s) {
+    const float x = s * code_value(second ? c : c & 127u, second ? LOW_V : LOW_M);
+    return second ? x * x : c & 128u ? -x : x;
+  };
+  if (i0 + (int64_t)(READS - 1) * NT * 4 + 4 > n) {
+    for (int j = 0; j < READS; ++j)
+      for (int64_t i = i0 + (int64_t)j * NT * 4; i < i0 + (int64_t)j * NT * 4 + 4 && i < n; ++i)
+        out[i] = value(codes[i], scales[i / ADAMW_BLOCK]);
+    return;
   }
-  store_some(out, SVL_TYPE_F32, i, valid, v);
+  uint32_t c[READS];
+  float s[READS];
+#pragma unroll
+  for (int j = 0; j < READS; ++j) {
+    const int64_t i = i0 + (int64_t)j * NT * 4;
+    c[j] = *reinterpret_cast<const uint32_t*>(codes + i);
+    s[j] = scales[i / ADAMW_BLOCK];
+  }
+#pragma unroll
+  for (int j = 0; j < READS; ++j)
+    *reinterpret_cast<float4*>(out + i0 + (int64_t)j * NT * 4) =
+        make_float4(value(c[j] & 255u, s[j]), value(c[j] >> 8 & 255u, s[j]), value(c[j] >> 16 & 255u, s[j]),
+                    value(c[j] >> 24, s[j]));
 }
 
 }  // namespace
@@ -228,7 +241,7 @@ hipError_t launch_adamw_read(bool second, int64_t n, const uint8_t* codes, const
   constexpr int64_t PART = (int64_t)1 << 32;
   for (int64_t i = 0; i < n; i += PART) {
     const int64_t part = n - i < PART ? n - i : PART;
-    adamw_read_kernel<<<(uint32_t)((part + NT * 8 - 1) / (NT * 8)), NT, 0, st>>>(second, part, codes + i,
+    adamw_read_kernel<<<(uint32_t)((part + READS * NT * 4 - 1) / (READS * NT * 4)), NT, 0, st>>>(second, part, codes + i,
                                                                                scales + i / ADAMW_BLOCK, out + i);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
