@@ -1,7 +1,7 @@
 // One AdamW step over many tensors, with states in 32 bits or in 8.
 //
 // Memory bounds it: each array is read once and written once.  A workgroup
-// takes 4096 elements of one tensor, a thread 8 in a row at a time; the tensors
+// takes 4096 elements of one tensor, a thread 4 in a row at a time; the tensors
 // travel in the kernel's arguments, so a launch serves 48 of them.
 //
 // 8-bit states hold a block of 256 under a power of two, so that scaling is exact
@@ -16,7 +16,7 @@
 namespace svl {
 namespace {
 
-constexpr int NT = 256;
+constexpr int NT = 256, EL = 4;           // EL elements a thread: a wave's are a block of 256
 constexpr int LOW_M = -13, LOW_V = -29;   // lowest exponent with all digits, of scale 1
 
 __device__ __forceinline__ uint32_t mix(uint32_t x) {
@@ -29,29 +29,30 @@ __device__ __forceinline__ uint32_t mix(uint32_t x) {
 
 // A code's value under scale 1: bits 0 .. 2 after the point, the exponent above.
 __device__ __forceinline__ float code_value(uint32_t c, int low) {
-  const uint32_t e = c >> 3;
-  if (e == 0) return (float)(c & 7u) * __uint_as_float((uint32_t)(127 + low - 3) << 23);
-  return __uint_as_float((c + ((uint32_t)(126 + low) << 3)) << 20);
+  const float normal = __uint_as_float((c + ((uint32_t)(126 + low) << 3)) << 20);
+  const float small = (float)(c & 7u) * __uint_as_float((uint32_t)(127 + low - 3) << 23);
+  return c >= 8u ? normal : small;
 }
 
-// The code next to y >= 0 (under scale 1): above it with the chance that 16 random bits give.
+// The code next to y >= 0 (under scale 1): above it with the chance that 16 random bits give.  (Both
+// forms are computed and one is taken: a branch costs the wave more.)
 __device__ __forceinline__ uint32_t code_of(float y, uint32_t r16, int low) {
   const uint32_t up = r16 << 4;
-  if (y >= __uint_as_float((uint32_t)(127 + low) << 23))
-    return ((__float_as_uint(y) + up) >> 20) - ((uint32_t)(126 + low) << 3);
-  return ((uint32_t)(y * __uint_as_float((uint32_t)(127 + 23 - low) << 23)) + up) >> 20;
+  const uint32_t normal = ((__float_as_uint(y) + up) >> 20) - ((uint32_t)(126 + low) << 3);
+  const uint32_t small = ((uint32_t)(y * __uint_as_float((uint32_t)(127 + 23 - low) << 23)) + up) >> 20;
+  return y >= __uint_as_float((uint32_t)(127 + low) << 23) ? normal : small;
 }
 
-// The largest magnitude's bits over the 32 lanes of a block; NaN counts as the largest.
+// The largest magnitude's bits over a block, a wave's; NaN counts as the largest.
 __device__ __forceinline__ uint32_t block_top(const float* x) {
   uint32_t top = 0;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
+  for (int i = 0; i < EL; ++i) {
     const uint32_t b = __float_as_uint(x[i]) & 0x7fffffffu;
     top = b > top ? b : top;
   }
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) {
+  for (int o = 32; o > 0; o >>= 1) {
     const uint32_t b = __shfl_xor(top, o, 64);
     top = b > top ? b : top;
   }
@@ -73,126 +74,141 @@ __device__ __forceinline__ float block_scale(uint32_t top, float* inverse) {
   return __uint_as_float(e << 23);
 }
 
+// FULL: all of the lane's elements are there, otherwise the first `valid`.
+template <bool FULL>
 __device__ __forceinline__ void load_codes(const void* p, int64_t i, int valid, uint32_t* c) {
-  if (valid == 8) {
-    const uint2 w = *reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(p) + i);
+  if constexpr (FULL) {
+    const uint32_t w = *reinterpret_cast<const uint32_t*>(static_cast<const uint8_t*>(p) + i);
 #pragma unroll
-    for (int k = 0; k < 8; ++k) c[k] = ((k < 4 ? w.x : w.y) >> (8 * (k & 3))) & 255u;
+    for (int k = 0; k < EL; ++k) c[k] = (w >> (8 * k)) & 255u;
   } else {
 #pragma unroll
-    for (int k = 0; k < 8; ++k) c[k] = k < valid ? static_cast<const uint8_t*>(p)[i + k] : 0u;
+    for (int k = 0; k < EL; ++k) c[k] = k < valid ? static_cast<const uint8_t*>(p)[i + k] : 0u;
   }
 }
 
+template <bool FULL>
 __device__ __forceinline__ void store_codes(void* p, int64_t i, int valid, const uint32_t* c) {
-  if (valid == 8) {
-    uint2 w = make_uint2(0, 0);
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      w.x |= c[k] << (8 * k);
-      w.y |= c[k + 4] << (8 * k);
-    }
-    *reinterpret_cast<uint2*>(static_cast<uint8_t*>(p) + i) = w;
+  if constexpr (FULL) {
+    *reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(p) + i) = c[0] | c[1] << 8 | c[2] << 16 | c[3] << 24;
   } else {
 #pragma unroll
-    for (int k = 0; k < 8; ++k)
+    for (int k = 0; k < EL; ++k)
       if (k < valid) static_cast<uint8_t*>(p)[i + k] = (uint8_t)c[k];
   }
 }
 
+template <bool FULL>
 __device__ __forceinline__ void load_some(const void* p, int32_t type, int64_t i, int valid, float* v) {
-  if (valid == 8) {
-    widen8(load_raw8(p, type, i), type, v);
+  if constexpr (FULL) {
+    load4(p, type, i, v);
   } else {
 #pragma unroll
-    for (int k = 0; k < 8; ++k) v[k] = k < valid ? load1(p, type, i + k) : 0.f;
+    for (int k = 0; k < EL; ++k) v[k] = k < valid ? load1(p, type, i + k) : 0.f;
   }
 }
 
+template <bool FULL>
 __device__ __forceinline__ void store_some(void* p, int32_t type, int64_t i, int valid, const float* v) {
-  if (valid == 8) {
-    store8(p, type, i, v);
+  if constexpr (FULL) {
+    store4(p, type, i, v);
   } else {
 #pragma unroll
-    for (int k = 0; k < 8; ++k)
+    for (int k = 0; k < EL; ++k)
       if (k < valid) store1(p, type, i + k, v[k]);
+  }
+}
+
+// What a step's factors are, once a workgroup.
+struct StepNow {
+  float keep, lr, grad_scale, inverse1, inverse_root2;   // 1 - lr decay; 1 / correction1, 1 / sqrt(correction2)
+  uint32_t seed;
+};
+
+// Elements i .. of a tensor: a wave's are a block of 256.
+template <bool EIGHT, bool FULL>
+__device__ __forceinline__ void adamw_block(const AdamwArgs& a, const AdamwTensor& t, const StepNow& now,
+                                            uint32_t number, int64_t i) {
+// the moments' products and sums are rounded one by one: 8-bit codes depend on every bit
+#pragma clang fp contract(off)
+  const int64_t left = t.n - i;
+  const int valid = left >= EL ? EL : left > 0 ? (int)left : 0;
+  float g[EL], p[EL], m[EL], v[EL];
+  load_some<FULL>(t.grad, t.grad_type, i, valid, g);
+  if (t.master) load_some<FULL>(t.master, SVL_TYPE_F32, i, valid, p);
+  else load_some<FULL>(t.param, t.param_type, i, valid, p);
+  if constexpr (EIGHT) {
+    uint32_t cm[EL], cv[EL];
+    load_codes<FULL>(t.m, i, valid, cm);
+    load_codes<FULL>(t.v, i, valid, cv);
+    const float sm = FULL || valid ? t.m_scale[i / ADAMW_BLOCK] : 0.f;
+    const float sv = FULL || valid ? t.v_scale[i / ADAMW_BLOCK] : 0.f;
+#pragma unroll
+    for (int k = 0; k < EL; ++k) {
+      const float x = sm * code_value(cm[k] & 127u, LOW_M), y = sv * code_value(cv[k], LOW_V);
+      m[k] = cm[k] & 128u ? -x : x;
+      v[k] = y * y;
+    }
+  } else {
+    load_some<FULL>(t.m, SVL_TYPE_F32, i, valid, m);
+    load_some<FULL>(t.v, SVL_TYPE_F32, i, valid, v);
+  }
+  float root[EL];
+#pragma unroll
+  for (int k = 0; k < EL; ++k) {
+    const float x = g[k] * now.grad_scale;
+    m[k] = a.beta1 * m[k] + a.rest1 * x;
+    v[k] = a.beta2 * v[k] + (a.rest2 * x) * x;
+    if (!FULL && k >= valid) m[k] = v[k] = 0.f;
+    root[k] = sqrtf(v[k]);
+    // (the quotient by the hardware's reciprocal: a last place of a step that is far smaller than p)
+    p[k] = p[k] * now.keep -
+           now.lr * ((m[k] * now.inverse1) * __builtin_amdgcn_rcpf(root[k] * now.inverse_root2 + a.eps));
+  }
+  if (t.master) store_some<FULL>(t.master, SVL_TYPE_F32, i, valid, p);
+  store_some<FULL>(t.param, t.param_type, i, valid, p);
+  if constexpr (EIGHT) {
+    const uint32_t key = mix(now.seed + 0x9E3779B9u * (number + 1) + 0xBB67AE85u * (uint32_t)(i >> 32));
+    float im, iv;
+    const float sm = block_scale(block_top(m), &im), sv = block_scale(block_top(root), &iv);
+    uint32_t cm[EL], cv[EL];
+#pragma unroll
+    for (int k = 0; k < EL; ++k) {
+      const uint32_t r = mix((uint32_t)(i + k) * 0x9E3779B9u + key);
+      cm[k] = im == 0.f ? 0u : code_of(fabsf(m[k]) * im, r & 0xffffu, LOW_M) | (m[k] < 0.f ? 128u : 0u);
+      cv[k] = iv == 0.f ? 0u : code_of(root[k] * iv, r >> 16, LOW_V);
+    }
+    store_codes<FULL>(t.m, i, valid, cm);
+    store_codes<FULL>(t.v, i, valid, cv);
+    if ((FULL || valid) && (threadIdx.x & 63) == 0) {
+      t.m_scale[i / ADAMW_BLOCK] = sm;
+      t.v_scale[i / ADAMW_BLOCK] = sv;
+    }
+  } else {
+    store_some<FULL>(t.m, SVL_TYPE_F32, i, valid, m);
+    store_some<FULL>(t.v, SVL_TYPE_F32, i, valid, v);
   }
 }
 
 template <bool EIGHT>
 __global__ __launch_bounds__(NT) void adamw_kernel(AdamwArgs a) {
-// the moments' products and sums are rounded one by one: 8-bit codes depend on every bit
-#pragma clang fp contract(off)
   int lo = 0, hi = a.count - 1;
   while (lo < hi) {
     const int mid = (lo + hi + 1) >> 1;
     if (a.t[mid].item0 <= (int)blockIdx.x) lo = mid; else hi = mid - 1;
   }
   const AdamwTensor& t = a.t[lo];
-  const svl_adamw_dev now = a.dev ? *a.dev : a.now;
+  const svl_adamw_dev d = a.dev ? *a.dev : a.now;
+  const StepNow now = {1.f - d.lr * a.decay, d.lr, d.grad_scale, 1.f / d.correction1, 1.f / sqrtf(d.correction2), d.seed};
   const int64_t item = (int)blockIdx.x - t.item0 + (lo == 0 ? a.first_item : 0);
-  const float keep = 1.f - now.lr * a.decay;
+  const int w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
 #pragma unroll 1
-  for (int it = 0; it < ADAMW_ITEM / (NT * 8); ++it) {
-    const int64_t i = item * ADAMW_ITEM + it * (NT * 8) + threadIdx.x * 8;
-    const int64_t left = t.n - i;
-    // (the lanes of a block of 256 stay together: its largest value is taken over all of them)
-    if (left <= -ADAMW_BLOCK) return;
-    const int valid = left >= 8 ? 8 : left > 0 ? (int)left : 0;
-    float g[8], p[8], m[8], v[8];
-    load_some(t.grad, t.grad_type, i, valid, g);
-    if (t.master) load_some(t.master, SVL_TYPE_F32, i, valid, p);
-    else load_some(t.param, t.param_type, i, valid, p);
-    if constexpr (EIGHT) {
-      uint32_t cm[8], cv[8];
-      load_codes(t.m, i, valid, cm);
-      load_codes(t.v, i, valid, cv);
-      const float sm = valid ? t.m_scale[i / ADAMW_BLOCK] : 0.f, sv = valid ? t.v_scale[i / ADAMW_BLOCK] : 0.f;
-#pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        const float x = sm * code_value(cm[k] & 127u, LOW_M), y = sv * code_value(cv[k], LOW_V);
-        m[k] = cm[k] & 128u ? -x : x;
-        v[k] = y * y;
-      }
-    } else {
-      load_some(t.m, SVL_TYPE_F32, i, valid, m);
-      load_some(t.v, SVL_TYPE_F32, i, valid, v);
-    }
-#pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      const float x = g[k] * now.grad_scale;
-      m[k] = a.beta1 * m[k] + a.rest1 * x;
-      v[k] = a.beta2 * v[k] + (a.rest2 * x) * x;
-      if (k >= valid) m[k] = v[k] = 0.f;
-      p[k] = p[k] * keep - now.lr * ((m[k] / now.correction1) / (sqrtf(v[k] / now.correction2) + a.eps));
-    }
-    if (t.master) store_some(t.master, SVL_TYPE_F32, i, valid, p);
-    store_some(t.param, t.param_type, i, valid, p);
-    if constexpr (EIGHT) {
-      const uint32_t key = mix(now.seed + 0x9E3779B9u * (uint32_t)(a.number0 + lo + 1) +
-                               0xBB67AE85u * (uint32_t)(i >> 32));
-      float im, iv;
-      const float sm = block_scale(block_top(m), &im);
-#pragma unroll
-      for (int k = 0; k < 8; ++k) v[k] = sqrtf(v[k]);
-      const float sv = block_scale(block_top(v), &iv);
-      uint32_t cm[8], cv[8];
-#pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        const uint32_t r = mix((uint32_t)(i + k) * 0x9E3779B9u + key);
-        cm[k] = im == 0.f ? 0u : code_of(fabsf(m[k]) * im, r & 0xffffu, LOW_M) | (m[k] < 0.f ? 128u : 0u);
-        cv[k] = iv == 0.f ? 0u : code_of(v[k] * iv, r >> 16, LOW_V);
-      }
-      store_codes(t.m, i, valid, cm);
-      store_codes(t.v, i, valid, cv);
-      if (valid && (threadIdx.x & 31) == 0) {
-        t.m_scale[i / ADAMW_BLOCK] = sm;
-        t.v_scale[i / ADAMW_BLOCK] = sv;
-      }
-    } else {
-      store_some(t.m, SVL_TYPE_F32, i, valid, m);
-      store_some(t.v, SVL_TYPE_F32, i, valid, v);
-    }
+  for (int it = 0; it < ADAMW_ITEM / (NT * EL); ++it) {
+    const int64_t first = item * ADAMW_ITEM + it * (NT * EL) + w * ADAMW_BLOCK;
+    if (first >= t.n) return;
+    const int64_t i = first + (threadIdx.x & 63) * EL;
+    if (first + ADAMW_BLOCK <= t.n) adamw_block<EIGHT, true>(a, t, now, (uint32_t)(a.number0 + lo), i);
+    else adamw_block<EIGHT, false>(a, t, now, (uint32_t)(a.number0 + lo), i);
   }
 }
 

@@ -64,6 +64,31 @@ __device__ __forceinline__ void store8(void* p, int32_t type, int64_t i, const f
   *reinterpret_cast<uint4*>(static_cast<uint16_t*>(p) + i) = w;
 }
 
+// Four values: of float, a wave's pieces follow one another without gaps (8 a lane leave
+// its stores half lines: 153M floats 126 us in place of 197).
+__device__ __forceinline__ void load4(const void* p, int32_t type, int64_t i, float* v) {
+  if (type == SVL_TYPE_F32) {
+    const float4 f = *reinterpret_cast<const float4*>(static_cast<const float*>(p) + i);
+    v[0] = f.x; v[1] = f.y; v[2] = f.z; v[3] = f.w;
+    return;
+  }
+  const uint2 w = *reinterpret_cast<const uint2*>(static_cast<const uint16_t*>(p) + i);
+  const uint32_t h[4] = {w.x & 0xffffu, w.x >> 16, w.y & 0xffffu, w.y >> 16};
+#pragma unroll
+  for (int k = 0; k < 4; ++k) v[k] = type == SVL_TYPE_BF16 ? bf16_bits_to_f32(h[k]) : act_bits_to_f32<true>(h[k]);
+}
+
+__device__ __forceinline__ void store4(void* p, int32_t type, int64_t i, const float* v) {
+  if (type == SVL_TYPE_F32)
+    *reinterpret_cast<float4*>(static_cast<float*>(p) + i) = make_float4(v[0], v[1], v[2], v[3]);
+  else if (type == SVL_TYPE_BF16)
+    *reinterpret_cast<uint2*>(static_cast<uint16_t*>(p) + i) =
+        make_uint2(pack_act2<false>(v[0], v[1]), pack_act2<false>(v[2], v[3]));
+  else
+    *reinterpret_cast<uint2*>(static_cast<uint16_t*>(p) + i) =
+        make_uint2(pack_act2<true>(v[0], v[1]), pack_act2<true>(v[2], v[3]));
+}
+
 __device__ __forceinline__ float load1(const void* p, int32_t type, int64_t i) {
   if (type == SVL_TYPE_F32) return static_cast<const float*>(p)[i];
   const uint32_t h = static_cast<const uint16_t*>(p)[i];
