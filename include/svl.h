@@ -760,7 +760,8 @@ typedef struct {
 
 /* Workspace bytes of svl_lm_loss with the gradients named (0 on bad arguments).  With
  * gradients it holds 16 bits for each of the vocabulary of at most a piece of the rows
- * (about 1 GiB of them), never the logits. */
+ * (about 1 GiB of them, 1024 rows at least), at most 200 MB of float32 pieces of sums,
+ * and with more rows than a piece the head's gradient in float32; never the logits. */
 size_t svl_lm_loss_workspace_bytes(const svl_lm_head *head, int32_t rows, int32_t want_grad_x,
                                    int32_t want_grad_w);
 
@@ -772,7 +773,7 @@ size_t svl_lm_loss_workspace_bytes(const svl_lm_head *head, int32_t rows, int32_
  * 0, and its x may hold anything.  Rows without a label cost next to nothing.
  *   x          dev [rows][d_model];  w dev [vocab][d_model] (compute's type)
  *   labels     dev int32 [rows] (4-byte aligned)
- *   row_weight dev float [rows] or NULL (1): 1 / n for a mean; with fp16 a loss scale
+ *   row_weight dev float [rows] or NULL (1), finite: 1 / n for a mean; with fp16 a loss scale
  *              belongs here too
  *   loss       dev float [rows];  lse dev float [rows] or NULL (all three 4-byte aligned)
  *   grad_x     dev [rows][d_model] or NULL;  grad_w dev [vocab][d_model] or NULL, written,

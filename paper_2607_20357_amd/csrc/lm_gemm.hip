@@ -290,6 +290,7 @@ __global__ __launch_bounds__(NT, W == 128 ? 1 : 2) void lm_product_kernel(LmArgs
   constexpr bool TA = P != LM_LOGITS, TB = P == LM_GRAD_W;
   __shared__ __attribute__((aligned(1024))) uint16_t lds[5 * STEP];   // three steps of one operand, two of the other: 160 or 80 KB
   const Sizes s = sizes_of(a, P);
+  if (P == LM_GRAD_W && s.nk == 0 && !a.first && !a.last) return;   // nothing to add to the sums
   Tile t;
   if (!tile_of((s.m + T - 1) / T, (s.n + T - 1) / T, s.nk, P != LM_LOGITS && T == LM_TILE, &t)) return;
   const int m0 = t.m * T, n0 = t.n * T;

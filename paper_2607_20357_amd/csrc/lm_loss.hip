@@ -59,15 +59,17 @@ __global__ __launch_bounds__(1024) void lm_count_kernel(LmArgs a) {
 // of 64, are zeros); a row without a label gets its zeros.
 __global__ __launch_bounds__(NT) void lm_pack_kernel(LmArgs a, int packed) {
   const uint4 zero = make_uint4(0, 0, 0, 0);
-  if ((int)blockIdx.x < packed) {
-    const int i = blockIdx.x, n = a.head->rows;
+  const int block = (int)(blockIdx.y * gridDim.x + blockIdx.x);
+  if (block >= packed + a.rows) return;
+  if (block < packed) {
+    const int i = block, n = a.head->rows;
     if (i >= (n + LM_ROWS - 1) / LM_ROWS * LM_ROWS) return;
     const uint16_t* from = i < n ? a.x + (int64_t)a.row_of[i] * a.ldx : nullptr;
     for (int c = threadIdx.x * 8; c < a.d; c += NT * 8)
       *reinterpret_cast<uint4*>(a.xc + (int64_t)i * a.d + c) = from ? *reinterpret_cast<const uint4*>(from + c) : zero;
     return;
   }
-  const int i = blockIdx.x - packed, label = a.labels[i];
+  const int i = block - packed, label = a.labels[i];
   if (label >= 0 && label < a.vocab) return;
   if (threadIdx.x == 0) {
     a.loss[i] = 0.f;
@@ -284,7 +286,9 @@ hipError_t launch_lm_rows(const LmArgs& a, hipStream_t st) {
   }
   lm_count_kernel<<<1, 1024, 0, st>>>(a);
   const int packed = (a.rows + LM_ROWS - 1) / LM_ROWS * LM_ROWS;
-  lm_pack_kernel<<<packed + a.rows, NT, 0, st>>>(a, packed);
+  // (a grid's first dimension times its threads stays under 2^32)
+  const uint32_t blocks = (uint32_t)(packed + a.rows), nx = blocks < (1u << 22) ? blocks : 1u << 22;
+  lm_pack_kernel<<<dim3(nx, (blocks + nx - 1) / nx), NT, 0, st>>>(a, packed);
   return hipGetLastError();
 }
 

@@ -90,6 +90,20 @@ def test_cut_sums(compute):
 
 
 @pytest.mark.parametrize("compute", COMPUTES)
+@pytest.mark.parametrize("rows", [5, 90, 768, 769])
+def test_added_to_what_is_there(compute, rows):
+    """Small tiles of the head's gradient (up to 768 rows) and large ones, edges in both directions."""
+    _check(rows, 192, 500, compute, ignored=0.2, held=True, weights="any", seed=rows)
+
+
+@pytest.mark.parametrize("rows", [60, 1500])
+def test_sums_cut_in_more_than_a_round(rows):
+    """Tiles of the rows' gradient that fill the CUs' rounds only in pieces, by the rows that have a label."""
+    for ignored in (0.0, 0.7):
+        _check(rows, 1024, 2100, "bf16", ignored=ignored, want_w=False)
+
+
+@pytest.mark.parametrize("compute", COMPUTES)
 @pytest.mark.parametrize("want", [(False, False), (True, False), (False, True)])
 def test_outputs_alone(compute, want):
     head, x, w, labels, weight, got = _check(90, 128, 500, compute, ignored=0.4, want_x=want[0], want_w=want[1])
