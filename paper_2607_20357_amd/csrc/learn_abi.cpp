@@ -214,7 +214,8 @@ int64_t lm_layout(const svl_lm_head& h, int32_t rows, bool want_x, bool want_w, 
   a->xc = l.take<uint16_t>(cdiv(rows, LM_ROWS) * LM_ROWS * h.d_model);
   a->label_logit = l.take<float>(a->chunk);
   a->log_sum = l.take<float>(a->chunk);
-  a->stats = l.take<float2>((int64_t)a->chunk * (a->vp / LM_SLAB));
+  a->slab = rows > LM_FEW && (int64_t)(a->vp / LM_TILE) * (a->chunk / LM_TILE) <= LM_SMALL ? 64 : LM_SLAB;
+  a->stats = l.take<float2>((int64_t)a->chunk * (a->vp / a->slab));
   if (want_x || want_w) {
     a->e = l.take<uint16_t>((int64_t)a->chunk * a->vp);
     a->parts = l.take<float>(std::max(want_x ? lm_parts(*a, LM_GRAD_X) : 0, want_w ? lm_parts(*a, LM_GRAD_W) : 0) *

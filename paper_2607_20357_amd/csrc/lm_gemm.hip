@@ -229,34 +229,34 @@ __device__ __forceinline__ u32x4 get(const uint16_t* own, int row, int piece) {
   return *reinterpret_cast<const u32x4*>(own + row * W + (piece ^ (row & (W / 8 - 1))) * 8);
 }
 
-// Logits of 128 entries of the vocabulary (a wave's) become exponentials under their
-// row's largest; a lane holds 32 of the row's, three others the rest.
-template <bool F16>
+// Logits of W entries of the vocabulary (a wave's, a slab) become exponentials under their
+// row's largest; a lane holds a quarter of the row's, three others the rest.
+template <bool F16, int W>
 __device__ __forceinline__ void store_logits(const LmArgs& a, int m0, int n, bool there, uint16_t* own, int row,
-                                             floatx4 (&acc)[8]) {
+                                             floatx4 (&acc)[W / 16]) {
   const int g = (threadIdx.x & 63) >> 4;
   float top = -INFINITY;
-  if (m0 + LM_SLAB > a.vocab) {
+  if (m0 + W > a.vocab) {
     const int end = a.vocab - m0 - 4 * g;
 #pragma unroll
-    for (int b = 0; b < 8; ++b)
+    for (int b = 0; b < W / 16; ++b)
 #pragma unroll
       for (int i = 0; i < 4; ++i)
         if (b * 16 + i >= end) acc[b][i] = -INFINITY;
   }
 #pragma unroll
-  for (int b = 0; b < 8; ++b)
+  for (int b = 0; b < W / 16; ++b)
 #pragma unroll
     for (int i = 0; i < 4; ++i) top = fmaxf(top, acc[b][i]);
   top = fmaxf(top, __shfl_xor(top, 16, 64));
   top = fmaxf(top, __shfl_xor(top, 32, 64));
   const int label = there ? a.label[a.chunk0 + n] - m0 : -1;
-  const bool here = label >= 0 && label < LM_SLAB && (label >> 2 & 3) == g;
+  const bool here = label >= 0 && label < W && (label >> 2 & 3) == g;
   float sum = 0.f;
   if (__any(here)) {
     float mine = 0.f;
 #pragma unroll
-    for (int b = 0; b < 8; ++b)
+    for (int b = 0; b < W / 16; ++b)
 #pragma unroll
       for (int i = 0; i < 4; ++i)
         if (b * 16 + i == label - 4 * g) mine = acc[b][i];
@@ -266,7 +266,7 @@ __device__ __forceinline__ void store_logits(const LmArgs& a, int m0, int n, boo
   constexpr float LOG2E = 1.44269504088896340736f;
   const float from = 14.f - (top == -INFINITY ? 0.f : top * LOG2E);
 #pragma unroll
-  for (int b = 0; b < 8; ++b)
+  for (int b = 0; b < W / 16; ++b)
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       acc[b][i] = exp2_raw(fmaf(acc[b][i], LOG2E, from));
@@ -275,18 +275,18 @@ __device__ __forceinline__ void store_logits(const LmArgs& a, int m0, int n, boo
   sum += __shfl_xor(sum, 16, 64);
   sum += __shfl_xor(sum, 32, 64);
   if (there && g == 0)
-    a.stats[(int64_t)n * (a.vp / LM_SLAB) + m0 / LM_SLAB] = make_float2(top, sum * (1.f / LM_E_SCALE));
+    a.stats[(int64_t)n * (a.vp / W) + m0 / W] = make_float2(top, sum * (1.f / LM_E_SCALE));
   if (!a.e) return;
 #pragma unroll
-  for (int b = 0; b < 8; ++b)
-    put<LM_SLAB>(own, row, 2 * b + (g >> 1), g & 1,
+  for (int b = 0; b < W / 16; ++b)
+    put<W>(own, row, 2 * b + (g >> 1), g & 1,
         make_uint2(pack_act2<true>(acc[b][0], acc[b][1]), pack_act2<true>(acc[b][2], acc[b][3])));
 }
 
 template <LmProduct P, bool F16, int W>
 __global__ __launch_bounds__(NT, W == 128 ? 1 : 2) void lm_product_kernel(LmArgs a) {
   constexpr int T = 2 * W, NB = W / 16, STEP = T * LM_BK;   // tile, a wave's blocks a side, elements of an operand's step
-  static_assert(P == LM_GRAD_W || W == 128, "");            // (a slab is a wave's; sums are cut in tiles of LM_TILE)
+  static_assert(P != LM_GRAD_X || W == 128, "");            // (sums are cut in tiles of LM_TILE)
   constexpr bool TA = P != LM_LOGITS, TB = P == LM_GRAD_W;
   __shared__ __attribute__((aligned(1024))) uint16_t lds[5 * STEP];   // three steps of one operand, two of the other: 160 or 80 KB
   const Sizes s = sizes_of(a, P);
@@ -433,7 +433,7 @@ __global__ __launch_bounds__(NT, W == 128 ? 1 : 2) void lm_product_kernel(LmArgs
   for (int i = 0; i < NB; ++i) {
     const int row = i * 16 + (lane & 15), n = n0 + wn * W + row;
     if constexpr (P == LM_LOGITS) {
-      store_logits<F16>(a, m, n, n < s.n, own, row, acc[i]);
+      store_logits<F16, W>(a, m, n, n < s.n, own, row, acc[i]);
     } else {
 #pragma unroll
       for (int j = 0; j < NB; ++j)
@@ -458,24 +458,25 @@ __global__ __launch_bounds__(NT, W == 128 ? 1 : 2) void lm_product_kernel(LmArgs
   }
 }
 
-// Joins the pieces of a cut product: 16 of a tile's rows a workgroup, 64 lanes a row.
-template <LmProduct P, bool F16>
+// Joins the pieces of a cut product: 4 K of a tile's rows a workgroup, 64 lanes a row.
+template <LmProduct P, bool F16, int K>
 __global__ __launch_bounds__(256) void lm_join_kernel(LmArgs a) {
+  constexpr int GROUPS = LM_TILE / (4 * K);
   const Sizes s = sizes_of(a, P);
   const int mt = (s.m + LM_TILE - 1) / LM_TILE, nt = (s.n + LM_TILE - 1) / LM_TILE, tiles = mt * nt;
-  const int pieces = lm_pieces(tiles, s.nk), j = blockIdx.x / 16;
+  const int pieces = lm_pieces(tiles, s.nk), j = blockIdx.x / GROUPS;
   if (pieces <= 1 || j >= tiles) return;
   const int group = j / (8 * nt), in = j % (8 * nt), gm = mt - group * 8 < 8 ? mt - group * 8 : 8;
   const int c = (threadIdx.x & 63) * 4, m = (group * 8 + in % gm) * LM_TILE + c;
   if (m >= s.m) return;
   const float scale = grad_scale<F16>(a);
 #pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    const int r = (blockIdx.x % 16) * 16 + k * 4 + (threadIdx.x >> 6), n = in / gm * LM_TILE + r;
+  for (int k = 0; k < K; ++k) {
+    const int r = (blockIdx.x % GROUPS) * 4 * K + k * 4 + (threadIdx.x >> 6), n = in / gm * LM_TILE + r;
     if (n >= s.n) return;
     const float* p = a.parts + ((int64_t)j * LM_TILE + r) * LM_TILE + c;
     floatx4 v = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
+#pragma unroll 8
     for (int i = 0; i < pieces; ++i) v += *reinterpret_cast<const floatx4*>(p + (int64_t)i * tiles * LM_TILE * LM_TILE);
     if constexpr (P == LM_GRAD_X) {
       *reinterpret_cast<uint2*>(a.grad_x + (int64_t)a.row_of[a.chunk0 + n] * a.ldgx + m) =
@@ -498,7 +499,9 @@ hipError_t launch(const LmArgs& a, hipStream_t st) {
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || parts == 0) return e;
   const int64_t cut = tiles < 2 * LM_CUS ? tiles : 2 * LM_CUS;      // tiles that may be cut
-  lm_join_kernel<P, F16><<<(uint32_t)(cut * 16), 256, 0, st>>>(a);
+  // (few tiles have many pieces: a row a wave; 40 rows, 1024, 20000: 6 us against 18)
+  if (cut <= 32) lm_join_kernel<P, F16, 1><<<(uint32_t)(cut * 64), 256, 0, st>>>(a);
+  else lm_join_kernel<P, F16, 4><<<(uint32_t)(cut * 16), 256, 0, st>>>(a);
   return hipGetLastError();
 }
 
@@ -512,7 +515,7 @@ int64_t lm_parts(const LmArgs& a, LmProduct p) {
       const int32_t tiles = tiles_of(a.d) * nt, s = lm_pieces(tiles, (a.vocab + LM_BK - 1) / LM_BK);
       if (s > 1 && (int64_t)tiles * s > most) most = (int64_t)tiles * s;
     }
-  } else {
+  } else if (a.chunk > LM_SHORT) {
     const int64_t tiles = (int64_t)tiles_of(a.d) * tiles_of(a.vocab);
     if (tiles <= 2 * LM_CUS)
       for (int32_t nk = 1; nk <= (a.chunk + LM_BK - 1) / LM_BK; ++nk) {
@@ -524,11 +527,13 @@ int64_t lm_parts(const LmArgs& a, LmProduct p) {
 }
 
 hipError_t launch_lm_product(const LmArgs& a, LmProduct p, bool f16, hipStream_t st) {
+  if (p == LM_LOGITS && a.slab == 64)
+    return f16 ? launch<LM_LOGITS, true, 64>(a, st) : launch<LM_LOGITS, false, 64>(a, st);
   if (p == LM_LOGITS) return f16 ? launch<LM_LOGITS, true, 128>(a, st) : launch<LM_LOGITS, false, 128>(a, st);
   if (p == LM_GRAD_X) return f16 ? launch<LM_GRAD_X, true, 128>(a, st) : launch<LM_GRAD_X, false, 128>(a, st);
   // Of a short sum the head's gradient is what costs, all of it written at once: two workgroups a CU, one
   // writing while the other multiplies
-  if (a.chunk <= LM_SHORT && lm_parts(a, LM_GRAD_W) == 0)
+  if (a.chunk <= LM_SHORT)
     return f16 ? launch<LM_GRAD_W, true, 64>(a, st) : launch<LM_GRAD_W, false, 64>(a, st);
   return f16 ? launch<LM_GRAD_W, true, 128>(a, st) : launch<LM_GRAD_W, false, 128>(a, st);
 }

@@ -10,16 +10,22 @@ namespace svl {
 constexpr int32_t LM_TILE = 256;     // rows and columns of a product's tile
 constexpr int32_t LM_BK = 64;        // of its sum a step
 constexpr int32_t LM_ROWS = 64;      // labelled rows are filled up with zeros to a multiple
-constexpr int32_t LM_SLAB = 128;     // vocabulary entries whose exponentials share a maximum
+constexpr int32_t LM_SLAB = 128;     // vocabulary entries whose exponentials share a maximum, in whole tiles
 // Rows of a call whose logits a wave's products take straight from memory (vocabulary 32000, 4096: 8 rows
 // 62 us against 80 in tiles; 24 rows 97 against 89).
 constexpr int32_t LM_FEW = 16;
 // Rows up to which the head's gradient comes in tiles of a quarter the size (with the softmax before it: 320
-// rows 136 us against 165, 640 222 against 237, 1024 308 against 307).
+// rows 136 us against 165, 640 222 against 237, 1024 308 against 307), also where the sums of whole tiles would
+// be cut (300 rows, 256, 3000: 7 us against 20).
 constexpr int32_t LM_SHORT = 768;
+// Tiles of the logits up to which they come in tiles of a quarter the size, of which a CU holds two: then
+// 128 tiles are at work on all CUs (vocabulary 32000, 4096, the whole call: 24 rows 58 us against 89, 128
+// rows 60 against 86, 256 80 against 83; twice the tiles, 512 rows, 135 against 107).
+constexpr int32_t LM_SMALL = 128;
 constexpr int32_t LM_PACK = 1024;    // rows of a call that are packed in one launch
 constexpr int32_t LM_CUS = 256;      // tiles at work at once
-constexpr int32_t LM_CUT = 8;        // least steps of LM_BK of a piece of a sum
+constexpr int32_t LM_CUT = 4;        // least steps of LM_BK of a piece of a sum (40 rows, 1024, 20000:
+                                     // grad_x and its join 29 us, of 8 steps 44)
 // Exponentials are held as fp16 under 2^14 (normal down to 2^-28 of their slab's largest), P
 // in fp16 likewise (of the largest weight).
 constexpr float LM_E_SCALE = 16384.f;
@@ -34,6 +40,7 @@ struct LmArgs {
   LmHead* head;
   int32_t rows, d, vocab;       // of the call
   int32_t vp;                   // vocabulary rounded up to tiles: the stride of e and stats' slabs
+  int32_t slab;                 // 128, or 64 in small tiles
   int32_t chunk0, chunk;        // labelled rows chunk0 .. + chunk of this pass
   const uint16_t* x;            // the call's rows
   int64_t ldx;
@@ -55,7 +62,7 @@ struct LmArgs {
   uint16_t* xc;                 // [rows to a multiple of LM_ROWS][d]
   float* label_logit;           // [chunk]
   float* log_sum;               // [chunk]
-  float2* stats;                // [chunk][vp / LM_SLAB] (maximum, sum of exponentials)
+  float2* stats;                // [chunk][vp / slab] (maximum, sum of exponentials)
   uint16_t* e;                  // [chunk][vp] exponentials, then P; or nullptr
   float* parts;                 // tiles of a cut sum's pieces
   float* sum_w;                 // [vocab][d] the head's gradient of earlier passes, or nullptr

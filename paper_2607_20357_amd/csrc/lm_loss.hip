@@ -224,8 +224,8 @@ __global__ __launch_bounds__(512) void lm_few_logits_kernel(LmArgs a) {
 __global__ __launch_bounds__(NT) void lm_stats_kernel(LmArgs a) {
   const int i = blockIdx.x * (NT / 64) + (threadIdx.x >> 6), lane = threadIdx.x & 63;
   if (i >= a.chunk || a.chunk0 + i >= a.head->rows) return;
-  const int slabs = (a.vocab + LM_SLAB - 1) / LM_SLAB;
-  const float2* st = a.stats + (int64_t)i * (a.vp / LM_SLAB);
+  const int slabs = (a.vocab + a.slab - 1) / a.slab;
+  const float2* st = a.stats + (int64_t)i * (a.vp / a.slab);
   float top = -INFINITY;
   for (int k = lane; k < slabs; k += 64) top = fmaxf(top, st[k].x);
 #pragma unroll
@@ -257,7 +257,7 @@ __global__ __launch_bounds__(NT) void lm_softmax_kernel(LmArgs a) {
   }
   float v[8];
   widen8(Raw8{*reinterpret_cast<const uint4*>(p), make_uint4(0, 0, 0, 0)}, SVL_TYPE_F16, v);
-  const float top = a.stats[(int64_t)i * (a.vp / LM_SLAB) + col / LM_SLAB].x;
+  const float top = a.stats[(int64_t)i * (a.vp / a.slab) + col / a.slab].x;
   const float factor = top == -INFINITY ? 1.f : expf(top - a.log_sum[i]);
   const float most = a.head->weight;
   // (weights that are all 0: no gradient)

@@ -47,7 +47,7 @@ def _operands(line):
 
 
 def test_products_are_kept_apart(kernels):
-    assert len(kernels) == 8           # logits, grad_x, grad_w of large and small tiles; two types
+    assert len(kernels) == 10          # logits and grad_w of large and small tiles, grad_x; two types
     for name, code in kernels.items():
         products = [i for i, l in enumerate(code) if l.startswith("v_mfma")]
         side = 4 if "ELi64E" in name else 8
