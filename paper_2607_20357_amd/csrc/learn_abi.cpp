@@ -214,7 +214,7 @@ int64_t lm_layout(const svl_lm_head& h, int32_t rows, bool want_x, bool want_w, 
   a->xc = l.take<uint16_t>(cdiv(rows, LM_ROWS) * LM_ROWS * h.d_model);
   a->label_logit = l.take<float>(a->chunk);
   a->log_sum = l.take<float>(a->chunk);
-  a->slab = rows > LM_FEW && (int64_t)(a->vp / LM_TILE) * (a->chunk / LM_TILE) <= LM_SMALL ? 64 : LM_SLAB;
+  a->slab = rows <= LM_FEW || (int64_t)(a->vp / LM_TILE) * (a->chunk / LM_TILE) <= LM_SMALL ? 64 : LM_SLAB;
   a->stats = l.take<float2>((int64_t)a->chunk * (a->vp / a->slab));
   if (want_x || want_w) {
     a->e = l.take<uint16_t>((int64_t)a->chunk * a->vp);
@@ -425,7 +425,7 @@ svl_status svl_lm_loss(const svl_lm_head* head, int32_t rows, const void* x, int
     for (a.chunk0 = 0; e == hipSuccess && a.chunk0 < rows; a.chunk0 += a.chunk) {
       a.first = a.chunk0 == 0;
       a.last = a.chunk0 + a.chunk >= rows;
-      if (e == hipSuccess) e = rows <= LM_FEW ? launch_lm_few_logits(a, f16, st) : launch_lm_product(a, LM_LOGITS, f16, st);
+      if (e == hipSuccess) e = launch_lm_product(a, LM_LOGITS, f16, st);
       if (e == hipSuccess) e = launch_lm_stats(a, st);
       if (e == hipSuccess && a.e) e = launch_lm_softmax(a, f16, st);
       if (e == hipSuccess && grad_x) e = launch_lm_product(a, LM_GRAD_X, f16, st);

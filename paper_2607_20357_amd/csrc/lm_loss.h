@@ -11,17 +11,16 @@ constexpr int32_t LM_TILE = 256;     // rows and columns of a product's tile
 constexpr int32_t LM_BK = 64;        // of its sum a step
 constexpr int32_t LM_ROWS = 64;      // labelled rows are filled up with zeros to a multiple
 constexpr int32_t LM_SLAB = 128;     // vocabulary entries whose exponentials share a maximum, in whole tiles
-// Rows of a call whose logits a wave's products take straight from memory (vocabulary 32000, 4096: 8 rows
-// 62 us against 80 in tiles; 24 rows 97 against 89).
-constexpr int32_t LM_FEW = 16;
 // Rows up to which the head's gradient comes in tiles of a quarter the size (with the softmax before it: 320
 // rows 136 us against 165, 640 222 against 237, 1024 308 against 307), also where the sums of whole tiles would
 // be cut (300 rows, 256, 3000: 7 us against 20).
 constexpr int32_t LM_SHORT = 768;
-// Tiles of the logits up to which they come in tiles of a quarter the size, of which a CU holds two: then
-// 128 tiles are at work on all CUs (vocabulary 32000, 4096, the whole call: 24 rows 58 us against 89, 128
-// rows 60 against 86, 256 80 against 83; twice the tiles, 512 rows, 135 against 107).
-constexpr int32_t LM_SMALL = 128;
+// The logits come in tiles of a quarter the size, of which a CU holds two, where the call has at most
+// LM_FEW rows (one such tile across: w is what there is to read, once, and twice the loads are on their way;
+// vocabulary 65537, 1024, 128 rows: 47 us the call, of whole tiles 65; 151936, 5120, 8 rows: 321 against 368) and
+// where whole tiles are at most LM_SMALL, half the CUs (32000, 4096: 24 rows 58 us against 89, 256 80 against
+// 83; twice the tiles, 512 rows, 135 against 107).
+constexpr int32_t LM_FEW = 128, LM_SMALL = 128;
 constexpr int32_t LM_PACK = 1024;    // rows of a call that are packed in one launch
 constexpr int32_t LM_CUS = 256;      // tiles at work at once
 constexpr int32_t LM_CUT = 4;        // least steps of LM_BK of a piece of a sum (40 rows, 1024, 20000:
@@ -94,7 +93,6 @@ hipError_t launch_lm_rows(const LmArgs& a, hipStream_t st);                 // l
 hipError_t launch_lm_stats(const LmArgs& a, hipStream_t st);                // log-sums and losses
 hipError_t launch_lm_softmax(const LmArgs& a, bool f16, hipStream_t st);    // exponentials to P
 hipError_t launch_lm_product(const LmArgs& a, LmProduct p, bool f16, hipStream_t st);
-hipError_t launch_lm_few_logits(const LmArgs& a, bool f16, hipStream_t st); // logits of at most LM_FEW rows
 // Most pieces of all tiles that a product is cut into, whatever rows have a label (0: it is never cut).
 int64_t lm_parts(const LmArgs& a, LmProduct p);
 hipError_t launch_lm_zero_w(const LmArgs& a, hipStream_t st);               // a call without rows

@@ -3,7 +3,7 @@
 // the exponentials turned into P.
 //
 // The logits are never in memory.  A product's tile leaves exponentials under the
-// largest logit of 128 (a slab) as fp16, and per row and slab that largest and the sum
+// largest logit of 128 or 64 (a slab) as fp16, and per row and slab that largest and the sum
 // in float32; once all slabs are known, e^(slab's - log-sum) makes them the softmax.  That
 // costs one pass over 16-bit values in place of a second product of the same size as the
 // first, and no rounding that P would not have: fp16 digits under 2^14, before bf16's.
@@ -138,88 +138,6 @@ __global__ __launch_bounds__(NT) void lm_pack_few_kernel(LmArgs a) {
       *reinterpret_cast<uint4*>(a.grad_x + (int64_t)i * a.ldgx + c) = zero;
 }
 
-// Logits of at most 16 rows: w is what there is to read, and is read once.  A workgroup takes a slab of
-// the vocabulary, a wave 16 entries of it and their whole rows, straight into the products' registers;
-// the rows of x come from the caches.  Results as lm_gemm.hip's.  (8 rows, 32000 x 4096: 262 MB in 62 us.)
-template <bool F16>
-__global__ __launch_bounds__(512) void lm_few_logits_kernel(LmArgs a) {
-  __shared__ float s_top[8][16], s_sum[8][16];
-  const int rows = a.head->rows;
-  if (rows == 0) return;
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, g = lane >> 4, l = lane & 15;
-  const int m0 = blockIdx.x * LM_SLAB + w * 16;
-  const int v = m0 + l < a.vocab ? m0 + l : a.vocab - 1;
-  const uint16_t* pw = a.w + (int64_t)v * a.ldw + g * 16;
-  const uint16_t* px = a.xc + (int64_t)(l < rows ? l : rows - 1) * a.d + g * 16;
-  // Of 64 of the sum a lane takes 16 in a row, 8 for each of two products: a line is asked for whole.
-  typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-  const auto at = [](int i) { return 64 * (i / 2) + 8 * (i & 1); };
-  const auto load = [](const uint16_t* p) { return *reinterpret_cast<const uint4*>(p); };
-  const auto once = [](const uint16_t* p) {
-    return __builtin_bit_cast(uint4, __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p)));
-  };
-  floatx4 acc = {0.f, 0.f, 0.f, 0.f};
-  constexpr int DEEP = 8;               // loads of w ahead, 1 KB each a wave, beside as many in use
-  int k = 0;
-  if (a.d >= 32 * DEEP) {
-    uint4 next[DEEP];
-#pragma unroll
-    for (int i = 0; i < DEEP; ++i) next[i] = once(pw + at(i));
-    for (; k + 32 * DEEP <= a.d; k += 32 * DEEP) {
-      uint4 wf[DEEP], xf[DEEP];
-#pragma unroll
-      for (int i = 0; i < DEEP; ++i) xf[i] = load(px + k + at(i));
-#pragma unroll
-      for (int i = 0; i < DEEP; ++i) wf[i] = next[i];
-      const int ahead = k + 64 * DEEP <= a.d ? k + 32 * DEEP : k;    // (the last ones once more)
-#pragma unroll
-      for (int i = 0; i < DEEP; ++i) next[i] = once(pw + ahead + at(i));
-      __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-      for (int i = 0; i < DEEP; ++i) acc = mfma16x16x32<F16>(wf[i], xf[i], acc);
-    }
-  }
-  for (; k < a.d; k += 64)
-#pragma unroll
-    for (int i = 0; i < 2; ++i) acc = mfma16x16x32<F16>(once(pw + k + at(i)), load(px + k + at(i)), acc);
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-    if (m0 + 4 * g + i >= a.vocab) acc[i] = -INFINITY;
-  float top = fmaxf(fmaxf(acc[0], acc[1]), fmaxf(acc[2], acc[3]));
-  top = fmaxf(top, __shfl_xor(top, 16, 64));
-  top = fmaxf(top, __shfl_xor(top, 32, 64));
-  if (g == 0) s_top[w][l] = top;
-  __syncthreads();
-#pragma unroll
-  for (int i = 0; i < 8; ++i) top = fmaxf(top, s_top[i][l]);
-  const int label = l < rows ? a.label[l] - m0 - 4 * g : -1;
-  const float from = top == -INFINITY ? 0.f : top;
-  float sum = 0.f;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    if (i == label) a.label_logit[l] = acc[i];
-    acc[i] = expf(acc[i] - from);
-    sum += acc[i];
-  }
-  sum += __shfl_xor(sum, 16, 64);
-  sum += __shfl_xor(sum, 32, 64);
-  if (g == 0) s_sum[w][l] = sum;
-  if (a.e && l < rows)
-    *reinterpret_cast<uint2*>(a.e + (int64_t)l * a.vp + m0 + 4 * g) =
-        make_uint2(pack_act2<true>(acc[0] * LM_E_SCALE, acc[1] * LM_E_SCALE),
-                   pack_act2<true>(acc[2] * LM_E_SCALE, acc[3] * LM_E_SCALE));
-  __syncthreads();
-  const int n = threadIdx.x;
-  if (n >= 16 || n >= rows) return;
-  sum = 0.f;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    sum += s_sum[i][n];
-    top = fmaxf(top, s_top[i][n]);     // (threads of the first wave: lane n holds row n's already)
-  }
-  a.stats[(int64_t)n * (a.vp / LM_SLAB) + blockIdx.x] = make_float2(top, sum);
-}
-
 // A row a wave.
 __global__ __launch_bounds__(NT) void lm_stats_kernel(LmArgs a) {
   const int i = blockIdx.x * (NT / 64) + (threadIdx.x >> 6), lane = threadIdx.x & 63;
@@ -301,12 +219,6 @@ hipError_t launch_lm_softmax(const LmArgs& a, bool f16, hipStream_t st) {
   const dim3 grid((a.chunk + LM_ROWS - 1) / LM_ROWS * LM_ROWS, (a.vp + NT * 8 - 1) / (NT * 8));
   if (f16) lm_softmax_kernel<true><<<grid, NT, 0, st>>>(a);
   else lm_softmax_kernel<false><<<grid, NT, 0, st>>>(a);
-  return hipGetLastError();
-}
-
-hipError_t launch_lm_few_logits(const LmArgs& a, bool f16, hipStream_t st) {
-  if (f16) lm_few_logits_kernel<true><<<a.vp / LM_SLAB, 512, 0, st>>>(a);
-  else lm_few_logits_kernel<false><<<a.vp / LM_SLAB, 512, 0, st>>>(a);
   return hipGetLastError();
 }
 
