@@ -76,6 +76,19 @@ def test_rows(compute, rows):
 
 
 @pytest.mark.parametrize("compute", COMPUTES)
+@pytest.mark.parametrize("vocab", [16384, 16385, 16640 + 63, 16640 + 127, 16640 + 129, 16640 + 255, 17152])
+def test_logits_in_whole_tiles(compute, vocab):
+    """More than 128 tiles of logits, and more rows than small tiles are taken for; 16384: the last in small ones."""
+    _check(300, 64, vocab, compute, ignored=0.2, seed=vocab, weights="any", held=vocab % 2 == 0)
+
+
+@pytest.mark.parametrize("compute", COMPUTES)
+@pytest.mark.parametrize("rows", [128, 129, 256, 257])
+def test_logits_of_rows_at_the_choice_of_tiles(compute, rows):
+    _check(rows, 128, 129 * 256 - 5, compute, ignored=0.1, seed=rows)
+
+
+@pytest.mark.parametrize("compute", COMPUTES)
 @pytest.mark.parametrize("d", [64, 192, 256, 320, 1024, 3584])
 def test_widths(compute, d):
     _check(40, d, 300, compute, seed=d, spread=d % 128 == 64)
