@@ -262,14 +262,16 @@ __device__ __forceinline__ void store_logits(const LmArgs& a, int m0, int n, boo
         if (b * 16 + i == label - 4 * g) mine = acc[b][i];
     if (here) a.label_logit[n] = mine;
   }
-  // 2^(log2(e) (s - top) + 14): what is kept.  (top -inf: nothing of the vocabulary here, or no probability)
+  // 2^(log2(e) (s - top) + 14): what is kept.  The difference comes first: the largest is 2^14 whatever
+  // its size (a product of top that is rounded by itself is off by parts of |top| 2^-24 of all values, and past
+  // 2^24 leaves fp16's range).  (top -inf: nothing of the vocabulary here, or no probability)
   constexpr float LOG2E = 1.44269504088896340736f;
-  const float from = 14.f - (top == -INFINITY ? 0.f : top * LOG2E);
+  const float from = top == -INFINITY ? 0.f : top;
 #pragma unroll
   for (int b = 0; b < W / 16; ++b)
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      acc[b][i] = exp2_raw(fmaf(acc[b][i], LOG2E, from));
+      acc[b][i] = exp2_raw(fmaf(acc[b][i] - from, LOG2E, 14.f));
       sum += acc[b][i];
     }
   sum += __shfl_xor(sum, 16, 64);
