@@ -213,7 +213,7 @@ int64_t lm_layout(const svl_lm_head& h, int32_t rows, bool want_x, bool want_w, 
   a->weight = l.take<float>(rows);
   a->xc = l.take<uint16_t>(cdiv(rows, LM_ROWS) * LM_ROWS * h.d_model);
   a->label_logit = l.take<float>(a->chunk);
-  a->log_sum = l.take<float>(a->chunk);
+  a->total = l.take<float2>(a->chunk);
   a->slab = rows <= LM_FEW || (int64_t)(a->vp / LM_TILE) * (a->chunk / LM_TILE) <= LM_SMALL ? 64 : LM_SLAB;
   a->stats = l.take<float2>((int64_t)a->chunk * (a->vp / a->slab));
   if (want_x || want_w) {

@@ -60,7 +60,7 @@ struct LmArgs {
   float* weight;                // [rows]
   uint16_t* xc;                 // [rows to a multiple of LM_ROWS][d]
   float* label_logit;           // [chunk]
-  float* log_sum;               // [chunk]
+  float2* total;                // [chunk] the row's largest logit, 1 / (sum of exponentials under it)
   float2* stats;                // [chunk][vp / slab] (maximum, sum of exponentials)
   uint16_t* e;                  // [chunk][vp] exponentials, then P; or nullptr
   float* parts;                 // tiles of a cut sum's pieces

@@ -4,7 +4,7 @@
 //
 // The logits are never in memory.  A product's tile leaves exponentials under the
 // largest logit of 128 or 64 (a slab) as fp16, and per row and slab that largest and the sum
-// in float32; once all slabs are known, e^(slab's - log-sum) makes them the softmax.  That
+// in float32; once all slabs are known, e^(slab's - row's largest) / sum makes them the softmax.  That
 // costs one pass over 16-bit values in place of a second product of the same size as the
 // first, and no rounding that P would not have: fp16 digits under 2^14, before bf16's.
 #include "learn_ops.h"
@@ -155,11 +155,13 @@ __global__ __launch_bounds__(NT) void lm_stats_kernel(LmArgs a) {
   }
   sum = warp_sum(sum);
   if (lane != 0) return;
-  const float lse = top + logf(sum);
+  // The largest and the sum stay apart: their log-sum is rounded at the logits' size, which would be all that
+  // is left of a sure row's loss and P (30: 2e-6).
+  const float log_sum = logf(sum);
   const int row = a.row_of[a.chunk0 + i];
-  a.log_sum[i] = lse;
-  a.loss[row] = lse - a.label_logit[i];
-  if (a.lse) a.lse[row] = lse;
+  a.total[i] = make_float2(top, 1.f / sum);
+  a.loss[row] = (top - a.label_logit[i]) + log_sum;
+  if (a.lse) a.lse[row] = top + log_sum;
 }
 
 // P of a row's 2048 columns a workgroup; rows behind the last, to a multiple of 64, are zeros.
@@ -176,7 +178,8 @@ __global__ __launch_bounds__(NT) void lm_softmax_kernel(LmArgs a) {
   float v[8];
   widen8(Raw8{*reinterpret_cast<const uint4*>(p), make_uint4(0, 0, 0, 0)}, SVL_TYPE_F16, v);
   const float top = a.stats[(int64_t)i * (a.vp / a.slab) + col / a.slab].x;
-  const float factor = top == -INFINITY ? 1.f : expf(top - a.log_sum[i]);
+  const float2 total = a.total[i];
+  const float factor = top == -INFINITY ? 1.f : expf(top - total.x) * total.y;
   const float most = a.head->weight;
   // (weights that are all 0: no gradient)
   const float weight = most == 0.f ? 0.f : a.weight[a.chunk0 + i] / most;

@@ -6,7 +6,8 @@ import pytest
 import torch
 
 import paper_2607_20357_amd as svl
-from learn_helpers import TYPES, f64, run_loss
+from learn_helpers import TINY, TYPES, U, assert_within, f64, half, run_loss
+from oracle import learning as ol
 
 pytestmark = pytest.mark.gpu
 COMPUTES = ["bf16", "f16"]
@@ -52,3 +53,52 @@ def test_large_logits_of_one_entry(compute, a, b, vocab, rows):
     want[top] = x[away].sum(0)
     want[other] = -want[top]
     assert np.array_equal(f64(gw), f64(torch.from_numpy(want).to(TYPES[compute])))
+
+
+def _sum_bound(s, top):
+    """Relative error of a row's sum of exponentials under its largest logit.  Each exponential: its argument's
+    difference, two products and a sum (3 U far + 14 U log 2), the exponential itself (2 U), and the slab's to the
+    row's (far U + 4 U and a product).  Sums: at most as many inexact additions as there are entries beside the
+    largest, and no more than 32 of a lane, 2 + 6 between lanes, and the slabs of a lane."""
+    far = top - s
+    p = np.exp(-far)
+    others = (p > 2.0 ** -150).sum(1, keepdims=True) - 1
+    p[far == 0] = 0.0
+    return 1.01 * U * (np.minimum(others, 40 + s.shape[1] / 4096) + (p * (4 * far + 18)).sum(1, keepdims=True))
+
+
+@pytest.mark.parametrize("compute", COMPUTES)
+@pytest.mark.parametrize("b", [1.0, 64.0])
+@pytest.mark.parametrize("vocab, rows", [(3, 1), (700, 40), (33000, 200)])
+def test_sure_rows_keep_their_small_losses(compute, b, vocab, rows):
+    """A loss of 1e-6 beside logits of hundreds: its error is the sum's, not the log-sum's rounding, and P of the
+    label balances P of the others."""
+    top, near, last = 0, 1, vocab - 1
+    at = {top: 0.0, near: 13.75, last: 9.25}
+    tops = [((30.0, 200.0, -200.0, 2000.0, 0.0)[r % 5], b) for r in range(rows)]
+    labels = [(top, top, top, near)[r // 5 % 4] for r in range(rows)]
+    x, w, tx, tw, tl = _exact(compute, vocab, at, tops, labels)
+    weight = np.full(rows, 1024.0)
+    loss, lse, gx, _ = run_loss(svl.make_lm_head(D, vocab, compute), tx, tw, tl,
+                                torch.from_numpy(weight).float().cuda(), want_w=False)
+    ref = ol.lm_loss(x, w, labels, weight)
+    s = x @ w.T
+    most = s.max(1, keepdims=True)
+    far, e = most - s, _sum_bound(s, most)
+    log_sum = np.log(np.exp(-far).sum(1))
+    away = far[np.arange(rows), labels]
+    # the logarithm (2 U of itself), the label's distance and the sum of both
+    b_loss = e[:, 0] + U * (2 * log_sum + away + 2 * (away + log_sum)) + U * 2 ** -20
+    want = away + log_sum              # (as ref.loss, without float64's own cancellation)
+    assert np.abs(want - ref.loss).max() < 1e-10
+    assert_within(loss, want, b_loss, "loss")
+    assert_within(lse, ref.lse, e[:, 0] + U * (2 * log_sum + 2 * np.abs(ref.lse)), "lse")
+    # P: exponentials in fp16 digits but for the largest (2^14), their own errors, the sum's and its quotient's, then
+    # P's rounding
+    dp = ref.p * (e + 2 * U + (far > 0) * (2.0 ** -11 + U * (4 * far + 30))) * 1.01
+    dp = weight[:, None] * dp
+    dp = dp + half(compute) * (np.abs(ref.ds) + dp) + (ref.p > 0) * weight[:, None] * 2.0 ** -37
+    bx = dp @ np.abs(w) + 6 * U * (np.abs(ref.ds) @ np.abs(w))       # (three entries count: few inexact sums)
+    bx = 1.01 * bx + half(compute) * (np.abs(ref.grad_x) + bx) + TINY[compute]
+    bx[:, 2:] = 0.0
+    assert_within(gx, ref.grad_x, bx, "grad_x")
