@@ -214,8 +214,11 @@ int64_t lm_layout(const svl_lm_head& h, int32_t rows, bool want_x, bool want_w, 
   a->xc = l.take<uint16_t>(cdiv(rows, LM_ROWS) * LM_ROWS * h.d_model);
   a->label_logit = l.take<float>(a->chunk);
   a->total = l.take<float2>(a->chunk);
-  a->slab = rows <= LM_FEW || (int64_t)(a->vp / LM_TILE) * (a->chunk / LM_TILE) <= LM_SMALL ? 64 : LM_SLAB;
-  a->stats = l.take<float2>((int64_t)a->chunk * (a->vp / a->slab));
+  const int64_t across = a->vp / LM_TILE;
+  a->slab = rows <= LM_FEW || across * (a->chunk / LM_TILE) <= LM_SMALL ? 64 : LM_SLAB;
+  // room for the small slabs of fewer rows too, so that a workspace serves any call of at most its rows
+  const int64_t small = std::min<int64_t>(a->chunk, LM_TILE * std::max<int64_t>(1, LM_SMALL / across));
+  a->stats = l.take<float2>(std::max((int64_t)a->chunk * (a->vp / a->slab), small * (a->vp / 64)));
   if (want_x || want_w) {
     a->e = l.take<uint16_t>((int64_t)a->chunk * a->vp);
     a->parts = l.take<float>(std::max(want_x ? lm_parts(*a, LM_GRAD_X) : 0, want_w ? lm_parts(*a, LM_GRAD_W) : 0) *

@@ -6,7 +6,7 @@ import pytest
 import torch
 
 import paper_2607_20357_amd as svl
-from learn_helpers import TINY, TYPES, U, assert_within, f64, half, run_loss
+from learn_helpers import TINY, TYPES, U, assert_within, f64, gen_of, half, randn, run_loss
 from oracle import learning as ol
 
 pytestmark = pytest.mark.gpu
@@ -102,3 +102,20 @@ def test_sure_rows_keep_their_small_losses(compute, b, vocab, rows):
     bx = 1.01 * bx + half(compute) * (np.abs(ref.grad_x) + bx) + TINY[compute]
     bx[:, 2:] = 0.0
     assert_within(gx, ref.grad_x, bx, "grad_x")
+
+
+@pytest.mark.parametrize("compute", COMPUTES)
+@pytest.mark.parametrize("want", [(False, False), (True, False), (False, True), (True, True)])
+def test_a_large_workspace_serves_fewer_rows(compute, want):
+    """A workspace made for more rows serves calls on both sides of the choice of tiles, with the same bits."""
+    for d, vocab, most, sizes in ((64, 65537, 300, (1, 65, 128, 129, 256, 257)), (64, 10240, 1024, (705, 768, 769))):
+        gen = gen_of(vocab)
+        head = svl.make_lm_head(d, vocab, compute)
+        x, w = randn(gen, (most, d), compute), randn(gen, (vocab, d), compute, d ** -0.5)
+        labels = torch.randint(0, vocab, (most,), generator=gen, device="cuda").to(torch.int32)
+        ws = svl.alloc_lm_loss_workspace(head, most, *want)
+        for n in sizes:
+            ws.fill_(255)
+            got = run_loss(head, x[:n], w, labels[:n], None, *want, ws=ws)
+            own = run_loss(head, x[:n], w, labels[:n], None, *want)
+            assert all(a is None or torch.equal(a, b) for a, b in zip(got, own)), n
