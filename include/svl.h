@@ -778,9 +778,11 @@ size_t svl_lm_loss_workspace_bytes(const svl_lm_head *head, int32_t rows, int32_
  *   loss       dev float [rows];  lse dev float [rows] or NULL (all three 4-byte aligned)
  *   grad_x     dev [rows][d_model] or NULL;  grad_w dev [vocab][d_model] or NULL, written,
  *              or added to what is there (accumulate = 1)
- * Row strides here are at most 2^21.  Logits and sums are float32.  P is rounded to 16 bits once more than softmax itself
- * was held in (fp16 digits), in fp16 under 2^14 over the largest weight, so weights down
- * to 2^-20 of the largest keep their digits. */
+ * Row strides here are at most 2^21.  Logits and sums are float32.  P is rounded to 16 bits
+ * once more than softmax itself was held in (fp16 digits).  With fp16 an entry of P keeps
+ * its digits in grad_x where the softmax is 2^-28 at least, whatever the row's weight; in
+ * grad_w, which sums over rows, where the softmax times row_weight's part of the largest is
+ * (smaller ones are off by 2^-37 of the largest weight at most). */
 svl_status svl_lm_loss(const svl_lm_head *head, int32_t rows, const void *x, int64_t ld_x,
                        const void *w, int64_t ld_w, const int32_t *labels, const float *row_weight,
                        float *loss, float *lse, void *grad_x, int64_t ld_grad_x, void *grad_w,

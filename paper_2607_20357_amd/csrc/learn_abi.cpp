@@ -432,6 +432,7 @@ svl_status svl_lm_loss(const svl_lm_head* head, int32_t rows, const void* x, int
       if (e == hipSuccess) e = launch_lm_stats(a, st);
       if (e == hipSuccess && a.e) e = launch_lm_softmax(a, f16, st);
       if (e == hipSuccess && grad_x) e = launch_lm_product(a, LM_GRAD_X, f16, st);
+      if (e == hipSuccess && f16 && grad_x && grad_w && row_weight) e = launch_lm_weigh(a, st);
       if (e == hipSuccess && grad_w) e = launch_lm_product(a, LM_GRAD_W, f16, st);
     }
     return e;

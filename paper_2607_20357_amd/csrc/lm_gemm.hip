@@ -188,8 +188,13 @@ __device__ __forceinline__ uint2 round_grad(floatx4 v, uint2 old, bool add) {
   }
   return make_uint2(pack_act2<F16>(v[0], v[1]), pack_act2<F16>(v[2], v[3]));
 }
-template <bool F16>
-__device__ __forceinline__ float grad_scale(const LmArgs& a) { return a.head->weight * (F16 ? 1.f / LM_E_SCALE : 1.f); }
+// What a gradient's sums are multiplied by: of the rows' gradient in fp16 by the row (n of s.n), otherwise the call's.
+template <LmProduct P, bool F16>
+__device__ __forceinline__ float grad_scale(const LmArgs& a, int n, int rows) {
+  if (!F16) return a.head->weight;
+  if (P != LM_GRAD_X) return lm_power(a.head->weight) * (1.f / LM_E_SCALE);
+  return n < rows ? lm_power(a.weight[a.chunk0 + n]) * (1.f / LM_E_SCALE) : 0.f;
+}
 
 // N quads along d of one row of grad_w, 16 apart: sums of passes, and what is there already.
 template <bool F16, int N>
@@ -415,7 +420,8 @@ __global__ __launch_bounds__(NT, W == 128 ? 1 : 2) void lm_product_kernel(LmArgs
     }
     return;
   }
-  const float scale = P == LM_LOGITS ? 1.f : grad_scale<F16>(a);
+  constexpr bool BY_ROW = P == LM_GRAD_X && F16;
+  const float all = P == LM_LOGITS || BY_ROW ? 1.f : grad_scale<P, F16>(a, 0, 0);
   if (P == LM_GRAD_W && (a.accumulate || a.sum_w)) {
 #pragma unroll
     for (int i = 0; i < NB; ++i) {
@@ -424,7 +430,7 @@ __global__ __launch_bounds__(NT, W == 128 ? 1 : 2) void lm_product_kernel(LmArgs
       for (int j = 0; j < NB; j += 4) {
         if (n >= s.n || m + j * 16 >= s.m) continue;         // (d is a multiple of 64)
         floatx4 v[4] = {acc[i][j], acc[i][j + 1], acc[i][j + 2], acc[i][j + 3]};
-        add_grad_w<F16>(a, n, m + j * 16 + g * 4, scale, v);
+        add_grad_w<F16>(a, n, m + j * 16 + g * 4, all, v);
       }
     }
     return;
@@ -437,6 +443,7 @@ __global__ __launch_bounds__(NT, W == 128 ? 1 : 2) void lm_product_kernel(LmArgs
     if constexpr (P == LM_LOGITS) {
       store_logits<F16, W>(a, m, n, n < s.n, own, row, acc[i]);
     } else {
+      const float scale = BY_ROW ? grad_scale<P, F16>(a, n, s.n) : all;
 #pragma unroll
       for (int j = 0; j < NB; ++j)
         put<W>(own, row, 2 * j + (g >> 1), g & 1, round_grad<F16>(acc[i][j] * scale, make_uint2(0, 0), false));
@@ -471,11 +478,11 @@ __global__ __launch_bounds__(256) void lm_join_kernel(LmArgs a) {
   const int group = j / (8 * nt), in = j % (8 * nt), gm = mt - group * 8 < 8 ? mt - group * 8 : 8;
   const int c = (threadIdx.x & 63) * 4, m = (group * 8 + in % gm) * LM_TILE + c;
   if (m >= s.m) return;
-  const float scale = grad_scale<F16>(a);
 #pragma unroll
   for (int k = 0; k < K; ++k) {
     const int r = (blockIdx.x % GROUPS) * 4 * K + k * 4 + (threadIdx.x >> 6), n = in / gm * LM_TILE + r;
     if (n >= s.n) return;
+    const float scale = grad_scale<P, F16>(a, n, s.n);
     const float* p = a.parts + ((int64_t)j * LM_TILE + r) * LM_TILE + c;
     floatx4 v = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 8

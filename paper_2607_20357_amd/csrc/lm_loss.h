@@ -26,8 +26,16 @@ constexpr int32_t LM_CUS = 256;      // tiles at work at once
 constexpr int32_t LM_CUT = 4;        // least steps of LM_BK of a piece of a sum (40 rows, 1024, 20000:
                                      // grad_x and its join 29 us, of 8 steps 44)
 // Exponentials are held as fp16 under 2^14 (normal down to 2^-28 of their slab's largest), P
-// in fp16 likewise (of the largest weight).
+// in fp16 likewise: times the weight over a power of two (lm_power), the row's own for the rows' gradient, so
+// that a row of small weight beside one of large keeps its digits, and the largest's for the head's, whose sum
+// runs over rows.  (bf16 has float32's range: P over the largest weight for both.)
 constexpr float LM_E_SCALE = 16384.f;
+
+// The power of two at or below |w|, at least 2^-126: w over it is exact, and less than 2.
+__device__ __forceinline__ float lm_power(float w) {
+  const uint32_t e = __float_as_uint(w) & 0x7f800000u;
+  return __uint_as_float(e ? e : 0x00800000u);
+}
 
 // What is known of a call's rows only on the device.
 struct LmHead {
@@ -92,6 +100,7 @@ __host__ __device__ inline int32_t lm_pieces(int32_t tiles, int32_t nk) {
 hipError_t launch_lm_rows(const LmArgs& a, hipStream_t st);                 // labelled rows, packed
 hipError_t launch_lm_stats(const LmArgs& a, hipStream_t st);                // log-sums and losses
 hipError_t launch_lm_softmax(const LmArgs& a, bool f16, hipStream_t st);    // exponentials to P
+hipError_t launch_lm_weigh(const LmArgs& a, hipStream_t st);                // fp16: P of grad_x to P of grad_w
 hipError_t launch_lm_product(const LmArgs& a, LmProduct p, bool f16, hipStream_t st);
 // Most pieces of all tiles that a product is cut into, whatever rows have a label (0: it is never cut).
 int64_t lm_parts(const LmArgs& a, LmProduct p);

@@ -180,9 +180,9 @@ __global__ __launch_bounds__(NT) void lm_softmax_kernel(LmArgs a) {
   const float top = a.stats[(int64_t)i * (a.vp / a.slab) + col / a.slab].x;
   const float2 total = a.total[i];
   const float factor = top == -INFINITY ? 1.f : expf(top - total.x) * total.y;
-  const float most = a.head->weight;
+  const float most = a.head->weight, own = a.weight[a.chunk0 + i];
   // (weights that are all 0: no gradient)
-  const float weight = most == 0.f ? 0.f : a.weight[a.chunk0 + i] / most;
+  const float weight = F16 ? own / lm_power(a.grad_x ? own : most) : most == 0.f ? 0.f : own / most;
   const float in = factor * weight * (F16 ? 1.f : 1.f / LM_E_SCALE), one = weight * (F16 ? LM_E_SCALE : 1.f);
   const int label = a.label[a.chunk0 + i] - col;
 #pragma unroll
@@ -191,6 +191,24 @@ __global__ __launch_bounds__(NT) void lm_softmax_kernel(LmArgs a) {
     if (k == label) v[k] -= one;
   }
   store8(p, F16 ? SVL_TYPE_F16 : SVL_TYPE_BF16, 0, v);
+}
+
+// fp16: a row's P from its own power of two to the largest weight's, exact but for what falls below fp16's
+// normal values there.  A row a workgroup; rows that are there already (a mean's: all) end at once.
+__global__ __launch_bounds__(NT) void lm_weigh_kernel(LmArgs a) {
+  const int i = blockIdx.x;
+  if (i >= a.head->rows - a.chunk0) return;
+  const float factor = lm_power(a.weight[a.chunk0 + i]) / lm_power(a.head->weight);
+  if (factor == 1.f) return;
+  uint16_t* p = a.e + (int64_t)i * a.vp;
+#pragma unroll 4
+  for (int c = threadIdx.x * 8; c < a.vp; c += NT * 8) {
+    float v[8];
+    widen8(Raw8{*reinterpret_cast<const uint4*>(p + c), make_uint4(0, 0, 0, 0)}, SVL_TYPE_F16, v);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] *= factor;
+    store8(p, SVL_TYPE_F16, c, v);
+  }
 }
 
 __global__ __launch_bounds__(NT) void lm_zero_w_kernel(uint16_t* w, int64_t ld, int d) {
@@ -222,6 +240,11 @@ hipError_t launch_lm_softmax(const LmArgs& a, bool f16, hipStream_t st) {
   const dim3 grid((a.chunk + LM_ROWS - 1) / LM_ROWS * LM_ROWS, (a.vp + NT * 8 - 1) / (NT * 8));
   if (f16) lm_softmax_kernel<true><<<grid, NT, 0, st>>>(a);
   else lm_softmax_kernel<false><<<grid, NT, 0, st>>>(a);
+  return hipGetLastError();
+}
+
+hipError_t launch_lm_weigh(const LmArgs& a, hipStream_t st) {
+  lm_weigh_kernel<<<a.chunk, NT, 0, st>>>(a);
   return hipGetLastError();
 }
 

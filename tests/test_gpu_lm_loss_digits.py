@@ -6,7 +6,7 @@ import pytest
 import torch
 
 import paper_2607_20357_amd as svl
-from learn_helpers import TINY, TYPES, U, assert_within, f64, gen_of, half, randn, run_loss
+from learn_helpers import (TINY, TYPES, U, assert_within, f64, gen_of, half, loss_bounds, randn, run_loss)
 from oracle import learning as ol
 
 pytestmark = pytest.mark.gpu
@@ -102,6 +102,32 @@ def test_sure_rows_keep_their_small_losses(compute, b, vocab, rows):
     bx = 1.01 * bx + half(compute) * (np.abs(ref.grad_x) + bx) + TINY[compute]
     bx[:, 2:] = 0.0
     assert_within(gx, ref.grad_x, bx, "grad_x")
+
+
+@pytest.mark.parametrize("grad_w", [False, True])
+@pytest.mark.parametrize("rows, ignored", [(40, 0), (300, 3)])
+def test_fp16_rows_of_small_weights_keep_their_gradient(grad_w, rows, ignored):
+    """Weights 2^20 apart over a vocabulary of small and even probabilities, whose roundings do not cancel (the head's
+    entries have a mean in common): each row's gradient is judged by its own size."""
+    vocab = 70001
+    gen = gen_of(rows)
+    w = (1.0 + randn(gen, (vocab, D), "f32", 1.0 / 8)).half()
+    x = randn(gen, (rows, D), "f16", 1.0 / 64)
+    labels = torch.randint(0, vocab, (rows,), generator=gen, device="cuda").to(torch.int32)
+    if ignored:
+        labels[::ignored] = -1
+    weight = torch.where(torch.arange(rows, device="cuda") % 5 == 1, 2.0 ** 12 * 1.1, 2.0 ** -8 * 1.3)
+    weight[::11] = 0.0
+    _, _, gx, gw = run_loss(svl.make_lm_head(D, vocab, "f16"), x, w, labels, weight, want_w=grad_w)
+    x64, w64, wt, l = f64(x), f64(w), f64(weight), labels.cpu().numpy().astype(np.int64)
+    for size in (wt > 1, (wt > 0) & (wt < 1), wt == 0):
+        own = np.where(size, l, -1)              # rows of one size alone
+        ref = ol.lm_loss(x64, w64, own, wt)
+        _, _, bx, _ = loss_bounds(x64, w64, own, wt, "f16", ref)
+        assert_within(f64(gx)[size & (l >= 0)], ref.grad_x[size & (l >= 0)], bx[size & (l >= 0)], "grad_x")
+    if grad_w:
+        ref = ol.lm_loss(x64, w64, l, wt)
+        assert_within(gw, ref.grad_w, loss_bounds(x64, w64, l, wt, "f16", ref)[3], "grad_w")
 
 
 @pytest.mark.parametrize("compute", COMPUTES)
