@@ -1486,11 +1486,13 @@ class AdamwTensors:
                                              grad_type=_DTYPE_TYPE[t["grad"].dtype], **place)
 
 
-def svl_adamw_step(adam: svl_adamw, tensors, step: int = 1, seed: int = 0, grad_scale: float = 1.0,
+def svl_adamw_step(adam: svl_adamw, tensors, step: int = 1, seed: Optional[int] = None, grad_scale: float = 1.0,
                    dev: Optional[torch.Tensor] = None, stream=None) -> None:
-    """One AdamW step of an AdamwTensors (or a list of its dicts).  dev: 5 32-bit words on the GPU (lr,
-    1 - beta1^step, 1 - beta2^step, grad_scale as float32, the seed as uint32) in place of lr, step,
-    grad_scale and seed; a captured step reads them at each replay."""
+    """One AdamW step of an AdamwTensors (or a list of its dicts).  seed: of the bits by which 8-bit states are
+    rounded, another each step (with the same ones over and over small changes are lost): step's own number
+    where none is given.  dev: 5 32-bit words on the GPU (lr, 1 - beta1^step, 1 - beta2^step, grad_scale as
+    float32, the seed as uint32) in place of lr, step, grad_scale and seed; a captured step reads them at each
+    replay, and without them repeats its own step and seed."""
     if not isinstance(tensors, AdamwTensors):
         tensors = AdamwTensors(tensors)
     if tensors.tensors and tensors.state_bits != adam.state_bits:
@@ -1499,6 +1501,8 @@ def svl_adamw_step(adam: svl_adamw, tensors, step: int = 1, seed: int = 0, grad_
         raise ValueError(f"the tensors are on cuda:{tensors.device}, the library launches on cuda:{_here()}")
     if dev is not None and (not isinstance(dev, torch.Tensor) or dev.element_size() != 4 or dev.numel() < 5):
         raise ValueError("dev must hold 5 words of 32 bits")
+    if seed is None:
+        seed = step
     _check(load_library().svl_adamw_step(
         ctypes.byref(adam), len(tensors.tensors), tensors.array, int(step), int(seed) & 0xFFFFFFFF,
         float(grad_scale), None if dev is None else _dev(dev, "dev"), _launch_stream(stream)))
