@@ -1430,7 +1430,9 @@ def make_adamw(lr: float, beta1: float = 0.9, beta2: float = 0.999, eps: float =
 
 class AdamwTensors:
     """The tensors of an optimizer step, marshalled once: dicts of param, grad, m and v, where wanted
-    master, and for 8-bit states m_scale and v_scale.  It keeps references, not copies."""
+    master, and for 8-bit states m_scale and v_scale.  It keeps references, not copies: a gradient that is a
+    new tensor each step needs a new list (what the list holds is what a step reads).  A step refuses a tensor
+    whose memory is no longer where it was when the list was made."""
 
     FIELDS = ("param", "grad", "master", "m", "v", "m_scale", "v_scale")
 
@@ -1471,6 +1473,7 @@ class AdamwTensors:
                     raise ValueError(f"tensor {i}: {k} must be contiguous")
         self.state_bits = 8 if eight else 32
         self.device = None
+        self._held, self._places, self._names = [], [], []   # tensors, the addresses that the array has of them
         self.array = (svl_adamw_tensor * max(len(self.tensors), 1))()
         for i, t in enumerate(self.tensors):
             place = {}
@@ -1480,10 +1483,21 @@ class AdamwTensors:
                     continue
                 if not x.is_cuda:
                     raise ValueError(f"{k} of tensor {i} must be a GPU tensor (no CPU path exists)")
-                place[k] = _on_gpu(x, f"{k} of tensor {i}", _here())
+                name = f"{k} of tensor {i}"
+                place[k] = _on_gpu(x, name, _here())
+                self._held.append(x)
+                self._places.append(place[k])
+                self._names.append(name)
                 self.device = x.get_device()
             self.array[i] = svl_adamw_tensor(n=t["param"].numel(), param_type=_DTYPE_TYPE[t["param"].dtype],
                                              grad_type=_DTYPE_TYPE[t["grad"].dtype], **place)
+
+    def check_places(self) -> None:
+        """Refuses tensors that moved (x.data = ...): the array's addresses may be another's by now."""
+        if [x.data_ptr() for x in self._held] == self._places:
+            return
+        name = next(n for x, p, n in zip(self._held, self._places, self._names) if x.data_ptr() != p)
+        raise ValueError(f"{name} has moved since the list was made: make a new AdamwTensors")
 
 
 def svl_adamw_step(adam: svl_adamw, tensors, step: int = 1, seed: Optional[int] = None, grad_scale: float = 1.0,
@@ -1493,7 +1507,9 @@ def svl_adamw_step(adam: svl_adamw, tensors, step: int = 1, seed: Optional[int] 
     where none is given.  dev: 5 32-bit words on the GPU (lr, 1 - beta1^step, 1 - beta2^step, grad_scale as
     float32, the seed as uint32) in place of lr, step, grad_scale and seed; a captured step reads them at each
     replay, and without them repeats its own step and seed."""
-    if not isinstance(tensors, AdamwTensors):
+    if isinstance(tensors, AdamwTensors):
+        tensors.check_places()
+    else:
         tensors = AdamwTensors(tensors)
     if tensors.tensors and tensors.state_bits != adam.state_bits:
         raise ValueError(f"states of {tensors.state_bits} bits, the description says {adam.state_bits}")

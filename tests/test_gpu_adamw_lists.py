@@ -1,5 +1,5 @@
 """Optimizer steps over kept lists of tensors: 8-bit states without a seed of the
-caller's own."""
+caller's own, and tensors that moved behind a list's back."""
 import pytest
 import torch
 
@@ -44,3 +44,19 @@ def test_the_seed_of_a_step_is_its_number():
     free, seven, zero = run(), run(seed=7), run(seed=0)
     assert torch.equal(free["m"], seven["m"]) and torch.equal(free["v"], seven["v"])
     assert not torch.equal(free["m"], zero["m"])
+
+
+@pytest.mark.parametrize("bits, name", [(32, "param"), (32, "grad"), (32, "m"), (32, "master"), (8, "v"), (8, "m_scale")])
+def test_tensors_that_moved_are_refused(bits, name):
+    t = _zeros(1000, bits)
+    if name == "master":
+        t["master"] = torch.zeros(1000, device="cuda")
+    adam, table = svl.make_adamw(1e-3, state_bits=bits), svl.AdamwTensors([_zeros(10, bits), t])
+    svl.svl_adamw_step(adam, table, step=1)
+    kept = t[name].data
+    t[name].data = t[name].data.clone()
+    with pytest.raises(ValueError, match=f"{name} of tensor 1 .*moved"):
+        svl.svl_adamw_step(adam, table, step=2)
+    t[name].data = kept
+    svl.svl_adamw_step(adam, table, step=2)
+    assert torch.isfinite(t["param"]).all()
