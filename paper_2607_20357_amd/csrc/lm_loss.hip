@@ -175,16 +175,18 @@ __global__ __launch_bounds__(NT) void lm_softmax_kernel(LmArgs a) {
     *reinterpret_cast<uint4*>(p) = make_uint4(0, 0, 0, 0);
     return;
   }
-  float v[8];
-  widen8(Raw8{*reinterpret_cast<const uint4*>(p), make_uint4(0, 0, 0, 0)}, SVL_TYPE_F16, v);
-  const float top = a.stats[(int64_t)i * (a.vp / a.slab) + col / a.slab].x;
+  // (what is known of the row is asked for first: its arrival is waited for once)
   const float2 total = a.total[i];
-  const float factor = top == -INFINITY ? 1.f : expf(top - total.x) * total.y;
   const float most = a.head->weight, own = a.weight[a.chunk0 + i];
+  const int label = a.label[a.chunk0 + i] - col;
+  const float top = a.stats[(int64_t)i * (a.vp / a.slab) + col / a.slab].x;
+  const Raw8 raw = {*reinterpret_cast<const uint4*>(p), make_uint4(0, 0, 0, 0)};
+  float v[8];
+  widen8(raw, SVL_TYPE_F16, v);
+  const float under = expf(top - total.x) * total.y, factor = top == -INFINITY ? 1.f : under;
   // (weights that are all 0: no gradient)
   const float weight = F16 ? own / lm_power(a.grad_x ? own : most) : most == 0.f ? 0.f : own / most;
   const float in = factor * weight * (F16 ? 1.f : 1.f / LM_E_SCALE), one = weight * (F16 ? LM_E_SCALE : 1.f);
-  const int label = a.label[a.chunk0 + i] - col;
 #pragma unroll
   for (int k = 0; k < 8; ++k) {
     v[k] *= in;
