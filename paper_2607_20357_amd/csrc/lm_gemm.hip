@@ -188,12 +188,12 @@ __device__ __forceinline__ uint2 round_grad(floatx4 v, uint2 old, bool add) {
   }
   return make_uint2(pack_act2<F16>(v[0], v[1]), pack_act2<F16>(v[2], v[3]));
 }
-// What a gradient's sums are multiplied by: of the rows' gradient in fp16 by the row (n of s.n), otherwise the call's.
+// What a gradient's sums are multiplied by: of the rows' gradient in fp16 by the row (n of `rows`), otherwise the call's.
 template <LmProduct P, bool F16>
 __device__ __forceinline__ float grad_scale(const LmArgs& a, int n, int rows) {
-  if (!F16) return a.head->weight;
-  if (P != LM_GRAD_X) return lm_power(a.head->weight) * (1.f / LM_E_SCALE);
-  return n < rows ? lm_power(a.weight[a.chunk0 + n]) * (1.f / LM_E_SCALE) : 0.f;
+  const float most = a.head->weight, all = most * (F16 ? 1.f / LM_E_SCALE : 1.f);
+  if (!F16 || P != LM_GRAD_X) return all;
+  return n < rows ? lm_power(lm_part(a.weight[a.chunk0 + n], most)) * all : 0.f;
 }
 
 // N quads along d of one row of grad_w, 16 apart: sums of passes, and what is there already.

@@ -26,14 +26,19 @@ constexpr int32_t LM_CUS = 256;      // tiles at work at once
 constexpr int32_t LM_CUT = 4;        // least steps of LM_BK of a piece of a sum (40 rows, 1024, 20000:
                                      // grad_x and its join 29 us, of 8 steps 44)
 // Exponentials are held as fp16 under 2^14 (normal down to 2^-28 of their slab's largest), P
-// in fp16 likewise: times the weight over a power of two (lm_power), the row's own for the rows' gradient, so
-// that a row of small weight beside one of large keeps its digits, and the largest's for the head's, whose sum
-// runs over rows.  (bf16 has float32's range: P over the largest weight for both.)
+// in fp16 likewise, P over the largest weight of the call.  A row's part of it is 1 where weights are equal: the
+// label's entry, most of a gradient's size, is then p - 1, just under 1, where a rounding is least of the value
+// (times a weight over a power of two in its place, just over 1: gradients of 284 rows off by 38e-5 of themselves, not
+// 23e-5).  fp16's range does not hold rows of small weight beside large ones, so for the rows' gradient the part's
+// power of two (lm_power) is left out of P and multiplied in by the row; for the head's, whose sum runs over
+// rows, it is in P.  (bf16 has float32's range: P over the largest weight for both.)
 constexpr float LM_E_SCALE = 16384.f;
 
-// The power of two at or below |w|, at least 2^-126: w over it is exact, and less than 2.
-__device__ __forceinline__ float lm_power(float w) {
-  const uint32_t e = __float_as_uint(w) & 0x7f800000u;
+// A row's part of the largest weight, and the power of two at or below its size, at least 2^-126: the part over it is
+// exact, and less than 2.
+__device__ __forceinline__ float lm_part(float weight, float most) { return most == 0.f ? 0.f : weight / most; }
+__device__ __forceinline__ float lm_power(float part) {
+  const uint32_t e = __float_as_uint(part) & 0x7f800000u;
   return __uint_as_float(e ? e : 0x00800000u);
 }
 

@@ -184,8 +184,7 @@ __global__ __launch_bounds__(NT) void lm_softmax_kernel(LmArgs a) {
   float v[8];
   widen8(raw, SVL_TYPE_F16, v);
   const float under = expf(top - total.x) * total.y, factor = top == -INFINITY ? 1.f : under;
-  // (weights that are all 0: no gradient)
-  const float weight = F16 ? own / lm_power(a.grad_x ? own : most) : most == 0.f ? 0.f : own / most;
+  const float part = lm_part(own, most), weight = F16 && a.grad_x ? part / lm_power(part) : part;
   const float in = factor * weight * (F16 ? 1.f : 1.f / LM_E_SCALE), one = weight * (F16 ? LM_E_SCALE : 1.f);
 #pragma unroll
   for (int k = 0; k < 8; ++k) {
@@ -195,12 +194,12 @@ __global__ __launch_bounds__(NT) void lm_softmax_kernel(LmArgs a) {
   store8(p, F16 ? SVL_TYPE_F16 : SVL_TYPE_BF16, 0, v);
 }
 
-// fp16: a row's P from its own power of two to the largest weight's, exact but for what falls below fp16's
-// normal values there.  A row a workgroup; rows that are there already (a mean's: all) end at once.
+// fp16: the power of two of a row's part of the largest weight into its P, exact but for what falls below fp16's
+// normal values there.  A row a workgroup; rows whose power is 1 (of equal weights: all) end at once.
 __global__ __launch_bounds__(NT) void lm_weigh_kernel(LmArgs a) {
   const int i = blockIdx.x;
   if (i >= a.head->rows - a.chunk0) return;
-  const float factor = lm_power(a.weight[a.chunk0 + i]) / lm_power(a.head->weight);
+  const float factor = lm_power(lm_part(a.weight[a.chunk0 + i], a.head->weight));
   if (factor == 1.f) return;
   uint16_t* p = a.e + (int64_t)i * a.vp;
 #pragma unroll 4

@@ -130,6 +130,33 @@ def test_fp16_rows_of_small_weights_keep_their_gradient(grad_w, rows, ignored):
         assert_within(gw, ref.grad_w, loss_bounds(x64, w64, l, wt, "f16", ref)[3], "grad_w")
 
 
+@pytest.mark.parametrize("weight", [1.01, 1.3, 1.0 / 3000, -1.01])
+@pytest.mark.parametrize("grad_w", [False, True])
+def test_fp16_equal_weights_cost_no_digits(weight, grad_w):
+    """P of a label that is not sure is just under 1, where fp16 rounds by 2^-12 at most, and equal weights leave it
+    there: they are multiplied back in float32."""
+    vocab, rows = 1000, 300
+    gen = gen_of(1)
+    x, w = np.zeros((rows, D)), np.zeros((vocab, D))
+    w[7, 0] = 1.9375                                   # the label's alone: grad_x[:, 0] is P of the label times it
+    w[:, 1] = f64(torch.randint(-64, 64, (vocab,), generator=gen, device="cuda")) / 32
+    x[:, 1] = f64(torch.randint(0, 256, (rows,), generator=gen, device="cuda")) / 256
+    tx, tw = (torch.from_numpy(t).half().cuda() for t in (x, w))
+    labels = torch.full((rows,), 7, dtype=torch.int32, device="cuda")
+    wt = torch.full((rows,), weight, device="cuda")
+    _, _, gx, _ = run_loss(svl.make_lm_head(D, vocab, "f16"), tx, tw, labels, wt, want_w=grad_w)
+    s = x @ w.T
+    p = np.exp(s - s.max(1, keepdims=True))
+    p = (p / p.sum(1, keepdims=True))[:, 7]
+    assert 0 < p.min() and p.max() < 0.2
+    want = f64(wt) * (p - 1.0) * 1.9375
+    # P: half a step under 1, and p's own digits; float32's are some U; then half a step of the result
+    bound = np.abs(f64(wt)) * 1.9375 * (2.0 ** -12 + p * 2.0 ** -11 + 100 * U)
+    step = np.exp2(np.floor(np.log2(np.abs(want) + bound)) - 11)
+    assert step.min() > TINY["f16"]
+    assert_within(f64(gx)[:, 0], want, bound + step, "grad_x")
+
+
 @pytest.mark.parametrize("compute", COMPUTES)
 @pytest.mark.parametrize("want", [(False, False), (True, False), (False, True), (True, True)])
 def test_a_large_workspace_serves_fewer_rows(compute, want):
