@@ -686,7 +686,7 @@ svl_status svl_decode_step4(const svl_config *cfg, const svl_layer_weights *laye
  * Rows are [row][width] with a stride ld in elements, at least width, at most 2^23
  * and a multiple of 8; widths are multiples of 8.  Arrays are 16-byte aligned unless
  * said otherwise.  rows = 0 is a call without work (gradients of weights that are not
- * accumulated are then zero).  At most 2^24 rows.  Sums, statistics and moments are
+ * accumulated are then zero).  Fewer than 2^24 rows.  Sums, statistics and moments are
  * float32, in an order that depends on the sizes alone: the same bits on every call.
  * Nothing that a call writes may be part of another of its arrays, but where it is
  * said.  A workspace needs no state: two captured graphs may share one as long as
@@ -760,8 +760,9 @@ typedef struct {
 
 /* Workspace bytes of svl_lm_loss with the gradients named (0 on bad arguments).  With
  * gradients it holds 16 bits for each of the vocabulary of at most a piece of the rows
- * (about 1 GiB of them, 1024 rows at least), at most 200 MB of float32 pieces of sums,
- * and with more rows than a piece the head's gradient in float32; never the logits. */
+ * (about 1 GiB of them, 1024 rows at least), at most 192 MiB of float32 pieces of sums,
+ * and with more rows than a piece the head's gradient in float32; no float32 logits.  Never
+ * less for more rows: a workspace serves any call of fewer. */
 size_t svl_lm_loss_workspace_bytes(const svl_lm_head *head, int32_t rows, int32_t want_grad_x,
                                    int32_t want_grad_w);
 

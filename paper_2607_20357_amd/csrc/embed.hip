@@ -113,7 +113,7 @@ __device__ __forceinline__ uint32_t block_before(uint32_t v, uint32_t* s, uint32
   return before + x - v;
 }
 
-// One workgroup, the rows in LDS between the passes: 16384 rows of a vocabulary of 32000 37 us (8192 21,
+// One workgroup, the rows in LDS between the passes: 16384 rows of a vocabulary of 32000 41 us (8192 21,
 // 1024 8), most of it the ballots of move_unit; several workgroups take six launches for it.
 __global__ __launch_bounds__(1024) void sort_alone_kernel(SortArgs s) {
   __shared__ uint32_t cnt[16][256];

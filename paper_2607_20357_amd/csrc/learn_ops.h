@@ -17,8 +17,6 @@ struct Raw8 {
   uint4 a, b;
 };
 
-__host__ __device__ constexpr int type_bytes(int32_t type) { return type == SVL_TYPE_F32 ? 4 : 2; }
-
 // The type is the same for all lanes: the branches are scalar.
 __device__ __forceinline__ Raw8 load_raw8(const void* p, int32_t type, int64_t i) {
   Raw8 r;

@@ -2,7 +2,7 @@
 // a label packed together, log-sums and losses from the slabs' maxima and sums, and
 // the exponentials turned into P.
 //
-// The logits are never in memory.  A product's tile leaves exponentials under the
+// No float32 logits are in memory.  A product's tile leaves exponentials under the
 // largest logit of 128 or 64 (a slab) as fp16, and per row and slab that largest and the sum
 // in float32; once all slabs are known, e^(slab's - row's largest) / sum makes them the softmax.  That
 // costs one pass over 16-bit values in place of a second product of the same size as the
