@@ -188,7 +188,7 @@ __device__ __forceinline__ uint2 round_grad(floatx4 v, uint2 old, bool add) {
   }
   return make_uint2(pack_act2<F16>(v[0], v[1]), pack_act2<F16>(v[2], v[3]));
 }
-// What a gradient's sums are multiplied by: of the rows' gradient in fp16 by the row (n of `rows`), otherwise the call's.
+// What a gradient's sums are multiplied by: the rows' gradient in fp16 by the row (n of `rows`), otherwise one for all.
 template <LmProduct P, bool F16>
 __device__ __forceinline__ float grad_scale(const LmArgs& a, int n, int rows) {
   const float most = a.head->weight, all = most * (F16 ? 1.f / LM_E_SCALE : 1.f);

@@ -11,9 +11,9 @@ constexpr int32_t LM_TILE = 256;     // rows and columns of a product's tile
 constexpr int32_t LM_BK = 64;        // of its sum a step
 constexpr int32_t LM_ROWS = 64;      // labelled rows are filled up with zeros to a multiple
 constexpr int32_t LM_SLAB = 128;     // vocabulary entries whose exponentials share a maximum, in whole tiles
-// Rows up to which the head's gradient comes in tiles of a quarter the size (with the softmax before it, 4096, 32000: 320
-// rows 155 us against 169, 640 217 against 227, 1024 308 against 307), also where the sums of whole tiles would
-// be cut (300 rows, 256, 3000: 7 us against 20).
+// Rows up to which the head's gradient comes in tiles of a quarter the size (with the softmax before it, 4096,
+// 32000: 320 rows 155 us against 169, 640 217 against 227, 1024 308 against 307), also where the sums of whole
+// tiles would be cut (300 rows, 256, 3000: 7 us against 20).
 constexpr int32_t LM_SHORT = 768;
 // The logits come in tiles of a quarter the size, of which a CU holds two, where the call has at most
 // LM_FEW rows (one such tile across: w is what there is to read, once, and twice the loads are on their way;

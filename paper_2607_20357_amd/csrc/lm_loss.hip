@@ -155,8 +155,8 @@ __global__ __launch_bounds__(NT) void lm_stats_kernel(LmArgs a) {
   }
   sum = warp_sum(sum);
   if (lane != 0) return;
-  // The largest and the sum stay apart: their log-sum is rounded at the logits' size, which would be all that
-  // is left of a sure row's loss and P (30: 2e-6).
+  // The largest and the sum stay apart: their log-sum is rounded at the logits' size (at 30 in steps of 2e-6),
+  // which would be all that is left of a sure row's loss and P.
   const float log_sum = logf(sum);
   const int row = a.row_of[a.chunk0 + i];
   a.total[i] = make_float2(top, 1.f / sum);

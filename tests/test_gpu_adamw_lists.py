@@ -46,7 +46,8 @@ def test_the_seed_of_a_step_is_its_number():
     assert not torch.equal(free["m"], zero["m"])
 
 
-@pytest.mark.parametrize("bits, name", [(32, "param"), (32, "grad"), (32, "m"), (32, "master"), (8, "v"), (8, "m_scale")])
+@pytest.mark.parametrize("bits, name", [(32, "param"), (32, "grad"), (32, "m"), (32, "master"), (8, "v"),
+                                        (8, "m_scale")])
 def test_tensors_that_moved_are_refused(bits, name):
     t = _zeros(1000, bits)
     if name == "master":

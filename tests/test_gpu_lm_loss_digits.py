@@ -130,6 +130,28 @@ def test_fp16_rows_of_small_weights_keep_their_gradient(grad_w, rows, ignored):
         assert_within(gw, ref.grad_w, loss_bounds(x64, w64, l, wt, "f16", ref)[3], "grad_w")
 
 
+def test_fp16_weights_that_differ_over_several_passes():
+    """A vocabulary whose passes are of 1280 rows: rows of both passes keep their gradients beside larger weights of
+    their own and of the other pass, and the head's gradient sums them all."""
+    vocab, rows = 400001, 1400
+    gen = gen_of(9)
+    w, x = randn(gen, (vocab, D), "f16", 1.0 / 8), randn(gen, (rows, D), "f16")
+    labels = torch.randint(0, vocab, (rows,), generator=gen, device="cuda").to(torch.int32)
+    weight = torch.exp2(-(torch.arange(rows, device="cuda") % 21).float()) * 1.7 * 2 ** 10
+    _, _, gx, gw = run_loss(svl.make_lm_head(D, vocab, "f16"), x, w, labels, weight)
+    w64, want_w = w.double(), torch.zeros((vocab, D), dtype=torch.float64, device="cuda")
+    for a in range(0, rows, 200):
+        p = torch.softmax(x[a:a + 200].double() @ w64.t().contiguous(), 1)
+        p[torch.arange(200, device="cuda"), labels[a:a + 200].long()] -= 1
+        p *= weight[a:a + 200, None].double()
+        want = p @ w64
+        # norms: half a step of 16 bits for the exponentials, P and the result, so at most their sum
+        off = (gx[a:a + 200].double() - want).norm(dim=1) / want.norm(dim=1)
+        assert off.max().item() < 3 * half("f16"), a
+        want_w += p.t().contiguous() @ x[a:a + 200].double()
+    assert ((gw.double() - want_w).norm() / want_w.norm()).item() < 3 * half("f16")
+
+
 @pytest.mark.parametrize("weight", [1.01, 1.3, 1.0 / 3000, -1.01])
 @pytest.mark.parametrize("grad_w", [False, True])
 def test_fp16_equal_weights_cost_no_digits(weight, grad_w):
